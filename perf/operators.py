@@ -214,7 +214,8 @@ def _run_own(s):
     stream = torch.cuda.current_stream()
     if kind == "scan_step":
         sp.scan_step(case["rows"], case["channels"], s["code"], s["gate"], s["x"], s["state"], s["state_out"], s["y"],
-                     slots=s["slots"], gate_ld=s["gate"].stride(0), x_ld=s["x"].stride(0), stream=stream)
+                     slots=s["slots"], n_slots=case["slots"], gate_ld=s["gate"].stride(0), x_ld=s["x"].stride(0),
+                     stream=stream)
         return dict(y=s["y"], state=s["state_out"])
     if kind == "scan_forward":
         plan.forward(s["gate"], s["x"], s["y"], h0=s["h0"], summary=s["summary"], stream=stream)
