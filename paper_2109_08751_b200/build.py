@@ -12,13 +12,15 @@ from pathlib import Path
 HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libsparbit_b200.so"
-SOURCES = [CSRC / "api.cu", CSRC / "multi.cu", CSRC / "schedule.cpp"]
+SOURCES = [CSRC / "api.cu", CSRC / "multi.cu", CSRC / "schedule.cpp", CSRC / "train_scan.cu",
+           CSRC / "train_router.cu"]
 HEADERS = [CSRC / "kernels.cuh", CSRC / "phase_desc.h", CSRC / "schedule.h", CSRC / "plan_access.h",
-           HERE.parent / "include" / "sparbit.h"]
+           CSRC / "train_common.cuh", HERE.parent / "include" / "sparbit.h",
+           HERE.parent / "include" / "sparbit_train.h"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-lineinfo", "-O3", "-std=c++17",
+    "-lineinfo", "-O3", "-std=c++20",
     "-Xcompiler", "-fPIC", "-shared",
 ]
 
