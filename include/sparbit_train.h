@@ -182,6 +182,67 @@ int sparbit_router_backward(sparbit_router_plan_t* plan, const void* logits, siz
                             const int32_t* gathered, int G, const float* dweights, float alpha, float beta,
                             const float* dloss, void* dlogits, size_t dlogits_ld, void* stream);
 
+/* ---- orthogonalised update ---------------------------------------------------------------------
+ *
+ * X = U / (|U| + eps) in the Frobenius norm, then for every step with its coefficients (a, b, c)
+ *   A = X X^T,  X = a X + (b A + c A A) X
+ * (X^T X for a tall matrix): the singular vectors of U with every singular value driven towards
+ * one.  A matrix that holds a NaN or an infinity gives NaN throughout; a zero matrix gives zeros.
+ */
+typedef struct sparbit_ortho_plan_s sparbit_ortho_plan_t;
+
+/* Products of 16-bit operands that make up one product of the iteration.  ONE: error about 1e-3 of
+ * the result's norm, below the rounding of a bf16 result.  THREE: about 1e-6, three times the work.
+ * AUTO: ONE for SPARBIT_BF16 matrices, THREE for the types with more bits. */
+enum { SPARBIT_PRODUCTS_AUTO = 0, SPARBIT_PRODUCTS_ONE = 1, SPARBIT_PRODUCTS_THREE = 3 };
+
+/*
+ * A plan for `count` matrices of rows x cols, element type dtype.  coefficients: host array
+ * [steps][3], copied; NULL = (3.4445, -4.7750, 2.0315) in every step (five steps are usual).
+ * Errors: ERR_ARG (count, rows, cols or steps < 1, unknown type, eps negative or not finite,
+ * coefficients under which singular values from 0 .. 1 leave 0 .. 7 or the polynomial b s^2 + c s^4
+ * leaves -48 .. 48), ERR_LIMIT (rows or cols > 65536, count > 4096, steps > 64, 2^31 tiles of work),
+ * ERR_NOMEM.  Host-only.
+ */
+int sparbit_ortho_plan_create(int count, size_t rows, size_t cols, int dtype, int steps, const float* coefficients,
+                              float eps, sparbit_ortho_plan_t** out);
+int sparbit_ortho_plan_destroy(sparbit_ortho_plan_t* plan);
+/* Before sparbit_ortho_plan_workspace_bytes: the plan forgets a workspace it had. */
+int sparbit_ortho_plan_set_products(sparbit_ortho_plan_t* plan, int products);
+size_t sparbit_ortho_plan_workspace_bytes(const sparbit_ortho_plan_t* plan);
+int sparbit_ortho_plan_set_workspace(sparbit_ortho_plan_t* plan, void* dev, size_t bytes);
+
+/* Synchronises the device; SPARBIT_OK, or SPARBIT_ERR_TIMEOUT if a wait inside a kernel of the plan
+ * gave up since the last call (its results are then incomplete). */
+int sparbit_ortho_plan_status(sparbit_ortho_plan_t* plan);
+
+/* update and out: matrix i starts i * stride elements behind the first (stride is ignored for
+ * count 1). */
+int sparbit_orthogonalize(sparbit_ortho_plan_t* plan, const void* update, size_t ld, size_t stride, void* out,
+                          size_t out_ld, size_t out_stride, void* stream);
+
+/*
+ * The update of the Muon optimiser, with X the orthogonalised U:
+ *   M' = momentum * M + G;   U = nesterov ? G + momentum * M' : M'
+ *   W' = (1 - lr * weight_decay) W - lr * scale * X
+ * grad has the plan's type, the momentum is 32-bit, the weights have weight_dtype.  The outputs may
+ * be the inputs (updated in place); other overlaps are ERR_ALIAS.  ld, stride: in and out alike.
+ */
+typedef struct {
+    const void* grad;
+    size_t grad_ld, grad_stride;
+    const float* momentum_in;
+    float* momentum_out;
+    size_t momentum_ld, momentum_stride;
+    const void* weight_in;
+    void* weight_out;
+    size_t weight_ld, weight_stride;
+    int weight_dtype;
+    int nesterov;
+    float lr, momentum, weight_decay, scale;
+} sparbit_muon;
+int sparbit_muon_step(sparbit_ortho_plan_t* plan, const sparbit_muon* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

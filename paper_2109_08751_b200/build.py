@@ -13,7 +13,7 @@ HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libsparbit_b200.so"
 SOURCES = [CSRC / "api.cu", CSRC / "multi.cu", CSRC / "schedule.cpp", CSRC / "train_scan.cu",
-           CSRC / "train_router.cu"]
+           CSRC / "train_router.cu", CSRC / "train_ortho.cu"]
 HEADERS = [CSRC / "kernels.cuh", CSRC / "phase_desc.h", CSRC / "schedule.h", CSRC / "plan_access.h",
            CSRC / "train_common.cuh", HERE.parent / "include" / "sparbit.h",
            HERE.parent / "include" / "sparbit_train.h"]

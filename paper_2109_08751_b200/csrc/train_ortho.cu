@@ -1,0 +1,892 @@
+// A matrix update orthogonalised by Newton-Schulz products on the tensor cores (sm_100a).
+//
+// With m the smaller side, X (m x n) = U / (|U| + eps), tall matrices transposed on the way in and
+// out.  Each step of the iteration is three products with fp32 accumulators:
+//   Gram    A = X X^T            m x m, symmetric
+//   Poly    P = b A + c A A + d I   symmetric
+//   Apply   X' = (a - d) X + P X
+// Only tiles that reach the diagonal or lie above it are computed for A and P; their epilogue
+// writes the mirror image too.
+//
+// Precision.  Operands are fp16 pairs hi + lo with power-of-two scales; 22 bits.  One product a
+// step (16-bit matrices): the tensor cores see hi alone, 11 bits, but the term (a - d) X, through
+// which the small singular values grow 3.4-fold a step, is formed from hi + lo, and in the first
+// step X is U itself (16-bit inputs are exact in hi; 1 / |U| is folded into the epilogues).  With
+// rounded X in that term the result of a low-rank gradient is 1-2 % off, with the pair 0.1 %, below
+// the rounding of a bf16 result.  Three products (32-bit matrices): hi hi + hi lo + lo hi, and that
+// term from an fp32 copy of X, which hi + lo would cut to 22 bits: about 1e-6.  The shift d = -3/4 (b + c) of the last step takes most of P's diagonal out of its fp16
+// rounding; in earlier steps it would feed the rounding of hi back into small singular values.
+#include <cuda.h>
+#include <math.h>
+#include <string.h>
+
+#include <new>
+#include <vector>
+
+#include "train_common.cuh"
+
+using namespace spb;
+
+namespace {
+
+// ---- tile geometry ------------------------------------------------------------------------------
+constexpr int kTileM = 128, kTileN = 256, kTileK = 64;  // one tcgen05 accumulator: 256 TMEM columns
+constexpr int kStages = 4;
+constexpr int kABytes = kTileM * kTileK * 2, kBBytes = kTileN * kTileK * 2, kStageBytes = kABytes + kBBytes;
+constexpr int kThreads = 320;  // warp 0 loads, warp 1 multiplies, warps 2-9 write out
+// The tensor cores cut each partial sum towards zero: over K = 4096 a relative error of 1e-5, which
+// three products would not survive.  They hand over every 256 of K to a sum rounded in registers.
+constexpr int kFlush = 4;
+constexpr int kSmem = kStages * kStageBytes + 1024;
+constexpr int kNormParts = 256;                         // CTAs a matrix's norm is summed by
+constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;   // X and A, P are held times these
+constexpr unsigned long long kWaitNs = 2000000000ull;   // a wait inside the kernel gives up after this
+
+enum { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
+
+// ---- PTX ----------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 0x989680;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// Bounded: false once the time is up or another role of the CTA gave up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+    if (bar_try(bar, parity)) return true;
+    const unsigned long long until = now_ns() + kWaitNs;
+    while (!bar_try(bar, parity)) {
+        if (*gave_up) return false;
+        if (now_ns() > until) {
+            *gave_up = 1;
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+            dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+// Shared-memory operand of 128-byte swizzled rows.  K-major: groups of 8 rows `sbo` apart.  MN-major:
+// blocks of 64 elements `lbo` apart, groups of 8 k `sbo` apart.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; i++) v[i] = __uint_as_float(r[i]);
+}
+
+// ---- arguments ----------------------------------------------------------------------------------
+
+// A user's matrix: element (r, c) of matrix b at p[b * stride + r * ld + c], seen transposed where
+// the plan works on the transpose.
+struct Mat {
+    void* p;
+    int64_t ld, stride;
+    int type;
+    bool wide;  // every row starts on a multiple of 16 bytes
+};
+
+struct ProductArgs {
+    int M, N, K;            // of the product
+    int segments;           // 1: hi hi; 3: hi hi + hi lo + lo hi
+    int flush;              // blocks of K a TMEM accumulator takes before it is added up in registers
+    int n_tiles;            // tiles of one matrix, listed in `tiles` as (row tile << 16 | column tile)
+    int total;              // tiles of all matrices
+    const uint32_t* tiles;
+    const float* q;         // per matrix: true X per stored X of the first step
+    int first;              // first step: X is the scaled update
+    float a, b, c, d;       // coefficients of the step, d already taken off a
+    // hi and lo of: the epilogue's addend (Poly: A; Apply: X) and of the result; pitch in elements
+    const __half *in_hi, *in_lo;
+    __half *out_hi, *out_lo;
+    const float* in_full;   // three products: X in fp32, in and out
+    float* out_full;
+    int64_t ld_in, ld_out, z_in, z_out;  // z: elements between matrices
+    // last step: the result, or the weights it updates
+    Mat out, weight;
+    int transposed, muon;
+    float keep, rate;       // W' = keep W - rate X
+    uint32_t* status;
+};
+
+__device__ __forceinline__ float load_any(const Mat& m, int64_t i) {
+    if (m.type == SPARBIT_F32) return ((const float*)m.p)[i];
+    if (m.type == SPARBIT_BF16) return __bfloat162float(((const __nv_bfloat16*)m.p)[i]);
+    return __half2float(((const __half*)m.p)[i]);
+}
+__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
+    hi = __float2half_rn(v);
+    lo = __float2half_rn(v - __half2float(hi));
+}
+
+// 32 values that follow one another, at any alignment (wide: 16-byte aligned); `step` elements apart
+template <typename T>
+__device__ __forceinline__ void read32(const T* p, bool wide, int64_t step, int n, float (&v)[32]) {
+    constexpr int kPer = 16 / sizeof(T);
+    if (wide && n >= 32) {
+#pragma unroll
+        for (int i = 0; i < 32 / kPer; i++) {
+            const Pack<T, kPer> k = reinterpret_cast<const Pack<T, kPer>*>(p)[i];
+#pragma unroll
+            for (int u = 0; u < kPer; u++) v[i * kPer + u] = to_float(k.v[u]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; i++) v[i] = i < n ? to_float(p[i * step]) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void write32(T* p, bool wide, int64_t step, int n, const float (&v)[32]) {
+    constexpr int kPer = 16 / sizeof(T);
+    if (wide && n >= 32) {
+#pragma unroll
+        for (int i = 0; i < 32 / kPer; i++) {
+            Pack<T, kPer> k;
+#pragma unroll
+            for (int u = 0; u < kPer; u++) k.v[u] = from_float<T>(v[i * kPer + u]);
+            reinterpret_cast<Pack<T, kPer>*>(p)[i] = k;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; i++)
+            if (i < n) p[i * step] = from_float<T>(v[i]);
+    }
+}
+__device__ __forceinline__ void write32_any(const Mat& m, int64_t at, int64_t step, int n, const float (&v)[32]) {
+    const bool wide = m.wide && step == 1;
+    if (m.type == SPARBIT_F32) write32((float*)m.p + at, wide, step, n, v);
+    else if (m.type == SPARBIT_BF16) write32((__nv_bfloat16*)m.p + at, wide, step, n, v);
+    else write32((__half*)m.p + at, wide, step, n, v);
+}
+__device__ __forceinline__ void read32_any(const Mat& m, int64_t at, int64_t step, int n, float (&v)[32]) {
+    const bool wide = m.wide && step == 1;
+    if (m.type == SPARBIT_F32) read32((const float*)m.p + at, wide, step, n, v);
+    else if (m.type == SPARBIT_BF16) read32((const __nv_bfloat16*)m.p + at, wide, step, n, v);
+    else read32((const __half*)m.p + at, wide, step, n, v);
+}
+
+// 32 columns of a row of a product, on their way out.  The pitches of X, A and P are multiples of 64
+// elements: a run of 32 columns that starts inside a row may be read and written whole (the columns
+// past the matrix are outside the tensor maps).
+template <int kOp>
+__device__ __forceinline__ void write_out(const ProductArgs& g, int z, int row, int row0, int col, float q,
+                                          float (&v)[32]) {
+    if constexpr (kOp == kGram || kOp == kPoly) {
+        const float scale = kOp == kGram ? q * q * kScaleP : g.c / kScaleP;  // result held times kScaleP
+#pragma unroll
+        for (int i = 0; i < 32; i++) v[i] *= scale;
+        if (kOp == kPoly) {
+            const int64_t at = z * g.z_in + row * g.ld_in + col;
+            float add[32];
+            read32(g.in_hi + at, true, 1, 32, add);
+#pragma unroll
+            for (int i = 0; i < 32; i++) v[i] += g.b * add[i] + (col + i == row ? g.d * kScaleP : 0.0f);
+            if (g.segments == 3) {
+                read32(g.in_lo + at, true, 1, 32, add);
+#pragma unroll
+                for (int i = 0; i < 32; i++) v[i] += g.b * add[i];
+            }
+        }
+        const int64_t zo = z * g.z_out;
+        __half hi[32];
+#pragma unroll
+        for (int i = 0; i < 32; i++) hi[i] = __float2half_rn(v[i]);
+#pragma unroll 1
+        for (int part = 0; part < (g.segments == 3 ? 2 : 1); part++) {
+            __half* out = (part ? g.out_lo : g.out_hi) + zo;
+            if (part)
+#pragma unroll
+                for (int i = 0; i < 32; i++) hi[i] = __float2half_rn(v[i] - __half2float(hi[i]));
+            uint4* o = reinterpret_cast<uint4*>(out + row * g.ld_out + col);
+#pragma unroll
+            for (int i = 0; i < 4; i++) o[i] = reinterpret_cast<const uint4*>(hi)[i];
+            if (col > row0)  // off the diagonal: the mirror image; lanes hold neighbouring rows
+#pragma unroll
+                for (int i = 0; i < 32; i++)
+                    if (col + i < g.N) out[(col + i) * g.ld_out + row] = hi[i];
+        }
+    } else {
+        // stored X' = (a stored X + (P X) / kScaleP) * (true per stored) * kScaleX
+        const int64_t at = z * g.z_in + row * g.ld_in + col;
+        const float scale = q * (kOp == kLast ? 1.0f : kScaleX);
+        float x[32];
+        if (g.in_full) {
+            read32(g.in_full + at, true, 1, 32, x);
+        } else {
+            float lo[32];
+            read32(g.in_hi + at, true, 1, 32, x);
+            read32(g.in_lo + at, true, 1, 32, lo);
+#pragma unroll
+            for (int i = 0; i < 32; i++) x[i] += lo[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i++) v[i] = (g.a * x[i] + v[i] * (1.0f / kScaleP)) * scale;
+        if (kOp == kApply) {
+            const int64_t to = z * g.z_out + row * g.ld_out + col;
+            write32(g.out_hi + to, true, 1, 32, v);
+            if (g.out_full) write32(g.out_full + to, true, 1, 32, v);
+#pragma unroll
+            for (int i = 0; i < 32; i++) v[i] -= __half2float(__float2half_rn(v[i]));
+            write32(g.out_lo + to, true, 1, 32, v);
+        } else {
+            const int64_t r = g.transposed ? col : row, c = g.transposed ? row : col;
+            const int n = g.N - col < 32 ? g.N - col : 32;
+            if (g.muon) {
+                read32_any(g.weight, z * g.weight.stride + r * g.weight.ld + c, g.transposed ? g.weight.ld : 1, n, x);
+#pragma unroll
+                for (int i = 0; i < 32; i++) v[i] = g.keep * x[i] - g.rate * v[i];
+            }
+            write32_any(g.out, z * g.out.stride + r * g.out.ld + c, g.transposed ? g.out.ld : 1, n, v);
+        }
+    }
+}
+
+// ---- the product kernel -------------------------------------------------------------------------
+// Persistent, one CTA per SM.  Maps: A hi, A lo, B hi, B lo; boxes of 64 columns x tile rows (Gram,
+// Poly) or of 64 columns x 64 rows (Apply's B, used MN-major).
+template <int kOp>
+__global__ void __launch_bounds__(kThreads, 1)
+    product_kernel(const __grid_constant__ CUtensorMap a_hi, const __grid_constant__ CUtensorMap a_lo,
+                   const __grid_constant__ CUtensorMap b_hi, const __grid_constant__ CUtensorMap b_lo,
+                   const __grid_constant__ ProductArgs g) {
+    constexpr bool kSquare = kOp == kGram || kOp == kPoly;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * kStages + 4];
+    __shared__ uint32_t tmem_base;
+    __shared__ uint32_t gave_up;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; i++) bar_init(done + 8 * i, 1), bar_init(drained + 8 * i, 8);
+        gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base))
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_base;
+    pdl_wait();
+    pdl_trigger();
+
+    const int k_blocks = (g.K + kTileK - 1) / kTileK, blocks = k_blocks * g.segments;
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t n = 0;  // stages filled so far
+            bool ok = true;
+            for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+                const int z = t / g.n_tiles;
+                const uint32_t rc = g.tiles[t - z * g.n_tiles];
+                const int row = (int)(rc >> 16) * kTileM, col = (int)(rc & 0xffff) * kTileN;
+                for (int s = 0; s < blocks; s++, n++) {
+                    const uint32_t st = n % kStages;
+                    if (n >= kStages && !bar_wait(empty + 8 * st, (n / kStages - 1) & 1, &gave_up)) {
+                        ok = false;
+                        break;
+                    }
+                    const int seg = s / k_blocks, k = (s - seg * k_blocks) * kTileK;
+                    const uint32_t dst = ring + st * kStageBytes, bar = full + 8 * st;
+                    bar_expect(bar, kStageBytes);
+                    tma_load(dst, seg == 2 ? &a_lo : &a_hi, bar, k, row, z);
+                    const CUtensorMap* bm = seg == 1 ? &b_lo : &b_hi;
+                    if (kSquare) {
+                        tma_load(dst + kABytes, bm, bar, k, col, z);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kTileN / 64; i++)
+                            tma_load(dst + kABytes + i * kTileK * 128, bm, bar, col + i * 64, k, z);
+                    }
+                }
+            }
+            // all copies have landed before the CTA may end, whatever happened
+            for (uint32_t i = n > kStages ? n - kStages : 0; i < n; i++) {
+                const unsigned long long until = now_ns() + kWaitNs;
+                while (!bar_try(full + 8 * (i % kStages), (i / kStages) & 1) && now_ns() < until) {
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            // fp16 operands, fp32 accumulator, 128 x 256; B MN-major for Apply
+            constexpr uint32_t idesc = (1u << 4) | (kSquare ? 0u : 1u << 16) | ((uint32_t)(kTileN >> 3) << 17) |
+                                       ((uint32_t)(kTileM >> 4) << 24);
+            uint32_t n = 0, group = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+                for (int s0 = 0; s0 < blocks && ok; s0 += g.flush, group++) {
+                    const uint32_t slot = group & 1;
+                    if (group >= 2 && !bar_wait(drained + 8 * slot, (group / 2 - 1) & 1, &gave_up)) {
+                        ok = false;
+                        break;
+                    }
+                    fence_after();
+                    const int end = s0 + g.flush < blocks ? s0 + g.flush : blocks;
+                    for (int s = s0; s < end; s++, n++) {
+                        const uint32_t st = n % kStages;
+                        if (!bar_wait(full + 8 * st, (n / kStages) & 1, &gave_up)) {
+                            ok = false;
+                            break;
+                        }
+                        fence_after();
+                        const uint32_t at = ring + st * kStageBytes;
+#pragma unroll
+                        for (int k = 0; k < kTileK / 16; k++) {
+                            const uint64_t da = smem_desc(at + k * 32, 16, 1024);
+                            const uint64_t db = kSquare ? smem_desc(at + kABytes + k * 32, 16, 1024)
+                                                        : smem_desc(at + kABytes + k * 2048, kTileK * 128, 1024);
+                            mma_f16(tmem + slot * kTileN, da, db, idesc, s > s0 || k > 0);
+                        }
+                        mma_commit(empty + 8 * st);
+                    }
+                    if (ok) mma_commit(done + 8 * slot);
+                }
+            }
+        }
+    } else {
+        // TMEM lanes go by the warp's number mod 4; the two warps of a quarter take half the columns each
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        uint32_t group = 0;
+        for (int t = blockIdx.x; t < g.total; t += gridDim.x) {
+            const int z = t / g.n_tiles;
+            const uint32_t rc = g.tiles[t - z * g.n_tiles];
+            const int row0 = (int)(rc >> 16) * kTileM + quad * 32, row = row0 + lane;
+            const int col0 = (int)(rc & 0xffff) * kTileN + half * (kTileN / 2);
+            float acc[kTileN / 2 / 32][32];
+            bool ok = true;
+            for (int s = 0; s < blocks; s += g.flush, group++) {
+                const uint32_t slot = group & 1;
+                ok = bar_wait(done + 8 * slot, (group / 2) & 1, &gave_up);
+                if (!ok) break;
+                fence_after();
+#pragma unroll
+                for (int j = 0; j < kTileN / 2 / 32; j++) {
+                    float v[32];
+                    __syncwarp();
+                    tmem_load32(tmem + slot * kTileN + half * (kTileN / 2) + j * 32 + lanes, v);
+#pragma unroll
+                    for (int i = 0; i < 32; i++) acc[j][i] = s == 0 ? v[i] : acc[j][i] + v[i];
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(drained + 8 * slot);
+            }
+            if (!ok) break;
+            if (row >= g.M) continue;
+            const float q = g.first ? g.q[z] : 1.0f / kScaleX;
+#pragma unroll
+            for (int j = 0; j < kTileN / 2 / 32; j++) {
+                const int col = col0 + j * 32;
+                if (col < g.N && !(kSquare && col < row0)) write_out<kOp>(g, z, row, row0, col, q, acc[j]);
+            }
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && gave_up) *g.status = 2;
+    if (warp == 1) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+// ---- before the products ------------------------------------------------------------------------
+
+struct PrepareArgs {
+    Mat update;                  // U, or the gradient
+    const float* mom_in;         // Muon: momentum, null otherwise
+    float* mom_out;
+    int64_t mom_in_ld, mom_in_stride, mom_out_ld, mom_out_stride;
+    float mu;
+    int nesterov;
+    int rows, cols;              // of the user's matrix
+    int transposed;
+    float eps;
+    double* parts;               // [count][kNormParts]
+    float* q;                    // [count]
+    __half *hi, *lo;
+    float* full;                 // three products
+    int64_t ld, z;
+};
+
+// Sum of squares of every matrix, in parts; and the new momentum.
+__global__ void __launch_bounds__(256) norm_kernel(const PrepareArgs g) {
+    __shared__ double s[8];
+    pdl_wait();
+    pdl_trigger();
+    const int z = blockIdx.y;
+    double sum = 0.0;
+    for (int64_t r = blockIdx.x; r < g.rows; r += kNormParts)
+        for (int c = threadIdx.x; c < g.cols; c += 256) {
+            float u = load_any(g.update, z * g.update.stride + r * g.update.ld + c);
+            if (g.mom_in) {
+                const float m = g.mu * g.mom_in[z * g.mom_in_stride + r * g.mom_in_ld + c] + u;
+                g.mom_out[z * g.mom_out_stride + r * g.mom_out_ld + c] = m;
+                u = g.nesterov ? u + g.mu * m : m;
+            }
+            sum += (double)u * (double)u;
+        }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; i++) sum += s[i];
+        g.parts[(int64_t)z * kNormParts + blockIdx.x] = sum;
+    }
+}
+
+// X of the first step: U times a power of two that brings its norm to 2048 .. 4096, as hi + lo, and
+// the factor from that to U / (|U| + eps).
+__global__ void __launch_bounds__(256) convert_kernel(const PrepareArgs g) {
+    __shared__ double s[8];
+    __shared__ float tile[32][33];
+    pdl_wait();
+    pdl_trigger();
+    const int z = blockIdx.z;
+    double sum = g.parts[(int64_t)z * kNormParts + threadIdx.x];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int i = 0; i < 8; i++) sum += s[i];
+    const double norm = sqrt(sum);
+    const bool fine = norm > 0.0 && norm < INFINITY;
+    int e = 0;
+    if (fine) frexp(norm, &e);
+    e = min(12 - e, 120);
+    const float scale = fine ? ldexpf(1.0f, e) : 1.0f;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
+        g.q[z] = norm < INFINITY ? (float)(1.0 / (ldexp(norm, fine ? e : 0) + ldexp((double)g.eps, fine ? e : 0))) : NAN;
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int64_t r0 = (int64_t)blockIdx.y * 32, c0 = (int64_t)blockIdx.x * 32;
+    for (int i = ty; i < 32; i += 8) {
+        const int64_t r = r0 + i, c = c0 + tx;
+        float u = 0.0f;
+        if (r < g.rows && c < g.cols) {
+            u = g.mom_in && !g.nesterov ? 0.0f : load_any(g.update, z * g.update.stride + r * g.update.ld + c);
+            if (g.mom_in) {
+                const float m = g.mom_out[z * g.mom_out_stride + r * g.mom_out_ld + c];
+                u = g.nesterov ? u + g.mu * m : m;
+            }
+        }
+        tile[i][tx] = u * scale;
+    }
+    __syncthreads();
+    for (int i = ty; i < 32; i += 8) {
+        const int64_t r = g.transposed ? c0 + i : r0 + i, c = g.transposed ? r0 + tx : c0 + tx;
+        if (r >= (g.transposed ? g.cols : g.rows) || c >= (g.transposed ? g.rows : g.cols)) continue;
+        __half hi, lo;
+        const float u = g.transposed ? tile[tx][i] : tile[i][tx];
+        split(u, hi, lo);
+        if (g.full) g.full[z * g.z + r * g.ld + c] = u;
+        g.hi[z * g.z + r * g.ld + c] = hi;
+        g.lo[z * g.z + r * g.ld + c] = lo;
+    }
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+struct Step {
+    float a, b, c;
+};
+
+}  // namespace
+
+struct sparbit_ortho_plan_s {
+    int count = 0, dtype = 0, products = SPARBIT_PRODUCTS_AUTO;
+    size_t rows = 0, cols = 0;
+    int m = 0, n = 0;
+    bool transposed = false;
+    float eps = 0.0f;
+    std::vector<Step> steps;
+    std::vector<uint32_t> square, wide;  // tile lists: symmetric results, X
+    char* work = nullptr;
+    int device = -1, sm_count = 0;
+    // tensor maps: A operand boxes of 128 rows, B boxes of 256 rows (K-major) or 64 rows (MN-major)
+    CUtensorMap xa[2][2], xb[2][2], xn[2][2], ga[2], gb[2], pa[2];  // [buffer][hi, lo]
+
+    int64_t ldx() const { return (int64_t)round_up(n, 64); }
+    int64_t ldg() const { return (int64_t)round_up(m, 64); }
+    int64_t zx() const { return ldx() * m; }
+    int64_t zg() const { return ldg() * m; }
+    int parts() const { return products == SPARBIT_PRODUCTS_AUTO ? (dtype == SPARBIT_BF16 ? 1 : 3) : products; }
+    size_t x_bytes() const { return round_up((size_t)count * zx() * 2, 1024); }
+    size_t g_bytes() const { return round_up((size_t)count * zg() * 2, 1024); }
+    // layout: status, tiles, parts, q | X hi, lo (two buffers) | A hi, lo | P hi, lo | X fp32 (two buffers)
+    size_t off_square() const { return 256; }
+    size_t off_wide() const { return off_square() + round_up(square.size() * 4, 256); }
+    size_t off_parts() const { return off_wide() + round_up(wide.size() * 4, 256); }
+    size_t off_q() const { return off_parts() + (size_t)count * kNormParts * 8; }
+    size_t off_x() const { return round_up(off_q() + (size_t)count * 4, 1024); }
+    size_t off_g() const { return off_x() + 4 * x_bytes(); }
+    size_t off_full() const { return off_g() + 4 * g_bytes(); }
+    // 1024: alignment of the base
+    size_t work_bytes() const { return off_full() + (parts() == 3 ? 4 * x_bytes() : 0) + 1024; }
+    char* base() const { return (char*)round_up((size_t)work, 1024); }
+    __half* x(int buffer, int lo) const { return (__half*)(base() + off_x() + (size_t)(2 * buffer + lo) * x_bytes()); }
+    float* full(int buffer) const {
+        return parts() == 3 ? (float*)(base() + off_full() + (size_t)(2 * buffer) * x_bytes()) : nullptr;
+    }
+    __half* gram(int lo) const { return (__half*)(base() + off_g() + (size_t)lo * g_bytes()); }
+    __half* poly(int lo) const { return (__half*)(base() + off_g() + (size_t)(2 + lo) * g_bytes()); }
+};
+
+namespace {
+
+int encode(EncodeFn fn, CUtensorMap* map, void* p, int64_t cols, int64_t rows, int64_t count, int64_t ld, int64_t z,
+           int box_rows) {
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
+    const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)z * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, p, dims, strides, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SPARBIT_OK : record_cuda_error((int)cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+}
+
+bool wide_rows(const void* q, size_t es, size_t ld, size_t stride) {
+    return common_alignment((uintptr_t)q | ld * es | stride * es, 16) == 16;
+}
+
+// The largest |value| the iteration can reach over singular values 0 .. 1, and whether X, A and P
+// stay within what the scaled fp16 operands hold.
+bool bounded(const std::vector<Step>& steps) {
+    double s = 1.0;
+    for (const Step& k : steps) {
+        if (!isfinite(k.a) || !isfinite(k.b) || !isfinite(k.c)) return false;
+        double next = 0.0, p = 0.0;
+        for (int i = 0; i <= 4096; i++) {
+            const double v = s * i / 4096, l = v * v, q = k.b * l + k.c * l * l;
+            next = fmax(next, fabs(v * (k.a + q)));
+            p = fmax(p, fmax(fabs(q), fabs(q - 0.75 * ((double)k.b + k.c))));
+        }
+        if (!(p <= 48.0) || !(s * s <= 48.0)) return false;
+        s = next * 1.02 + 1e-3;  // what roundings add, and between the points
+        if (!(s <= 64.0)) return false;
+    }
+    return true;
+}
+
+int ready(const sparbit_ortho_plan_s* p) {
+    if (!p->work) return SPARBIT_ERR_WORKSPACE;
+    int cur = -1;
+    CU(cudaGetDevice(&cur));
+    return cur == p->device ? SPARBIT_OK : SPARBIT_ERR_ARG;
+}
+
+template <int kOp>
+int product(const sparbit_ortho_plan_s* p, const CUtensorMap& ah, const CUtensorMap& al, const CUtensorMap& bh,
+            const CUtensorMap& bl, ProductArgs g, cudaStream_t st) {
+    const std::vector<uint32_t>& list = kOp == kGram || kOp == kPoly ? p->square : p->wide;
+    g.tiles = (const uint32_t*)(p->base() + (kOp == kGram || kOp == kPoly ? p->off_square() : p->off_wide()));
+    g.n_tiles = (int)list.size();
+    g.total = g.n_tiles * p->count;
+    g.segments = p->parts();
+    g.flush = g.segments == 3 ? kFlush : 1 << 30;
+    g.status = (uint32_t*)p->base();
+    const int grid = g.total < p->sm_count ? g.total : p->sm_count;
+    CU(launch(product_kernel<kOp>, dim3(grid), dim3(kThreads), kSmem, st, ah, al, bh, bl, g));
+    return SPARBIT_OK;
+}
+
+// prepare: update, momentum and scalars filled in; last: out, weight, muon, keep, rate filled in
+int iterate(const sparbit_ortho_plan_s* p, PrepareArgs prep, ProductArgs last, cudaStream_t st) {
+    prep.rows = (int)p->rows;
+    prep.cols = (int)p->cols;
+    prep.transposed = p->transposed;
+    prep.eps = p->eps;
+    prep.parts = (double*)(p->base() + p->off_parts());
+    prep.q = (float*)(p->base() + p->off_q());
+    prep.hi = p->x(0, 0);
+    prep.lo = p->x(0, 1);
+    prep.full = p->full(0);
+    prep.ld = p->ldx();
+    prep.z = p->zx();
+    CU(launch(norm_kernel, dim3(kNormParts, p->count), dim3(256), 0, st, prep));
+    CU(launch(convert_kernel, dim3((unsigned)((p->cols + 31) / 32), (unsigned)((p->rows + 31) / 32), p->count),
+              dim3(256), 0, st, prep));
+    int cur = 0;
+    for (size_t i = 0; i < p->steps.size(); i++) {
+        const bool end = i + 1 == p->steps.size();
+        ProductArgs g = last;
+        const Step& k = p->steps[i];
+        g.first = i == 0;
+        g.q = prep.q;
+        g.b = k.b;
+        g.c = k.c;
+        g.d = end ? -0.75f * (k.b + k.c) : 0.0f;
+        g.a = k.a - g.d;
+        g.M = g.N = p->m;
+        g.K = p->n;
+        g.out_hi = p->gram(0);
+        g.out_lo = p->gram(1);
+        g.ld_out = p->ldg();
+        g.z_out = p->zg();
+        int e = product<kGram>(p, p->xa[cur][0], p->xa[cur][1], p->xb[cur][0], p->xb[cur][1], g, st);
+        if (e != SPARBIT_OK) return e;
+        g.K = p->m;
+        g.in_hi = p->gram(0);
+        g.in_lo = p->gram(1);
+        g.ld_in = p->ldg();
+        g.z_in = p->zg();
+        g.out_hi = p->poly(0);
+        g.out_lo = p->poly(1);
+        e = product<kPoly>(p, p->ga[0], p->ga[1], p->gb[0], p->gb[1], g, st);
+        if (e != SPARBIT_OK) return e;
+        g.N = p->n;
+        g.in_hi = p->x(cur, 0);
+        g.in_lo = p->x(cur, 1);
+        g.in_full = p->full(cur);
+        g.out_full = p->full(cur ^ 1);
+        g.ld_in = g.ld_out = p->ldx();
+        g.z_in = g.z_out = p->zx();
+        g.out_hi = p->x(cur ^ 1, 0);
+        g.out_lo = p->x(cur ^ 1, 1);
+        e = end ? product<kLast>(p, p->pa[0], p->pa[1], p->xn[cur][0], p->xn[cur][1], g, st)
+                : product<kApply>(p, p->pa[0], p->pa[1], p->xn[cur][0], p->xn[cur][1], g, st);
+        if (e != SPARBIT_OK) return e;
+        cur ^= 1;
+    }
+    return SPARBIT_OK;
+}
+
+Region region(const sparbit_ortho_plan_s* p, const void* q, size_t es, size_t ld, size_t stride) {
+    // a batch laid out as one matrix of rows where its stride is a multiple of the pitch; the whole range otherwise
+    if (p->count == 1) return {q, p->rows, p->cols * es, ld * es};
+    if (stride % ld == 0) return {q, (stride / ld) * (p->count - 1) + p->rows, p->cols * es, ld * es};
+    return {q, 1, ((p->count - 1) * stride + (p->rows - 1) * ld + p->cols) * es, 0};
+}
+bool bad_layout(const sparbit_ortho_plan_s* p, size_t ld, size_t stride) {
+    return ld < p->cols || (p->count > 1 && stride < (p->rows - 1) * ld + p->cols);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sparbit_ortho_plan_create(int count, size_t rows, size_t cols, int dtype, int steps, const float* coefficients,
+                              float eps, sparbit_ortho_plan_t** out) {
+    if (!out) return SPARBIT_ERR_ARG;
+    *out = nullptr;
+    if (count < 1 || rows < 1 || cols < 1 || !known_dtype(dtype) || steps < 1 || !(eps >= 0.0f) || !isfinite(eps))
+        return SPARBIT_ERR_ARG;
+    if (rows > 65536 || cols > 65536 || steps > 64 || count > 4096) return SPARBIT_ERR_LIMIT;
+    sparbit_ortho_plan_s* p = new (std::nothrow) sparbit_ortho_plan_s();
+    if (!p) return SPARBIT_ERR_NOMEM;
+    bool ok = true;
+    try {
+        for (int i = 0; i < steps; i++)
+            p->steps.push_back(coefficients ? Step{coefficients[3 * i], coefficients[3 * i + 1], coefficients[3 * i + 2]}
+                                            : Step{3.4445f, -4.7750f, 2.0315f});
+        ok = bounded(p->steps);
+        p->count = count;
+        p->dtype = dtype;
+        p->rows = rows;
+        p->cols = cols;
+        p->transposed = rows > cols;
+        p->m = (int)(rows < cols ? rows : cols);
+        p->n = (int)(rows < cols ? cols : rows);
+        p->eps = eps;
+        const int tm = (p->m + kTileM - 1) / kTileM;
+        for (int i = 0; i < tm; i++)
+            for (int j = i * kTileM / kTileN; j * kTileN < p->m; j++) p->square.push_back((uint32_t)(i << 16 | j));
+        // column tiles in the outer loop: the CTAs that run together share the columns of X and walk down P
+        for (int j = 0; j * kTileN < p->n; j++)
+            for (int i = 0; i < tm; i++) p->wide.push_back((uint32_t)(i << 16 | j));
+    } catch (const std::bad_alloc&) {
+        delete p;
+        return SPARBIT_ERR_NOMEM;
+    }
+    const size_t most = 0x7fffffffu / (size_t)count;
+    if (!ok || p->wide.size() > most || p->square.size() > most) {
+        delete p;
+        return ok ? SPARBIT_ERR_LIMIT : SPARBIT_ERR_ARG;
+    }
+    *out = p;
+    return SPARBIT_OK;
+}
+
+int sparbit_ortho_plan_destroy(sparbit_ortho_plan_t* p) {
+    delete p;
+    return SPARBIT_OK;
+}
+
+int sparbit_ortho_plan_set_products(sparbit_ortho_plan_t* p, int products) {
+    if (!p || (products != SPARBIT_PRODUCTS_AUTO && products != SPARBIT_PRODUCTS_ONE && products != SPARBIT_PRODUCTS_THREE))
+        return SPARBIT_ERR_ARG;
+    p->products = products;
+    p->work = nullptr;  // the workspace's layout goes by it
+    return SPARBIT_OK;
+}
+
+size_t sparbit_ortho_plan_workspace_bytes(const sparbit_ortho_plan_t* p) { return p ? p->work_bytes() : 0; }
+
+int sparbit_ortho_plan_set_workspace(sparbit_ortho_plan_t* p, void* dev, size_t bytes) {
+    if (!p) return SPARBIT_ERR_ARG;
+    if (!dev || bytes < p->work_bytes() || (uintptr_t)dev % 16) return SPARBIT_ERR_WORKSPACE;
+    p->work = nullptr;
+    CU(cudaGetDevice(&p->device));
+    CU(cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device));
+    CU(cudaFuncSetAttribute(product_kernel<kGram>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    CU(cudaFuncSetAttribute(product_kernel<kPoly>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    CU(cudaFuncSetAttribute(product_kernel<kApply>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    CU(cudaFuncSetAttribute(product_kernel<kLast>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    CU(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found));
+    if (!fn || found != cudaDriverEntryPointSuccess)
+        return record_cuda_error((int)cudaErrorNotSupported, "cuTensorMapEncodeTiled");
+    p->work = (char*)dev;
+    const EncodeFn f = (EncodeFn)fn;
+    int e = SPARBIT_OK;
+    for (int lo = 0; lo < 2 && e == SPARBIT_OK; lo++) {
+        for (int b = 0; b < 2 && e == SPARBIT_OK; b++) {
+            e = encode(f, &p->xa[b][lo], p->x(b, lo), p->n, p->m, p->count, p->ldx(), p->zx(), kTileM);
+            if (e == SPARBIT_OK) e = encode(f, &p->xb[b][lo], p->x(b, lo), p->n, p->m, p->count, p->ldx(), p->zx(), kTileN);
+            if (e == SPARBIT_OK) e = encode(f, &p->xn[b][lo], p->x(b, lo), p->n, p->m, p->count, p->ldx(), p->zx(), kTileK);
+        }
+        if (e == SPARBIT_OK) e = encode(f, &p->ga[lo], p->gram(lo), p->m, p->m, p->count, p->ldg(), p->zg(), kTileM);
+        if (e == SPARBIT_OK) e = encode(f, &p->gb[lo], p->gram(lo), p->m, p->m, p->count, p->ldg(), p->zg(), kTileN);
+        if (e == SPARBIT_OK) e = encode(f, &p->pa[lo], p->poly(lo), p->m, p->m, p->count, p->ldg(), p->zg(), kTileM);
+    }
+    char* base = p->base();
+    p->work = nullptr;
+    if (e != SPARBIT_OK) return e;
+    CU(cudaMemset(base, 0, 256));
+    CU(cudaMemcpy(base + p->off_square(), p->square.data(), p->square.size() * 4, cudaMemcpyHostToDevice));
+    CU(cudaMemcpy(base + p->off_wide(), p->wide.data(), p->wide.size() * 4, cudaMemcpyHostToDevice));
+    CU(cudaDeviceSynchronize());
+    p->work = (char*)dev;
+    return SPARBIT_OK;
+}
+
+int sparbit_ortho_plan_status(sparbit_ortho_plan_t* p) {
+    if (!p) return SPARBIT_ERR_ARG;
+    const int e = ready(p);
+    if (e != SPARBIT_OK) return e;
+    CU(cudaDeviceSynchronize());
+    uint32_t word = 0;
+    CU(cudaMemcpy(&word, p->base(), 4, cudaMemcpyDeviceToHost));
+    if (word == 0) return SPARBIT_OK;
+    CU(cudaMemset(p->base(), 0, 4));
+    return SPARBIT_ERR_TIMEOUT;
+}
+
+int sparbit_orthogonalize(sparbit_ortho_plan_t* p, const void* update, size_t ld, size_t stride, void* out,
+                          size_t out_ld, size_t out_stride, void* stream) {
+    if (!p || !update || !out) return SPARBIT_ERR_ARG;
+    if (bad_layout(p, ld, stride) || bad_layout(p, out_ld, out_stride)) return SPARBIT_ERR_ARG;
+    const size_t es = elem_size(p->dtype);
+    const Region ro = region(p, out, es, out_ld, out_stride), rw{p->work, 1, p->work_bytes(), 0};
+    if (regions_overlap(ro, region(p, update, es, ld, stride)) || regions_overlap(ro, rw)) return SPARBIT_ERR_ALIAS;
+    const int e = ready(p);
+    if (e != SPARBIT_OK) return e;
+    PrepareArgs prep = {};
+    prep.update = Mat{(void*)update, (int64_t)ld, (int64_t)stride, p->dtype, false};
+    ProductArgs last = {};
+    last.out = Mat{out, (int64_t)out_ld, (int64_t)out_stride, p->dtype, wide_rows(out, es, out_ld, out_stride)};
+    last.transposed = p->transposed;
+    return iterate(p, prep, last, (cudaStream_t)stream);
+}
+
+int sparbit_muon_step(sparbit_ortho_plan_t* p, const sparbit_muon* a, void* stream) {
+    if (!p || !a || !a->grad || !a->momentum_in || !a->momentum_out || !a->weight_in || !a->weight_out)
+        return SPARBIT_ERR_ARG;
+    if (!known_dtype(a->weight_dtype)) return SPARBIT_ERR_ARG;
+    if (bad_layout(p, a->grad_ld, a->grad_stride) || bad_layout(p, a->momentum_ld, a->momentum_stride) ||
+        bad_layout(p, a->weight_ld, a->weight_stride))
+        return SPARBIT_ERR_ARG;
+    const size_t ws = elem_size(a->weight_dtype);
+    const Region rg = region(p, a->grad, elem_size(p->dtype), a->grad_ld, a->grad_stride),
+                 mi = region(p, a->momentum_in, 4, a->momentum_ld, a->momentum_stride),
+                 mo = region(p, a->momentum_out, 4, a->momentum_ld, a->momentum_stride),
+                 wi = region(p, a->weight_in, ws, a->weight_ld, a->weight_stride),
+                 wo = region(p, a->weight_out, ws, a->weight_ld, a->weight_stride), rw{p->work, 1, p->work_bytes(), 0};
+    if (regions_overlap(mo, rg) || regions_overlap(wo, rg) || regions_overlap(mo, wi) || regions_overlap(wo, mi) ||
+        regions_overlap(mo, wo) || regions_overlap(mo, rw) || regions_overlap(wo, rw) ||
+        (a->momentum_in != a->momentum_out && regions_overlap(mi, mo)) ||
+        (a->weight_in != a->weight_out && regions_overlap(wi, wo)))
+        return SPARBIT_ERR_ALIAS;
+    const int e = ready(p);
+    if (e != SPARBIT_OK) return e;
+    PrepareArgs prep = {};
+    prep.update = Mat{(void*)a->grad, (int64_t)a->grad_ld, (int64_t)a->grad_stride, p->dtype, false};
+    prep.mom_in = a->momentum_in;
+    prep.mom_out = a->momentum_out;
+    prep.mom_in_ld = prep.mom_out_ld = (int64_t)a->momentum_ld;
+    prep.mom_in_stride = prep.mom_out_stride = (int64_t)a->momentum_stride;
+    prep.mu = a->momentum;
+    prep.nesterov = a->nesterov;
+    ProductArgs last = {};
+    last.out = Mat{a->weight_out, (int64_t)a->weight_ld, (int64_t)a->weight_stride, a->weight_dtype,
+                   wide_rows(a->weight_out, ws, a->weight_ld, a->weight_stride)};
+    last.weight = Mat{(void*)a->weight_in, (int64_t)a->weight_ld, (int64_t)a->weight_stride, a->weight_dtype,
+                      wide_rows(a->weight_in, ws, a->weight_ld, a->weight_stride)};
+    last.transposed = p->transposed;
+    last.muon = 1;
+    last.keep = 1.0f - a->lr * a->weight_decay;
+    last.rate = a->lr * a->scale;
+    return iterate(p, prep, last, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -8,14 +8,26 @@ from __future__ import annotations
 
 import ctypes
 
-from .binding import _check, _i, _ptr, _stream_handle, _sz, _vp, lib
+from .binding import ERR_TIMEOUT, _check, _i, _ptr, _stream_handle, _sz, _vp, lib
 
 F32, BF16, F16 = range(3)
+PRODUCTS_AUTO, PRODUCTS_ONE, PRODUCTS_THREE = 0, 1, 3
 ROUTER_MAX_EXPERTS, ROUTER_MAX_K = 1024, 32
 
 _f = ctypes.c_float
 _ps = ctypes.POINTER(_sz)
 _pp = ctypes.POINTER(_vp)
+
+
+class MuonArgs(ctypes.Structure):
+    """sparbit_muon"""
+
+    _fields_ = [("grad", _vp), ("grad_ld", _sz), ("grad_stride", _sz), ("momentum_in", _vp), ("momentum_out", _vp),
+                ("momentum_ld", _sz), ("momentum_stride", _sz), ("weight_in", _vp), ("weight_out", _vp),
+                ("weight_ld", _sz), ("weight_stride", _sz), ("weight_dtype", _i), ("nesterov", _i), ("lr", _f),
+                ("momentum", _f), ("weight_decay", _f), ("scale", _f)]
+
+
 #: every symbol include/sparbit_train.h declares, with (restype, argtypes)
 SYMBOLS = {
     "sparbit_scan_plan_create": (_i, [_i, _ps, _sz, _i, _pp]),
@@ -27,6 +39,14 @@ SYMBOLS = {
     "sparbit_scan_backward": (_i, [_vp, _vp, _sz, _vp, _sz, _vp, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp]),
     "sparbit_scan_step": (_i, [_sz, _sz, _i, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _sz, _vp, _sz, _vp]),
     "sparbit_scan_join": (_i, [_i, _i, _i, _sz, _vp, _vp, _vp, _sz, _i, _vp]),
+    "sparbit_ortho_plan_create": (_i, [_i, _sz, _sz, _i, _i, ctypes.POINTER(_f), _f, _pp]),
+    "sparbit_ortho_plan_destroy": (_i, [_vp]),
+    "sparbit_ortho_plan_set_products": (_i, [_vp, _i]),
+    "sparbit_ortho_plan_workspace_bytes": (_sz, [_vp]),
+    "sparbit_ortho_plan_set_workspace": (_i, [_vp, _vp, _sz]),
+    "sparbit_ortho_plan_status": (_i, [_vp]),
+    "sparbit_orthogonalize": (_i, [_vp, _vp, _sz, _sz, _vp, _sz, _sz, _vp]),
+    "sparbit_muon_step": (_i, [_vp, ctypes.POINTER(MuonArgs), _vp]),
     "sparbit_router_plan_create": (_i, [_i, _ps, _i, _i, _i, _i, _pp]),
     "sparbit_router_plan_destroy": (_i, [_vp]),
     "sparbit_router_plan_workspace_bytes": (_sz, [_vp]),
@@ -154,3 +174,52 @@ class RouterPlan(_TrainPlan):
                                            _ptr(weights), _ptr(lse), _ptr(gathered), G, _ptr(dweights), alpha, beta,
                                            _ptr(dloss), _ptr(dlogits), dlogits_ld or self.experts,
                                            _stream_handle(stream)), "sparbit_router_backward")
+
+
+class OrthoPlan(_TrainPlan):
+    """`count` matrices of rows x cols, orthogonalised by Newton-Schulz products (sparbit_ortho_plan_create).
+    coefficients: `steps` triples (a, b, c), or None for the usual quintic.  Strides between matrices
+    default to rows * ld."""
+
+    _kind = "ortho"
+
+    def __init__(self, count: int, rows: int, cols: int, dtype: int = BF16, steps: int = 5, coefficients=None,
+                 eps: float = 1e-7, products: int = PRODUCTS_AUTO):
+        arr = None
+        if coefficients is not None:
+            flat = [float(v) for triple in coefficients for v in triple]
+            if len(flat) != 3 * steps:
+                raise ValueError(f"{steps} steps need {steps} triples of coefficients")
+            arr = (_f * len(flat))(*flat)
+        self._create(count, rows, cols, dtype, steps, arr, eps)
+        self.rows, self.cols = rows, cols
+        if products != PRODUCTS_AUTO:
+            self.set_products(products)
+
+    def set_products(self, products: int) -> None:
+        _check(lib.sparbit_ortho_plan_set_products(self._h, products), "sparbit_ortho_plan_set_products")
+
+    def status(self) -> int:
+        """Synchronises; OK or ERR_TIMEOUT (raises on other errors)."""
+        code = lib.sparbit_ortho_plan_status(self._h)
+        if code != ERR_TIMEOUT:
+            _check(code, "sparbit_ortho_plan_status")
+        return code
+
+    def orthogonalize(self, update, out, stream=None, ld=None, stride=None, out_ld=None, out_stride=None) -> None:
+        ld, out_ld = ld or self.cols, out_ld or self.cols
+        _check(lib.sparbit_orthogonalize(self._h, _ptr(update), ld, self.rows * ld if stride is None else stride,
+                                         _ptr(out), out_ld, self.rows * out_ld if out_stride is None else out_stride,
+                                         _stream_handle(stream)), "sparbit_orthogonalize")
+
+    def muon_step(self, grad, momentum_in, momentum_out, weight_in, weight_out, weight_dtype: int, lr: float,
+                  momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale: float = 1.0,
+                  stream=None, grad_ld=None, grad_stride=None, momentum_ld=None, momentum_stride=None, weight_ld=None,
+                  weight_stride=None) -> None:
+        gl, ml, wl = grad_ld or self.cols, momentum_ld or self.cols, weight_ld or self.cols
+        r = self.rows
+        args = MuonArgs(_ptr(grad), gl, r * gl if grad_stride is None else grad_stride, _ptr(momentum_in),
+                        _ptr(momentum_out), ml, r * ml if momentum_stride is None else momentum_stride,
+                        _ptr(weight_in), _ptr(weight_out), wl, r * wl if weight_stride is None else weight_stride,
+                        weight_dtype, int(bool(nesterov)), lr, momentum, weight_decay, scale)
+        _check(lib.sparbit_muon_step(self._h, ctypes.byref(args), _stream_handle(stream)), "sparbit_muon_step")

@@ -148,3 +148,43 @@ def test_router_refusals():
     refused(sp.ERR_ARG, plan.balance, None, 3, a[1], a[2], alpha=1.0)
     refused(sp.ERR_ARG, plan.balance, a[0], 0, a[1], a[2], alpha=1.0)
     refused(sp.ERR_ALIAS, plan.balance, a[0], 3, a[1], a[1], alpha=1.0)
+
+
+def test_ortho_refusals():
+    refused(sp.ERR_ARG, sp.OrthoPlan, 0, 8, 8)
+    refused(sp.ERR_ARG, sp.OrthoPlan, 1, 0, 8)
+    refused(sp.ERR_ARG, sp.OrthoPlan, 1, 8, 8, 9)
+    refused(sp.ERR_ARG, sp.OrthoPlan, 1, 8, 8, sp.F32, steps=0)
+    refused(sp.ERR_ARG, sp.OrthoPlan, 1, 8, 8, sp.F32, eps=-1.0)
+    refused(sp.ERR_ARG, sp.OrthoPlan, 1, 8, 8, sp.F32, eps=float("nan"))
+    refused(sp.ERR_LIMIT, sp.OrthoPlan, 1, 65537, 8)
+    refused(sp.ERR_LIMIT, sp.OrthoPlan, 4097, 8, 8)
+    refused(sp.ERR_LIMIT, sp.OrthoPlan, 1, 8, 8, steps=65)
+    # an iteration that diverges, and one whose polynomial does not fit the operands
+    refused(sp.ERR_ARG, sp.OrthoPlan, 1, 8, 8, steps=3, coefficients=[(4.0, 4.0, 4.0)] * 3)
+    refused(sp.ERR_ARG, sp.OrthoPlan, 1, 8, 8, steps=1, coefficients=[(1.0, 300.0, -300.0)])
+    refused(sp.ERR_ARG, sp.OrthoPlan, 1, 8, 8, steps=1, coefficients=[(float("nan"), 0.0, 0.0)])
+    sp.OrthoPlan(1, 8, 8, steps=2, coefficients=[(1.875, -1.25, 0.375)] * 2).destroy()
+    plan = sp.OrthoPlan(2, 64, 96, sp.BF16)
+    refused(sp.ERR_ARG, plan.set_products, 2)
+    a = [GPU_SIZED * (i + 1) for i in range(8)]
+    refused(sp.ERR_WORKSPACE, plan.set_workspace, a[0], 1024)
+    refused(sp.ERR_WORKSPACE, plan.orthogonalize, a[0], a[1])
+    refused(sp.ERR_WORKSPACE, plan.status)
+    refused(sp.ERR_ARG, plan.orthogonalize, None, a[1])
+    refused(sp.ERR_ARG, plan.orthogonalize, a[0], a[1], ld=95)
+    refused(sp.ERR_ARG, plan.orthogonalize, a[0], a[1], out_stride=64 * 96 - 1)
+    refused(sp.ERR_ALIAS, plan.orthogonalize, a[0], a[0])
+    refused(sp.ERR_ALIAS, plan.orthogonalize, a[0], a[0] + 2 * 64 * 96 * 2 - 2)
+    refused(sp.ERR_WORKSPACE, plan.orthogonalize, a[0], a[0] + 96 * 2, ld=192, out_ld=192)   # side by side
+    step = lambda **kw: plan.muon_step(**{**dict(grad=a[0], momentum_in=a[1], momentum_out=a[1], weight_in=a[2],  # noqa: E731
+                                                 weight_out=a[2], weight_dtype=sp.F32, lr=0.1), **kw})
+    refused(sp.ERR_WORKSPACE, step)
+    refused(sp.ERR_ARG, step, weight_dtype=4)
+    refused(sp.ERR_ARG, step, momentum_out=None)
+    refused(sp.ERR_ARG, step, momentum_ld=90)
+    refused(sp.ERR_ALIAS, step, momentum_out=a[2])
+    refused(sp.ERR_ALIAS, step, weight_out=a[2] + 4)
+    refused(sp.ERR_ALIAS, step, weight_out=a[0])
+    with pytest.raises(ValueError):
+        sp.OrthoPlan(1, 8, 8, steps=2, coefficients=[(1.0, 0.0, 0.0)])
