@@ -58,7 +58,7 @@ typedef struct sparbit_scan_plan_s sparbit_scan_plan_t;
 /*
  * lengths: host array of n_seqs counts, copied.  Errors: ERR_ARG (null, n_seqs < 1, channels < 1,
  * unknown type), ERR_OVERFLOW (rows x channels beyond 2^46), ERR_LIMIT (more than 2^20 channels,
- * 65535 sequences or 2^24 pieces of up to 128 rows), ERR_NOMEM.  Host-only.
+ * 65535 sequences or 2^30 pieces of up to 128 rows and 32 channels), ERR_NOMEM.  Host-only.
  */
 int sparbit_scan_plan_create(int n_seqs, const size_t* lengths, size_t channels, int dtype,
                              sparbit_scan_plan_t** out);
@@ -99,6 +99,15 @@ int sparbit_scan_forward(sparbit_scan_plan_t* plan, const void* gate, size_t gat
 int sparbit_scan_backward(sparbit_scan_plan_t* plan, const void* gate, size_t gate_ld, const void* x, size_t x_ld,
                           const float* carry, const void* dy, size_t dy_ld, const float* dlast, size_t dlast_ld,
                           void* dgate, size_t dgate_ld, void* dx, size_t dx_ld, float* dsummary, void* stream);
+
+/* Synchronises the device; SPARBIT_OK, or SPARBIT_ERR_TIMEOUT if a wait inside a kernel of the plan
+ * (for the state that an earlier piece of a sequence leaves) gave up since the last call; results of
+ * that launch are then incomplete. */
+int sparbit_scan_plan_status(sparbit_scan_plan_t* plan);
+
+/* Test hook for that bounded wait: with `withhold` set, later launches never publish the states that
+ * sequences of more than 2048 steps wait for, and give up after timeout_ns (0 = the default 2 s). */
+int sparbit_scan_plan_set_wait_test(sparbit_scan_plan_t* plan, int withhold, uint64_t timeout_ns);
 
 /*
  * One token for each of `rows` running sequences (serving).  Row i uses row slots[i] of the table

@@ -35,6 +35,8 @@ SYMBOLS = {
     "sparbit_scan_plan_workspace_bytes": (_sz, [_vp]),
     "sparbit_scan_plan_carry_bytes": (_sz, [_vp]),
     "sparbit_scan_plan_set_workspace": (_i, [_vp, _vp, _sz]),
+    "sparbit_scan_plan_status": (_i, [_vp]),
+    "sparbit_scan_plan_set_wait_test": (_i, [_vp, _i, ctypes.c_uint64]),
     "sparbit_scan_forward": (_i, [_vp, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _vp]),
     "sparbit_scan_backward": (_i, [_vp, _vp, _sz, _vp, _sz, _vp, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp]),
     "sparbit_scan_step": (_i, [_sz, _sz, _i, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _sz, _vp, _sz, _vp]),
@@ -82,6 +84,14 @@ class _TrainPlan:
         _check(getattr(lib, name)(self._h, _ptr(dev), nbytes), name)
         self._workspace = dev  # keep the owner alive
 
+    def status(self) -> int:
+        """Synchronises; OK or ERR_TIMEOUT (raises on other errors).  Plans with waits in their kernels."""
+        name = f"sparbit_{self._kind}_plan_status"
+        code = getattr(lib, name)(self._h)
+        if code != ERR_TIMEOUT:
+            _check(code, name)
+        return code
+
     def destroy(self) -> None:
         if getattr(self, "_h", None):
             h, self._h = self._h, None
@@ -115,6 +125,10 @@ class ScanPlan(_TrainPlan):
     @property
     def carry_bytes(self) -> int:
         return lib.sparbit_scan_plan_carry_bytes(self._h)
+
+    def set_wait_test(self, withhold: bool, timeout_ns: int = 0) -> None:
+        _check(lib.sparbit_scan_plan_set_wait_test(self._h, int(bool(withhold)), timeout_ns),
+               "sparbit_scan_plan_set_wait_test")
 
     def forward(self, gate, x, y, h0=None, summary=None, carry=None, stream=None, gate_ld=None, x_ld=None, y_ld=None,
                 h0_ld=None) -> None:
@@ -198,13 +212,6 @@ class OrthoPlan(_TrainPlan):
 
     def set_products(self, products: int) -> None:
         _check(lib.sparbit_ortho_plan_set_products(self._h, products), "sparbit_ortho_plan_set_products")
-
-    def status(self) -> int:
-        """Synchronises; OK or ERR_TIMEOUT (raises on other errors)."""
-        code = lib.sparbit_ortho_plan_status(self._h)
-        if code != ERR_TIMEOUT:
-            _check(code, "sparbit_ortho_plan_status")
-        return code
 
     def orthogonalize(self, update, out, stream=None, ld=None, stride=None, out_ld=None, out_stride=None) -> None:
         ld, out_ld = ld or self.cols, out_ld or self.cols

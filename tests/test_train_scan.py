@@ -347,6 +347,21 @@ def test_divided_by_time_over_ranks(P):
     assert zero.sum() == 0
 
 
+def test_a_wait_that_runs_out_is_reported():
+    """States withheld on purpose: the kernel gives up after the limit, says so, and works again afterwards."""
+    plan = with_workspace(sp.ScanPlan([5000], 64, sp.BF16))
+    c = {k: v.cuda() for k, v in case([5000], 64, "bf16").items()}
+    y, again = dev(5000, 64, dtype=torch.bfloat16), dev(5000, 64, dtype=torch.bfloat16)
+    plan.forward(c["gate"], c["x"], y)
+    assert plan.status() == sp.OK
+    plan.set_wait_test(True, 20_000_000)
+    plan.forward(c["gate"], c["x"], again)
+    assert plan.status() == sp.ERR_TIMEOUT
+    plan.set_wait_test(False)
+    plan.forward(c["gate"], c["x"], again)
+    assert plan.status() == sp.OK and torch.equal(y, again)
+
+
 def test_a_plan_without_workspace_or_on_no_buffer_is_refused():
     plan = sp.ScanPlan([10], 8, sp.F32)
     v = dev(10, 8)
