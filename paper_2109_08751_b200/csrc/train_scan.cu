@@ -28,7 +28,7 @@ constexpr int kThreads = 256;  // 16 runs of 8 steps (two channels a thread) or 
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
 // A piece in the order of one direction's chain.
-struct Piece {
+struct alignas(16) Piece {
     int64_t row0;
     int32_t seq, len;
     int32_t slot;   // where its pair is published; those of one chain follow one another
@@ -36,7 +36,7 @@ struct Piece {
     int32_t group;  // where the state behind its group is published
     int32_t last;   // it ends its chain
     int32_t carry;  // where the forward pass leaves the state that enters it; -1: no rows
-    int32_t pad;
+    int32_t pad[3];
 };
 
 // First words of the workspace.
@@ -44,29 +44,73 @@ struct Control {
     unsigned ticket, done, epoch, status;
 };
 
-// a = 1/(1+exp(-g)) and 1 - a, neither of them by cancellation.  Below -80 a is held at exp(-80);
-// NaN stays NaN.
-__device__ __forceinline__ void gate_pair(float g, float& a, float& keep) {
-    float c;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(g), "f"(-80.0f));
-    const float t = __expf(-c);
-    a = __fdividef(1.0f, 1.0f + t);
-    keep = t * a;
+// V channels of a thread; two of them go through the packed fp32 instructions of sm_100.
+template <int V>
+struct F {
+    float v[V];
+};
+__device__ __forceinline__ unsigned long long bits2(const F<2>& a) {
+    return (unsigned long long)__float_as_uint(a.v[1]) << 32 | __float_as_uint(a.v[0]);
+}
+__device__ __forceinline__ F<2> from_bits2(unsigned long long b) {
+    return F<2>{{__uint_as_float((unsigned)b), __uint_as_float((unsigned)(b >> 32))}};
+}
+__device__ __forceinline__ F<1> fma(const F<1>& a, const F<1>& b, const F<1>& c) { return {{fmaf(a.v[0], b.v[0], c.v[0])}}; }
+__device__ __forceinline__ F<1> mul(const F<1>& a, const F<1>& b) { return {{a.v[0] * b.v[0]}}; }
+__device__ __forceinline__ F<1> add(const F<1>& a, const F<1>& b) { return {{a.v[0] + b.v[0]}}; }
+__device__ __forceinline__ F<2> fma(const F<2>& a, const F<2>& b, const F<2>& c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+    return from_bits2(d);
+}
+__device__ __forceinline__ F<2> mul(const F<2>& a, const F<2>& b) {
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+    return from_bits2(d);
+}
+__device__ __forceinline__ F<2> add(const F<2>& a, const F<2>& b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+    return from_bits2(d);
+}
+template <int V>
+__device__ __forceinline__ F<V> all(float x) {
+    F<V> f;
+#pragma unroll
+    for (int i = 0; i < V; i++) f.v[i] = x;
+    return f;
+}
+
+// a = 1/(1+exp(-g)) and 1 - a, neither of them by cancellation: with t = exp(-g), a = 1/(1+t) and
+// 1 - a = t a.  t is held at 2^115, so that t a stays 1 for gates below -80; NaN stays NaN.
+template <int V>
+__device__ __forceinline__ void gate_pair(const F<V>& g, F<V>& a, F<V>& keep) {
+    F<V> t = mul(g, all<V>(-1.4426950408889634f));
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        asm("min.NaN.f32 %0, %0, %1;" : "+f"(t.v[i]) : "f"(115.0f));
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.v[i]));
+    }
+    a = add(t, all<V>(1.0f));
+#pragma unroll
+    for (int i = 0; i < V; i++) asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a.v[i]));
+    keep = mul(t, a);
 }
 
 template <typename T, int V>
-__device__ __forceinline__ void load_row(const T* p, int64_t row, int64_t ld, int channel, bool on, float (&out)[V]) {
-    Pack<T, V> v;
-    if (on) v = *reinterpret_cast<const Pack<T, V>*>(p + row * ld + channel);
+__device__ __forceinline__ F<V> unpack(const T* p) {
+    const Pack<T, V> k = *reinterpret_cast<const Pack<T, V>*>(p);
+    F<V> f;
 #pragma unroll
-    for (int i = 0; i < V; i++) out[i] = on ? to_float(v.v[i]) : 0.0f;
+    for (int i = 0; i < V; i++) f.v[i] = to_float(k.v[i]);
+    return f;
 }
 template <typename T, int V>
-__device__ __forceinline__ void store_row(T* p, int64_t row, int64_t ld, int channel, const float (&in)[V]) {
-    Pack<T, V> v;
+__device__ __forceinline__ void pack(T* p, const F<V>& f) {
+    Pack<T, V> k;
 #pragma unroll
-    for (int i = 0; i < V; i++) v.v[i] = from_float<T>(in[i]);
-    *reinterpret_cast<Pack<T, V>*>(p + row * ld + channel) = v;
+    for (int i = 0; i < V; i++) k.v[i] = from_float<T>(f.v[i]);
+    *reinterpret_cast<Pack<T, V>*>(p) = k;
 }
 
 // ---- published words ----------------------------------------------------------------------------
@@ -129,40 +173,41 @@ struct ScanArgs {
 };
 
 // Row t of a staged tensor; a pad of one row every 8 keeps the two runs of a warp in different banks.
-__device__ __forceinline__ int stage_row(int t) {
-    return (t + (t >> 3)) * kTile;
-}
+__device__ __forceinline__ int stage_row(int t) { return (t + (t >> 3)) * kTile; }
 constexpr int kStageElems = (kPiece + kPiece / 8) * kTile;  // of one tensor
 
 // Starts the copy of a piece's rows of one tensor into shared memory.
 template <typename T>
-__device__ __forceinline__ void stage_tensor(T* dst, const T* src, int64_t ld, const Piece& pc, int ch0, int D,
+__device__ __forceinline__ void stage_tensor(T* dst, const T* src, int64_t ld, int64_t row0, int len, int ch0, int D,
                                              bool wide) {
-    constexpr int kPer = 16 / sizeof(T), kChunks = kTile / kPer;
+    constexpr int kPer = 16 / sizeof(T), kChunks = kTile / kPer, kRows = kThreads / kChunks;
     if (wide) {
+        const int t0 = threadIdx.x / kChunks, e = threadIdx.x % kChunks * kPer, left = D - ch0 - e;
+        if (left <= 0) return;
+        const int bytes = left < kPer ? left * (int)sizeof(T) : 16;  // the rest becomes zero
+        const T* from = src + (row0 + t0) * ld + ch0 + e;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + stage_row(t0) + e);
+        static_assert(kRows % 8 == 0, "whole groups of 8 rows between the copies of a thread");
 #pragma unroll
-        for (int c = threadIdx.x; c < kPiece * kChunks; c += kThreads) {
-            const int t = c / kChunks, e = (c % kChunks) * kPer, left = D - ch0 - e;
-            if (t < pc.len && left > 0) {
-                const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + stage_row(t) + e);
-                const int bytes = left < kPer ? left * (int)sizeof(T) : 16;  // the rest becomes zero
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to),
-                             "l"(src + (pc.row0 + t) * ld + ch0 + e), "r"(bytes)
+        for (int i = 0; i < kPiece / kRows; i++) {
+            if (t0 + i * kRows < len)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                 to + (uint32_t)(i * (kRows + kRows / 8) * kTile * sizeof(T))),
+                             "l"(from), "r"(bytes)
                              : "memory");
-            }
+            from += kRows * ld;
         }
     } else {
-        for (int c = threadIdx.x; c < kPiece * kTile; c += kThreads) {
-            const int t = c / kTile, e = c % kTile;
-            if (t < pc.len && ch0 + e < D) dst[stage_row(t) + e] = src[(pc.row0 + t) * ld + ch0 + e];
+        // one channel a lane, as many rows a step as there are warps
+        const int e = threadIdx.x % kTile;
+        if (ch0 + e >= D) return;
+        const T* from = src + (row0 + threadIdx.x / kTile) * ld + ch0 + e;
+#pragma unroll 8
+        for (int t = threadIdx.x / kTile; t < len; t += kThreads / kTile) {
+            dst[stage_row(t) + e] = *from;
+            from += kThreads / kTile * ld;
         }
     }
-}
-template <typename T, int V>
-__device__ __forceinline__ void staged(const T* row, int e, float (&out)[V]) {
-    const Pack<T, V> v = *reinterpret_cast<const Pack<T, V>*>(row + e);
-#pragma unroll
-    for (int i = 0; i < V; i++) out[i] = to_float(v.v[i]);
 }
 
 // What a CTA learns about the state that enters its piece.
@@ -172,8 +217,8 @@ struct Shared {
     float enter[kTile];
     float hold[kThreads * 2 / kTile][kTile];   // backward: states at the start of each run
     float2 after[kThreads * 2 / kTile][kTile]; // backward: what the runs behind make of the entering gradient
-    Piece piece[2];
-    int ticket[2];
+    Piece piece[4];
+    int ticket[4];
     unsigned epoch;
 };
 
@@ -238,22 +283,21 @@ __device__ __forceinline__ float enter_piece(const ScanArgs& g, const Piece& pc,
     return h;
 }
 
-// Tickets, kept by thread 0 one tile ahead of the copies: the counter's and the list's latency pass
-// while a tile is worked on.
-struct Next {
-    int ticket;
-    Piece piece;
-};
-__device__ __forceinline__ void draw_ticket(const ScanArgs& g, Next& n) {
-    if (threadIdx.x == 0) n.ticket = (int)atomicAdd(&g.ctl->ticket, 1u);
+// Tickets n, n + 1 and n + 2 (n: the tile worked on, n + 1: its copies under way) live in slots of
+// s.ticket and s.piece; thread 0 draws one and starts the copy of its entry of the list while a tile is
+// worked on, so that neither latency is waited for.
+__device__ __forceinline__ int draw_ticket(const ScanArgs& g) {
+    return threadIdx.x == 0 ? (int)atomicAdd(&g.ctl->ticket, 1u) : 0;
 }
-__device__ __forceinline__ void read_piece(const ScanArgs& g, Next& n) {
-    if (threadIdx.x == 0 && n.ticket < g.total) n.piece = g.pieces[n.ticket / g.tiles];
-}
-__device__ __forceinline__ void post_ticket(const Next& n, Shared& s, int i) {
-    if (threadIdx.x == 0) {
-        s.ticket[i] = n.ticket;
-        s.piece[i] = n.piece;
+__device__ __forceinline__ void post_ticket(const ScanArgs& g, Shared& s, int slot, int ticket) {
+    if (threadIdx.x != 0) return;
+    s.ticket[slot] = ticket;
+    if (ticket < g.total) {
+        const char* from = (const char*)(g.pieces + ticket / g.tiles);
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(&s.piece[slot]);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(Piece); i += 16)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to + i), "l"(from + i) : "memory");
     }
 }
 __device__ __forceinline__ void finish(const ScanArgs& g) {
@@ -275,73 +319,72 @@ constexpr int kStagesOf = sizeof(T) == 4 ? 1 : 2;
 
 // Starts the copies of a piece: gate and x, gate and dy, or all three.
 template <typename T, int kTensors>
-__device__ __forceinline__ void stage_piece(const ScanArgs& g, T* buf, const Piece& pc, int ch0, bool against_time) {
-    stage_tensor<T>(buf, (const T*)g.gate, g.gate_ld, pc, ch0, g.D, g.wide);
+__device__ __forceinline__ void stage_piece(const ScanArgs& g, T* buf, const Shared& s, int slot, bool against_time) {
+    const int64_t row0 = s.piece[slot].row0;
+    const int len = s.piece[slot].len, ch0 = s.ticket[slot] % g.tiles * kTile;
+    stage_tensor<T>(buf, (const T*)g.gate, g.gate_ld, row0, len, ch0, g.D, g.wide);
     if (kTensors == 3 || !against_time)
-        stage_tensor<T>(buf + kStageElems, (const T*)g.x, g.x_ld, pc, ch0, g.D, g.wide);
+        stage_tensor<T>(buf + kStageElems, (const T*)g.x, g.x_ld, row0, len, ch0, g.D, g.wide);
     if (against_time)
-        stage_tensor<T>(buf + (kTensors - 1) * kStageElems, (const T*)g.dy, g.dy_ld, pc, ch0, g.D, g.wide);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+        stage_tensor<T>(buf + (kTensors - 1) * kStageElems, (const T*)g.dy, g.dy_ld, row0, len, ch0, g.D, g.wide);
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// What both kernels begin with; returns this launch's tag.
+template <typename T, int kTensors>
+__device__ __forceinline__ unsigned begin(const ScanArgs& g, T* stages, Shared& s, bool against_time) {
+    pdl_wait();
+    pdl_trigger();
+    post_ticket(g, s, 0, draw_ticket(g));
+    post_ticket(g, s, 1, draw_ticket(g));
+    if (threadIdx.x == 0) s.epoch = g.ctl->epoch;
+    copies_wait();
+    __syncthreads();
+    if (kStagesOf<T> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors>(g, stages, s, 0, against_time);
+    return s.epoch;
 }
 
 // ---- forward (kBack: only what the pieces do to a gradient, for a summary against time) ------------
 template <typename T, int V, bool kBack>
 __global__ void __launch_bounds__(kThreads, 4) scan_forward_kernel(const __grid_constant__ ScanArgs g) {
-    constexpr int kLanes = kTile / V, kRuns = kThreads / kLanes, R = kPiece / kRuns;
+    constexpr int kLanes = kTile / V, kRuns = kThreads / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
     T* stages = reinterpret_cast<T*>(raw);
-    pdl_wait();
-    pdl_trigger();
-    Next next;
-    next.piece = Piece{};
-    draw_ticket(g, next);
-    read_piece(g, next);
-    post_ticket(next, s, 0);
-    if (threadIdx.x == 0) s.epoch = g.ctl->epoch;
-    draw_ticket(g, next);
-    read_piece(g, next);
-    __syncthreads();
-    const unsigned tag = s.epoch;
+    const unsigned tag = begin<T, 2>(g, stages, s, kBack);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int S = kStagesOf<T>;
-    int cur = 0;
-    if (S == 2 && s.ticket[0] < g.total)
-        stage_piece<T, 2>(g, stages, s.piece[0], s.ticket[0] % g.tiles * kTile, kBack);
-    for (; s.ticket[cur] < g.total; cur ^= 1) {
-        if (S == 1) stage_piece<T, 2>(g, stages, s.piece[cur], s.ticket[cur] % g.tiles * kTile, kBack);
-        post_ticket(next, s, cur ^ 1);
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    for (int n = 0; s.ticket[n & 3] < g.total; n++) {
+        if (S == 1) stage_piece<T, 2>(g, stages, s, n & 3, kBack);
+        copies_wait();
         __syncthreads();
-        draw_ticket(g, next);
-        const Piece pc = s.piece[cur];
-        const int tile = s.ticket[cur] % g.tiles, ch = tile * kTile + e;
-        if (S == 2 && s.ticket[cur ^ 1] < g.total)
-            stage_piece<T, 2>(g, stages + (cur ^ 1) * 2 * kStageElems, s.piece[cur ^ 1],
-                              s.ticket[cur ^ 1] % g.tiles * kTile, kBack);
-        const T* in0 = stages + (S == 2 ? cur : 0) * 2 * kStageElems;
+        const int drawn = draw_ticket(g);
+        if (S == 2 && s.ticket[(n + 1) & 3] < g.total)
+            stage_piece<T, 2>(g, stages + ((n + 1) & 1) * 2 * kStageElems, s, (n + 1) & 3, kBack);
+        const Piece& pc = s.piece[n & 3];
+        const int tile = s.ticket[n & 3] % g.tiles, len = pc.len;
+        const T* in0 = stages + (S == 2 ? n & 1 : 0) * 2 * kStageElems + stage_row(run * R) + e;
         const T* in1 = in0 + kStageElems;
-        float a[R][V], b[R][V], A[V], H[V];
-#pragma unroll
-        for (int i = 0; i < V; i++) A[i] = 1.0f, H[i] = 0.0f;
+        F<V> a[R], b[R], A = all<V>(1.0f), H = all<V>(0.0f);
 #pragma unroll
         for (int j = 0; j < R; j++) {
-            const int t = run * R + j;
-            staged<T, V>(in0 + stage_row(t), e, a[j]);
-            staged<T, V>(in1 + stage_row(t), e, b[j]);
+            F<V> keep;
+            gate_pair(unpack<T, V>(in0 + stage_row(j)), a[j], keep);
+            b[j] = unpack<T, V>(in1 + stage_row(j));
+            if (!kBack) b[j] = mul(b[j], keep);
+        }
+        if (len < kPiece) {  // steps past the end change nothing
 #pragma unroll
-            for (int i = 0; i < V; i++) {
-                float keep;
-                gate_pair(a[j][i], a[j][i], keep);
-                if (!kBack) b[j][i] *= keep;
-                if (t >= pc.len) a[j][i] = 1.0f, b[j][i] = 0.0f;
-                A[i] *= a[j][i];
-                // against time the map is built front to back: this step's dy seen through the steps before
-                H[i] = kBack ? H[i] + A[i] * b[j][i] : a[j][i] * H[i] + b[j][i];
-            }
+            for (int j = 0; j < R; j++)
+                if (run * R + j >= len) a[j] = all<V>(1.0f), b[j] = all<V>(0.0f);
         }
 #pragma unroll
-        for (int i = 0; i < V; i++) s.run[run][e + i] = make_float2(A[i], H[i]);
+        for (int j = 0; j < R; j++) {
+            A = mul(A, a[j]);
+            // against time the map is built front to back: this step's dy seen through the steps before
+            H = kBack ? fma(A, b[j], H) : fma(a[j], H, b[j]);
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) s.run[run][e + i] = make_float2(A.v[i], H.v[i]);
         const Looked seen = look_back(g, pc, tile);
         __syncthreads();
         float2 own = make_float2(1.0f, 0.0f);
@@ -357,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 4) scan_forward_kernel(const __grid_
             publish(g.pairs + ((int64_t)pc.slot * g.tiles + tile) * kTile + lane, own.x, own.y, tag);
         }
         settle(g, pc, tile, seen, tag, s);
-        read_piece(g, next);
+        post_ticket(g, s, (n + 2) & 3, drawn);
         __syncthreads();
         if (warp == 0) {
             const float h = enter_piece(g, pc, tile, own, tag, s);
@@ -366,16 +409,24 @@ __global__ void __launch_bounds__(kThreads, 4) scan_forward_kernel(const __grid_
                 g.carry[(int64_t)pc.carry * g.D + tile * kTile + lane] = h;
         }
         __syncthreads();
+        const int ch = tile * kTile + e;
         if (!kBack && g.y && ch < g.D) {
-            float h[V];
+            F<V> h;
 #pragma unroll
-            for (int i = 0; i < V; i++) h[i] = s.run[run][e + i].x * s.enter[e + i] + s.run[run][e + i].y;
+            for (int i = 0; i < V; i++) h.v[i] = s.run[run][e + i].x * s.enter[e + i] + s.run[run][e + i].y;
             T* y = (T*)g.y + (pc.row0 + run * R) * g.y_ld + ch;
+            if (len == kPiece) {
 #pragma unroll
-            for (int j = 0; j < R; j++) {
+                for (int j = 0; j < R; j++, y += g.y_ld) {
+                    h = fma(a[j], h, b[j]);
+                    pack<T, V>(y, h);
+                }
+            } else {
 #pragma unroll
-                for (int i = 0; i < V; i++) h[i] = a[j][i] * h[i] + b[j][i];
-                if (run * R + j < pc.len) store_row<T, V>(y, j, g.y_ld, 0, h);
+                for (int j = 0; j < R; j++, y += g.y_ld) {
+                    h = fma(a[j], h, b[j]);
+                    if (run * R + j < len) pack<T, V>(y, h);
+                }
             }
         }
     }
@@ -385,86 +436,55 @@ __global__ void __launch_bounds__(kThreads, 4) scan_forward_kernel(const __grid_
 // ---- backward -------------------------------------------------------------------------------------
 // The states of the piece are computed again from the one that the forward pass left at its start.
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) scan_backward_kernel(const __grid_constant__ ScanArgs g) {
-    constexpr int kLanes = kTile / V, kRuns = kThreads / kLanes, R = kPiece / kRuns;
+__global__ void __launch_bounds__(kThreads, 3) scan_backward_kernel(const __grid_constant__ ScanArgs g) {
+    constexpr int kLanes = kTile / V, kRuns = kThreads / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
     T* stages = reinterpret_cast<T*>(raw);
-    pdl_wait();
-    pdl_trigger();
-    Next next;
-    next.piece = Piece{};
-    draw_ticket(g, next);
-    read_piece(g, next);
-    post_ticket(next, s, 0);
-    if (threadIdx.x == 0) s.epoch = g.ctl->epoch;
-    draw_ticket(g, next);
-    read_piece(g, next);
-    __syncthreads();
-    const unsigned tag = s.epoch;
+    const unsigned tag = begin<T, 3>(g, stages, s, true);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int S = kStagesOf<T>;
-    int cur = 0;
-    if (S == 2 && s.ticket[0] < g.total)
-        stage_piece<T, 3>(g, stages, s.piece[0], s.ticket[0] % g.tiles * kTile, true);
-    for (; s.ticket[cur] < g.total; cur ^= 1) {
+    for (int n = 0; s.ticket[n & 3] < g.total; n++) {
         if (S == 1) {
             __syncthreads();  // the last piece's dy has been read
-            stage_piece<T, 3>(g, stages, s.piece[cur], s.ticket[cur] % g.tiles * kTile, true);
+            stage_piece<T, 3>(g, stages, s, n & 3, true);
         }
-        post_ticket(next, s, cur ^ 1);
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        copies_wait();
         __syncthreads();
-        draw_ticket(g, next);
-        const Piece pc = s.piece[cur];
-        const int tile = s.ticket[cur] % g.tiles, ch = tile * kTile + e;
-        if (S == 2 && s.ticket[cur ^ 1] < g.total)
-            stage_piece<T, 3>(g, stages + (cur ^ 1) * 3 * kStageElems, s.piece[cur ^ 1],
-                              s.ticket[cur ^ 1] % g.tiles * kTile, true);
-        const T* in_g = stages + (S == 2 ? cur : 0) * 3 * kStageElems;
+        const int drawn = draw_ticket(g);
+        if (S == 2 && s.ticket[(n + 1) & 3] < g.total)
+            stage_piece<T, 3>(g, stages + ((n + 1) & 1) * 3 * kStageElems, s, (n + 1) & 3, true);
+        const Piece& pc = s.piece[n & 3];
+        const int tile = s.ticket[n & 3] % g.tiles, len = pc.len;
+        const T* in_g = stages + (S == 2 ? n & 1 : 0) * 3 * kStageElems + stage_row(run * R) + e;
         const T* in_x = in_g + kStageElems;
         const T* in_d = in_x + kStageElems;
         float carried = 0.0f;
         if (warp == 1 && pc.carry >= 0 && tile * kTile + lane < g.D)
             carried = g.carry[(int64_t)pc.carry * g.D + tile * kTile + lane];
-        float a[R][V], k[R][V], A[V], H[V], G[V];
+        F<V> a[R], k[R], A = all<V>(1.0f), H = all<V>(0.0f), G = all<V>(0.0f);
 #pragma unroll
-        for (int i = 0; i < V; i++) A[i] = 1.0f, H[i] = 0.0f, G[i] = 0.0f;
+        for (int j = 0; j < R; j++) gate_pair(unpack<T, V>(in_g + stage_row(j)), a[j], k[j]);
+        if (len < kPiece) {
+#pragma unroll
+            for (int j = 0; j < R; j++)
+                if (run * R + j >= len) a[j] = all<V>(1.0f), k[j] = all<V>(0.0f);
+        }
 #pragma unroll
         for (int j = 0; j < R; j++) {
-            const int t = run * R + j;
-            float x[V], d[V];
-            staged<T, V>(in_g + stage_row(t), e, a[j]);
-            staged<T, V>(in_x + stage_row(t), e, x);
-            staged<T, V>(in_d + stage_row(t), e, d);
-            const bool on = t < pc.len;
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                gate_pair(a[j][i], a[j][i], k[j][i]);
-                if (!on) a[j][i] = 1.0f, k[j][i] = x[i] = d[i] = 0.0f;
-                A[i] *= a[j][i];
-                H[i] = a[j][i] * H[i] + k[j][i] * x[i];
-                // the map of a gradient, front to back: this step's dy seen through the steps before
-                G[i] += A[i] * d[i];
-            }
+            if (run * R + j >= len) break;  // what is staged there may be anything
+            A = mul(A, a[j]);
+            H = fma(a[j], H, mul(k[j], unpack<T, V>(in_x + stage_row(j))));
+            // the map of a gradient, front to back: this step's dy seen through the steps before
+            G = fma(A, unpack<T, V>(in_d + stage_row(j)), G);
         }
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            s.run[run][e + i] = make_float2(A[i], G[i]);
-            s.hold[run][e + i] = H[i];
+            s.run[run][e + i] = make_float2(A.v[i], G.v[i]);
+            s.hold[run][e + i] = H.v[i];
         }
         const Looked seen = look_back(g, pc, tile);
         __syncthreads();
         float2 own = make_float2(1.0f, 0.0f);
-        if (warp == 1) {  // states at the start of each run
-            float h = carried;
-#pragma unroll
-            for (int u = 0; u < kRuns; u++) {
-                const float next = s.run[u][lane].x * h + s.hold[u][lane];
-                s.hold[u][lane] = h;
-                h = next;
-            }
-        }
         if (warp == 0) {
 #pragma unroll
             for (int u = kRuns - 1; u >= 0; u--) {
@@ -475,46 +495,44 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) scan_backwar
             }
             publish(g.pairs + ((int64_t)pc.slot * g.tiles + tile) * kTile + lane, own.x, own.y, tag);
         }
-        __syncthreads();
-        // (h_{t-1} - x_t) a_t (1 - a_t), while the words travel
-        float f[R][V], h[V];
+        if (warp == 1) {  // states at the start of each run
+            float h = carried;
 #pragma unroll
-        for (int i = 0; i < V; i++) h[i] = s.hold[run][e + i];
-#pragma unroll
-        for (int j = 0; j < R; j++) {
-            float x[V];
-            staged<T, V>(in_x + stage_row(run * R + j), e, x);
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                f[j][i] = (h[i] - x[i]) * a[j][i] * k[j][i];
-                h[i] = a[j][i] * h[i] + k[j][i] * x[i];
+            for (int u = 0; u < kRuns; u++) {
+                const float next = s.run[u][lane].x * h + s.hold[u][lane];
+                s.hold[u][lane] = h;
+                h = next;
             }
         }
         settle(g, pc, tile, seen, tag, s);
-        read_piece(g, next);
+        post_ticket(g, s, (n + 2) & 3, drawn);
         __syncthreads();
         if (warp == 0) s.enter[lane] = enter_piece(g, pc, tile, own, tag, s);
+        // (h_{t-1} - x_t) a_t (1 - a_t), while the first warp works out what enters
+        F<V> f[R], h;
+#pragma unroll
+        for (int i = 0; i < V; i++) h.v[i] = s.hold[run][e + i];
+#pragma unroll
+        for (int j = 0; j < R; j++) {
+            const F<V> x = unpack<T, V>(in_x + stage_row(j)), ak = mul(a[j], k[j]);
+            f[j] = mul(fma(x, all<V>(-1.0f), h), ak);
+            h = fma(a[j], h, mul(k[j], x));
+        }
         __syncthreads();
+        const int ch = tile * kTile + e;
         if (ch < g.D) {
-            float c[V];
+            F<V> c;
 #pragma unroll
-            for (int i = 0; i < V; i++) c[i] = s.after[run][e + i].x * s.enter[e + i] + s.after[run][e + i].y;
-            T* dg = (T*)g.dgate + (pc.row0 + run * R) * g.dgate_ld + ch;
-            T* dx = (T*)g.dx + (pc.row0 + run * R) * g.dx_ld + ch;
+            for (int i = 0; i < V; i++) c.v[i] = s.after[run][e + i].x * s.enter[e + i] + s.after[run][e + i].y;
+            T* dg = (T*)g.dgate + (pc.row0 + run * R + R - 1) * g.dgate_ld + ch;
+            T* dx = (T*)g.dx + (pc.row0 + run * R + R - 1) * g.dx_ld + ch;
 #pragma unroll
-            for (int j = R - 1; j >= 0; j--) {
-                if (run * R + j >= pc.len) continue;
-                float d[V];
-                staged<T, V>(in_d + stage_row(run * R + j), e, d);
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    const float q = d[i] + c[i];
-                    f[j][i] *= q;
-                    c[i] = a[j][i] * q;
-                    k[j][i] *= q;
-                }
-                store_row<T, V>(dg, j, g.dgate_ld, 0, f[j]);
-                store_row<T, V>(dx, j, g.dx_ld, 0, k[j]);
+            for (int j = R - 1; j >= 0; j--, dg -= g.dgate_ld, dx -= g.dx_ld) {
+                if (run * R + j >= len) continue;
+                const F<V> q = add(unpack<T, V>(in_d + stage_row(j)), c);
+                c = mul(a[j], q);
+                pack<T, V>(dg, mul(f[j], q));
+                pack<T, V>(dx, mul(k[j], q));
             }
         }
     }
@@ -531,19 +549,13 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const T* gate, int64_t g
     const int ch = (blockIdx.y * 128 + threadIdx.x) * V;
     if (ch >= D) return;
     const int64_t slot = slots ? slots[row] : row;
-    float g[V], v[V], h[V];
-    load_row<T, V>(gate, row, gate_ld, ch, true, g);
-    load_row<T, V>(x, row, x_ld, ch, true, v);
-    const bool on = slot >= 0 && slot < n_slots;
-    load_row<float, V>(state_in, on ? slot : 0, state_ld, ch, on, h);
-#pragma unroll
-    for (int i = 0; i < V; i++) {
-        float a, keep;
-        gate_pair(g[i], a, keep);
-        h[i] = on ? a * h[i] + keep * v[i] : 0.0f;
+    F<V> a, keep, y_row = all<V>(0.0f);
+    if (slot >= 0 && slot < n_slots) {
+        gate_pair(unpack<T, V>(gate + row * gate_ld + ch), a, keep);
+        y_row = fma(a, unpack<float, V>(state_in + slot * state_ld + ch), mul(keep, unpack<T, V>(x + row * x_ld + ch)));
+        pack<float, V>(state_out + slot * state_ld + ch, y_row);
     }
-    if (on) store_row<float, V>(state_out, slot, state_ld, ch, h);
-    store_row<T, V>(y, row, y_ld, ch, h);
+    pack<T, V>(y + row * y_ld + ch, y_row);
 }
 
 __global__ void __launch_bounds__(128) scan_join_kernel(int P, int first_rank, int D, const float* gathered,
@@ -678,7 +690,7 @@ int sparbit_scan_plan_create(int n_seqs, const size_t* lengths, size_t channels,
                     const int32_t q = back ? n - 1 - i : i;
                     const size_t t = (size_t)q * kPiece, left = lengths[s] - t;
                     chains[back].push_back(Piece{row + (int64_t)t, s, (int32_t)(left < kPiece ? left : kPiece), slot + i, i,
-                                                 group + i / kGroup, i == n - 1, lengths[s] ? carry + q : -1, 0});
+                                                 group + i / kGroup, i == n - 1, lengths[s] ? carry + q : -1, {}});
                 }
             }
             slot += n;
