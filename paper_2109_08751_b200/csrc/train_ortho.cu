@@ -37,7 +37,7 @@ constexpr int kThreads = 320;  // warp 0 loads, warp 1 multiplies, warps 2-9 wri
 // The tensor cores cut each partial sum towards zero: over K = 4096 a relative error of 1e-5, which
 // three products would not survive.  They hand over every 256 of K to a sum rounded in registers.
 constexpr int kFlush = 4;
-constexpr int kSmem = kStages * kStageBytes + 1024;
+constexpr int kSmem = kStages * kStageBytes + 8 * 32 * 33 * 4 + 1024;  // ring, a block for each warp that writes, alignment
 constexpr int kNormParts = 256;                         // CTAs a matrix's norm is summed by
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;   // X and A, P are held times these
 constexpr unsigned long long kWaitNs = 2000000000ull;   // a wait inside the kernel gives up after this
@@ -109,21 +109,18 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
-    uint32_t r[32];
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
+    uint32_t r[16];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
         "tcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr)
         : "memory");
 #pragma unroll
-    for (int i = 0; i < 32; i++) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 16; i++) v[i] = __uint_as_float(r[i]);
 }
 
 // ---- arguments ----------------------------------------------------------------------------------
@@ -170,124 +167,141 @@ __device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
     lo = __float2half_rn(v - __half2float(hi));
 }
 
-// 32 values that follow one another, at any alignment (wide: 16-byte aligned); `step` elements apart
+// Four values of a row, the first n of them inside the matrix; `wide`: every row starts on a multiple
+// of 16 bytes and c on a multiple of four elements, so that four values are 8 or 16 aligned bytes.
 template <typename T>
-__device__ __forceinline__ void read32(const T* p, bool wide, int64_t step, int n, float (&v)[32]) {
-    constexpr int kPer = 16 / sizeof(T);
-    if (wide && n >= 32) {
+__device__ __forceinline__ void read4(const T* p, bool wide, int n, float (&v)[4]) {
+    if (wide && n >= 4) {
+        const Pack<T, 4> k = *reinterpret_cast<const Pack<T, 4>*>(p);
 #pragma unroll
-        for (int i = 0; i < 32 / kPer; i++) {
-            const Pack<T, kPer> k = reinterpret_cast<const Pack<T, kPer>*>(p)[i];
-#pragma unroll
-            for (int u = 0; u < kPer; u++) v[i * kPer + u] = to_float(k.v[u]);
-        }
+        for (int i = 0; i < 4; i++) v[i] = to_float(k.v[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; i++) v[i] = i < n ? to_float(p[i * step]) : 0.0f;
+        for (int i = 0; i < 4; i++) v[i] = i < n ? to_float(p[i]) : 0.0f;
     }
 }
 template <typename T>
-__device__ __forceinline__ void write32(T* p, bool wide, int64_t step, int n, const float (&v)[32]) {
-    constexpr int kPer = 16 / sizeof(T);
-    if (wide && n >= 32) {
+__device__ __forceinline__ void write4(T* p, bool wide, int n, const float (&v)[4]) {
+    if (wide && n >= 4) {
+        Pack<T, 4> k;
 #pragma unroll
-        for (int i = 0; i < 32 / kPer; i++) {
-            Pack<T, kPer> k;
-#pragma unroll
-            for (int u = 0; u < kPer; u++) k.v[u] = from_float<T>(v[i * kPer + u]);
-            reinterpret_cast<Pack<T, kPer>*>(p)[i] = k;
-        }
+        for (int i = 0; i < 4; i++) k.v[i] = from_float<T>(v[i]);
+        *reinterpret_cast<Pack<T, 4>*>(p) = k;
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; i++)
-            if (i < n) p[i * step] = from_float<T>(v[i]);
+        for (int i = 0; i < 4; i++)
+            if (i < n) p[i] = from_float<T>(v[i]);
     }
 }
-__device__ __forceinline__ void write32_any(const Mat& m, int64_t at, int64_t step, int n, const float (&v)[32]) {
-    const bool wide = m.wide && step == 1;
-    if (m.type == SPARBIT_F32) write32((float*)m.p + at, wide, step, n, v);
-    else if (m.type == SPARBIT_BF16) write32((__nv_bfloat16*)m.p + at, wide, step, n, v);
-    else write32((__half*)m.p + at, wide, step, n, v);
+__device__ __forceinline__ void write_any(const Mat& m, int z, int64_t r, int64_t c, int n, const float (&v)[4]) {
+    const int64_t at = z * m.stride + r * m.ld + c;
+    if (m.type == SPARBIT_F32) write4((float*)m.p + at, m.wide, n, v);
+    else if (m.type == SPARBIT_BF16) write4((__nv_bfloat16*)m.p + at, m.wide, n, v);
+    else write4((__half*)m.p + at, m.wide, n, v);
 }
-__device__ __forceinline__ void read32_any(const Mat& m, int64_t at, int64_t step, int n, float (&v)[32]) {
-    const bool wide = m.wide && step == 1;
-    if (m.type == SPARBIT_F32) read32((const float*)m.p + at, wide, step, n, v);
-    else if (m.type == SPARBIT_BF16) read32((const __nv_bfloat16*)m.p + at, wide, step, n, v);
-    else read32((const __half*)m.p + at, wide, step, n, v);
+__device__ __forceinline__ void read_any(const Mat& m, int z, int64_t r, int64_t c, int n, float (&v)[4]) {
+    const int64_t at = z * m.stride + r * m.ld + c;
+    if (m.type == SPARBIT_F32) read4((const float*)m.p + at, m.wide, n, v);
+    else if (m.type == SPARBIT_BF16) read4((const __nv_bfloat16*)m.p + at, m.wide, n, v);
+    else read4((const __half*)m.p + at, m.wide, n, v);
+}
+// The last step's result for four elements of a row of the user's matrix.
+__device__ __forceinline__ void write_result(const ProductArgs& g, int z, int64_t r, int64_t c, int n, float (&v)[4]) {
+    if (g.muon) {
+        float w[4];
+        read_any(g.weight, z, r, c, n, w);
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] = g.keep * w[i] - g.rate * v[i];
+    }
+    write_any(g.out, z, r, c, n, v);
 }
 
-// 32 columns of a row of a product, on their way out.  The pitches of X, A and P are multiples of 64
-// elements: a run of 32 columns that starts inside a row may be read and written whole (the columns
-// past the matrix are outside the tensor maps).
+constexpr int kBlock = 32, kPitch = kBlock + 1;  // a warp's block of a product in shared memory, without bank conflicts
+constexpr int kBlockBytes = kBlock * kPitch * 4;
+
+// A block of 32 x 32 elements of a product, on its way out: eight lanes to a row, so that rows leave in
+// 64-byte runs; then, where its mirror image or transpose goes out (too), the same by columns.  The
+// pitches of X, A and P are multiples of 64 elements: four elements that start inside a row may be read
+// and written whole (the columns past the matrix are outside the tensor maps).
 template <int kOp>
-__device__ __forceinline__ void write_out(const ProductArgs& g, int z, int row, int row0, int col, float q,
-                                          float (&v)[32]) {
-    if constexpr (kOp == kGram || kOp == kPoly) {
-        const float scale = kOp == kGram ? q * q * kScaleP : g.c / kScaleP;  // result held times kScaleP
+__device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int z, int row0, int col0, float q) {
+    constexpr bool kSquare = kOp == kGram || kOp == kPoly;
+    const int lane = threadIdx.x & 31, lr = lane >> 3, lc = (lane & 7) * 4;
+    const bool turn = kSquare ? col0 > row0 : kOp == kLast && g.transposed;
+    const bool lows = kOp != kLast && (g.segments == 3 || kOp == kApply);
+#pragma unroll 4
+    for (int it = 0; it < kBlock / 4; it++) {
+        const int row = row0 + it * 4 + lr, col = col0 + lc;
+        if (row >= g.M || col >= g.N) continue;
+        float* const at = sm + (it * 4 + lr) * kPitch + lc;
+        float v[4], x[4], y[4];
 #pragma unroll
-        for (int i = 0; i < 32; i++) v[i] *= scale;
-        if (kOp == kPoly) {
-            const int64_t at = z * g.z_in + row * g.ld_in + col;
-            float add[32];
-            read32(g.in_hi + at, true, 1, 32, add);
+        for (int i = 0; i < 4; i++) v[i] = at[i];
+        const int64_t from = z * g.z_in + row * g.ld_in + col;
+        if (kSquare) {
+            const float scale = kOp == kGram ? q * q * kScaleP : g.c / kScaleP;  // result held times kScaleP
 #pragma unroll
-            for (int i = 0; i < 32; i++) v[i] += g.b * add[i] + (col + i == row ? g.d * kScaleP : 0.0f);
-            if (g.segments == 3) {
-                read32(g.in_lo + at, true, 1, 32, add);
+            for (int i = 0; i < 4; i++) v[i] *= scale;
+            if (kOp == kPoly) {
+                read4(g.in_hi + from, true, 4, x);
+                if (g.segments == 3) {
+                    read4(g.in_lo + from, true, 4, y);
 #pragma unroll
-                for (int i = 0; i < 32; i++) v[i] += g.b * add[i];
+                    for (int i = 0; i < 4; i++) x[i] += y[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] += g.b * x[i] + (col + i == row ? g.d * kScaleP : 0.0f);
             }
-        }
-        const int64_t zo = z * g.z_out;
-        __half hi[32];
-#pragma unroll
-        for (int i = 0; i < 32; i++) hi[i] = __float2half_rn(v[i]);
-#pragma unroll 1
-        for (int part = 0; part < (g.segments == 3 ? 2 : 1); part++) {
-            __half* out = (part ? g.out_lo : g.out_hi) + zo;
-            if (part)
-#pragma unroll
-                for (int i = 0; i < 32; i++) hi[i] = __float2half_rn(v[i] - __half2float(hi[i]));
-            uint4* o = reinterpret_cast<uint4*>(out + row * g.ld_out + col);
-#pragma unroll
-            for (int i = 0; i < 4; i++) o[i] = reinterpret_cast<const uint4*>(hi)[i];
-            if (col > row0)  // off the diagonal: the mirror image; lanes hold neighbouring rows
-#pragma unroll
-                for (int i = 0; i < 32; i++)
-                    if (col + i < g.N) out[(col + i) * g.ld_out + row] = hi[i];
-        }
-    } else {
-        // stored X' = (a stored X + (P X) / kScaleP) * (true per stored) * kScaleX
-        const int64_t at = z * g.z_in + row * g.ld_in + col;
-        const float scale = q * (kOp == kLast ? 1.0f : kScaleX);
-        float x[32];
-        if (g.in_full) {
-            read32(g.in_full + at, true, 1, 32, x);
         } else {
-            float lo[32];
-            read32(g.in_hi + at, true, 1, 32, x);
-            read32(g.in_lo + at, true, 1, 32, lo);
+            // stored X' = (a stored X + (P X) / kScaleP) * (true per stored) * kScaleX
+            if (g.in_full) {
+                read4(g.in_full + from, true, 4, x);
+            } else {
+                read4(g.in_hi + from, true, 4, x);
+                read4(g.in_lo + from, true, 4, y);
 #pragma unroll
-            for (int i = 0; i < 32; i++) x[i] += lo[i];
+                for (int i = 0; i < 4; i++) x[i] += y[i];
+            }
+            const float scale = q * (kOp == kLast ? 1.0f : kScaleX);
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[i] = (g.a * x[i] + v[i] * (1.0f / kScaleP)) * scale;
         }
+        if (turn) {
 #pragma unroll
-        for (int i = 0; i < 32; i++) v[i] = (g.a * x[i] + v[i] * (1.0f / kScaleP)) * scale;
-        if (kOp == kApply) {
+            for (int i = 0; i < 4; i++) at[i] = v[i];
+        }
+        if (kOp == kLast) {
+            if (!turn) write_result(g, z, row, col, g.N - col, v);
+        } else {
             const int64_t to = z * g.z_out + row * g.ld_out + col;
-            write32(g.out_hi + to, true, 1, 32, v);
-            if (g.out_full) write32(g.out_full + to, true, 1, 32, v);
+            write4(g.out_hi + to, true, 4, v);
+            if (kOp == kApply && g.out_full) write4(g.out_full + to, true, 4, v);
+            if (lows) {
 #pragma unroll
-            for (int i = 0; i < 32; i++) v[i] -= __half2float(__float2half_rn(v[i]));
-            write32(g.out_lo + to, true, 1, 32, v);
-        } else {
-            const int64_t r = g.transposed ? col : row, c = g.transposed ? row : col;
-            const int n = g.N - col < 32 ? g.N - col : 32;
-            if (g.muon) {
-                read32_any(g.weight, z * g.weight.stride + r * g.weight.ld + c, g.transposed ? g.weight.ld : 1, n, x);
-#pragma unroll
-                for (int i = 0; i < 32; i++) v[i] = g.keep * x[i] - g.rate * v[i];
+                for (int i = 0; i < 4; i++) v[i] -= __half2float(__float2half_rn(v[i]));
+                write4(g.out_lo + to, true, 4, v);
             }
-            write32_any(g.out, z * g.out.stride + r * g.out.ld + c, g.transposed ? g.out.ld : 1, n, v);
+        }
+    }
+    if (!turn) return;
+    __syncwarp();
+#pragma unroll 4
+    for (int it = 0; it < kBlock / 4; it++) {
+        const int col = col0 + it * 4 + lr, row = row0 + lc;
+        if (row >= g.M || col >= g.N) continue;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] = sm[(lc + i) * kPitch + it * 4 + lr];
+        if (kOp == kLast) {
+            write_result(g, z, col, row, g.M - row, v);
+        } else {
+            const int64_t to = z * g.z_out + col * g.ld_out + row;
+            write4(g.out_hi + to, true, 4, v);
+            if (lows) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] -= __half2float(__float2half_rn(v[i]));
+                write4(g.out_lo + to, true, 4, v);
+            }
         }
     }
 }
@@ -407,9 +421,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int t = blockIdx.x; t < g.total; t += gridDim.x) {
             const int z = t / g.n_tiles;
             const uint32_t rc = g.tiles[t - z * g.n_tiles];
-            const int row0 = (int)(rc >> 16) * kTileM + quad * 32, row = row0 + lane;
+            const int row0 = (int)(rc >> 16) * kTileM + quad * 32;
             const int col0 = (int)(rc & 0xffff) * kTileN + half * (kTileN / 2);
-            float acc[kTileN / 2 / 32][32];
+            float acc[kTileN / 2];
+#pragma unroll
+            for (int i = 0; i < kTileN / 2; i++) acc[i] = 0.0f;
             bool ok = true;
             for (int s = 0; s < blocks; s += g.flush, group++) {
                 const uint32_t slot = group & 1;
@@ -417,24 +433,32 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!ok) break;
                 fence_after();
 #pragma unroll
-                for (int j = 0; j < kTileN / 2 / 32; j++) {
-                    float v[32];
+                for (int j = 0; j < kTileN / 2 / 16; j++) {
+                    float v[16];
                     __syncwarp();
-                    tmem_load32(tmem + slot * kTileN + half * (kTileN / 2) + j * 32 + lanes, v);
+                    tmem_load16(tmem + slot * kTileN + half * (kTileN / 2) + j * 16 + lanes, v);
 #pragma unroll
-                    for (int i = 0; i < 32; i++) acc[j][i] = s == 0 ? v[i] : acc[j][i] + v[i];
+                    for (int i = 0; i < 16; i++) acc[j * 16 + i] += v[i];
                 }
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(drained + 8 * slot);
             }
             if (!ok) break;
-            if (row >= g.M) continue;
             const float q = g.first ? g.q[z] : 1.0f / kScaleX;
+            float* const sm = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + kStages * kStageBytes) +
+                              (warp - 2) * (kBlockBytes / 4);
 #pragma unroll
-            for (int j = 0; j < kTileN / 2 / 32; j++) {
-                const int col = col0 + j * 32;
-                if (col < g.N && !(kSquare && col < row0)) write_out<kOp>(g, z, row, row0, col, q, acc[j]);
+            for (int j = 0; j < kTileN / 2 / kBlock; j++) {
+                const int col = col0 + j * kBlock;
+                // blocks below the diagonal are the mirror images of others
+                if (row0 < g.M && col < g.N && !(kSquare && col < row0)) {
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < kBlock; i++) sm[lane * kPitch + i] = acc[j * kBlock + i];
+                    __syncwarp();
+                    write_block<kOp>(g, sm, z, row0, col, q);
+                }
             }
         }
     }

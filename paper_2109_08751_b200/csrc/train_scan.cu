@@ -23,8 +23,11 @@ namespace {
 
 constexpr int kPiece = 128;    // steps of a piece
 constexpr int kTile = 32;      // channels of a tile
-constexpr int kGroup = 16;     // pieces of a group
-constexpr int kThreads = 256;  // 16 runs of 8 steps (two channels a thread) or 8 runs of 16 (one)
+constexpr int kGroup = 8;      // pieces of a group
+// A thread's share of a piece: V channels of a run of steps.  16 runs of 8 steps with two or four
+// channels a thread, 8 runs of 16 with one.
+template <int V>
+constexpr int kThreads = V == 4 ? 128 : 256;
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
 // A piece in the order of one direction's chain.
@@ -44,34 +47,64 @@ struct Control {
     unsigned ticket, done, epoch, status;
 };
 
-// V channels of a thread; two of them go through the packed fp32 instructions of sm_100.
+// V channels of a thread; pairs of them go through the packed fp32 instructions of sm_100.
 template <int V>
 struct F {
     float v[V];
 };
-__device__ __forceinline__ unsigned long long bits2(const F<2>& a) {
-    return (unsigned long long)__float_as_uint(a.v[1]) << 32 | __float_as_uint(a.v[0]);
+__device__ __forceinline__ unsigned long long pair_bits(float a, float b) {
+    return (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a);
 }
-__device__ __forceinline__ F<2> from_bits2(unsigned long long b) {
-    return F<2>{{__uint_as_float((unsigned)b), __uint_as_float((unsigned)(b >> 32))}};
+__device__ __forceinline__ void from_pair(unsigned long long p, float& a, float& b) {
+    a = __uint_as_float((unsigned)p);
+    b = __uint_as_float((unsigned)(p >> 32));
 }
-__device__ __forceinline__ F<1> fma(const F<1>& a, const F<1>& b, const F<1>& c) { return {{fmaf(a.v[0], b.v[0], c.v[0])}}; }
-__device__ __forceinline__ F<1> mul(const F<1>& a, const F<1>& b) { return {{a.v[0] * b.v[0]}}; }
-__device__ __forceinline__ F<1> add(const F<1>& a, const F<1>& b) { return {{a.v[0] + b.v[0]}}; }
-__device__ __forceinline__ F<2> fma(const F<2>& a, const F<2>& b, const F<2>& c) {
-    unsigned long long d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
-    return from_bits2(d);
+template <int V>
+__device__ __forceinline__ F<V> fma(const F<V>& a, const F<V>& b, const F<V>& c) {
+    F<V> r;
+    if constexpr (V == 1) {
+        r.v[0] = fmaf(a.v[0], b.v[0], c.v[0]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            unsigned long long d;
+            asm("fma.rn.f32x2 %0, %1, %2, %3;"
+                : "=l"(d)
+                : "l"(pair_bits(a.v[i], a.v[i + 1])), "l"(pair_bits(b.v[i], b.v[i + 1])), "l"(pair_bits(c.v[i], c.v[i + 1])));
+            from_pair(d, r.v[i], r.v[i + 1]);
+        }
+    }
+    return r;
 }
-__device__ __forceinline__ F<2> mul(const F<2>& a, const F<2>& b) {
-    unsigned long long d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
-    return from_bits2(d);
+template <int V>
+__device__ __forceinline__ F<V> mul(const F<V>& a, const F<V>& b) {
+    F<V> r;
+    if constexpr (V == 1) {
+        r.v[0] = a.v[0] * b.v[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            unsigned long long d;
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pair_bits(a.v[i], a.v[i + 1])), "l"(pair_bits(b.v[i], b.v[i + 1])));
+            from_pair(d, r.v[i], r.v[i + 1]);
+        }
+    }
+    return r;
 }
-__device__ __forceinline__ F<2> add(const F<2>& a, const F<2>& b) {
-    unsigned long long d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
-    return from_bits2(d);
+template <int V>
+__device__ __forceinline__ F<V> add(const F<V>& a, const F<V>& b) {
+    F<V> r;
+    if constexpr (V == 1) {
+        r.v[0] = a.v[0] + b.v[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            unsigned long long d;
+            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pair_bits(a.v[i], a.v[i + 1])), "l"(pair_bits(b.v[i], b.v[i + 1])));
+            from_pair(d, r.v[i], r.v[i + 1]);
+        }
+    }
+    return r;
 }
 template <int V>
 __device__ __forceinline__ F<V> all(float x) {
@@ -172,27 +205,29 @@ struct ScanArgs {
     int64_t y_ld, dgate_ld, dx_ld;
 };
 
-// Row t of a staged tensor; a pad of one row every 8 keeps the two runs of a warp in different banks.
-__device__ __forceinline__ int stage_row(int t) { return (t + (t >> 3)) * kTile; }
+// Row t of a staged tensor; a pad of one row after every run keeps the runs of a warp in different
+// banks (R: steps of a run).
+template <int R>
+__device__ __forceinline__ int stage_row(int t) { return (t + t / R) * kTile; }
 constexpr int kStageElems = (kPiece + kPiece / 8) * kTile;  // of one tensor
 
 // Starts the copy of a piece's rows of one tensor into shared memory.
-template <typename T>
+template <typename T, int R, int kThr>
 __device__ __forceinline__ void stage_tensor(T* dst, const T* src, int64_t ld, int64_t row0, int len, int ch0, int D,
                                              bool wide) {
-    constexpr int kPer = 16 / sizeof(T), kChunks = kTile / kPer, kRows = kThreads / kChunks;
+    constexpr int kPer = 16 / sizeof(T), kChunks = kTile / kPer, kRows = kThr / kChunks;
     if (wide) {
         const int t0 = threadIdx.x / kChunks, e = threadIdx.x % kChunks * kPer, left = D - ch0 - e;
         if (left <= 0) return;
         const int bytes = left < kPer ? left * (int)sizeof(T) : 16;  // the rest becomes zero
         const T* from = src + (row0 + t0) * ld + ch0 + e;
-        const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + stage_row(t0) + e);
-        static_assert(kRows % 8 == 0, "whole groups of 8 rows between the copies of a thread");
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + stage_row<R>(t0) + e);
+        static_assert(kRows % 8 == 0 && (kRows % R == 0 || R % kRows == 0), "");
 #pragma unroll
         for (int i = 0; i < kPiece / kRows; i++) {
             if (t0 + i * kRows < len)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                 to + (uint32_t)(i * (kRows + kRows / 8) * kTile * sizeof(T))),
+                                 to + (uint32_t)((i * kRows + i * kRows / R) * kTile * sizeof(T))),
                              "l"(from), "r"(bytes)
                              : "memory");
             from += kRows * ld;
@@ -203,22 +238,24 @@ __device__ __forceinline__ void stage_tensor(T* dst, const T* src, int64_t ld, i
         if (ch0 + e >= D) return;
         const T* from = src + (row0 + threadIdx.x / kTile) * ld + ch0 + e;
 #pragma unroll 8
-        for (int t = threadIdx.x / kTile; t < len; t += kThreads / kTile) {
-            dst[stage_row(t) + e] = *from;
-            from += kThreads / kTile * ld;
+        for (int t = threadIdx.x / kTile; t < len; t += kThr / kTile) {
+            dst[stage_row<R>(t) + e] = *from;
+            from += kThr / kTile * ld;
         }
     }
 }
 
+constexpr int kMostRuns = 16;
+
 // What a CTA learns about the state that enters its piece.
 struct Shared {
-    float2 run[kThreads * 2 / kTile][kTile];   // pairs of the runs, then what the runs before make of the entering state
+    float2 run[kMostRuns][kTile];   // pairs of the runs, then what the runs before make of the entering state
     float2 before[kGroup][kTile];              // pairs of the group's earlier pieces; last: end of the group before
     float enter[kTile];
-    float hold[kThreads * 2 / kTile][kTile];   // backward: states at the start of each run
-    float2 after[kThreads * 2 / kTile][kTile]; // backward: what the runs behind make of the entering gradient
+    float hold[kMostRuns][kTile];   // backward: states at the start of each run
+    float2 after[kMostRuns][kTile]; // backward: what the runs behind make of the entering gradient
     Piece piece[4];
-    int ticket[4];
+    int ticket[4], tile[4];
     unsigned epoch;
 };
 
@@ -293,7 +330,9 @@ __device__ __forceinline__ void post_ticket(const ScanArgs& g, Shared& s, int sl
     if (threadIdx.x != 0) return;
     s.ticket[slot] = ticket;
     if (ticket < g.total) {
-        const char* from = (const char*)(g.pieces + ticket / g.tiles);
+        const int piece = ticket / g.tiles;
+        s.tile[slot] = ticket - piece * g.tiles;
+        const char* from = (const char*)(g.pieces + piece);
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(&s.piece[slot]);
 #pragma unroll
         for (int i = 0; i < (int)sizeof(Piece); i += 16)
@@ -318,20 +357,20 @@ template <typename T>
 constexpr int kStagesOf = sizeof(T) == 4 ? 1 : 2;
 
 // Starts the copies of a piece: gate and x, gate and dy, or all three.
-template <typename T, int kTensors>
+template <typename T, int kTensors, int R, int kThr>
 __device__ __forceinline__ void stage_piece(const ScanArgs& g, T* buf, const Shared& s, int slot, bool against_time) {
     const int64_t row0 = s.piece[slot].row0;
-    const int len = s.piece[slot].len, ch0 = s.ticket[slot] % g.tiles * kTile;
-    stage_tensor<T>(buf, (const T*)g.gate, g.gate_ld, row0, len, ch0, g.D, g.wide);
+    const int len = s.piece[slot].len, ch0 = s.tile[slot] * kTile;
+    stage_tensor<T, R, kThr>(buf, (const T*)g.gate, g.gate_ld, row0, len, ch0, g.D, g.wide);
     if (kTensors == 3 || !against_time)
-        stage_tensor<T>(buf + kStageElems, (const T*)g.x, g.x_ld, row0, len, ch0, g.D, g.wide);
+        stage_tensor<T, R, kThr>(buf + kStageElems, (const T*)g.x, g.x_ld, row0, len, ch0, g.D, g.wide);
     if (against_time)
-        stage_tensor<T>(buf + (kTensors - 1) * kStageElems, (const T*)g.dy, g.dy_ld, row0, len, ch0, g.D, g.wide);
+        stage_tensor<T, R, kThr>(buf + (kTensors - 1) * kStageElems, (const T*)g.dy, g.dy_ld, row0, len, ch0, g.D, g.wide);
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // What both kernels begin with; returns this launch's tag.
-template <typename T, int kTensors>
+template <typename T, int kTensors, int R, int kThr>
 __device__ __forceinline__ unsigned begin(const ScanArgs& g, T* stages, Shared& s, bool against_time) {
     pdl_wait();
     pdl_trigger();
@@ -340,36 +379,36 @@ __device__ __forceinline__ unsigned begin(const ScanArgs& g, T* stages, Shared& 
     if (threadIdx.x == 0) s.epoch = g.ctl->epoch;
     copies_wait();
     __syncthreads();
-    if (kStagesOf<T> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors>(g, stages, s, 0, against_time);
+    if (kStagesOf<T> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors, R, kThr>(g, stages, s, 0, against_time);
     return s.epoch;
 }
 
 // ---- forward (kBack: only what the pieces do to a gradient, for a summary against time) ------------
 template <typename T, int V, bool kBack>
-__global__ void __launch_bounds__(kThreads, 4) scan_forward_kernel(const __grid_constant__ ScanArgs g) {
-    constexpr int kLanes = kTile / V, kRuns = kThreads / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
+__global__ void __launch_bounds__(kThreads<V>, 4) scan_forward_kernel(const __grid_constant__ ScanArgs g) {
+    constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
     T* stages = reinterpret_cast<T*>(raw);
-    const unsigned tag = begin<T, 2>(g, stages, s, kBack);
+    const unsigned tag = begin<T, 2, R, kThr>(g, stages, s, kBack);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int n = 0; s.ticket[n & 3] < g.total; n++) {
-        if (S == 1) stage_piece<T, 2>(g, stages, s, n & 3, kBack);
+        if (S == 1) stage_piece<T, 2, R, kThr>(g, stages, s, n & 3, kBack);
         copies_wait();
         __syncthreads();
         const int drawn = draw_ticket(g);
         if (S == 2 && s.ticket[(n + 1) & 3] < g.total)
-            stage_piece<T, 2>(g, stages + ((n + 1) & 1) * 2 * kStageElems, s, (n + 1) & 3, kBack);
+            stage_piece<T, 2, R, kThr>(g, stages + ((n + 1) & 1) * 2 * kStageElems, s, (n + 1) & 3, kBack);
         const Piece& pc = s.piece[n & 3];
-        const int tile = s.ticket[n & 3] % g.tiles, len = pc.len;
-        const T* in0 = stages + (S == 2 ? n & 1 : 0) * 2 * kStageElems + stage_row(run * R) + e;
+        const int tile = s.tile[n & 3], len = pc.len;
+        const T* in0 = stages + (S == 2 ? n & 1 : 0) * 2 * kStageElems + stage_row<R>(run * R) + e;
         const T* in1 = in0 + kStageElems;
         F<V> a[R], b[R], A = all<V>(1.0f), H = all<V>(0.0f);
 #pragma unroll
         for (int j = 0; j < R; j++) {
             F<V> keep;
-            gate_pair(unpack<T, V>(in0 + stage_row(j)), a[j], keep);
-            b[j] = unpack<T, V>(in1 + stage_row(j));
+            gate_pair(unpack<T, V>(in0 + stage_row<R>(j)), a[j], keep);
+            b[j] = unpack<T, V>(in1 + stage_row<R>(j));
             if (!kBack) b[j] = mul(b[j], keep);
         }
         if (len < kPiece) {  // steps past the end change nothing
@@ -436,26 +475,26 @@ __global__ void __launch_bounds__(kThreads, 4) scan_forward_kernel(const __grid_
 // ---- backward -------------------------------------------------------------------------------------
 // The states of the piece are computed again from the one that the forward pass left at its start.
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 3) scan_backward_kernel(const __grid_constant__ ScanArgs g) {
-    constexpr int kLanes = kTile / V, kRuns = kThreads / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
+__global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __grid_constant__ ScanArgs g) {
+    constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
     T* stages = reinterpret_cast<T*>(raw);
-    const unsigned tag = begin<T, 3>(g, stages, s, true);
+    const unsigned tag = begin<T, 3, R, kThr>(g, stages, s, true);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int n = 0; s.ticket[n & 3] < g.total; n++) {
         if (S == 1) {
             __syncthreads();  // the last piece's dy has been read
-            stage_piece<T, 3>(g, stages, s, n & 3, true);
+            stage_piece<T, 3, R, kThr>(g, stages, s, n & 3, true);
         }
         copies_wait();
         __syncthreads();
         const int drawn = draw_ticket(g);
         if (S == 2 && s.ticket[(n + 1) & 3] < g.total)
-            stage_piece<T, 3>(g, stages + ((n + 1) & 1) * 3 * kStageElems, s, (n + 1) & 3, true);
+            stage_piece<T, 3, R, kThr>(g, stages + ((n + 1) & 1) * 3 * kStageElems, s, (n + 1) & 3, true);
         const Piece& pc = s.piece[n & 3];
-        const int tile = s.ticket[n & 3] % g.tiles, len = pc.len;
-        const T* in_g = stages + (S == 2 ? n & 1 : 0) * 3 * kStageElems + stage_row(run * R) + e;
+        const int tile = s.tile[n & 3], len = pc.len;
+        const T* in_g = stages + (S == 2 ? n & 1 : 0) * 3 * kStageElems + stage_row<R>(run * R) + e;
         const T* in_x = in_g + kStageElems;
         const T* in_d = in_x + kStageElems;
         float carried = 0.0f;
@@ -463,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 3) scan_backward_kernel(const __grid
             carried = g.carry[(int64_t)pc.carry * g.D + tile * kTile + lane];
         F<V> a[R], k[R], A = all<V>(1.0f), H = all<V>(0.0f), G = all<V>(0.0f);
 #pragma unroll
-        for (int j = 0; j < R; j++) gate_pair(unpack<T, V>(in_g + stage_row(j)), a[j], k[j]);
+        for (int j = 0; j < R; j++) gate_pair(unpack<T, V>(in_g + stage_row<R>(j)), a[j], k[j]);
         if (len < kPiece) {
 #pragma unroll
             for (int j = 0; j < R; j++)
@@ -473,9 +512,9 @@ __global__ void __launch_bounds__(kThreads, 3) scan_backward_kernel(const __grid
         for (int j = 0; j < R; j++) {
             if (run * R + j >= len) break;  // what is staged there may be anything
             A = mul(A, a[j]);
-            H = fma(a[j], H, mul(k[j], unpack<T, V>(in_x + stage_row(j))));
+            H = fma(a[j], H, mul(k[j], unpack<T, V>(in_x + stage_row<R>(j))));
             // the map of a gradient, front to back: this step's dy seen through the steps before
-            G = fma(A, unpack<T, V>(in_d + stage_row(j)), G);
+            G = fma(A, unpack<T, V>(in_d + stage_row<R>(j)), G);
         }
 #pragma unroll
         for (int i = 0; i < V; i++) {
@@ -514,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 3) scan_backward_kernel(const __grid
         for (int i = 0; i < V; i++) h.v[i] = s.hold[run][e + i];
 #pragma unroll
         for (int j = 0; j < R; j++) {
-            const F<V> x = unpack<T, V>(in_x + stage_row(j)), ak = mul(a[j], k[j]);
+            const F<V> x = unpack<T, V>(in_x + stage_row<R>(j)), ak = mul(a[j], k[j]);
             f[j] = mul(fma(x, all<V>(-1.0f), h), ak);
             h = fma(a[j], h, mul(k[j], x));
         }
@@ -529,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 3) scan_backward_kernel(const __grid
 #pragma unroll
             for (int j = R - 1; j >= 0; j--, dg -= g.dgate_ld, dx -= g.dx_ld) {
                 if (run * R + j >= len) continue;
-                const F<V> q = add(unpack<T, V>(in_d + stage_row(j)), c);
+                const F<V> q = add(unpack<T, V>(in_d + stage_row<R>(j)), c);
                 c = mul(a[j], q);
                 pack<T, V>(dg, mul(f[j], q));
                 pack<T, V>(dx, mul(k[j], q));
@@ -589,6 +628,11 @@ struct sparbit_scan_plan_s {
     int device = -1, sm_count = 0;
     unsigned long long limit = kWaitNs;
     int publish_groups = 1;
+    // CTAs per SM of the kernels used so far
+    struct {
+        void (*kernel)(ScanArgs);
+        int per_sm;
+    } fits[4] = {};
 
     size_t tiles() const { return ((size_t)D + kTile - 1) / kTile; }
     size_t off_forward() const { return 256; }
@@ -622,32 +666,43 @@ ScanArgs common_args(const sparbit_scan_plan_s* p, bool against_time) {
 }
 
 // As many CTAs as fit, each taking tickets until there are none.
-int run(const sparbit_scan_plan_s* p, void (*kernel)(ScanArgs), int tensors, const ScanArgs& g, cudaStream_t st) {
-    const size_t smem = (p->dtype == SPARBIT_F32 ? kStagesOf<float> : kStagesOf<__half>) * tensors *
-                        (size_t)kStageElems * elem_size(p->dtype);
-    CU(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    int per_sm = 0;
-    CU(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, smem));
-    const int most = (per_sm > 0 ? per_sm : 1) * p->sm_count;
-    CU(launch(kernel, dim3(g.total < most ? g.total : most), dim3(kThreads), smem, st, g));
+int run(sparbit_scan_plan_s* p, void (*kernel)(ScanArgs), int threads, int tensors, const ScanArgs& g, cudaStream_t st) {
+    const size_t smem = (p->dtype == SPARBIT_F32 ? kStagesOf<float> : kStagesOf<__half>) * tensors * (size_t)kStageElems *
+                        elem_size(p->dtype);
+    auto* fit = p->fits;
+    while (fit < p->fits + 3 && fit->kernel && fit->kernel != kernel) fit++;
+    if (fit->kernel != kernel) {
+        CU(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        CU(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit->per_sm, kernel, threads, smem));
+        fit->kernel = kernel;
+    }
+    const int most = (fit->per_sm > 0 ? fit->per_sm : 1) * p->sm_count;
+    CU(launch(kernel, dim3(g.total < most ? g.total : most), dim3(threads), smem, st, g));
     return SPARBIT_OK;
 }
 
-// Calls f.template operator()<T, V>() for the plan's type and the number of channels a lane takes.
-template <typename F>
-int by_type(int dtype, int V, F f) {
-    switch (dtype) {
-        case SPARBIT_F32: return V == 2 ? f.template operator()<float, 2>() : f.template operator()<float, 1>();
-        case SPARBIT_BF16:
-            return V == 2 ? f.template operator()<__nv_bfloat16, 2>() : f.template operator()<__nv_bfloat16, 1>();
-        default: return V == 2 ? f.template operator()<__half, 2>() : f.template operator()<__half, 1>();
-    }
+// Calls f.template operator()<T, V>() for the plan's type and the number of channels a thread takes.
+template <typename T, int kMost, typename Fn>
+int by_channels(int V, Fn f) {
+    if constexpr (kMost >= 4)
+        if (V == 4) return f.template operator()<T, 4>();
+    if (V >= 2) return f.template operator()<T, 2>();
+    return f.template operator()<T, 1>();
+}
+template <int kMost16, int kMost32, typename Fn>
+int by_type(int dtype, int V, Fn f) {
+    if (dtype == SPARBIT_F32) return by_channels<float, kMost32>(V, f);
+    if (dtype == SPARBIT_BF16) return by_channels<__nv_bfloat16, kMost16>(V, f);
+    return by_channels<__half, kMost16>(V, f);
 }
 
-// Channels a lane takes: two where every row starts on a multiple of two elements.
-int lane_channels(int dtype, size_t D, uintptr_t bits16, uintptr_t bits32) {
+// Channels a thread takes: the most whose rows start on multiples of them, in the tensors of the
+// plan's type (bits of their addresses and pitches) and in 32-bit ones.
+int lane_channels(int dtype, size_t D, uintptr_t bits, uintptr_t bits32) {
     const int es = (int)elem_size(dtype);
-    return D % 2 == 0 && common_alignment(bits16, 2 * es) == 2 * es && common_alignment(bits32, 8) == 8 ? 2 : 1;
+    for (int V = 4; V > 1; V /= 2)
+        if (D % V == 0 && bits % (V * es) == 0 && bits32 % (V * 4) == 0) return V;
+    return 1;
 }
 
 }  // namespace
@@ -729,6 +784,7 @@ int sparbit_scan_plan_set_workspace(sparbit_scan_plan_t* p, void* dev, size_t by
     if (!p) return SPARBIT_ERR_ARG;
     if (!dev || bytes < p->work_bytes() || (uintptr_t)dev % 16) return SPARBIT_ERR_WORKSPACE;
     p->work = nullptr;
+    for (auto& fit : p->fits) fit = {};
     CU(cudaGetDevice(&p->device));
     CU(cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device));
     char* base = (char*)dev;
@@ -777,8 +833,10 @@ int sparbit_scan_forward(sparbit_scan_plan_t* p, const void* gate, size_t gate_l
     g.summary = summary;
     g.carry = carry;
     const int V = lane_channels(p->dtype, D, y ? (uintptr_t)y | y_ld * es : 0, 0);
-    return by_type(p->dtype, V, [&]<typename T, int kV>() {
-        return run(p, scan_forward_kernel<T, kV, false>, 2, g, (cudaStream_t)stream);
+    // eight bytes of a row a thread: 8 x 4096 x 2048 bf16 95 us against 106 with four; 32-bit elements
+    // 148 us with eight against 157 with sixteen
+    return by_type<4, 2>(p->dtype, V, [&]<typename T, int kV>() {
+        return run(p, scan_forward_kernel<T, kV, false>, kThreads<kV>, 2, g, (cudaStream_t)stream);
     });
 }
 
@@ -815,8 +873,8 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     uintptr_t in_bits = (uintptr_t)gate | (uintptr_t)dy | gate_ld * es | dy_ld * es;
     if (!dx) {
         g.wide = common_alignment(in_bits, 16) == 16;
-        return by_type(p->dtype, lane_channels(p->dtype, 2, 0, 0), [&]<typename T, int kV>() {
-            return run(p, scan_forward_kernel<T, kV, true>, 2, g, (cudaStream_t)stream);
+        return by_type<4, 2>(p->dtype, lane_channels(p->dtype, 4, 0, 0), [&]<typename T, int kV>() {
+            return run(p, scan_forward_kernel<T, kV, true>, kThreads<kV>, 2, g, (cudaStream_t)stream);
         });
     }
     in_bits |= (uintptr_t)x | x_ld * es;
@@ -829,8 +887,9 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     g.dx = dx;
     g.dx_ld = (int64_t)dx_ld;
     const uintptr_t out_bits = (uintptr_t)dgate | (uintptr_t)dx | dgate_ld * es | dx_ld * es;
-    return by_type(p->dtype, lane_channels(p->dtype, D, out_bits, 0), [&]<typename T, int kV>() {
-        return run(p, scan_backward_kernel<T, kV>, 3, g, (cudaStream_t)stream);
+    // two channels a thread: with four, registers leave half as many warps (174 us against 167)
+    return by_type<2, 2>(p->dtype, lane_channels(p->dtype, D, out_bits, 0), [&]<typename T, int kV>() {
+        return run(p, scan_backward_kernel<T, kV>, kThreads<kV>, 3, g, (cudaStream_t)stream);
     });
 }
 
@@ -872,7 +931,7 @@ int sparbit_scan_step(size_t rows, size_t channels, int dtype, const void* gate,
         return SPARBIT_ERR_ALIAS;
     const uintptr_t bits = (uintptr_t)gate | (uintptr_t)x | (uintptr_t)y | gate_ld * es | x_ld * es | y_ld * es;
     const int V = lane_channels(dtype, channels, bits, (uintptr_t)state_in | (uintptr_t)state_out | state_ld * 4);
-    return by_type(dtype, V, [&]<typename T, int kV>() {
+    return by_type<4, 4>(dtype, V, [&]<typename T, int kV>() {
         CU(launch(scan_step_kernel<T, kV>, dim3((unsigned)rows, (unsigned)((channels + 128 * kV - 1) / (128 * kV))),
                   dim3(128), 0, (cudaStream_t)stream, (const T*)gate, (int64_t)gate_ld, (const T*)x, (int64_t)x_ld,
                   slots, (int64_t)n_slots, (int)channels, state_in, state_out, (int64_t)state_ld, (T*)y,
