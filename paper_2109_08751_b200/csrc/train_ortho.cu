@@ -30,15 +30,18 @@ using namespace spb;
 namespace {
 
 // ---- tile geometry ------------------------------------------------------------------------------
-constexpr int kTileM = 128, kTileN = 256, kTileK = 64;  // one tcgen05 accumulator: 256 TMEM columns
-constexpr int kStages = 4;
-constexpr int kABytes = kTileM * kTileK * 2, kBBytes = kTileN * kTileK * 2, kStageBytes = kABytes + kBBytes;
+// A pair of CTAs (cta_group::2) makes a tile of 256 x kN: each holds 128 rows of A, half of B and, in
+// its tensor memory, 128 rows of the accumulator.  An SM takes in about 64 bytes a clock; alone a CTA
+// would need 96 for 128 x 256 (measured: two thirds of the pair's rate).
+constexpr int kTileM = 256, kTileK = 64;
+constexpr int kRing = 196608;  // stages of a CTA: 6 of 32 KiB (kN = 256) or 8 of 24 KiB, three products 3 or 4
+constexpr int kABytes = kTileM / 2 * kTileK * 2;
 constexpr int kThreads = 320;  // warp 0 loads, warp 1 multiplies, warps 2-9 write out
 // The tensor cores cut each partial sum towards zero: over K = 4096 a relative error of 1e-5, which
-// three products would not survive.  They hand over every 256 of K to a sum rounded in registers.
-constexpr int kFlush = 4;
-constexpr int kSmem = kStages * kStageBytes + 8 * 32 * 33 * 4 + 1024;  // ring, a block for each warp that writes, alignment
-constexpr int kNormParts = 256;                         // CTAs a matrix's norm is summed by
+// three products would not survive.  They hand over every 128 of K to a sum rounded in registers.
+constexpr int kFlush = 2;
+constexpr int kSmem = kRing + 8 * 32 * 33 * 4 + 1024;   // ring, a block for each warp that writes, alignment
+constexpr int kNormParts = 512;                         // CTAs a matrix's norm is summed by
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;   // X and A, P are held times these
 constexpr unsigned long long kWaitNs = 2000000000ull;   // a wait inside the kernel gives up after this
 
@@ -51,9 +54,6 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t n) {
 }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
@@ -84,12 +84,29 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     }
     return true;
 }
+// Arrival at the barrier at the same place in the pair's first CTA.
+__device__ __forceinline__ void bar_arrive_first(uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\t"
+        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar)
+        : "memory");
+}
+// A copy into this CTA's shared memory that reports to the barrier of the pair's first CTA (the bit
+// that tells the two apart cleared in the barrier's address).
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
     asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-            dst),
-        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(map), "r"(bar & 0xfeffffffu), "r"(x), "r"(y), "r"(z)
         : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Shared-memory operand of 128-byte swizzled rows.  K-major: groups of 8 rows `sbo` apart.  MN-major:
 // blocks of 64 elements `lbo` apart, groups of 8 k `sbo` apart.
@@ -100,12 +117,16 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint3
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
         : "memory");
 }
+// Arrives at the barrier at this place in both CTAs once the products issued so far are done.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+        "h"((uint16_t)3)
+        : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -136,8 +157,6 @@ struct Mat {
 
 struct ProductArgs {
     int M, N, K;            // of the product
-    int segments;           // 1: hi hi; 3: hi hi + hi lo + lo hi
-    int flush;              // blocks of K a TMEM accumulator takes before it is added up in registers
     int n_tiles;            // tiles of one matrix, listed in `tiles` as (row tile << 16 | column tile)
     int total;              // tiles of all matrices
     const uint32_t* tiles;
@@ -156,16 +175,6 @@ struct ProductArgs {
     float keep, rate;       // W' = keep W - rate X
     uint32_t* status;
 };
-
-__device__ __forceinline__ float load_any(const Mat& m, int64_t i) {
-    if (m.type == SPARBIT_F32) return ((const float*)m.p)[i];
-    if (m.type == SPARBIT_BF16) return __bfloat162float(((const __nv_bfloat16*)m.p)[i]);
-    return __half2float(((const __half*)m.p)[i]);
-}
-__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
-    hi = __float2half_rn(v);
-    lo = __float2half_rn(v - __half2float(hi));
-}
 
 // Four values of a row, the first n of them inside the matrix; `wide`: every row starts on a multiple
 // of 16 bytes and c on a multiple of four elements, so that four values are 8 or 16 aligned bytes.
@@ -219,49 +228,78 @@ __device__ __forceinline__ void write_result(const ProductArgs& g, int z, int64_
 constexpr int kBlock = 32, kPitch = kBlock + 1;  // a warp's block of a product in shared memory, without bank conflicts
 constexpr int kBlockBytes = kBlock * kPitch * 4;
 
+// What the epilogue adds to a block: the lane's four elements of every fourth row, as stored - fp16 hi
+// and lo, or fp32.  Loaded before the products are done where registers allow.
+template <int kIts>
+struct Addend {
+    uint4 raw[kIts];
+};
+template <int kOp, bool kThree, int kIts>
+__device__ __forceinline__ void load_addend(const ProductArgs& g, int z, int row0, int col0, Addend<kIts>& d) {
+    if (kOp == kGram) return;
+    const int lane = threadIdx.x & 31, row = row0 + (lane >> 3), col = col0 + (lane & 7) * 4;
+    const int64_t at = z * g.z_in + row * g.ld_in + col;
+#pragma unroll
+    for (int it = 0; it < kIts; it++) {
+        if (row + it * 4 >= g.M || col >= g.N) continue;
+        const int64_t i = at + (int64_t)(it * 4) * g.ld_in;
+        if (kOp != kPoly && kThree) {
+            d.raw[it] = *reinterpret_cast<const uint4*>(g.in_full + i);
+        } else {
+            const uint2 hi = *reinterpret_cast<const uint2*>(g.in_hi + i);
+            uint2 lo = make_uint2(0u, 0u);
+            if (kOp != kPoly || kThree) lo = *reinterpret_cast<const uint2*>(g.in_lo + i);
+            d.raw[it] = make_uint4(hi.x, hi.y, lo.x, lo.y);
+        }
+    }
+}
+__device__ __forceinline__ void unpack_halves(uint32_t a, uint32_t b, float (&v)[4]) {
+    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&a));
+    const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&b));
+    v[0] = p.x, v[1] = p.y, v[2] = q.x, v[3] = q.y;
+}
+
 // A block of 32 x 32 elements of a product, on its way out: eight lanes to a row, so that rows leave in
 // 64-byte runs; then, where its mirror image or transpose goes out (too), the same by columns.  The
 // pitches of X, A and P are multiples of 64 elements: four elements that start inside a row may be read
 // and written whole (the columns past the matrix are outside the tensor maps).
-template <int kOp>
-__device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int z, int row0, int col0, float q) {
-    constexpr bool kSquare = kOp == kGram || kOp == kPoly;
+template <int kOp, bool kThree, bool kAhead, int kIts>
+__device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int z, int row0, int col0, float q,
+                                            Addend<kIts>& d) {
+    constexpr bool kSquare = kOp == kGram || kOp == kPoly, kLows = kOp == kApply || (kSquare && kThree);
     const int lane = threadIdx.x & 31, lr = lane >> 3, lc = (lane & 7) * 4;
     const bool turn = kSquare ? col0 > row0 : kOp == kLast && g.transposed;
-    const bool lows = kOp != kLast && (g.segments == 3 || kOp == kApply);
-#pragma unroll 4
+#pragma unroll
     for (int it = 0; it < kBlock / 4; it++) {
         const int row = row0 + it * 4 + lr, col = col0 + lc;
+        if (!kAhead && it % kIts == 0) load_addend<kOp, kThree>(g, z, row0 + it * 4, col0, d);
         if (row >= g.M || col >= g.N) continue;
         float* const at = sm + (it * 4 + lr) * kPitch + lc;
         float v[4], x[4], y[4];
 #pragma unroll
         for (int i = 0; i < 4; i++) v[i] = at[i];
-        const int64_t from = z * g.z_in + row * g.ld_in + col;
-        if (kSquare) {
-            const float scale = kOp == kGram ? q * q * kScaleP : g.c / kScaleP;  // result held times kScaleP
-#pragma unroll
-            for (int i = 0; i < 4; i++) v[i] *= scale;
-            if (kOp == kPoly) {
-                read4(g.in_hi + from, true, 4, x);
-                if (g.segments == 3) {
-                    read4(g.in_lo + from, true, 4, y);
+        if (kOp != kGram) {
+            if (kOp != kPoly && kThree) {
+                x[0] = __uint_as_float(d.raw[it % kIts].x), x[1] = __uint_as_float(d.raw[it % kIts].y);
+                x[2] = __uint_as_float(d.raw[it % kIts].z), x[3] = __uint_as_float(d.raw[it % kIts].w);
+            } else {
+                unpack_halves(d.raw[it % kIts].x, d.raw[it % kIts].y, x);
+                if (kOp != kPoly || kThree) {
+                    unpack_halves(d.raw[it % kIts].z, d.raw[it % kIts].w, y);
 #pragma unroll
                     for (int i = 0; i < 4; i++) x[i] += y[i];
                 }
+            }
+        }
+        if (kSquare) {
+            const float scale = kOp == kGram ? q * q * kScaleP : g.c / kScaleP;  // result held times kScaleP
 #pragma unroll
-                for (int i = 0; i < 4; i++) v[i] += g.b * x[i] + (col + i == row ? g.d * kScaleP : 0.0f);
+            for (int i = 0; i < 4; i++) {
+                v[i] *= scale;
+                if (kOp == kPoly) v[i] += g.b * x[i] + (col + i == row ? g.d * kScaleP : 0.0f);
             }
         } else {
             // stored X' = (a stored X + (P X) / kScaleP) * (true per stored) * kScaleX
-            if (g.in_full) {
-                read4(g.in_full + from, true, 4, x);
-            } else {
-                read4(g.in_hi + from, true, 4, x);
-                read4(g.in_lo + from, true, 4, y);
-#pragma unroll
-                for (int i = 0; i < 4; i++) x[i] += y[i];
-            }
             const float scale = q * (kOp == kLast ? 1.0f : kScaleX);
 #pragma unroll
             for (int i = 0; i < 4; i++) v[i] = (g.a * x[i] + v[i] * (1.0f / kScaleP)) * scale;
@@ -275,8 +313,8 @@ __device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int
         } else {
             const int64_t to = z * g.z_out + row * g.ld_out + col;
             write4(g.out_hi + to, true, 4, v);
-            if (kOp == kApply && g.out_full) write4(g.out_full + to, true, 4, v);
-            if (lows) {
+            if (kOp == kApply && kThree) write4(g.out_full + to, true, 4, v);
+            if (kLows) {
 #pragma unroll
                 for (int i = 0; i < 4; i++) v[i] -= __half2float(__float2half_rn(v[i]));
                 write4(g.out_lo + to, true, 4, v);
@@ -297,7 +335,7 @@ __device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int
         } else {
             const int64_t to = z * g.z_out + col * g.ld_out + row;
             write4(g.out_hi + to, true, 4, v);
-            if (lows) {
+            if (kLows) {
 #pragma unroll
                 for (int i = 0; i < 4; i++) v[i] -= __half2float(__float2half_rn(v[i]));
                 write4(g.out_lo + to, true, 4, v);
@@ -307,91 +345,105 @@ __device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int
 }
 
 // ---- the product kernel -------------------------------------------------------------------------
-// Persistent, one CTA per SM.  Maps: A hi, A lo, B hi, B lo; boxes of 64 columns x tile rows (Gram,
-// Poly) or of 64 columns x 64 rows (Apply's B, used MN-major).
-template <int kOp>
-__global__ void __launch_bounds__(kThreads, 1)
+// Persistent, a pair of CTAs per pair of SMs.  Maps: A hi, A lo, B hi, B lo; boxes of 64 columns x 128
+// rows (A) and kN / 2 rows (B of Gram and Poly) or of 64 columns x 64 rows (Apply's B, used MN-major).
+template <int kOp, int kN, bool kThree>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ CUtensorMap a_hi, const __grid_constant__ CUtensorMap a_lo,
                    const __grid_constant__ CUtensorMap b_hi, const __grid_constant__ CUtensorMap b_lo,
                    const __grid_constant__ ProductArgs g) {
     constexpr bool kSquare = kOp == kGram || kOp == kPoly;
+    constexpr int kBBytes = kN / 2 * kTileK * 2, kParts = kThree ? 2 : 1;
+    constexpr int kStageBytes = kParts * (kABytes + kBBytes), kStages = kRing / kStageBytes;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bars[2 * kStages + 4];
     __shared__ uint32_t tmem_base;
     __shared__ uint32_t gave_up;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    // full, drained: in the first CTA, for both; empty, done: in each
     const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-        for (int i = 0; i < 2; i++) bar_init(done + 8 * i, 1), bar_init(drained + 8 * i, 8);
+        for (int i = 0; i < 2; i++) bar_init(done + 8 * i, 1), bar_init(drained + 8 * i, 16);
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base))
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)),
+                     "r"(2 * kN)
                      : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
     fence_before();
     __syncthreads();
+    cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_base;
     pdl_wait();
     pdl_trigger();
 
-    const int k_blocks = (g.K + kTileK - 1) / kTileK, blocks = k_blocks * g.segments;
+    const int blocks = (g.K + kTileK - 1) / kTileK, flush = kThree ? kFlush : blocks;
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     if (warp == 0) {
         if (lane == 0) {
             uint32_t n = 0;  // stages filled so far
             bool ok = true;
-            for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+            for (int t = pair; t < g.total && ok; t += pairs) {
                 const int z = t / g.n_tiles;
                 const uint32_t rc = g.tiles[t - z * g.n_tiles];
-                const int row = (int)(rc >> 16) * kTileM, col = (int)(rc & 0xffff) * kTileN;
+                const int row = (int)(rc >> 16) * kTileM + rank * (kTileM / 2), col = (int)(rc & 0xffff) * kN + rank * (kN / 2);
                 for (int s = 0; s < blocks; s++, n++) {
                     const uint32_t st = n % kStages;
                     if (n >= kStages && !bar_wait(empty + 8 * st, (n / kStages - 1) & 1, &gave_up)) {
                         ok = false;
                         break;
                     }
-                    const int seg = s / k_blocks, k = (s - seg * k_blocks) * kTileK;
-                    const uint32_t dst = ring + st * kStageBytes, bar = full + 8 * st;
-                    bar_expect(bar, kStageBytes);
-                    tma_load(dst, seg == 2 ? &a_lo : &a_hi, bar, k, row, z);
-                    const CUtensorMap* bm = seg == 1 ? &b_lo : &b_hi;
-                    if (kSquare) {
-                        tma_load(dst + kABytes, bm, bar, k, col, z);
-                    } else {
+                    const int k = s * kTileK;
+                    const uint32_t bar = full + 8 * st;
+                    uint32_t dst = ring + st * kStageBytes;
+                    if (rank == 0) bar_expect(bar, 2 * kStageBytes);
 #pragma unroll
-                        for (int i = 0; i < kTileN / 64; i++)
-                            tma_load(dst + kABytes + i * kTileK * 128, bm, bar, col + i * 64, k, z);
+                    for (int part = 0; part < kParts; part++) {
+                        tma_load(dst, part ? &a_lo : &a_hi, bar, k, row, z);
+                        dst += kABytes;
+                        if (kSquare) {
+                            tma_load(dst, part ? &b_lo : &b_hi, bar, k, col, z);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < kN / 128; i++)
+                                tma_load(dst + i * kTileK * 128, part ? &b_lo : &b_hi, bar, col + i * 64, k, z);
+                        }
+                        dst += kBBytes;
                     }
                 }
             }
-            // all copies have landed before the CTA may end, whatever happened
-            for (uint32_t i = n > kStages ? n - kStages : 0; i < n; i++) {
-                const unsigned long long until = now_ns() + kWaitNs;
-                while (!bar_try(full + 8 * (i % kStages), (i / kStages) & 1) && now_ns() < until) {
+            // the products have read every stage, and said so to both CTAs, before either may end
+            for (uint32_t i = n > kStages ? n - kStages : 0; i < n && ok; i++)
+                ok = bar_wait(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up);
+            if (!ok) {  // let the copies under way land before the CTA ends
+                const unsigned long long until = now_ns() + 1000000ull;
+                while (now_ns() < until) {
                 }
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            // fp16 operands, fp32 accumulator, 128 x 256; B MN-major for Apply
-            constexpr uint32_t idesc = (1u << 4) | (kSquare ? 0u : 1u << 16) | ((uint32_t)(kTileN >> 3) << 17) |
+        if (lane == 0 && rank == 0) {
+            // fp16 operands, fp32 accumulator, 256 x kN; B MN-major for Apply
+            constexpr uint32_t idesc = (1u << 4) | (kSquare ? 0u : 1u << 16) | ((uint32_t)(kN >> 3) << 17) |
                                        ((uint32_t)(kTileM >> 4) << 24);
             uint32_t n = 0, group = 0;
             bool ok = true;
-            for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
-                for (int s0 = 0; s0 < blocks && ok; s0 += g.flush, group++) {
+            for (int t = pair; t < g.total && ok; t += pairs) {
+                for (int s0 = 0; s0 < blocks && ok; s0 += flush, group++) {
                     const uint32_t slot = group & 1;
                     if (group >= 2 && !bar_wait(drained + 8 * slot, (group / 2 - 1) & 1, &gave_up)) {
                         ok = false;
                         break;
                     }
                     fence_after();
-                    const int end = s0 + g.flush < blocks ? s0 + g.flush : blocks;
+                    const int end = s0 + flush < blocks ? s0 + flush : blocks;
                     for (int s = s0; s < end; s++, n++) {
                         const uint32_t st = n % kStages;
                         if (!bar_wait(full + 8 * st, (n / kStages) & 1, &gave_up)) {
@@ -399,13 +451,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                             break;
                         }
                         fence_after();
-                        const uint32_t at = ring + st * kStageBytes;
+                        const uint32_t ah = ring + st * kStageBytes, bh = ah + kABytes;
 #pragma unroll
-                        for (int k = 0; k < kTileK / 16; k++) {
-                            const uint64_t da = smem_desc(at + k * 32, 16, 1024);
-                            const uint64_t db = kSquare ? smem_desc(at + kABytes + k * 32, 16, 1024)
-                                                        : smem_desc(at + kABytes + k * 2048, kTileK * 128, 1024);
-                            mma_f16(tmem + slot * kTileN, da, db, idesc, s > s0 || k > 0);
+                        for (int seg = 0; seg < (kThree ? 3 : 1); seg++) {
+                            // hi hi, hi lo, lo hi
+                            const uint32_t at = ah + (seg == 2 ? kABytes + kBBytes : 0);
+                            const uint32_t bt = bh + (seg == 1 ? kABytes + kBBytes : 0);
+#pragma unroll
+                            for (int k = 0; k < kTileK / 16; k++) {
+                                const uint64_t da = smem_desc(at + k * 32, 16, 1024);
+                                const uint64_t db = kSquare ? smem_desc(bt + k * 32, 16, 1024)
+                                                            : smem_desc(bt + k * 2048, kTileK * 128, 1024);
+                                mma_f16(tmem + slot * kN, da, db, idesc, s > s0 || seg > 0 || k > 0);
+                            }
                         }
                         mma_commit(empty + 8 * st);
                     }
@@ -415,41 +473,48 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else {
         // TMEM lanes go by the warp's number mod 4; the two warps of a quarter take half the columns each
+        constexpr int kCols = kN / 2, kBlocks = kCols / kBlock;
+        constexpr bool kAhead = kN <= 128;  // registers for all addends at once
         const int quad = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        float* const sm = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + kRing) +
+                          (warp - 2) * (kBlockBytes / 4);
         uint32_t group = 0;
-        for (int t = blockIdx.x; t < g.total; t += gridDim.x) {
+        for (int t = pair; t < g.total; t += pairs) {
             const int z = t / g.n_tiles;
             const uint32_t rc = g.tiles[t - z * g.n_tiles];
-            const int row0 = (int)(rc >> 16) * kTileM + quad * 32;
-            const int col0 = (int)(rc & 0xffff) * kTileN + half * (kTileN / 2);
-            float acc[kTileN / 2];
+            const int row0 = (int)(rc >> 16) * kTileM + rank * (kTileM / 2) + quad * 32;
+            const int col0 = (int)(rc & 0xffff) * kN + half * kCols;
+            const float q = g.first ? g.q[z] : 1.0f / kScaleX;
+            Addend<kAhead ? kBlock / 4 : 4> d[kAhead ? kBlocks : 1];
+            if (kAhead) {
 #pragma unroll
-            for (int i = 0; i < kTileN / 2; i++) acc[i] = 0.0f;
+                for (int j = 0; j < kBlocks; j++) load_addend<kOp, kThree>(g, z, row0, col0 + j * kBlock, d[j]);
+            }
+            float acc[kCols];
+#pragma unroll
+            for (int i = 0; i < kCols; i++) acc[i] = 0.0f;
             bool ok = true;
-            for (int s = 0; s < blocks; s += g.flush, group++) {
+            for (int s = 0; s < blocks; s += flush, group++) {
                 const uint32_t slot = group & 1;
                 ok = bar_wait(done + 8 * slot, (group / 2) & 1, &gave_up);
                 if (!ok) break;
                 fence_after();
 #pragma unroll
-                for (int j = 0; j < kTileN / 2 / 16; j++) {
+                for (int j = 0; j < kCols / 16; j++) {
                     float v[16];
                     __syncwarp();
-                    tmem_load16(tmem + slot * kTileN + half * (kTileN / 2) + j * 16 + lanes, v);
+                    tmem_load16(tmem + slot * kN + half * kCols + j * 16 + lanes, v);
 #pragma unroll
                     for (int i = 0; i < 16; i++) acc[j * 16 + i] += v[i];
                 }
                 fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(drained + 8 * slot);
+                if (lane == 0) bar_arrive_first(drained + 8 * slot);
             }
             if (!ok) break;
-            const float q = g.first ? g.q[z] : 1.0f / kScaleX;
-            float* const sm = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + kStages * kStageBytes) +
-                              (warp - 2) * (kBlockBytes / 4);
 #pragma unroll
-            for (int j = 0; j < kTileN / 2 / kBlock; j++) {
+            for (int j = 0; j < kBlocks; j++) {
                 const int col = col0 + j * kBlock;
                 // blocks below the diagonal are the mirror images of others
                 if (row0 < g.M && col < g.N && !(kSquare && col < row0)) {
@@ -457,16 +522,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int i = 0; i < kBlock; i++) sm[lane * kPitch + i] = acc[j * kBlock + i];
                     __syncwarp();
-                    write_block<kOp>(g, sm, z, row0, col, q);
+                    write_block<kOp, kThree, kAhead>(g, sm, z, row0, col, q, d[kAhead ? j : 0]);
                 }
             }
         }
     }
     __syncthreads();
     if (threadIdx.x == 0 && gave_up) *g.status = 2;
+    cluster_sync();  // nobody's barriers or tensor memory are needed any more
     if (warp == 1) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
     }
 }
 
@@ -476,7 +542,8 @@ struct PrepareArgs {
     Mat update;                  // U, or the gradient
     const float* mom_in;         // Muon: momentum, null otherwise
     float* mom_out;
-    int64_t mom_in_ld, mom_in_stride, mom_out_ld, mom_out_stride;
+    int64_t mom_ld, mom_stride;
+    bool mom_wide;
     float mu;
     int nesterov;
     int rows, cols;              // of the user's matrix
@@ -489,23 +556,47 @@ struct PrepareArgs {
     int64_t ld, z;
 };
 
+// Four elements of U; and the new momentum where `write`.
+__device__ __forceinline__ void update4(const PrepareArgs& g, int z, int64_t r, int c, bool write, float (&u)[4]) {
+    const int n = g.cols - c;
+    read_any(g.update, z, r, c, n, u);
+    if (!g.mom_in) return;
+    float m[4];
+    const Mat out{g.mom_out, g.mom_ld, g.mom_stride, SPARBIT_F32, g.mom_wide};
+    if (write) {
+        const Mat in{(void*)g.mom_in, g.mom_ld, g.mom_stride, SPARBIT_F32, g.mom_wide};
+        read_any(in, z, r, c, n, m);
+#pragma unroll
+        for (int i = 0; i < 4; i++) m[i] = g.mu * m[i] + u[i];
+        write_any(out, z, r, c, n, m);
+    } else {
+        read_any(out, z, r, c, n, m);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) u[i] = g.nesterov ? u[i] + g.mu * m[i] : m[i];
+}
+
 // Sum of squares of every matrix, in parts; and the new momentum.
-__global__ void __launch_bounds__(256) norm_kernel(const PrepareArgs g) {
+__global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ PrepareArgs g) {
     __shared__ double s[8];
     pdl_wait();
     pdl_trigger();
-    const int z = blockIdx.y;
+    const int z = blockIdx.y, across = (g.cols + 3) / 4;
+    const int64_t all = (int64_t)g.rows * across;
     double sum = 0.0;
-    for (int64_t r = blockIdx.x; r < g.rows; r += kNormParts)
-        for (int c = threadIdx.x; c < g.cols; c += 256) {
-            float u = load_any(g.update, z * g.update.stride + r * g.update.ld + c);
-            if (g.mom_in) {
-                const float m = g.mu * g.mom_in[z * g.mom_in_stride + r * g.mom_in_ld + c] + u;
-                g.mom_out[z * g.mom_out_stride + r * g.mom_out_ld + c] = m;
-                u = g.nesterov ? u + g.mu * m : m;
-            }
-            sum += (double)u * (double)u;
+#pragma unroll 4
+    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += kNormParts * 256) {
+        const int64_t r = all <= 0x7fffffff ? (int)i / across : i / across;
+        float u[4];
+        update4(g, z, r, (int)(i - r * across) * 4, true, u);
+        const float four = u[0] * u[0] + u[1] * u[1] + u[2] * u[2] + u[3] * u[3];
+        if (four > 1e-30f && four < 1e30f) {
+            sum += (double)four;
+        } else {  // squares that 32 bits may not hold
+#pragma unroll
+            for (int k = 0; k < 4; k++) sum += (double)u[k] * (double)u[k];
         }
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = sum;
@@ -517,14 +608,24 @@ __global__ void __launch_bounds__(256) norm_kernel(const PrepareArgs g) {
 }
 
 // X of the first step: U times a power of two that brings its norm to 2048 .. 4096, as hi + lo, and
-// the factor from that to U / (|U| + eps).
-__global__ void __launch_bounds__(256) convert_kernel(const PrepareArgs g) {
+// the factor from that to U / (|U| + eps).  Tiles of 64 x 64, transposed through shared memory.
+__global__ void __launch_bounds__(256) convert_kernel(const __grid_constant__ PrepareArgs g) {
     __shared__ double s[8];
-    __shared__ float tile[32][33];
+    __shared__ float tile[64][65];
     pdl_wait();
     pdl_trigger();
     const int z = blockIdx.z;
-    double sum = g.parts[(int64_t)z * kNormParts + threadIdx.x];
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < kNormParts; i += 256) sum += g.parts[(int64_t)z * kNormParts + i];
+    const int tx = (threadIdx.x & 15) * 4, ty = threadIdx.x >> 4;
+    const int64_t r0 = (int64_t)blockIdx.y * 64;
+    const int c0 = blockIdx.x * 64;
+    float u[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int64_t r = r0 + ty + i * 16;
+        if (r < g.rows && c0 + tx < g.cols) update4(g, z, r, c0 + tx, false, u[i]);
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, o);
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = sum;
@@ -539,30 +640,28 @@ __global__ void __launch_bounds__(256) convert_kernel(const PrepareArgs g) {
     const float scale = fine ? ldexpf(1.0f, e) : 1.0f;
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
         g.q[z] = norm < INFINITY ? (float)(1.0 / (ldexp(norm, fine ? e : 0) + ldexp((double)g.eps, fine ? e : 0))) : NAN;
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const int64_t r0 = (int64_t)blockIdx.y * 32, c0 = (int64_t)blockIdx.x * 32;
-    for (int i = ty; i < 32; i += 8) {
-        const int64_t r = r0 + i, c = c0 + tx;
-        float u = 0.0f;
-        if (r < g.rows && c < g.cols) {
-            u = g.mom_in && !g.nesterov ? 0.0f : load_any(g.update, z * g.update.stride + r * g.update.ld + c);
-            if (g.mom_in) {
-                const float m = g.mom_out[z * g.mom_out_stride + r * g.mom_out_ld + c];
-                u = g.nesterov ? u + g.mu * m : m;
-            }
-        }
-        tile[i][tx] = u * scale;
+    const int rows = g.transposed ? g.cols : g.rows, cols = g.transposed ? g.rows : g.cols;
+    if (g.transposed) {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) tile[ty + i * 16][tx + k] = u[i][k];
+        __syncthreads();
     }
-    __syncthreads();
-    for (int i = ty; i < 32; i += 8) {
-        const int64_t r = g.transposed ? c0 + i : r0 + i, c = g.transposed ? r0 + tx : c0 + tx;
-        if (r >= (g.transposed ? g.cols : g.rows) || c >= (g.transposed ? g.rows : g.cols)) continue;
-        __half hi, lo;
-        const float u = g.transposed ? tile[tx][i] : tile[i][tx];
-        split(u, hi, lo);
-        if (g.full) g.full[z * g.z + r * g.ld + c] = u;
-        g.hi[z * g.z + r * g.ld + c] = hi;
-        g.lo[z * g.z + r * g.ld + c] = lo;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int64_t r = (g.transposed ? c0 : r0) + ty + i * 16;
+        const int c = (g.transposed ? (int)r0 : c0) + tx;
+        if (r >= rows || c >= cols) continue;
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) v[k] = (g.transposed ? tile[tx + k][ty + i * 16] : u[i][k]) * scale;
+        const int64_t to = z * g.z + r * g.ld + c;
+        write4(g.hi + to, true, 4, v);
+        if (g.full) write4(g.full + to, true, 4, v);
+#pragma unroll
+        for (int k = 0; k < 4; k++) v[k] -= __half2float(__float2half_rn(v[k]));
+        write4(g.lo + to, true, 4, v);
     }
 }
 
@@ -574,6 +673,7 @@ struct Step {
     float a, b, c;
 };
 
+int pick_width(int rows, int cols, int count, bool square, bool three, std::vector<uint32_t>& out);
 }  // namespace
 
 struct sparbit_ortho_plan_s {
@@ -584,9 +684,10 @@ struct sparbit_ortho_plan_s {
     float eps = 0.0f;
     std::vector<Step> steps;
     std::vector<uint32_t> square, wide;  // tile lists: symmetric results, X
+    int square_n = 256, wide_n = 256;    // columns of their tiles
     char* work = nullptr;
     int device = -1, sm_count = 0;
-    // tensor maps: A operand boxes of 128 rows, B boxes of 256 rows (K-major) or 64 rows (MN-major)
+    // tensor maps: boxes of A operands, of B operands, of MN-major B operands
     CUtensorMap xa[2][2], xb[2][2], xn[2][2], ga[2], gb[2], pa[2];  // [buffer][hi, lo]
 
     int64_t ldx() const { return (int64_t)round_up(n, 64); }
@@ -594,6 +695,10 @@ struct sparbit_ortho_plan_s {
     int64_t zx() const { return ldx() * m; }
     int64_t zg() const { return ldg() * m; }
     int parts() const { return products == SPARBIT_PRODUCTS_AUTO ? (dtype == SPARBIT_BF16 ? 1 : 3) : products; }
+    void lay_out() {
+        square_n = pick_width(m, m, count, true, parts() == 3, square);
+        wide_n = pick_width(m, n, count, false, parts() == 3, wide);
+    }
     size_t x_bytes() const { return round_up((size_t)count * zx() * 2, 1024); }
     size_t g_bytes() const { return round_up((size_t)count * zg() * 2, 1024); }
     // layout: status, tiles, parts, q | X hi, lo (two buffers) | A hi, lo | P hi, lo | X fp32 (two buffers)
@@ -658,19 +763,63 @@ int ready(const sparbit_ortho_plan_s* p) {
     return cur == p->device ? SPARBIT_OK : SPARBIT_ERR_ARG;
 }
 
+template <int kOp, int kN, bool kThree>
+int launch_product(const sparbit_ortho_plan_s* p, const CUtensorMap& ah, const CUtensorMap& al, const CUtensorMap& bh,
+                   const CUtensorMap& bl, const ProductArgs& g, cudaStream_t st) {
+    const int pairs = p->sm_count / 2;
+    CU(launch(product_kernel<kOp, kN, kThree>, dim3(2 * (g.total < pairs ? g.total : pairs)), dim3(kThreads), kSmem, st,
+              ah, al, bh, bl, g));
+    return SPARBIT_OK;
+}
 template <int kOp>
 int product(const sparbit_ortho_plan_s* p, const CUtensorMap& ah, const CUtensorMap& al, const CUtensorMap& bh,
             const CUtensorMap& bl, ProductArgs g, cudaStream_t st) {
-    const std::vector<uint32_t>& list = kOp == kGram || kOp == kPoly ? p->square : p->wide;
-    g.tiles = (const uint32_t*)(p->base() + (kOp == kGram || kOp == kPoly ? p->off_square() : p->off_wide()));
+    constexpr bool kSquare = kOp == kGram || kOp == kPoly;
+    const std::vector<uint32_t>& list = kSquare ? p->square : p->wide;
+    g.tiles = (const uint32_t*)(p->base() + (kSquare ? p->off_square() : p->off_wide()));
     g.n_tiles = (int)list.size();
     g.total = g.n_tiles * p->count;
-    g.segments = p->parts();
-    g.flush = g.segments == 3 ? kFlush : 1 << 30;
     g.status = (uint32_t*)p->base();
-    const int grid = g.total < p->sm_count ? g.total : p->sm_count;
-    CU(launch(product_kernel<kOp>, dim3(grid), dim3(kThreads), kSmem, st, ah, al, bh, bl, g));
+    const int n = kSquare ? p->square_n : p->wide_n;
+    if (p->parts() == 3)
+        return n == 256 ? launch_product<kOp, 256, true>(p, ah, al, bh, bl, g, st)
+                        : launch_product<kOp, 128, true>(p, ah, al, bh, bl, g, st);
+    return n == 256 ? launch_product<kOp, 256, false>(p, ah, al, bh, bl, g, st)
+                    : launch_product<kOp, 128, false>(p, ah, al, bh, bl, g, st);
+}
+template <int kOp>
+int allow_smem() {
+    CU(cudaFuncSetAttribute(product_kernel<kOp, 256, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    CU(cudaFuncSetAttribute(product_kernel<kOp, 128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    CU(cudaFuncSetAttribute(product_kernel<kOp, 256, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    CU(cudaFuncSetAttribute(product_kernel<kOp, 128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
     return SPARBIT_OK;
+}
+
+// Tiles of 256 x n that a product needs: all of rows x cols, or those that reach the diagonal.
+void list_tiles(int rows, int cols, int n, bool square, std::vector<uint32_t>& out) {
+    out.clear();
+    const int tm = (rows + kTileM - 1) / kTileM, tn = (cols + n - 1) / n;
+    if (square) {
+        for (int i = 0; i < tm; i++)
+            for (int j = i * kTileM / n; j < tn; j++) out.push_back((uint32_t)(i << 16 | j));
+    } else {
+        // column tiles in the outer loop: the pairs that run together share columns of X and walk down P
+        for (int j = 0; j < tn; j++)
+            for (int i = 0; i < tm; i++) out.push_back((uint32_t)(i << 16 | j));
+    }
+}
+// The wider tile needs less per product, the narrower one fills the GPU where there are few: rounds of
+// 74 pairs (a B200's) times the width, the narrow tile's taken 1.3 times for one product, whose
+// operands an SM then takes in slower than it multiplies.
+int pick_width(int rows, int cols, int count, bool square, bool three, std::vector<uint32_t>& out) {
+    std::vector<uint32_t> narrow;
+    list_tiles(rows, cols, 256, square, out);
+    list_tiles(rows, cols, 128, square, narrow);
+    const double rounds = (double)((out.size() * count + 73) / 74), more = (double)((narrow.size() * count + 73) / 74);
+    if (more * 128 * (three ? 1.0 : 1.3) >= rounds * 256) return 256;
+    out.swap(narrow);
+    return 128;
 }
 
 // prepare: update, momentum and scalars filled in; last: out, weight, muon, keep, rate filled in
@@ -687,7 +836,7 @@ int iterate(const sparbit_ortho_plan_s* p, PrepareArgs prep, ProductArgs last, c
     prep.ld = p->ldx();
     prep.z = p->zx();
     CU(launch(norm_kernel, dim3(kNormParts, p->count), dim3(256), 0, st, prep));
-    CU(launch(convert_kernel, dim3((unsigned)((p->cols + 31) / 32), (unsigned)((p->rows + 31) / 32), p->count),
+    CU(launch(convert_kernel, dim3((unsigned)((p->cols + 63) / 64), (unsigned)((p->rows + 63) / 64), p->count),
               dim3(256), 0, st, prep));
     int cur = 0;
     for (size_t i = 0; i < p->steps.size(); i++) {
@@ -771,12 +920,7 @@ int sparbit_ortho_plan_create(int count, size_t rows, size_t cols, int dtype, in
         p->m = (int)(rows < cols ? rows : cols);
         p->n = (int)(rows < cols ? cols : rows);
         p->eps = eps;
-        const int tm = (p->m + kTileM - 1) / kTileM;
-        for (int i = 0; i < tm; i++)
-            for (int j = i * kTileM / kTileN; j * kTileN < p->m; j++) p->square.push_back((uint32_t)(i << 16 | j));
-        // column tiles in the outer loop: the CTAs that run together share the columns of X and walk down P
-        for (int j = 0; j * kTileN < p->n; j++)
-            for (int i = 0; i < tm; i++) p->wide.push_back((uint32_t)(i << 16 | j));
+        p->lay_out();
     } catch (const std::bad_alloc&) {
         delete p;
         return SPARBIT_ERR_NOMEM;
@@ -799,7 +943,12 @@ int sparbit_ortho_plan_set_products(sparbit_ortho_plan_t* p, int products) {
     if (!p || (products != SPARBIT_PRODUCTS_AUTO && products != SPARBIT_PRODUCTS_ONE && products != SPARBIT_PRODUCTS_THREE))
         return SPARBIT_ERR_ARG;
     p->products = products;
-    p->work = nullptr;  // the workspace's layout goes by it
+    p->work = nullptr;  // the tiles and the workspace's layout go by it
+    try {
+        p->lay_out();
+    } catch (const std::bad_alloc&) {
+        return SPARBIT_ERR_NOMEM;
+    }
     return SPARBIT_OK;
 }
 
@@ -811,10 +960,11 @@ int sparbit_ortho_plan_set_workspace(sparbit_ortho_plan_t* p, void* dev, size_t 
     p->work = nullptr;
     CU(cudaGetDevice(&p->device));
     CU(cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device));
-    CU(cudaFuncSetAttribute(product_kernel<kGram>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-    CU(cudaFuncSetAttribute(product_kernel<kPoly>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-    CU(cudaFuncSetAttribute(product_kernel<kApply>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-    CU(cudaFuncSetAttribute(product_kernel<kLast>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    int e = allow_smem<kGram>();
+    if (e == SPARBIT_OK) e = allow_smem<kPoly>();
+    if (e == SPARBIT_OK) e = allow_smem<kApply>();
+    if (e == SPARBIT_OK) e = allow_smem<kLast>();
+    if (e != SPARBIT_OK) return e;
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult found;
     CU(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found));
@@ -822,16 +972,16 @@ int sparbit_ortho_plan_set_workspace(sparbit_ortho_plan_t* p, void* dev, size_t 
         return record_cuda_error((int)cudaErrorNotSupported, "cuTensorMapEncodeTiled");
     p->work = (char*)dev;
     const EncodeFn f = (EncodeFn)fn;
-    int e = SPARBIT_OK;
+    const int half = p->square_n / 2;
     for (int lo = 0; lo < 2 && e == SPARBIT_OK; lo++) {
         for (int b = 0; b < 2 && e == SPARBIT_OK; b++) {
-            e = encode(f, &p->xa[b][lo], p->x(b, lo), p->n, p->m, p->count, p->ldx(), p->zx(), kTileM);
-            if (e == SPARBIT_OK) e = encode(f, &p->xb[b][lo], p->x(b, lo), p->n, p->m, p->count, p->ldx(), p->zx(), kTileN);
+            e = encode(f, &p->xa[b][lo], p->x(b, lo), p->n, p->m, p->count, p->ldx(), p->zx(), kTileM / 2);
+            if (e == SPARBIT_OK) e = encode(f, &p->xb[b][lo], p->x(b, lo), p->n, p->m, p->count, p->ldx(), p->zx(), half);
             if (e == SPARBIT_OK) e = encode(f, &p->xn[b][lo], p->x(b, lo), p->n, p->m, p->count, p->ldx(), p->zx(), kTileK);
         }
-        if (e == SPARBIT_OK) e = encode(f, &p->ga[lo], p->gram(lo), p->m, p->m, p->count, p->ldg(), p->zg(), kTileM);
-        if (e == SPARBIT_OK) e = encode(f, &p->gb[lo], p->gram(lo), p->m, p->m, p->count, p->ldg(), p->zg(), kTileN);
-        if (e == SPARBIT_OK) e = encode(f, &p->pa[lo], p->poly(lo), p->m, p->m, p->count, p->ldg(), p->zg(), kTileM);
+        if (e == SPARBIT_OK) e = encode(f, &p->ga[lo], p->gram(lo), p->m, p->m, p->count, p->ldg(), p->zg(), kTileM / 2);
+        if (e == SPARBIT_OK) e = encode(f, &p->gb[lo], p->gram(lo), p->m, p->m, p->count, p->ldg(), p->zg(), half);
+        if (e == SPARBIT_OK) e = encode(f, &p->pa[lo], p->poly(lo), p->m, p->m, p->count, p->ldg(), p->zg(), kTileM / 2);
     }
     char* base = p->base();
     p->work = nullptr;
@@ -866,7 +1016,7 @@ int sparbit_orthogonalize(sparbit_ortho_plan_t* p, const void* update, size_t ld
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
     PrepareArgs prep = {};
-    prep.update = Mat{(void*)update, (int64_t)ld, (int64_t)stride, p->dtype, false};
+    prep.update = Mat{(void*)update, (int64_t)ld, (int64_t)stride, p->dtype, wide_rows(update, es, ld, stride)};
     ProductArgs last = {};
     last.out = Mat{out, (int64_t)out_ld, (int64_t)out_stride, p->dtype, wide_rows(out, es, out_ld, out_stride)};
     last.transposed = p->transposed;
@@ -894,11 +1044,14 @@ int sparbit_muon_step(sparbit_ortho_plan_t* p, const sparbit_muon* a, void* stre
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
     PrepareArgs prep = {};
-    prep.update = Mat{(void*)a->grad, (int64_t)a->grad_ld, (int64_t)a->grad_stride, p->dtype, false};
+    prep.update = Mat{(void*)a->grad, (int64_t)a->grad_ld, (int64_t)a->grad_stride, p->dtype,
+                      wide_rows(a->grad, elem_size(p->dtype), a->grad_ld, a->grad_stride)};
     prep.mom_in = a->momentum_in;
     prep.mom_out = a->momentum_out;
-    prep.mom_in_ld = prep.mom_out_ld = (int64_t)a->momentum_ld;
-    prep.mom_in_stride = prep.mom_out_stride = (int64_t)a->momentum_stride;
+    prep.mom_ld = (int64_t)a->momentum_ld;
+    prep.mom_stride = (int64_t)a->momentum_stride;
+    prep.mom_wide = wide_rows(a->momentum_in, 4, a->momentum_ld, a->momentum_stride) &&
+                    wide_rows(a->momentum_out, 4, a->momentum_ld, a->momentum_stride);
     prep.mu = a->momentum;
     prep.nesterov = a->nesterov;
     ProductArgs last = {};
