@@ -1,9 +1,17 @@
 // Router: softmax over the experts' logits, the k largest, per-expert counts, balance loss and the
-// gradient of the logits.  One warp per token; a lane holds every 32nd expert's logit.
+// gradient of the logits.
+//
+// L lanes of a warp share a token (8, 16 or 32, whichever holds the experts with 16 bytes of logits a
+// lane, at least k), each with C runs of V = 16 bytes / element neighbouring experts.  The choice: every
+// lane sorts its keys once (a network, up to 8 of them), then k times the largest head of the group
+// wins and its lane moves up.  A key holds the logit's order and, below it, the complement of the
+// expert's index, so that keys differ and equal logits go to the lowest index.  Instructions bound
+// this: about 260 a token at 256 experts, k = 8, where its 512 bytes would take 80 ps.
 #include <float.h>
 #include <math.h>
 
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "train_common.cuh"
@@ -17,141 +25,278 @@ constexpr int kMaxExperts = SPARBIT_ROUTER_MAX_EXPERTS;
 constexpr int kMaxK = SPARBIT_ROUTER_MAX_K;
 // CTAs a forward or backward pass is cut into, at most
 constexpr int kSlices = 592;
+constexpr float kLog2e = 1.4426950408889634f;
 
 // A run of tokens of one rank, worked on by one CTA.
 struct Slice {
     int32_t row0, rows, rank, pad;
 };
 
-// Order of floats as unsigned integers; NaN and -inf become 0, the key of "cannot be chosen".
-__device__ __forceinline__ unsigned order_key(float v) {
-    if (!(v > -INFINITY)) return 0u;
-    const unsigned b = __float_as_uint(v + 0.0f);  // -0 counts as 0
-    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-__device__ __forceinline__ float key_value(unsigned k) {
-    return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
+
+// Keys: 32 bits (order of a 16-bit logit, complement of the index) or 64.  0: cannot be chosen (NaN,
+// -inf).  Zeros of either sign are equal.
+template <typename T>
+using Key = std::conditional_t<sizeof(T) == 2, uint32_t, unsigned long long>;
+__device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
+__device__ __forceinline__ uint32_t bits_of(__half v) { return __half_as_ushort(v); }
+template <typename T>
+__device__ __forceinline__ Key<T> make_key(T t, float v, int e) {
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t b = v == 0.0f ? 0u : bits_of(t);
+        const uint32_t o = (b & 0x8000u) ? ~b & 0xffffu : b | 0x8000u;
+        return v > -INFINITY ? o << 16 | (0xffffu - (uint32_t)e) : 0u;
+    } else {
+        const uint32_t b = __float_as_uint(v + 0.0f);
+        const uint32_t o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
+        return v > -INFINITY ? (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)e) : 0ull;
+    }
 }
-__device__ __forceinline__ float warp_sum(float v) {
+template <typename T>
+__device__ __forceinline__ int key_index(Key<T> k) {
+    if constexpr (sizeof(T) == 2) return (int)(0xffffu - (k & 0xffffu));
+    else return (int)(0xffffffffu - (uint32_t)k);
+}
+template <typename T>
+__device__ __forceinline__ float key_value(Key<T> k) {
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t o = k >> 16;
+        const unsigned short b = (unsigned short)((o & 0x8000u) ? o & 0x7fffu : ~o);
+        if constexpr (std::is_same_v<T, __half>) return __half2float(__ushort_as_half(b));
+        else return __bfloat162float(__ushort_as_bfloat16(b));
+    } else {
+        const uint32_t o = (uint32_t)(k >> 32);
+        return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
+    }
+}
+
+template <typename K>
+__device__ __forceinline__ void order(K& a, K& b) {
+    const K hi = a > b ? a : b, lo = a > b ? b : a;
+    a = hi;
+    b = lo;
+}
+// Largest first.
+template <typename K>
+__device__ __forceinline__ void sort_keys(K (&k)[4]) {
+    order(k[0], k[1]), order(k[2], k[3]), order(k[0], k[2]), order(k[1], k[3]), order(k[1], k[2]);
+}
+template <typename K>
+__device__ __forceinline__ void sort_keys(K (&k)[8]) {  // odd-even merges
+    order(k[0], k[1]), order(k[2], k[3]), order(k[4], k[5]), order(k[6], k[7]);
+    order(k[0], k[2]), order(k[1], k[3]), order(k[4], k[6]), order(k[5], k[7]);
+    order(k[1], k[2]), order(k[5], k[6]);
+    order(k[0], k[4]), order(k[1], k[5]), order(k[2], k[6]), order(k[3], k[7]);
+    order(k[2], k[4]), order(k[3], k[5]);
+    order(k[1], k[2]), order(k[3], k[4]), order(k[5], k[6]);
+}
+
+// Over the L lanes that share a token.
+template <int L>
+__device__ __forceinline__ uint32_t group_max(uint32_t k) {
+    if constexpr (L == 32) return __reduce_max_sync(kAllLanes, k);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kAllLanes, v, o);
+    for (int o = L / 2; o; o >>= 1) k = max(k, __shfl_xor_sync(kAllLanes, k, o));
+    return k;
+}
+template <int L>
+__device__ __forceinline__ unsigned long long group_max(unsigned long long k) {
+    const uint32_t hi = group_max<L>((uint32_t)(k >> 32));
+    const uint32_t lo = group_max<L>((uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+    return (unsigned long long)hi << 32 | lo;
+}
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) v += __shfl_xor_sync(kAllLanes, v, o);
     return v;
 }
 
-// S: logits a lane holds (experts <= 32 S).  Leaves partial[slice][E+1] of counts and of sums.
-template <typename T, int S>
+// A lane's logits of a row: experts (c L + l) V + i.  wide: rows start on multiples of 16 bytes.
+template <typename T, int L, int C>
+struct Row {
+    static constexpr int V = 16 / sizeof(T), N = V * C;
+    Pack<T, V> run[C];
+    __device__ __forceinline__ void load(const T* p, int l, int E, bool wide, bool on) {
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            const int e = (c * L + l) * V;
+            if (!on) {
+            } else if (wide && e + V <= E) {
+                run[c] = *reinterpret_cast<const Pack<T, V>*>(p + e);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i++)
+                    if (e + i < E) run[c].v[i] = p[e + i];
+            }
+        }
+    }
+    __device__ __forceinline__ static int expert(int l, int n) { return (n / V * L + l) * V + n % V; }
+};
+
+template <typename T, int L, int C>
 __global__ void __launch_bounds__(kWarps * 32) router_forward_kernel(const Slice* slices, const T* logits, int64_t ld,
-                                                                    const uint8_t* mask, int E, int k, int renormalize,
-                                                                    int32_t* indices, float* weights, float* lse_out,
-                                                                    int32_t* part_counts, float* part_sums) {
-    __shared__ int32_t s_count[kMaxExperts + 1];
-    __shared__ float s_sum[kWarps][32 * S + 1];
+                                                                    int wide, const uint8_t* mask, int E, int k,
+                                                                    int renormalize, int32_t* indices, float* weights,
+                                                                    float* lse_out, int32_t* part_counts,
+                                                                    float* part_sums) {
+    using R = Row<T, L, C>;
+    using K = Key<T>;
+    constexpr int N = R::N, kGroups = 32 / L;  // tokens of a warp
+    constexpr int kSpan = N * L;               // experts there is room for
+    __shared__ int32_t s_count[kSpan + 1];
+    __shared__ float s_sum[kWarps * kGroups][kSpan + 1];
     pdl_wait();
+    pdl_trigger();
     const Slice sl = slices[blockIdx.x];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    for (int e = threadIdx.x; e <= E; e += kWarps * 32) s_count[e] = 0;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, l = lane % L, group = w * kGroups + lane / L;
+    for (int e = threadIdx.x; e <= kSpan; e += kWarps * 32) s_count[e] = 0;
     __syncthreads();
-    float acc[S], z = 0.0f;
+    float acc[N], z = 0.0f;
     int taken = 0;
 #pragma unroll
-    for (int i = 0; i < S; i++) acc[i] = 0.0f;
-    for (int t = w; t < sl.rows; t += kWarps) {
+    for (int i = 0; i < N; i++) acc[i] = 0.0f;
+    R now;
+    bool on = group < sl.rows && (!mask || mask[(int64_t)sl.row0 + group] != 0);
+    now.load(logits + ((int64_t)sl.row0 + group) * ld, l, E, wide, on);
+    for (int t = group; t - lane / L < sl.rows; t += kWarps * kGroups) {
         const int64_t row = (int64_t)sl.row0 + t;
-        bool on = !mask || mask[row] != 0;
-        float l[S];
-        unsigned key[S];
+        const bool inside = t < sl.rows;
+        // the next token's logits travel while this one's are worked on
+        const int t2 = t + kWarps * kGroups;
+        const bool on2 = t2 < sl.rows && (!mask || mask[(int64_t)sl.row0 + t2] != 0);
+        R next;
+        next.load(logits + ((int64_t)sl.row0 + t2) * ld, l, E, wide, on2);
+        float v[N];
+        K key[N];
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const int e = R::expert(l, i);
+            const T raw = now.run[i / R::V].v[i % R::V];
+            v[i] = on && e < E ? to_float(raw) : -INFINITY;
+            key[i] = make_key<T>(raw, v[i], e);
+        }
+        if constexpr (N <= 8) sort_keys(key);
+        K head = key[0];
+        if constexpr (N > 8) {
+#pragma unroll
+            for (int i = 1; i < N; i++) head = key[i] > head ? key[i] : head;
+        }
+        const K first = group_max<L>(head);
+        const float top = first ? key_value<T>(first) : -INFINITY;
         bool nan = false;
 #pragma unroll
-        for (int i = 0; i < S; i++) {
-            const int e = i * 32 + lane;
-            l[i] = on && e < E ? to_float(logits[row * ld + e]) : -INFINITY;
-            key[i] = order_key(l[i]);
-            nan |= l[i] != l[i];
+        for (int i = 0; i < N; i++) nan |= v[i] != v[i];
+        nan = group_max<L>((uint32_t)nan) != 0;
+        const bool part = on && (first != 0 || nan);
+        // +inf: inf - inf below is the NaN it should be
+        const float from = (top > -INFINITY && top < INFINITY ? top : 0.0f) * kLog2e;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            v[i] = exp2_fast(fmaf(v[i], kLog2e, -from));
+            sum += v[i];
         }
-        nan = __any_sync(kAllLanes, nan);
-        int my_index = -1;
-        float my_logit = -INFINITY, top = -INFINITY;
+        sum = group_sum<L>(sum);
+        const float inv = __fdividef(1.0f, sum);
+        // the chosen ones: lane j gets the j-th
+        K mine = 0, won = first;
         for (int j = 0; j < k; j++) {
-            unsigned best = 0;
+            if (l == j) mine = won;
+            if (head == won && won != 0) {
+                if constexpr (N <= 8) {
 #pragma unroll
-            for (int i = 0; i < S; i++) best = max(best, key[i]);
-            best = __reduce_max_sync(kAllLanes, best);
-            if (best == 0) break;  // nothing left to choose
-            unsigned at = 0xffffffffu;
+                    for (int i = 0; i + 1 < N; i++) key[i] = key[i + 1];
+                    key[N - 1] = 0;
+                    head = key[0];
+                } else {
+                    head = 0;
 #pragma unroll
-            for (int i = S - 1; i >= 0; i--)
-                if (key[i] == best) at = i * 32 + lane;
-            at = __reduce_min_sync(kAllLanes, at);
-#pragma unroll
-            for (int i = 0; i < S; i++)
-                if (i * 32 + lane == at) key[i] = 0;
-            if (j == 0) top = key_value(best);
-            if (lane == j) my_index = (int)at, my_logit = key_value(best);
-        }
-        on = on && (top > -INFINITY || nan);
-        float sum = 0.0f, p[S], lse = 0.0f;
-        if (on) {
-            const float from = top < INFINITY ? top : 0.0f;  // +inf: inf - inf below is the NaN it should be
-#pragma unroll
-            for (int i = 0; i < S; i++) {
-                p[i] = i * 32 + lane < E ? expf(l[i] - from) : 0.0f;
-                sum += p[i];
+                    for (int i = 0; i < N; i++) head = key[i] < won && key[i] > head ? key[i] : head;
+                }
             }
-            sum = warp_sum(sum);
-            lse = from + logf(sum);
-            const float inv = 1.0f / sum;
-#pragma unroll
-            for (int i = 0; i < S; i++) acc[i] += p[i] * inv;
-            if (lane == 0) z += lse * lse, taken++;
+            if (j + 1 < k) won = group_max<L>(head);
         }
-        float wgt = on && my_index >= 0 ? expf(my_logit - lse) : 0.0f;
+        const int index = part && mine != 0 ? key_index<T>(mine) : -1;
+        float wgt = 0.0f;
+        if (index >= 0) {
+            wgt = exp2_fast(fmaf(key_value<T>(mine), kLog2e, -from)) * inv;
+            if (nan) wgt = NAN;
+            atomicAdd(&s_count[index], 1);
+        }
         if (renormalize) {
-            const float all = warp_sum(wgt);
-            wgt = my_index >= 0 ? wgt / all : 0.0f;
+            const float chosen = group_sum<L>(wgt);
+            if (index >= 0) wgt = __fdividef(wgt, chosen);
         }
-        if (nan && on && my_index >= 0) wgt = NAN;
-        if (on && my_index >= 0) atomicAdd(&s_count[my_index], 1);
-        if (lane < k) {
-            indices[row * k + lane] = on ? my_index : -1;
-            weights[row * k + lane] = wgt;
-        }
-        if (lane == 0) lse_out[row] = lse;
-    }
-    if (lane == 0 && taken) atomicAdd(&s_count[E], taken);
+        const float lse = part ? (from + __log2f(sum)) * 0.6931471805599453f : 0.0f;
+        if (part) {
 #pragma unroll
-    for (int i = 0; i < S; i++) s_sum[w][i * 32 + lane] = acc[i];
-    if (lane == 0) s_sum[w][32 * S] = z;
+            for (int i = 0; i < N; i++) acc[i] = fmaf(v[i], inv, acc[i]);
+            z = fmaf(lse, lse, z);
+            taken++;
+        }
+        if (inside) {
+            if (l < k) {
+                indices[row * k + l] = index;
+                weights[row * k + l] = wgt;
+            }
+            if (l == 0) lse_out[row] = lse;
+        }
+        now = next;
+        on = on2;
+    }
+    if (l == 0 && taken) atomicAdd(&s_count[kSpan], taken);
+#pragma unroll
+    for (int i = 0; i < N; i++) s_sum[group][R::expert(l, i)] = acc[i];
+    if (l == 0) s_sum[group][kSpan] = z;
     __syncthreads();
     for (int e = threadIdx.x; e <= E; e += kWarps * 32) {
+        const int at = e < E ? e : kSpan;
         float v = 0.0f;
-        for (int u = 0; u < kWarps; u++) v += s_sum[u][e < E ? e : 32 * S];
-        part_counts[(int64_t)blockIdx.x * (E + 1) + e] = s_count[e];
+#pragma unroll 8
+        for (int u = 0; u < kWarps * kGroups; u++) v += s_sum[u][at];
+        part_counts[(int64_t)blockIdx.x * (E + 1) + e] = s_count[at];
         part_sums[(int64_t)blockIdx.x * (E + 1) + e] = v;
     }
 }
 
-// Partial results of each rank's slices, added in slice order.
-__global__ void __launch_bounds__(128) router_reduce_kernel(const int2* ranks, int E, const int32_t* part_counts,
+// Partial results of each rank's slices, added in a fixed order: 8 threads take every 8th slice of an
+// expert, then one adds theirs.
+__global__ void __launch_bounds__(256) router_reduce_kernel(const int2* ranks, int E, const int32_t* part_counts,
                                                            const float* part_sums, int32_t* counts, float* sums) {
+    __shared__ int32_t s_c[8][32];
+    __shared__ float s_v[8][32];
     pdl_wait();
-    const int e = blockIdx.x * 128 + threadIdx.x;
-    if (e > E) return;
+    pdl_trigger();
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, e = blockIdx.x * 32 + x;
     const int2 r = ranks[blockIdx.y];  // first slice, number of slices
     int32_t c = 0;
     float v = 0.0f;
+    if (e <= E) {
 #pragma unroll 8
-    for (int i = 0; i < r.y; i++) {
-        c += part_counts[(int64_t)(r.x + i) * (E + 1) + e];
-        v += part_sums[(int64_t)(r.x + i) * (E + 1) + e];
+        for (int i = y; i < r.y; i += 8) {
+            c += part_counts[(int64_t)(r.x + i) * (E + 1) + e];
+            v += part_sums[(int64_t)(r.x + i) * (E + 1) + e];
+        }
     }
-    counts[(int64_t)blockIdx.y * (E + 1) + e] = c;
-    sums[(int64_t)blockIdx.y * (E + 1) + e] = v;
+    s_c[y][x] = c;
+    s_v[y][x] = v;
+    __syncthreads();
+    if (y == 0 && e <= E) {
+        for (int i = 1; i < 8; i++) c += s_c[i][x], v += s_v[i][x];
+        counts[(int64_t)blockIdx.y * (E + 1) + e] = c;
+        sums[(int64_t)blockIdx.y * (E + 1) + e] = v;
+    }
 }
 
 // Sum over the gathered blocks of one expert's count, or (e = E) of the tokens that take part.
 __device__ __forceinline__ int64_t gathered_count(const int32_t* gathered, int G, int E, int e) {
     int64_t c = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int g = 0; g < G; g++) c += gathered[(int64_t)g * (E + 1) + e];
     return c;
 }
@@ -160,6 +305,7 @@ __global__ void __launch_bounds__(256) router_balance_kernel(const int32_t* gath
                                                             const float* sums, float alpha, float beta, float* loss) {
     __shared__ float s[8];
     pdl_wait();
+    pdl_trigger();
     gathered += (int64_t)blockIdx.x * G * (E + 1);
     sums += (int64_t)blockIdx.x * (E + 1);
     const int64_t n = gathered_count(gathered, G, E, E);
@@ -167,7 +313,7 @@ __global__ void __launch_bounds__(256) router_balance_kernel(const int32_t* gath
     float v = 0.0f;
     for (int e = threadIdx.x; e < E; e += 256)
         v += (float)gathered_count(gathered, G, E, e) / (number * k) * sums[e];
-    v = warp_sum(v);
+    v = group_sum<32>(v);
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -176,71 +322,104 @@ __global__ void __launch_bounds__(256) router_balance_kernel(const int32_t* gath
     }
 }
 
-template <typename T, int S>
+template <typename T, int L, int C>
 __global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Slice* slices, const T* logits, int64_t ld,
-                                                                     const uint8_t* mask, int E, int k, int renormalize,
-                                                                     const int32_t* indices, const float* weights,
-                                                                     const float* lse_in, const int32_t* gathered,
-                                                                     int G, const float* dweights, float alpha,
-                                                                     float beta, const float* dloss, T* dlogits,
-                                                                     int64_t dld) {
-    __shared__ float s_extra[kWarps][32 * S];
+                                                                     int wide, const uint8_t* mask, int E, int k,
+                                                                     int renormalize, const int32_t* indices,
+                                                                     const float* weights, const float* lse_in,
+                                                                     const int32_t* gathered, int G,
+                                                                     const float* dweights, float alpha, float beta,
+                                                                     const float* dloss, T* dlogits, int64_t dld,
+                                                                     int wide_out) {
+    using R = Row<T, L, C>;
+    constexpr int N = R::N, V = R::V, kGroups = 32 / L, kSpan = N * L;
+    __shared__ __align__(16) float s_extra[kWarps * kGroups][kSpan];  // what the chosen weights add to a token's gradient
+    __shared__ float s_f[kSpan];
+    __shared__ float s_number;
     pdl_wait();
+    pdl_trigger();
     const Slice sl = slices[blockIdx.x];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, l = lane % L, group = w * kGroups + lane / L;
     gathered += (int64_t)sl.rank * G * (E + 1);
-    const int64_t n = gathered_count(gathered, G, E, E);
-    const float number = (float)(n > 0 ? n : 1), scale = dloss ? *dloss : 1.0f;
-    const float ca = scale * alpha * E / number, cb = scale * 2.0f * beta / number;
-    float f[S];
-#pragma unroll
-    for (int i = 0; i < S; i++) {
-        const int e = i * 32 + lane;
-        f[i] = e < E ? (float)gathered_count(gathered, G, E, e) / (number * k) : 0.0f;
-        s_extra[w][e] = 0.0f;
+    if (threadIdx.x == 0) {
+        const int64_t n = gathered_count(gathered, G, E, E);
+        s_number = (float)(n > 0 ? n : 1);
     }
-    __syncwarp();
-    for (int t = w; t < sl.rows; t += kWarps) {
+    for (int e = threadIdx.x; e < kSpan; e += kWarps * 32)
+        s_f[e] = e < E ? (float)gathered_count(gathered, G, E, e) : 0.0f;
+    for (int i = threadIdx.x; i < kWarps * kGroups * kSpan; i += kWarps * 32) (&s_extra[0][0])[i] = 0.0f;
+    __syncthreads();
+    const float number = s_number, scale = dloss ? *dloss : 1.0f;
+    const float ca = scale * alpha * E / number, cb = scale * 2.0f * beta / number;
+    float f[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) f[i] = s_f[R::expert(l, i)] / (number * k);
+
+    struct Token {
+        R row;
+        bool on;
+        float lse, wgt, dw;
+        int at;
+    };
+    auto fetch = [&](int t, Token& x) {
         const int64_t row = (int64_t)sl.row0 + t;
-        const float lse = lse_in[row];
-        int at = -1;
-        float wgt = 0.0f, dw = 0.0f;
-        if (lane < k) {
-            at = indices[row * k + lane];
-            wgt = weights[row * k + lane];
-            if (dweights) dw = dweights[row * k + lane];
+        const bool inside = t < sl.rows;
+        x.on = inside && (!mask || mask[row] != 0);
+        x.row.load(logits + row * ld, l, E, wide, x.on);
+        x.lse = inside ? lse_in[row] : 0.0f;
+        x.at = -1;
+        x.wgt = x.dw = 0.0f;
+        if (inside && l < k) {
+            x.at = indices[row * k + l];
+            x.wgt = weights[row * k + l];
+            if (dweights) x.dw = dweights[row * k + l];
         }
-        if (at < 0 || at >= E) at = -1, dw = 0.0f;
-        // a token without a chosen expert takes part only through NaN logits
-        bool on = !mask || mask[row] != 0;
-        float l[S], p[S], inner = 0.0f;
+        if (x.at < 0 || x.at >= E) x.at = -1, x.dw = 0.0f;
+    };
+    Token now, next;
+    fetch(group, now);
+    for (int t = group; t - lane / L < sl.rows; t += kWarps * kGroups) {
+        fetch(t + kWarps * kGroups, next);
+        float p[N], inner = 0.0f;
         bool any = false;
+        const float from = now.lse * kLog2e;
 #pragma unroll
-        for (int i = 0; i < S; i++) {
-            const int e = i * 32 + lane;
-            l[i] = on && e < E ? to_float(logits[row * ld + e]) : -INFINITY;
-            any |= !(l[i] == -INFINITY);
+        for (int i = 0; i < N; i++) {
+            const float v = now.on && R::expert(l, i) < E ? to_float(now.row.run[i / V].v[i % V]) : -INFINITY;
+            any |= !(v == -INFINITY);
+            p[i] = exp2_fast(fmaf(v, kLog2e, -from));
+            inner = fmaf(p[i], f[i], inner);
         }
-        on = __any_sync(kAllLanes, any);
+        const bool on = group_max<L>((uint32_t)any) != 0;  // some logit is not -inf
+        inner = group_sum<L>(inner);
+        const float dwsum = group_sum<L>(now.dw * now.wgt);
+        if (now.at >= 0) s_extra[group][now.at] = now.wgt * (renormalize ? now.dw - dwsum : now.dw);
+        __syncwarp();
+        const float common = cb * now.lse - ca * inner - (renormalize ? 0.0f : dwsum);
+        if (t < sl.rows) {
+            T* const out = dlogits + ((int64_t)sl.row0 + t) * dld;
 #pragma unroll
-        for (int i = 0; i < S; i++) {
-            p[i] = on && i * 32 + lane < E ? expf(l[i] - lse) : 0.0f;
-            inner += p[i] * f[i];
-        }
-        inner = warp_sum(inner);
-        const float dwsum = warp_sum(dw * wgt);
-        if (at >= 0) s_extra[w][at] = wgt * (renormalize ? dw - dwsum : dw);
-        __syncwarp();
-        const float common = cb * lse - ca * inner - (renormalize ? 0.0f : dwsum);
+            for (int c = 0; c < C; c++) {
+                const int e = (c * L + l) * V;
+                Pack<T, V> o;
 #pragma unroll
-        for (int i = 0; i < S; i++) {
-            const int e = i * 32 + lane;
-            if (e < E)
-                dlogits[row * dld + e] = from_float<T>(on ? p[i] * (ca * f[i] + common) + s_extra[w][e] : 0.0f);
+                for (int i = 0; i < V; i++) {
+                    const float d = fmaf(p[c * V + i], fmaf(ca, f[c * V + i], common), s_extra[group][e + i]);
+                    o.v[i] = from_float<T>(on ? d : 0.0f);
+                }
+                if (wide_out && e + V <= E) {
+                    *reinterpret_cast<Pack<T, V>*>(out + e) = o;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; i++)
+                        if (e + i < E) out[e + i] = o.v[i];
+                }
+            }
         }
         __syncwarp();
-        if (at >= 0) s_extra[w][at] = 0.0f;
+        if (now.at >= 0) s_extra[group][now.at] = 0.0f;
         __syncwarp();
+        now = next;
     }
 }
 
@@ -269,22 +448,28 @@ int ready(const sparbit_router_plan_s* p) {
     return cur == p->device ? SPARBIT_OK : SPARBIT_ERR_ARG;
 }
 
+// Lanes a token and runs of 16 bytes a lane: the fewest lanes that hold the experts in one run and
+// have one for each choice, then more runs.
 template <typename T, typename F>
-int by_experts(int E, F f) {
-    if (E <= 64) return f.template operator()<T, 2>();
-    if (E <= 128) return f.template operator()<T, 4>();
-    if (E <= 256) return f.template operator()<T, 8>();
-    if (E <= 512) return f.template operator()<T, 16>();
-    return f.template operator()<T, 32>();
+int by_experts(int E, int k, F f) {
+    constexpr int V = 16 / sizeof(T);
+    if (E <= 8 * V && k <= 8) return f.template operator()<T, 8, 1>();
+    if (E <= 16 * V && k <= 16) return f.template operator()<T, 16, 1>();
+    if (E <= 32 * V) return f.template operator()<T, 32, 1>();
+    if (E <= 64 * V) return f.template operator()<T, 32, 2>();
+    if (E <= 128 * V) return f.template operator()<T, 32, 4>();
+    if constexpr (V == 4) return f.template operator()<T, 32, 8>();
+    return SPARBIT_ERR_LIMIT;
 }
 template <typename F>
-int by_type(int dtype, int E, F f) {
+int by_type(int dtype, int E, int k, F f) {
     switch (dtype) {
-        case SPARBIT_F32: return by_experts<float>(E, f);
-        case SPARBIT_BF16: return by_experts<__nv_bfloat16>(E, f);
-        default: return by_experts<__half>(E, f);
+        case SPARBIT_F32: return by_experts<float>(E, k, f);
+        case SPARBIT_BF16: return by_experts<__nv_bfloat16>(E, k, f);
+        default: return by_experts<__half>(E, k, f);
     }
 }
+bool wide_rows(const void* p, size_t ld, size_t es) { return common_alignment((uintptr_t)p | ld * es, 16) == 16; }
 
 }  // namespace
 
@@ -370,15 +555,15 @@ int sparbit_router_forward(sparbit_router_plan_t* p, const void* logits, size_t 
     int32_t* pc = (int32_t*)(p->work + p->off_counts());
     float* ps = (float*)(p->work + p->off_sums());
     if (!p->slices.empty()) {
-        const int rc = by_type(p->dtype, p->E, [&]<typename T, int S>() {
-            CU(launch(router_forward_kernel<T, S>, dim3((unsigned)p->slices.size()), dim3(kWarps * 32), 0, st,
-                      (const Slice*)p->work, (const T*)logits, (int64_t)ld, mask, p->E, p->k, p->renormalize, indices,
-                      weights, lse, pc, ps));
+        const int rc = by_type(p->dtype, p->E, p->k, [&]<typename T, int L, int C>() {
+            CU(launch(router_forward_kernel<T, L, C>, dim3((unsigned)p->slices.size()), dim3(kWarps * 32), 0, st,
+                      (const Slice*)p->work, (const T*)logits, (int64_t)ld, (int)wide_rows(logits, ld, es), mask, p->E,
+                      p->k, p->renormalize, indices, weights, lse, pc, ps));
             return (int)SPARBIT_OK;
         });
         if (rc != SPARBIT_OK) return rc;
     }
-    CU(launch(router_reduce_kernel, dim3((unsigned)(p->E / 128 + 1), (unsigned)p->n_ranks), dim3(128), 0, st,
+    CU(launch(router_reduce_kernel, dim3((unsigned)(p->E / 32 + 1), (unsigned)p->n_ranks), dim3(256), 0, st,
               (const int2*)(p->work + p->off_ranks()), p->E, (const int32_t*)pc, (const float*)ps, counts, sums));
     return SPARBIT_OK;
 }
@@ -412,11 +597,11 @@ int sparbit_router_backward(sparbit_router_plan_t* p, const void* logits, size_t
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
     if (p->slices.empty()) return SPARBIT_OK;
-    return by_type(p->dtype, p->E, [&]<typename T, int S>() {
-        CU(launch(router_backward_kernel<T, S>, dim3((unsigned)p->slices.size()), dim3(kWarps * 32), 0,
-                  (cudaStream_t)stream, (const Slice*)p->work, (const T*)logits, (int64_t)ld, mask, p->E, p->k,
-                  p->renormalize, indices, weights, lse, gathered, G, dweights, alpha, beta, dloss, (T*)dlogits,
-                  (int64_t)dlogits_ld));
+    return by_type(p->dtype, p->E, p->k, [&]<typename T, int L, int C>() {
+        CU(launch(router_backward_kernel<T, L, C>, dim3((unsigned)p->slices.size()), dim3(kWarps * 32), 0,
+                  (cudaStream_t)stream, (const Slice*)p->work, (const T*)logits, (int64_t)ld,
+                  (int)wide_rows(logits, ld, es), mask, p->E, p->k, p->renormalize, indices, weights, lse, gathered, G,
+                  dweights, alpha, beta, dloss, (T*)dlogits, (int64_t)dlogits_ld, (int)wide_rows(dlogits, dlogits_ld, es)));
         return (int)SPARBIT_OK;
     });
 }
