@@ -25,5 +25,6 @@ def __getattr__(name):
         _train = importlib.import_module(".train", __name__)
     for module in (_binding, _train):
         if hasattr(module, name):
-            return getattr(module, name)
+            value = globals()[name] = getattr(module, name)  # found directly from now on
+            return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

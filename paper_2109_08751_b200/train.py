@@ -8,7 +8,8 @@ from __future__ import annotations
 
 import ctypes
 
-from .binding import ERR_TIMEOUT, _check, _i, _ptr, _stream_handle, _sz, _vp, lib
+from .binding import ERR_TIMEOUT, OK, SparbitError, _i, _sz, _vp, lib
+from .binding import _ptr as _address
 
 F32, BF16, F16 = range(3)
 PRODUCTS_AUTO, PRODUCTS_ONE, PRODUCTS_THREE = 0, 1, 3
@@ -61,6 +62,30 @@ for _name, (_res, _args) in SYMBOLS.items():
     _fn = getattr(lib, _name)  # AttributeError here means the library does not match the header
     _fn.restype = _res
     _fn.argtypes = _args
+_scan_forward, _scan_backward, _scan_step = lib.sparbit_scan_forward, lib.sparbit_scan_backward, lib.sparbit_scan_step
+
+
+# The calls below can be shorter than their own marshalling (a token's step takes the GPU 3 us), so
+# the common cases come first.
+def _ptr(x):
+    """Address of a tensor (or of anything binding._ptr knows)."""
+    if x is None:
+        return None
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return _address(x)
+
+
+def _stream_handle(stream):
+    if stream is None or isinstance(stream, int):
+        return stream
+    return stream.cuda_stream
+
+
+def _check(code: int, where: str) -> None:
+    if code != OK:
+        raise SparbitError(code, where)
 
 
 class _TrainPlan:
@@ -133,14 +158,14 @@ class ScanPlan(_TrainPlan):
     def forward(self, gate, x, y, h0=None, summary=None, carry=None, stream=None, gate_ld=None, x_ld=None, y_ld=None,
                 h0_ld=None) -> None:
         d = self.channels
-        _check(lib.sparbit_scan_forward(self._h, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(h0), h0_ld or d,
+        _check(_scan_forward(self._h, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(h0), h0_ld or d,
                                         _ptr(y), y_ld or d, _ptr(summary), _ptr(carry), _stream_handle(stream)),
                "sparbit_scan_forward")
 
     def backward(self, gate, x, carry, dy, dgate, dx, dlast=None, dsummary=None, stream=None, gate_ld=None, x_ld=None,
                  dy_ld=None, dgate_ld=None, dx_ld=None, dlast_ld=None) -> None:
         d = self.channels
-        _check(lib.sparbit_scan_backward(self._h, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(carry), _ptr(dy),
+        _check(_scan_backward(self._h, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(carry), _ptr(dy),
                                          dy_ld or d, _ptr(dlast), dlast_ld or d, _ptr(dgate), dgate_ld or d,
                                          _ptr(dx), dx_ld or d, _ptr(dsummary), _stream_handle(stream)),
                "sparbit_scan_backward")
@@ -150,7 +175,7 @@ def scan_step(rows: int, channels: int, dtype: int, gate, x, state_in, state_out
               stream=None, gate_ld=None, x_ld=None, y_ld=None, state_ld=None) -> None:
     """One token for each of `rows` running sequences; n_slots defaults to `rows`."""
     d = channels
-    _check(lib.sparbit_scan_step(rows, d, dtype, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(slots),
+    _check(_scan_step(rows, d, dtype, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(slots),
                                  rows if n_slots is None else n_slots, _ptr(state_in), _ptr(state_out), state_ld or d,
                                  _ptr(y), y_ld or d, _stream_handle(stream)), "sparbit_scan_step")
 
