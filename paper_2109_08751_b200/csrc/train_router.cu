@@ -23,8 +23,9 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kMaxExperts = SPARBIT_ROUTER_MAX_EXPERTS;
 constexpr int kMaxK = SPARBIT_ROUTER_MAX_K;
-// CTAs a forward or backward pass is cut into, at most
-constexpr int kSlices = 592;
+// CTAs a forward or backward pass is cut into (and one more a rank, at most): what four CTAs on each
+// of a B200's 148 SMs hold at once, so that there is no second round of a few
+constexpr int kSlices = 584;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // A run of tokens of one rank, worked on by one CTA.
@@ -38,23 +39,21 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
-// Keys: 32 bits (order of a 16-bit logit, complement of the index) or 64.  0: cannot be chosen (NaN,
-// -inf).  Zeros of either sign are equal.
+// Keys: 32 bits (order of a 16-bit logit, complement of the index) or 64.  Zeros of either sign are
+// equal.  A key below kLeast (-inf, or what a NaN is made into) cannot be chosen.
 template <typename T>
 using Key = std::conditional_t<sizeof(T) == 2, uint32_t, unsigned long long>;
-__device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
-__device__ __forceinline__ uint32_t bits_of(__half v) { return __half_as_ushort(v); }
 template <typename T>
-__device__ __forceinline__ Key<T> make_key(T t, float v, int e) {
-    if constexpr (sizeof(T) == 2) {
-        const uint32_t b = v == 0.0f ? 0u : bits_of(t);
-        const uint32_t o = (b & 0x8000u) ? ~b & 0xffffu : b | 0x8000u;
-        return v > -INFINITY ? o << 16 | (0xffffu - (uint32_t)e) : 0u;
-    } else {
-        const uint32_t b = __float_as_uint(v + 0.0f);
-        const uint32_t o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
-        return v > -INFINITY ? (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)e) : 0ull;
-    }
+constexpr Key<T> kLeast = std::is_same_v<T, float>           ? (Key<T>)0x00800000ull << (sizeof(T) == 2 ? 0 : 32)
+                          : std::is_same_v<T, __nv_bfloat16> ? (Key<T>)0x00800000u
+                                                             : (Key<T>)0x04000000u;
+__device__ __forceinline__ uint32_t plus_zero(__nv_bfloat16 a, __nv_bfloat16 b) {
+    const __nv_bfloat162 r = __hadd2(__halves2bfloat162(a, b), __float2bfloat162_rn(0.0f));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t plus_zero(__half a, __half b) {
+    const __half2 r = __hadd2(__halves2half2(a, b), __float2half2_rn(0.0f));
+    return *reinterpret_cast<const uint32_t*>(&r);
 }
 template <typename T>
 __device__ __forceinline__ int key_index(Key<T> k) {
@@ -116,30 +115,66 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
-// A lane's logits of a row: experts (c L + l) V + i.  wide: rows start on multiples of 16 bytes.
+// A lane's logits of a row: experts (c L + l) V + i; -inf where there is no expert.  wide: rows start on multiples of 16 bytes.
 template <typename T, int L, int C>
 struct Row {
     static constexpr int V = 16 / sizeof(T), N = V * C;
     Pack<T, V> run[C];
     __device__ __forceinline__ void load(const T* p, int l, int E, bool wide, bool on) {
+        const T none = from_float<T>(-INFINITY);
 #pragma unroll
         for (int c = 0; c < C; c++) {
             const int e = (c * L + l) * V;
-            if (!on) {
-            } else if (wide && e + V <= E) {
+            if (on && wide && e + V <= E) {
                 run[c] = *reinterpret_cast<const Pack<T, V>*>(p + e);
             } else {
 #pragma unroll
-                for (int i = 0; i < V; i++)
-                    if (e + i < E) run[c].v[i] = p[e + i];
+                for (int i = 0; i < V; i++) run[c].v[i] = none;
+                if (on) {
+#pragma unroll
+                    for (int i = 0; i < V; i++)
+                        if (e + i < E) run[c].v[i] = p[e + i];
+                }
             }
         }
     }
+    // A token that is left out: whatever was loaded, no expert can be chosen.  (Loading does not wait for
+    // the mask.)
+    __device__ __forceinline__ void leave_out() {
+        const T none = from_float<T>(-INFINITY);
+#pragma unroll
+        for (int n = 0; n < N; n++) run[n / V].v[n % V] = none;
+    }
+    __device__ __forceinline__ float value(int n) const { return to_float(run[n / V].v[n % V]); }
     __device__ __forceinline__ static int expert(int l, int n) { return (n / V * L + l) * V + n % V; }
+    // Keys of all logits; a NaN with a clear sign bit comes out above everything.
+    __device__ __forceinline__ void keys(int l, Key<T> (&key)[N]) const {
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int i = 0; i < V; i += 2) {
+                    // two at a time: adding zero makes -0 a 0, then the sign decides which bits turn
+                    const uint32_t u = plus_zero(run[c].v[i], run[c].v[i + 1]);
+                    const uint32_t o = u ^ (((u >> 15) & 0x00010001u) * 0x7fffu | 0x80008000u);
+                    const uint32_t e = 0xffffu - (uint32_t)((c * L + l) * V + i);
+                    key[c * V + i] = o << 16 | e;
+                    key[c * V + i + 1] = (o & 0xffff0000u) | (e - 1);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i++) {
+                    const uint32_t u = __float_as_uint(run[c].v[i] + 0.0f);
+                    const uint32_t o = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+                    key[c * V + i] = (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)((c * L + l) * V + i));
+                }
+            }
+        }
+    }
 };
 
 template <typename T, int L, int C>
-__global__ void __launch_bounds__(kWarps * 32) router_forward_kernel(const Slice* slices, const T* logits, int64_t ld,
+__global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_kernel(const Slice* slices, const T* logits, int64_t ld,
                                                                     int wide, const uint8_t* mask, int E, int k,
                                                                     int renormalize, int32_t* indices, float* weights,
                                                                     float* lse_out, int32_t* part_counts,
@@ -161,53 +196,63 @@ __global__ void __launch_bounds__(kWarps * 32) router_forward_kernel(const Slice
 #pragma unroll
     for (int i = 0; i < N; i++) acc[i] = 0.0f;
     R now;
-    bool on = group < sl.rows && (!mask || mask[(int64_t)sl.row0 + group] != 0);
-    now.load(logits + ((int64_t)sl.row0 + group) * ld, l, E, wide, on);
+    int on_byte = group < sl.rows;  // the mask's byte, looked at when the token's turn comes
+    now.load(logits + ((int64_t)sl.row0 + group) * ld, l, E, wide, on_byte);
+    if (mask && on_byte) on_byte = mask[(int64_t)sl.row0 + group];
     for (int t = group; t - lane / L < sl.rows; t += kWarps * kGroups) {
         const int64_t row = (int64_t)sl.row0 + t;
         const bool inside = t < sl.rows;
         // the next token's logits travel while this one's are worked on
         const int t2 = t + kWarps * kGroups;
-        const bool on2 = t2 < sl.rows && (!mask || mask[(int64_t)sl.row0 + t2] != 0);
+        int next_byte = t2 < sl.rows;
         R next;
-        next.load(logits + ((int64_t)sl.row0 + t2) * ld, l, E, wide, on2);
-        float v[N];
-        K key[N];
+        next.load(logits + ((int64_t)sl.row0 + t2) * ld, l, E, wide, next_byte);
+        if (mask && next_byte) next_byte = mask[(int64_t)sl.row0 + t2];
+        const bool on = on_byte != 0;
+        if (!on) now.leave_out();
+        K key[N], head, first;
+        now.keys(l, key);
+        auto find_first = [&]() {
+            if constexpr (N <= 8) sort_keys(key);
+            head = key[0];
+            if constexpr (N > 8) {
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-            const int e = R::expert(l, i);
-            const T raw = now.run[i / R::V].v[i % R::V];
-            v[i] = on && e < E ? to_float(raw) : -INFINITY;
-            key[i] = make_key<T>(raw, v[i], e);
+                for (int i = 1; i < N; i++) head = key[i] > head ? key[i] : head;
+            }
+            first = group_max<L>(head);
+        };
+        find_first();
+        float p[N], sum, from, top;
+        auto softmax = [&]() {
+            top = first >= kLeast<T> ? key_value<T>(first) : -INFINITY;
+            // +inf: inf - inf below is the NaN it should be
+            from = (top > -INFINITY && top < INFINITY ? top : 0.0f) * kLog2e;
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                p[i] = exp2_fast(fmaf(now.value(i), kLog2e, -from));
+                sum += p[i];
+            }
+            sum = group_sum<L>(sum);
+        };
+        softmax();
+        bool nan = sum != sum;
+        if (__any_sync(kAllLanes, nan)) {  // a NaN somewhere in the warp's tokens: not to be chosen
+            now.keys(l, key);
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                if (now.value(i) != now.value(i)) key[i] = 0;
+            find_first();
+            softmax();
+            nan = sum != sum;
         }
-        if constexpr (N <= 8) sort_keys(key);
-        K head = key[0];
-        if constexpr (N > 8) {
-#pragma unroll
-            for (int i = 1; i < N; i++) head = key[i] > head ? key[i] : head;
-        }
-        const K first = group_max<L>(head);
-        const float top = first ? key_value<T>(first) : -INFINITY;
-        bool nan = false;
-#pragma unroll
-        for (int i = 0; i < N; i++) nan |= v[i] != v[i];
-        nan = group_max<L>((uint32_t)nan) != 0;
-        const bool part = on && (first != 0 || nan);
-        // +inf: inf - inf below is the NaN it should be
-        const float from = (top > -INFINITY && top < INFINITY ? top : 0.0f) * kLog2e;
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; i++) {
-            v[i] = exp2_fast(fmaf(v[i], kLog2e, -from));
-            sum += v[i];
-        }
-        sum = group_sum<L>(sum);
+        const bool part = on && (first >= kLeast<T> || nan);
         const float inv = __fdividef(1.0f, sum);
         // the chosen ones: lane j gets the j-th
         K mine = 0, won = first;
         for (int j = 0; j < k; j++) {
             if (l == j) mine = won;
-            if (head == won && won != 0) {
+            if (head == won) {
                 if constexpr (N <= 8) {
 #pragma unroll
                     for (int i = 0; i + 1 < N; i++) key[i] = key[i + 1];
@@ -221,11 +266,10 @@ __global__ void __launch_bounds__(kWarps * 32) router_forward_kernel(const Slice
             }
             if (j + 1 < k) won = group_max<L>(head);
         }
-        const int index = part && mine != 0 ? key_index<T>(mine) : -1;
+        const int index = part && mine >= kLeast<T> ? key_index<T>(mine) : -1;
         float wgt = 0.0f;
         if (index >= 0) {
             wgt = exp2_fast(fmaf(key_value<T>(mine), kLog2e, -from)) * inv;
-            if (nan) wgt = NAN;
             atomicAdd(&s_count[index], 1);
         }
         if (renormalize) {
@@ -235,7 +279,7 @@ __global__ void __launch_bounds__(kWarps * 32) router_forward_kernel(const Slice
         const float lse = part ? (from + __log2f(sum)) * 0.6931471805599453f : 0.0f;
         if (part) {
 #pragma unroll
-            for (int i = 0; i < N; i++) acc[i] = fmaf(v[i], inv, acc[i]);
+            for (int i = 0; i < N; i++) acc[i] = fmaf(p[i], inv, acc[i]);
             z = fmaf(lse, lse, z);
             taken++;
         }
@@ -247,7 +291,7 @@ __global__ void __launch_bounds__(kWarps * 32) router_forward_kernel(const Slice
             if (l == 0) lse_out[row] = lse;
         }
         now = next;
-        on = on2;
+        on_byte = next_byte;
     }
     if (l == 0 && taken) atomicAdd(&s_count[kSpan], taken);
 #pragma unroll
@@ -323,7 +367,7 @@ __global__ void __launch_bounds__(256) router_balance_kernel(const int32_t* gath
 }
 
 template <typename T, int L, int C>
-__global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Slice* slices, const T* logits, int64_t ld,
+__global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_backward_kernel(const Slice* slices, const T* logits, int64_t ld,
                                                                      int wide, const uint8_t* mask, int E, int k,
                                                                      int renormalize, const int32_t* indices,
                                                                      const float* weights, const float* lse_in,
@@ -357,15 +401,16 @@ __global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Slic
 
     struct Token {
         R row;
-        bool on;
+        int on;  // the mask's byte, looked at when the token's turn comes
         float lse, wgt, dw;
         int at;
     };
     auto fetch = [&](int t, Token& x) {
         const int64_t row = (int64_t)sl.row0 + t;
         const bool inside = t < sl.rows;
-        x.on = inside && (!mask || mask[row] != 0);
-        x.row.load(logits + row * ld, l, E, wide, x.on);
+        x.row.load(logits + row * ld, l, E, wide, inside);
+        x.on = inside;
+        if (mask && inside) x.on = mask[row];
         x.lse = inside ? lse_in[row] : 0.0f;
         x.at = -1;
         x.wgt = x.dw = 0.0f;
@@ -374,23 +419,21 @@ __global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Slic
             x.wgt = weights[row * k + l];
             if (dweights) x.dw = dweights[row * k + l];
         }
-        if (x.at < 0 || x.at >= E) x.at = -1, x.dw = 0.0f;
     };
     Token now, next;
     fetch(group, now);
     for (int t = group; t - lane / L < sl.rows; t += kWarps * kGroups) {
         fetch(t + kWarps * kGroups, next);
+        if (!now.on) now.row.leave_out();
+        if (now.at < 0 || now.at >= E) now.at = -1, now.dw = 0.0f;
+        // a token that is left out has p = 0 and nothing chosen: its gradient comes out as 0
         float p[N], inner = 0.0f;
-        bool any = false;
         const float from = now.lse * kLog2e;
 #pragma unroll
         for (int i = 0; i < N; i++) {
-            const float v = now.on && R::expert(l, i) < E ? to_float(now.row.run[i / V].v[i % V]) : -INFINITY;
-            any |= !(v == -INFINITY);
-            p[i] = exp2_fast(fmaf(v, kLog2e, -from));
+            p[i] = exp2_fast(fmaf(now.row.value(i), kLog2e, -from));
             inner = fmaf(p[i], f[i], inner);
         }
-        const bool on = group_max<L>((uint32_t)any) != 0;  // some logit is not -inf
         inner = group_sum<L>(inner);
         const float dwsum = group_sum<L>(now.dw * now.wgt);
         if (now.at >= 0) s_extra[group][now.at] = now.wgt * (renormalize ? now.dw - dwsum : now.dw);
@@ -404,8 +447,7 @@ __global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Slic
                 Pack<T, V> o;
 #pragma unroll
                 for (int i = 0; i < V; i++) {
-                    const float d = fmaf(p[c * V + i], fmaf(ca, f[c * V + i], common), s_extra[group][e + i]);
-                    o.v[i] = from_float<T>(on ? d : 0.0f);
+                    o.v[i] = from_float<T>(fmaf(p[c * V + i], fmaf(ca, f[c * V + i], common), s_extra[group][e + i]));
                 }
                 if (wide_out && e + V <= E) {
                     *reinterpret_cast<Pack<T, V>*>(out + e) = o;
@@ -496,7 +538,7 @@ int sparbit_router_plan_create(int n_ranks, const size_t* tokens, int experts, i
         p->renormalize = renormalize != 0;
         p->rows = rows;
         size_t each = (rows + kSlices - 1) / kSlices;
-        each = round_up(each ? each : 1, kWarps);
+        each = round_up(each > 32 ? each : 32, kWarps);
         size_t row = 0;
         for (int r = 0; r < n_ranks; r++) {
             const int first = (int)p->slices.size();
