@@ -100,6 +100,11 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, u
         "l"(map), "r"(bar & 0xfeffffffu), "r"(x), "r"(y), "r"(z)
         : "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -362,7 +367,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // full, drained: in the first CTA, for both; empty, done: in each
     const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(kAllLanes, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
@@ -381,18 +386,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_base;
+    const int blocks = (g.K + kTileK - 1) / kTileK, flush = kThree ? kFlush : blocks;
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    // the list of tiles and the maps are the plan's own and do not change: read ahead of the wait
+    const uint32_t first_rc = g.tiles[pair % g.n_tiles];
+    if (threadIdx.x == 0) {
+        const CUtensorMap* maps[4] = {&a_hi, &b_hi, &a_lo, &b_lo};
+#pragma unroll
+        for (int i = 0; i < (kThree ? 4 : 2); i++) asm volatile("prefetch.tensormap [%0];" ::"l"(maps[i]) : "memory");
+    }
     pdl_wait();
     pdl_trigger();
 
-    const int blocks = (g.K + kTileK - 1) / kTileK, flush = kThree ? kFlush : blocks;
-    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     if (warp == 0) {
         if (lane == 0) {
             uint32_t n = 0;  // stages filled so far
             bool ok = true;
             for (int t = pair; t < g.total && ok; t += pairs) {
                 const int z = t / g.n_tiles;
-                const uint32_t rc = g.tiles[t - z * g.n_tiles];
+                const uint32_t rc = t == pair ? first_rc : g.tiles[t - z * g.n_tiles];
                 const int row = (int)(rc >> 16) * kTileM + rank * (kTileM / 2), col = (int)(rc & 0xffff) * kN + rank * (kN / 2);
                 for (int s = 0; s < blocks; s++, n++) {
                     const uint32_t st = n % kStages;
@@ -429,10 +441,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        // The whole warp walks the loop and one lane issues: what is the same for all lanes stays in uniform
+        // registers, and a product's issue fits the 64 clocks that one of 256 x 128 x 16 takes.
+        if (rank == 0) {
             // fp16 operands, fp32 accumulator, 256 x kN; B MN-major for Apply
             constexpr uint32_t idesc = (1u << 4) | (kSquare ? 0u : 1u << 16) | ((uint32_t)(kN >> 3) << 17) |
                                        ((uint32_t)(kTileM >> 4) << 24);
+            constexpr uint32_t kPart = (kABytes + kBBytes) >> 4;  // from hi to lo, in descriptor units
+            const uint64_t a0 = smem_desc(ring, 16, 1024);
+            const uint64_t b0 = smem_desc(ring + kABytes, kSquare ? 16 : kTileK * 128, 1024);
             uint32_t n = 0, group = 0;
             bool ok = true;
             for (int t = pair; t < g.total && ok; t += pairs) {
@@ -451,23 +468,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             break;
                         }
                         fence_after();
-                        const uint32_t ah = ring + st * kStageBytes, bh = ah + kABytes;
+                        const uint64_t at = a0 + st * (kStageBytes >> 4), bt = b0 + st * (kStageBytes >> 4);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int seg = 0; seg < (kThree ? 3 : 1); seg++) {
-                            // hi hi, hi lo, lo hi
-                            const uint32_t at = ah + (seg == 2 ? kABytes + kBBytes : 0);
-                            const uint32_t bt = bh + (seg == 1 ? kABytes + kBBytes : 0);
+                            for (int seg = 0; seg < (kThree ? 3 : 1); seg++) {
+                                // hi hi, hi lo, lo hi
 #pragma unroll
-                            for (int k = 0; k < kTileK / 16; k++) {
-                                const uint64_t da = smem_desc(at + k * 32, 16, 1024);
-                                const uint64_t db = kSquare ? smem_desc(bt + k * 32, 16, 1024)
-                                                            : smem_desc(bt + k * 2048, kTileK * 128, 1024);
-                                mma_f16(tmem + slot * kN, da, db, idesc, s > s0 || seg > 0 || k > 0);
+                                for (int k = 0; k < kTileK / 16; k++)
+                                    mma_f16(tmem + slot * kN, at + (seg == 2 ? kPart : 0) + k * (32 >> 4),
+                                            bt + (seg == 1 ? kPart : 0) + k * ((kSquare ? 32 : 2048) >> 4), idesc,
+                                            s > s0 || seg > 0 || k > 0);
                             }
+                            mma_commit(empty + 8 * st);
                         }
-                        mma_commit(empty + 8 * st);
+                        __syncwarp();
                     }
-                    if (ok) mma_commit(done + 8 * slot);
+                    if (ok && elect_one()) mma_commit(done + 8 * slot);
+                    __syncwarp();
                 }
             }
         }
@@ -482,7 +499,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t group = 0;
         for (int t = pair; t < g.total; t += pairs) {
             const int z = t / g.n_tiles;
-            const uint32_t rc = g.tiles[t - z * g.n_tiles];
+            const uint32_t rc = t == pair ? first_rc : g.tiles[t - z * g.n_tiles];
             const int row0 = (int)(rc >> 16) * kTileM + rank * (kTileM / 2) + quad * 32;
             const int col0 = (int)(rc & 0xffff) * kN + half * kCols;
             const float q = g.first ? g.q[z] : 1.0f / kScaleX;
