@@ -34,13 +34,20 @@ namespace {
 // its tensor memory, 128 rows of the accumulator.  An SM takes in about 64 bytes a clock; alone a CTA
 // would need 96 for 128 x 256 (measured: two thirds of the pair's rate).
 constexpr int kTileM = 256, kTileK = 64;
-constexpr int kRing = 196608;  // stages of a CTA: 6 of 32 KiB (kN = 256) or 8 of 24 KiB, three products 3 or 4
 constexpr int kABytes = kTileM / 2 * kTileK * 2;
-constexpr int kThreads = 320;  // warp 0 loads, warp 1 multiplies, warps 2-9 write out
+// Of the epilogue: warps, columns a warp has, stages, shared memory.  One product: 16 warps, each takes
+// its columns from tensor memory block by block.  Three: 8 warps with their columns' sums in registers.
+template <bool kThree>
+constexpr int kOutWarps = kThree ? 8 : 16;
+template <bool kThree>
+constexpr int kThreads = 64 + 32 * kOutWarps<kThree>;  // warp 0 loads, warp 1 multiplies, the others write out
+template <bool kThree>
+constexpr int kRing = kThree ? 196608 : 163840;        // 4 stages of 48 KiB; 5 of 32 or 6 of 24
+template <bool kThree>
+constexpr int kSmem = kRing<kThree> + kOutWarps<kThree> * 32 * 32 * 4 + 1024;  // ring, a block for each warp, alignment
 // The tensor cores cut each partial sum towards zero: over K = 4096 a relative error of 1e-5, which
 // three products would not survive.  They hand over every 128 of K to a sum rounded in registers.
 constexpr int kFlush = 2;
-constexpr int kSmem = kRing + 8 * 32 * 33 * 4 + 1024;   // ring, a block for each warp that writes, alignment
 constexpr int kNormParts = 512;                         // CTAs a matrix's norm is summed by
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;   // X and A, P are held times these
 constexpr unsigned long long kWaitNs = 2000000000ull;   // a wait inside the kernel gives up after this
@@ -230,22 +237,23 @@ __device__ __forceinline__ void write_result(const ProductArgs& g, int z, int64_
     write_any(g.out, z, r, c, n, v);
 }
 
-constexpr int kBlock = 32, kPitch = kBlock + 1;  // a warp's block of a product in shared memory, without bank conflicts
-constexpr int kBlockBytes = kBlock * kPitch * 4;
+// A warp's block of a product in shared memory: columns turned by the row's number, so that neither rows
+// nor columns meet a bank twice.
+constexpr int kBlock = 32;
+__device__ __forceinline__ int block_at(int r, int c) { return r * kBlock + (c ^ r); }
 
 // What the epilogue adds to a block: the lane's four elements of every fourth row, as stored - fp16 hi
 // and lo, or fp32.  Loaded before the products are done where registers allow.
-template <int kIts>
 struct Addend {
-    uint4 raw[kIts];
+    uint4 raw[kBlock / 4];
 };
-template <int kOp, bool kThree, int kIts>
-__device__ __forceinline__ void load_addend(const ProductArgs& g, int z, int row0, int col0, Addend<kIts>& d) {
+template <int kOp, bool kThree>
+__device__ __forceinline__ void load_addend(const ProductArgs& g, int z, int row0, int col0, Addend& d) {
     if (kOp == kGram) return;
     const int lane = threadIdx.x & 31, row = row0 + (lane >> 3), col = col0 + (lane & 7) * 4;
     const int64_t at = z * g.z_in + row * g.ld_in + col;
 #pragma unroll
-    for (int it = 0; it < kIts; it++) {
+    for (int it = 0; it < kBlock / 4; it++) {
         if (row + it * 4 >= g.M || col >= g.N) continue;
         const int64_t i = at + (int64_t)(it * 4) * g.ld_in;
         if (kOp != kPoly && kThree) {
@@ -268,29 +276,27 @@ __device__ __forceinline__ void unpack_halves(uint32_t a, uint32_t b, float (&v)
 // 64-byte runs; then, where its mirror image or transpose goes out (too), the same by columns.  The
 // pitches of X, A and P are multiples of 64 elements: four elements that start inside a row may be read
 // and written whole (the columns past the matrix are outside the tensor maps).
-template <int kOp, bool kThree, bool kAhead, int kIts>
+template <int kOp, bool kThree>
 __device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int z, int row0, int col0, float q,
-                                            Addend<kIts>& d) {
+                                            const Addend& d) {
     constexpr bool kSquare = kOp == kGram || kOp == kPoly, kLows = kOp == kApply || (kSquare && kThree);
     const int lane = threadIdx.x & 31, lr = lane >> 3, lc = (lane & 7) * 4;
     const bool turn = kSquare ? col0 > row0 : kOp == kLast && g.transposed;
 #pragma unroll
     for (int it = 0; it < kBlock / 4; it++) {
         const int row = row0 + it * 4 + lr, col = col0 + lc;
-        if (!kAhead && it % kIts == 0) load_addend<kOp, kThree>(g, z, row0 + it * 4, col0, d);
         if (row >= g.M || col >= g.N) continue;
-        float* const at = sm + (it * 4 + lr) * kPitch + lc;
         float v[4], x[4], y[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = at[i];
+        for (int i = 0; i < 4; i++) v[i] = sm[block_at(it * 4 + lr, lc + i)];
         if (kOp != kGram) {
             if (kOp != kPoly && kThree) {
-                x[0] = __uint_as_float(d.raw[it % kIts].x), x[1] = __uint_as_float(d.raw[it % kIts].y);
-                x[2] = __uint_as_float(d.raw[it % kIts].z), x[3] = __uint_as_float(d.raw[it % kIts].w);
+                x[0] = __uint_as_float(d.raw[it].x), x[1] = __uint_as_float(d.raw[it].y);
+                x[2] = __uint_as_float(d.raw[it].z), x[3] = __uint_as_float(d.raw[it].w);
             } else {
-                unpack_halves(d.raw[it % kIts].x, d.raw[it % kIts].y, x);
+                unpack_halves(d.raw[it].x, d.raw[it].y, x);
                 if (kOp != kPoly || kThree) {
-                    unpack_halves(d.raw[it % kIts].z, d.raw[it % kIts].w, y);
+                    unpack_halves(d.raw[it].z, d.raw[it].w, y);
 #pragma unroll
                     for (int i = 0; i < 4; i++) x[i] += y[i];
                 }
@@ -311,7 +317,7 @@ __device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int
         }
         if (turn) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) at[i] = v[i];
+            for (int i = 0; i < 4; i++) sm[block_at(it * 4 + lr, lc + i)] = v[i];
         }
         if (kOp == kLast) {
             if (!turn) write_result(g, z, row, col, g.N - col, v);
@@ -334,7 +340,7 @@ __device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int
         if (row >= g.M || col >= g.N) continue;
         float v[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = sm[(lc + i) * kPitch + it * 4 + lr];
+        for (int i = 0; i < 4; i++) v[i] = sm[block_at(lc + i, it * 4 + lr)];
         if (kOp == kLast) {
             write_result(g, z, col, row, g.M - row, v);
         } else {
@@ -353,31 +359,32 @@ __device__ __forceinline__ void write_block(const ProductArgs& g, float* sm, int
 // Persistent, a pair of CTAs per pair of SMs.  Maps: A hi, A lo, B hi, B lo; boxes of 64 columns x 128
 // rows (A) and kN / 2 rows (B of Gram and Poly) or of 64 columns x 64 rows (Apply's B, used MN-major).
 template <int kOp, int kN, bool kThree>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
     product_kernel(const __grid_constant__ CUtensorMap a_hi, const __grid_constant__ CUtensorMap a_lo,
                    const __grid_constant__ CUtensorMap b_hi, const __grid_constant__ CUtensorMap b_lo,
                    const __grid_constant__ ProductArgs g) {
     constexpr bool kSquare = kOp == kGram || kOp == kPoly;
     constexpr int kBBytes = kN / 2 * kTileK * 2, kParts = kThree ? 2 : 1;
-    constexpr int kStageBytes = kParts * (kABytes + kBBytes), kStages = kRing / kStageBytes;
+    constexpr int kStageBytes = kParts * (kABytes + kBBytes), kStages = kRing<kThree> / kStageBytes;
+    constexpr int kSlots = 512 / kN;  // accumulators: products run ahead of the warps that write out
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * kStages + 4];
+    __shared__ uint64_t bars[2 * kStages + 2 * kSlots];
     __shared__ uint32_t tmem_base;
     __shared__ uint32_t gave_up;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // full, drained: in the first CTA, for both; empty, done: in each
-    const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 8 * kSlots;
     const int warp = __shfl_sync(kAllLanes, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; i++) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-        for (int i = 0; i < 2; i++) bar_init(done + 8 * i, 1), bar_init(drained + 8 * i, 16);
+        for (int i = 0; i < kSlots; i++) bar_init(done + 8 * i, 1), bar_init(drained + 8 * i, 2 * kOutWarps<kThree>);
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)),
-                     "r"(2 * kN)
+                     "r"(512)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
@@ -454,8 +461,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             bool ok = true;
             for (int t = pair; t < g.total && ok; t += pairs) {
                 for (int s0 = 0; s0 < blocks && ok; s0 += flush, group++) {
-                    const uint32_t slot = group & 1;
-                    if (group >= 2 && !bar_wait(drained + 8 * slot, (group / 2 - 1) & 1, &gave_up)) {
+                    const uint32_t slot = group % kSlots;
+                    if (group >= kSlots && !bar_wait(drained + 8 * slot, (group / kSlots - 1) & 1, &gave_up)) {
                         ok = false;
                         break;
                     }
@@ -489,57 +496,88 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
         }
     } else {
-        // TMEM lanes go by the warp's number mod 4; the two warps of a quarter take half the columns each
-        constexpr int kCols = kN / 2, kBlocks = kCols / kBlock;
-        constexpr bool kAhead = kN <= 128;  // registers for all addends at once
-        const int quad = warp & 3, half = (warp - 2) >> 2;
+        // TMEM lanes go by the warp's number mod 4; the warps of a quarter share the columns
+        constexpr int kCols = kN / (kOutWarps<kThree> / 4), kBlocks = kCols / kBlock;
+        const int quad = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        float* const sm = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + kRing) +
-                          (warp - 2) * (kBlockBytes / 4);
+        float* const sm = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + kRing<kThree>) +
+                          (warp - 2) * (kBlock * kBlock);
         uint32_t group = 0;
         for (int t = pair; t < g.total; t += pairs) {
             const int z = t / g.n_tiles;
             const uint32_t rc = t == pair ? first_rc : g.tiles[t - z * g.n_tiles];
             const int row0 = (int)(rc >> 16) * kTileM + rank * (kTileM / 2) + quad * 32;
-            const int col0 = (int)(rc & 0xffff) * kN + half * kCols;
+            const int col0 = (int)(rc & 0xffff) * kN + part * kCols;
             const float q = g.first ? g.q[z] : 1.0f / kScaleX;
-            Addend<kAhead ? kBlock / 4 : 4> d[kAhead ? kBlocks : 1];
-            if (kAhead) {
-#pragma unroll
-                for (int j = 0; j < kBlocks; j++) load_addend<kOp, kThree>(g, z, row0, col0 + j * kBlock, d[j]);
-            }
-            float acc[kCols];
-#pragma unroll
-            for (int i = 0; i < kCols; i++) acc[i] = 0.0f;
+            // blocks below the diagonal are the mirror images of others
+            auto wanted = [&](int j) {
+                const int col = col0 + j * kBlock;
+                return row0 < g.M && col < g.N && !(kSquare && col < row0);
+            };
+            Addend d[2];
             bool ok = true;
-            for (int s = 0; s < blocks; s += flush, group++) {
-                const uint32_t slot = group & 1;
-                ok = bar_wait(done + 8 * slot, (group / 2) & 1, &gave_up);
+            if constexpr (!kThree) {
+                // the addend of the first block travels while the products run, each other's while its
+                // predecessor goes out
+                if (wanted(0)) load_addend<kOp, kThree>(g, z, row0, col0, d[0]);
+                const uint32_t slot = group % kSlots;
+                ok = bar_wait(done + 8 * slot, (group / kSlots) & 1, &gave_up);
                 if (!ok) break;
                 fence_after();
 #pragma unroll
-                for (int j = 0; j < kCols / 16; j++) {
+                for (int j = 0; j < kBlocks; j++) {
+                    const int col = col0 + j * kBlock;
                     float v[16];
                     __syncwarp();
-                    tmem_load16(tmem + slot * kN + half * kCols + j * 16 + lanes, v);
 #pragma unroll
-                    for (int i = 0; i < 16; i++) acc[j * 16 + i] += v[i];
+                    for (int h = 0; h < 2; h++) {
+                        tmem_load16(tmem + slot * kN + part * kCols + j * kBlock + h * 16 + lanes, v);
+#pragma unroll
+                        for (int i = 0; i < 16; i++) sm[block_at(lane, h * 16 + i)] = v[i];
+                    }
+                    if (j + 1 == kBlocks) fence_before();
+                    __syncwarp();
+                    if (j + 1 == kBlocks && lane == 0) bar_arrive_first(drained + 8 * slot);
+                    if (j + 1 < kBlocks && wanted(j + 1)) load_addend<kOp, kThree>(g, z, row0, col + kBlock, d[(j + 1) & 1]);
+                    if (wanted(j)) write_block<kOp, kThree>(g, sm, z, row0, col, q, d[j & 1]);
                 }
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive_first(drained + 8 * slot);
-            }
-            if (!ok) break;
+                group++;
+            } else {
+                static_assert(kBlocks == 2, "registers for all addends beside the sums");
 #pragma unroll
-            for (int j = 0; j < kBlocks; j++) {
-                const int col = col0 + j * kBlock;
-                // blocks below the diagonal are the mirror images of others
-                if (row0 < g.M && col < g.N && !(kSquare && col < row0)) {
-                    __syncwarp();
+                for (int j = 0; j < kBlocks; j++)
+                    if (wanted(j)) load_addend<kOp, kThree>(g, z, row0, col0 + j * kBlock, d[j]);
+                float acc[kCols];
 #pragma unroll
-                    for (int i = 0; i < kBlock; i++) sm[lane * kPitch + i] = acc[j * kBlock + i];
+                for (int i = 0; i < kCols; i++) acc[i] = 0.0f;
+                for (int s = 0; s < blocks; s += flush, group++) {
+                    const uint32_t slot = group % kSlots;
+                    ok = bar_wait(done + 8 * slot, (group / kSlots) & 1, &gave_up);
+                    if (!ok) break;
+                    fence_after();
+#pragma unroll
+                    for (int j = 0; j < kCols / 16; j++) {
+                        float v[16];
+                        __syncwarp();
+                        tmem_load16(tmem + slot * kN + part * kCols + j * 16 + lanes, v);
+#pragma unroll
+                        for (int i = 0; i < 16; i++) acc[j * 16 + i] += v[i];
+                    }
+                    fence_before();
                     __syncwarp();
-                    write_block<kOp, kThree, kAhead>(g, sm, z, row0, col, q, d[kAhead ? j : 0]);
+                    if (lane == 0) bar_arrive_first(drained + 8 * slot);
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int j = 0; j < kBlocks; j++) {
+                    if (wanted(j)) {
+                        const int col = col0 + j * kBlock;
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < kBlock; i++) sm[block_at(lane, i)] = acc[j * kBlock + i];
+                        __syncwarp();
+                        write_block<kOp, kThree>(g, sm, z, row0, col, q, d[j]);
+                    }
                 }
             }
         }
@@ -549,7 +587,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     cluster_sync();  // nobody's barriers or tensor memory are needed any more
     if (warp == 1) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
 }
 
@@ -784,7 +822,8 @@ template <int kOp, int kN, bool kThree>
 int launch_product(const sparbit_ortho_plan_s* p, const CUtensorMap& ah, const CUtensorMap& al, const CUtensorMap& bh,
                    const CUtensorMap& bl, const ProductArgs& g, cudaStream_t st) {
     const int pairs = p->sm_count / 2;
-    CU(launch(product_kernel<kOp, kN, kThree>, dim3(2 * (g.total < pairs ? g.total : pairs)), dim3(kThreads), kSmem, st,
+    CU(launch(product_kernel<kOp, kN, kThree>, dim3(2 * (g.total < pairs ? g.total : pairs)), dim3(kThreads<kThree>),
+              kSmem<kThree>, st,
               ah, al, bh, bl, g));
     return SPARBIT_OK;
 }
@@ -798,18 +837,15 @@ int product(const sparbit_ortho_plan_s* p, const CUtensorMap& ah, const CUtensor
     g.total = g.n_tiles * p->count;
     g.status = (uint32_t*)p->base();
     const int n = kSquare ? p->square_n : p->wide_n;
-    if (p->parts() == 3)
-        return n == 256 ? launch_product<kOp, 256, true>(p, ah, al, bh, bl, g, st)
-                        : launch_product<kOp, 128, true>(p, ah, al, bh, bl, g, st);
+    if (p->parts() == 3) return launch_product<kOp, 128, true>(p, ah, al, bh, bl, g, st);
     return n == 256 ? launch_product<kOp, 256, false>(p, ah, al, bh, bl, g, st)
                     : launch_product<kOp, 128, false>(p, ah, al, bh, bl, g, st);
 }
 template <int kOp>
 int allow_smem() {
-    CU(cudaFuncSetAttribute(product_kernel<kOp, 256, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-    CU(cudaFuncSetAttribute(product_kernel<kOp, 128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-    CU(cudaFuncSetAttribute(product_kernel<kOp, 256, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-    CU(cudaFuncSetAttribute(product_kernel<kOp, 128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    CU(cudaFuncSetAttribute(product_kernel<kOp, 128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<true>));
+    CU(cudaFuncSetAttribute(product_kernel<kOp, 256, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<false>));
+    CU(cudaFuncSetAttribute(product_kernel<kOp, 128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<false>));
     return SPARBIT_OK;
 }
 
@@ -826,17 +862,20 @@ void list_tiles(int rows, int cols, int n, bool square, std::vector<uint32_t>& o
             for (int i = 0; i < tm; i++) out.push_back((uint32_t)(i << 16 | j));
     }
 }
-// The wider tile needs less per product, the narrower one fills the GPU where there are few: rounds of
-// 74 pairs (a B200's) times the width, the narrow tile's taken 1.3 times for one product, whose
-// operands an SM then takes in slower than it multiplies.
+// Width of the tiles, and their list.  A product reads 6 KiB of shared memory for 256 x 128 x 16 and 8 for
+// twice that, so the wider tile multiplies 1.3 times as fast; the narrower one fills the GPU where there
+// are few: the rule compares rounds of 74 pairs (a B200's) times the width.  (bf16, narrow against wide:
+// 4096 x 8192 2.62 ms against 1.94; 4 x 256 x 256 101 us against 156.)  Three products always take the
+// narrow one: their sums then fit the registers beside the addends, and four accumulators fit tensor
+// memory (1024 x 4096 x 2 633 us against 756; 4096 x 4096 3.59 ms against 3.49).
 int pick_width(int rows, int cols, int count, bool square, bool three, std::vector<uint32_t>& out) {
-    std::vector<uint32_t> narrow;
-    list_tiles(rows, cols, 256, square, out);
-    list_tiles(rows, cols, 128, square, narrow);
-    const double rounds = (double)((out.size() * count + 73) / 74), more = (double)((narrow.size() * count + 73) / 74);
-    if (more * 128 * (three ? 1.0 : 1.3) >= rounds * 256) return 256;
-    out.swap(narrow);
-    return 128;
+    std::vector<uint32_t> wide;
+    list_tiles(rows, cols, 256, square, wide);
+    list_tiles(rows, cols, 128, square, out);
+    const double rounds = (double)((wide.size() * count + 73) / 74), more = (double)((out.size() * count + 73) / 74);
+    if (three || more * 128 * 1.3 < rounds * 256) return 128;
+    out.swap(wide);
+    return 256;
 }
 
 // prepare: update, momentum and scalars filled in; last: out, weight, muon, keep, rate filled in
