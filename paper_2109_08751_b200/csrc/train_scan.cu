@@ -171,18 +171,22 @@ __device__ __forceinline__ unsigned long long now_ns() {
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-// Waits for a word that was not there at the first look; gives up after the limit, or when anybody did.
-__device__ __noinline__ ulonglong2 wait_word(const ulonglong2* p, unsigned tag, unsigned* status,
-                                             unsigned long long limit) {
+// Waits for two neighbouring words that were not there at the first look; gives up after the limit, or when
+// anybody did.
+__device__ __noinline__ void wait_words(const ulonglong2* p, unsigned tag, unsigned* status, unsigned long long limit,
+                                        ulonglong2& a, ulonglong2& b) {
     const unsigned long long until = now_ns() + limit;
-    ulonglong2 v;
     for (;;) {
-        v = look(p);
-        if (ready_word(v, tag)) return v;
-        if (*(volatile unsigned*)status != 0) return v;
+        // a look is one trip to L2; what ends the wait early is asked for now and then only
+        for (int i = 0; i < 32; i++) {
+            a = look(p);
+            b = look(p + 1);
+            if (ready_word(a, tag) && ready_word(b, tag)) return;
+        }
+        if (*(volatile unsigned*)status != 0) return;
         if (now_ns() > until) {
             atomicExch(status, 1u);
-            return v;
+            return;
         }
     }
 }
@@ -259,9 +263,12 @@ struct Shared {
     unsigned epoch;
 };
 
-// First look at the words this thread is responsible for: thread = (piece of the group, channel pair).
+// First look at the words this thread is responsible for: 16 threads to a piece of the group (the last:
+// the group before), two channels each.
+template <int kThr>
 struct Looked {
-    ulonglong2 v[2];
+    static constexpr int kEach = (kGroup * 16 + kThr - 1) / kThr;
+    ulonglong2 v[kEach][2];
 };
 __device__ __forceinline__ const ulonglong2* word_of(const ScanArgs& g, const Piece& pc, int tile, int j) {
     const int rel = pc.at % kGroup;
@@ -269,32 +276,40 @@ __device__ __forceinline__ const ulonglong2* word_of(const ScanArgs& g, const Pi
     if (j == kGroup - 1 && pc.at >= kGroup) return g.groups + ((int64_t)(pc.group - 1) * g.tiles + tile) * kTile;
     return nullptr;
 }
-__device__ __forceinline__ Looked look_back(const ScanArgs& g, const Piece& pc, int tile) {
-    Looked l = {};
-    const ulonglong2* p = word_of(g, pc, tile, threadIdx.x / 16);
-    if (p) {
-        p += threadIdx.x % 16 * 2;
-        l.v[0] = look(p);
-        l.v[1] = look(p + 1);
+template <int kThr>
+__device__ __forceinline__ Looked<kThr> look_back(const ScanArgs& g, const Piece& pc, int tile) {
+    Looked<kThr> l = {};
+#pragma unroll
+    for (int i = 0; i < Looked<kThr>::kEach; i++) {
+        const ulonglong2* p = word_of(g, pc, tile, threadIdx.x / 16 + i * (kThr / 16));
+        if (p) {
+            p += threadIdx.x % 16 * 2;
+            l.v[i][0] = look(p);
+            l.v[i][1] = look(p + 1);
+        }
     }
     return l;
 }
 // Puts what the words say into shared memory, waiting where they are not there yet.
-__device__ __forceinline__ void settle(const ScanArgs& g, const Piece& pc, int tile, Looked l, unsigned tag,
+template <int kThr>
+__device__ __forceinline__ void settle(const ScanArgs& g, const Piece& pc, int tile, Looked<kThr> l, unsigned tag,
                                        Shared& s) {
-    const int j = threadIdx.x / 16, c = threadIdx.x % 16 * 2;
-    const ulonglong2* p = word_of(g, pc, tile, j);
-    if (p) {
+    const int c = threadIdx.x % 16 * 2;
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            if (!ready_word(l.v[i], tag)) l.v[i] = wait_word(p + c + i, tag, &g.ctl->status, g.limit);
-            s.before[j][c + i] = values(l.v[i]);
-        }
-    } else if (j == kGroup - 1) {  // the chain starts with this group
+    for (int u = 0; u < Looked<kThr>::kEach; u++) {
+        const int j = threadIdx.x / 16 + u * (kThr / 16);
+        const ulonglong2* p = word_of(g, pc, tile, j);
+        if (p) {
+            if (!ready_word(l.v[u][0], tag) || !ready_word(l.v[u][1], tag))
+                wait_words(p + c, tag, &g.ctl->status, g.limit, l.v[u][0], l.v[u][1]);
+            s.before[j][c] = values(l.v[u][0]);
+            s.before[j][c + 1] = values(l.v[u][1]);
+        } else if (j == kGroup - 1) {  // the chain starts with this group
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const int ch = tile * kTile + c + i;
-            s.before[j][c + i] = make_float2(1.0f, g.first && ch < g.D ? g.first[pc.seq * g.first_ld + ch] : 0.0f);
+            for (int i = 0; i < 2; i++) {
+                const int ch = tile * kTile + c + i;
+                s.before[j][c + i] = make_float2(1.0f, g.first && ch < g.D ? g.first[pc.seq * g.first_ld + ch] : 0.0f);
+            }
         }
     }
 }
@@ -424,7 +439,10 @@ __global__ void __launch_bounds__(kThreads<V>, 4) scan_forward_kernel(const __gr
         }
 #pragma unroll
         for (int i = 0; i < V; i++) s.run[run][e + i] = make_float2(A.v[i], H.v[i]);
-        const Looked seen = look_back(g, pc, tile);
+        // where only the summary is wanted, a piece inside a group has said all with its pair
+        const bool enters = (!kBack && (g.y || g.carry)) || pc.last || pc.at % kGroup == kGroup - 1;
+        Looked<kThr> seen = {};
+        if (enters) seen = look_back<kThr>(g, pc, tile);
         __syncthreads();
         float2 own = make_float2(1.0f, 0.0f);
         if (warp == 0) {
@@ -438,9 +456,10 @@ __global__ void __launch_bounds__(kThreads<V>, 4) scan_forward_kernel(const __gr
             }
             publish(g.pairs + ((int64_t)pc.slot * g.tiles + tile) * kTile + lane, own.x, own.y, tag);
         }
-        settle(g, pc, tile, seen, tag, s);
+        if (enters) settle<kThr>(g, pc, tile, seen, tag, s);
         post_ticket(g, s, (n + 2) & 3, drawn);
         __syncthreads();
+        if (!enters) continue;
         if (warp == 0) {
             const float h = enter_piece(g, pc, tile, own, tag, s);
             s.enter[lane] = h;
@@ -521,7 +540,7 @@ __global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __g
             s.run[run][e + i] = make_float2(A.v[i], G.v[i]);
             s.hold[run][e + i] = H.v[i];
         }
-        const Looked seen = look_back(g, pc, tile);
+        const Looked<kThr> seen = look_back<kThr>(g, pc, tile);
         __syncthreads();
         float2 own = make_float2(1.0f, 0.0f);
         if (warp == 0) {
@@ -543,7 +562,7 @@ __global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __g
                 h = next;
             }
         }
-        settle(g, pc, tile, seen, tag, s);
+        settle<kThr>(g, pc, tile, seen, tag, s);
         post_ticket(g, s, (n + 2) & 3, drawn);
         __syncthreads();
         if (warp == 0) s.enter[lane] = enter_piece(g, pc, tile, own, tag, s);
