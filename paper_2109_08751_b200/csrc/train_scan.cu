@@ -250,14 +250,16 @@ __device__ __forceinline__ void stage_tensor(T* dst, const T* src, int64_t ld, i
 }
 
 constexpr int kMostRuns = 16;
+struct SharedBack {
+    float hold[kMostRuns][kTile];    // states at the start of each run
+    float2 after[kMostRuns][kTile];  // what the runs behind make of the entering gradient
+};
 
 // What a CTA learns about the state that enters its piece.
 struct Shared {
     float2 run[kMostRuns][kTile];   // pairs of the runs, then what the runs before make of the entering state
     float2 before[kGroup][kTile];              // pairs of the group's earlier pieces; last: end of the group before
     float enter[kTile];
-    float hold[kMostRuns][kTile];   // backward: states at the start of each run
-    float2 after[kMostRuns][kTile]; // backward: what the runs behind make of the entering gradient
     Piece piece[4];
     int ticket[4], tile[4];
     unsigned epoch;
@@ -400,7 +402,7 @@ __device__ __forceinline__ unsigned begin(const ScanArgs& g, T* stages, Shared& 
 
 // ---- forward (kBack: only what the pieces do to a gradient, for a summary against time) ------------
 template <typename T, int V, bool kBack>
-__global__ void __launch_bounds__(kThreads<V>, 4) scan_forward_kernel(const __grid_constant__ ScanArgs g) {
+__global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs g) {
     constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
@@ -498,6 +500,7 @@ __global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __g
     constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
+    __shared__ SharedBack sb;
     T* stages = reinterpret_cast<T*>(raw);
     const unsigned tag = begin<T, 3, R, kThr>(g, stages, s, true);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -538,7 +541,7 @@ __global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __g
 #pragma unroll
         for (int i = 0; i < V; i++) {
             s.run[run][e + i] = make_float2(A.v[i], G.v[i]);
-            s.hold[run][e + i] = H.v[i];
+            sb.hold[run][e + i] = H.v[i];
         }
         const Looked<kThr> seen = look_back<kThr>(g, pc, tile);
         __syncthreads();
@@ -547,7 +550,7 @@ __global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __g
 #pragma unroll
             for (int u = kRuns - 1; u >= 0; u--) {
                 const float2 p = s.run[u][lane];
-                s.after[u][lane] = own;
+                sb.after[u][lane] = own;
                 own.y = p.x * own.y + p.y;
                 own.x *= p.x;
             }
@@ -557,8 +560,8 @@ __global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __g
             float h = carried;
 #pragma unroll
             for (int u = 0; u < kRuns; u++) {
-                const float next = s.run[u][lane].x * h + s.hold[u][lane];
-                s.hold[u][lane] = h;
+                const float next = s.run[u][lane].x * h + sb.hold[u][lane];
+                sb.hold[u][lane] = h;
                 h = next;
             }
         }
@@ -569,7 +572,7 @@ __global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __g
         // (h_{t-1} - x_t) a_t (1 - a_t), while the first warp works out what enters
         F<V> f[R], h;
 #pragma unroll
-        for (int i = 0; i < V; i++) h.v[i] = s.hold[run][e + i];
+        for (int i = 0; i < V; i++) h.v[i] = sb.hold[run][e + i];
 #pragma unroll
         for (int j = 0; j < R; j++) {
             const F<V> x = unpack<T, V>(in_x + stage_row<R>(j)), ak = mul(a[j], k[j]);
@@ -581,7 +584,7 @@ __global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __g
         if (ch < g.D) {
             F<V> c;
 #pragma unroll
-            for (int i = 0; i < V; i++) c.v[i] = s.after[run][e + i].x * s.enter[e + i] + s.after[run][e + i].y;
+            for (int i = 0; i < V; i++) c.v[i] = sb.after[run][e + i].x * s.enter[e + i] + sb.after[run][e + i].y;
             T* dg = (T*)g.dgate + (pc.row0 + run * R + R - 1) * g.dgate_ld + ch;
             T* dx = (T*)g.dx + (pc.row0 + run * R + R - 1) * g.dx_ld + ch;
 #pragma unroll
@@ -708,11 +711,11 @@ int by_channels(int V, Fn f) {
     if (V >= 2) return f.template operator()<T, 2>();
     return f.template operator()<T, 1>();
 }
-template <int kMost16, int kMost32, typename Fn>
+template <int kMost, typename Fn>
 int by_type(int dtype, int V, Fn f) {
-    if (dtype == SPARBIT_F32) return by_channels<float, kMost32>(V, f);
-    if (dtype == SPARBIT_BF16) return by_channels<__nv_bfloat16, kMost16>(V, f);
-    return by_channels<__half, kMost16>(V, f);
+    if (dtype == SPARBIT_F32) return by_channels<float, kMost>(V, f);
+    if (dtype == SPARBIT_BF16) return by_channels<__nv_bfloat16, kMost>(V, f);
+    return by_channels<__half, kMost>(V, f);
 }
 
 // Channels a thread takes: the most whose rows start on multiples of them, in the tensors of the
@@ -852,9 +855,8 @@ int sparbit_scan_forward(sparbit_scan_plan_t* p, const void* gate, size_t gate_l
     g.summary = summary;
     g.carry = carry;
     const int V = lane_channels(p->dtype, D, y ? (uintptr_t)y | y_ld * es : 0, 0);
-    // eight bytes of a row a thread: 8 x 4096 x 2048 bf16 95 us against 106 with four; 32-bit elements
-    // 148 us with eight against 157 with sixteen
-    return by_type<4, 2>(p->dtype, V, [&]<typename T, int kV>() {
+    // four channels a thread: 8 x 4096 x 2048 bf16 94 us, with two 106; 8 x 8192 x 1024 f32 162 us, with two 171
+    return by_type<4>(p->dtype, V, [&]<typename T, int kV>() {
         return run(p, scan_forward_kernel<T, kV, false>, kThreads<kV>, 2, g, (cudaStream_t)stream);
     });
 }
@@ -892,7 +894,7 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     uintptr_t in_bits = (uintptr_t)gate | (uintptr_t)dy | gate_ld * es | dy_ld * es;
     if (!dx) {
         g.wide = common_alignment(in_bits, 16) == 16;
-        return by_type<4, 2>(p->dtype, lane_channels(p->dtype, 4, 0, 0), [&]<typename T, int kV>() {
+        return by_type<4>(p->dtype, lane_channels(p->dtype, 4, 0, 0), [&]<typename T, int kV>() {
             return run(p, scan_forward_kernel<T, kV, true>, kThreads<kV>, 2, g, (cudaStream_t)stream);
         });
     }
@@ -907,7 +909,7 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     g.dx_ld = (int64_t)dx_ld;
     const uintptr_t out_bits = (uintptr_t)dgate | (uintptr_t)dx | dgate_ld * es | dx_ld * es;
     // two channels a thread: with four, registers leave half as many warps (174 us against 167)
-    return by_type<2, 2>(p->dtype, lane_channels(p->dtype, D, out_bits, 0), [&]<typename T, int kV>() {
+    return by_type<2>(p->dtype, lane_channels(p->dtype, D, out_bits, 0), [&]<typename T, int kV>() {
         return run(p, scan_backward_kernel<T, kV>, kThreads<kV>, 3, g, (cudaStream_t)stream);
     });
 }
@@ -950,7 +952,7 @@ int sparbit_scan_step(size_t rows, size_t channels, int dtype, const void* gate,
         return SPARBIT_ERR_ALIAS;
     const uintptr_t bits = (uintptr_t)gate | (uintptr_t)x | (uintptr_t)y | gate_ld * es | x_ld * es | y_ld * es;
     const int V = lane_channels(dtype, channels, bits, (uintptr_t)state_in | (uintptr_t)state_out | state_ld * 4);
-    return by_type<4, 4>(dtype, V, [&]<typename T, int kV>() {
+    return by_type<4>(dtype, V, [&]<typename T, int kV>() {
         CU(launch(scan_step_kernel<T, kV>, dim3((unsigned)rows, (unsigned)((channels + 128 * kV - 1) / (128 * kV))),
                   dim3(128), 0, (cudaStream_t)stream, (const T*)gate, (int64_t)gate_ld, (const T*)x, (int64_t)x_ld,
                   slots, (int64_t)n_slots, (int)channels, state_in, state_out, (int64_t)state_ld, (T*)y,
