@@ -320,7 +320,6 @@ def test_divided_by_time_over_ranks(P):
     T = sum(lengths)
     c = case([T], D, "f32", seed=P)
     d = {k: v.cuda() for k, v in c.items()}
-    zero = torch.zeros(D, dtype=torch.float64)
     want = reference(c["gate"].double(), c["x"].double(), c["h0"][0].double(), c["dy"].double(), c["dlast"][0].double())
     plan = with_workspace(sp.ScanPlan(lengths, D, sp.F32))
     gather = sp.Plan(P, 2 * D * 4)
@@ -344,7 +343,6 @@ def test_divided_by_time_over_ranks(P):
     for r in range(P):
         sp.scan_join(P, D, gathered[r], alone, h0=d["dlast"], reverse=True, first_rank=r, n_ranks=1)
         assert torch.equal(alone[0], last[r])
-    assert zero.sum() == 0
 
 
 def test_a_wait_that_runs_out_is_reported():
