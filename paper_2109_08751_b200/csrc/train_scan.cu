@@ -370,8 +370,8 @@ __device__ __forceinline__ void finish(const ScanArgs& g) {
 
 // Stages a piece has in shared memory: with two the next piece's copies run while one is worked on;
 // pieces of 32-bit elements are large enough that more CTAs per SM do better.
-template <typename T>
-constexpr int kStagesOf = sizeof(T) == 4 ? 1 : 2;
+template <typename T, int kTensors, int V>
+constexpr int kStagesOf = sizeof(T) == 4 || (kTensors == 3 && V == 4) ? 1 : 2;
 
 // Starts the copies of a piece: gate and x, gate and dy, or all three.
 template <typename T, int kTensors, int R, int kThr>
@@ -387,7 +387,7 @@ __device__ __forceinline__ void stage_piece(const ScanArgs& g, T* buf, const Sha
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // What both kernels begin with; returns this launch's tag.
-template <typename T, int kTensors, int R, int kThr>
+template <typename T, int kTensors, int V, int R, int kThr>
 __device__ __forceinline__ unsigned begin(const ScanArgs& g, T* stages, Shared& s, bool against_time) {
     pdl_wait();
     pdl_trigger();
@@ -396,18 +396,18 @@ __device__ __forceinline__ unsigned begin(const ScanArgs& g, T* stages, Shared& 
     if (threadIdx.x == 0) s.epoch = g.ctl->epoch;
     copies_wait();
     __syncthreads();
-    if (kStagesOf<T> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors, R, kThr>(g, stages, s, 0, against_time);
+    if (kStagesOf<T, kTensors, V> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors, R, kThr>(g, stages, s, 0, against_time);
     return s.epoch;
 }
 
 // ---- forward (kBack: only what the pieces do to a gradient, for a summary against time) ------------
 template <typename T, int V, bool kBack>
 __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs g) {
-    constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
+    constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T, 2, V>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
     T* stages = reinterpret_cast<T*>(raw);
-    const unsigned tag = begin<T, 2, R, kThr>(g, stages, s, kBack);
+    const unsigned tag = begin<T, 2, V, R, kThr>(g, stages, s, kBack);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int n = 0; s.ticket[n & 3] < g.total; n++) {
         if (S == 1) stage_piece<T, 2, R, kThr>(g, stages, s, n & 3, kBack);
@@ -496,13 +496,13 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kern
 // ---- backward -------------------------------------------------------------------------------------
 // The states of the piece are computed again from the one that the forward pass left at its start.
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads<V>, 3) scan_backward_kernel(const __grid_constant__ ScanArgs g) {
-    constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T>;
+__global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_kernel(const __grid_constant__ ScanArgs g) {
+    constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T, 3, V>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
     __shared__ SharedBack sb;
     T* stages = reinterpret_cast<T*>(raw);
-    const unsigned tag = begin<T, 3, R, kThr>(g, stages, s, true);
+    const unsigned tag = begin<T, 3, V, R, kThr>(g, stages, s, true);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int n = 0; s.ticket[n & 3] < g.total; n++) {
         if (S == 1) {
@@ -688,9 +688,10 @@ ScanArgs common_args(const sparbit_scan_plan_s* p, bool against_time) {
 }
 
 // As many CTAs as fit, each taking tickets until there are none.
-int run(sparbit_scan_plan_s* p, void (*kernel)(ScanArgs), int threads, int tensors, const ScanArgs& g, cudaStream_t st) {
-    const size_t smem = (p->dtype == SPARBIT_F32 ? kStagesOf<float> : kStagesOf<__half>) * tensors * (size_t)kStageElems *
-                        elem_size(p->dtype);
+template <typename T, int kTensors, int V>
+int run(sparbit_scan_plan_s* p, void (*kernel)(ScanArgs), const ScanArgs& g, cudaStream_t st) {
+    constexpr int threads = kThreads<V>;
+    constexpr size_t smem = kStagesOf<T, kTensors, V> * kTensors * kStageElems * sizeof(T);
     auto* fit = p->fits;
     while (fit < p->fits + 3 && fit->kernel && fit->kernel != kernel) fit++;
     if (fit->kernel != kernel) {
@@ -857,7 +858,7 @@ int sparbit_scan_forward(sparbit_scan_plan_t* p, const void* gate, size_t gate_l
     const int V = lane_channels(p->dtype, D, y ? (uintptr_t)y | y_ld * es : 0, 0);
     // four channels a thread: 8 x 4096 x 2048 bf16 94 us, with two 106; 8 x 8192 x 1024 f32 162 us, with two 171
     return by_type<4>(p->dtype, V, [&]<typename T, int kV>() {
-        return run(p, scan_forward_kernel<T, kV, false>, kThreads<kV>, 2, g, (cudaStream_t)stream);
+        return run<T, 2, kV>(p, scan_forward_kernel<T, kV, false>, g, (cudaStream_t)stream);
     });
 }
 
@@ -895,7 +896,7 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     if (!dx) {
         g.wide = common_alignment(in_bits, 16) == 16;
         return by_type<4>(p->dtype, lane_channels(p->dtype, 4, 0, 0), [&]<typename T, int kV>() {
-            return run(p, scan_forward_kernel<T, kV, true>, kThreads<kV>, 2, g, (cudaStream_t)stream);
+            return run<T, 2, kV>(p, scan_forward_kernel<T, kV, true>, g, (cudaStream_t)stream);
         });
     }
     in_bits |= (uintptr_t)x | x_ld * es;
@@ -908,10 +909,15 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     g.dx = dx;
     g.dx_ld = (int64_t)dx_ld;
     const uintptr_t out_bits = (uintptr_t)dgate | (uintptr_t)dx | dgate_ld * es | dx_ld * es;
-    // two channels a thread: with four, registers leave half as many warps (174 us against 167)
-    return by_type<2>(p->dtype, lane_channels(p->dtype, D, out_bits, 0), [&]<typename T, int kV>() {
-        return run(p, scan_backward_kernel<T, kV>, kThreads<kV>, 3, g, (cudaStream_t)stream);
-    });
+    // four channels a thread of 16-bit types: 8 x 4096 x 2048 bf16 161 us, with two 172; two of 32-bit types:
+    // 8 x 8192 x 1024 f32 238 us, with four 248
+    const int V = lane_channels(p->dtype, D, out_bits, 0);
+    const auto call = [&]<typename T, int kV>() {
+        return run<T, 3, kV>(p, scan_backward_kernel<T, kV>, g, (cudaStream_t)stream);
+    };
+    if (p->dtype == SPARBIT_F32) return by_channels<float, 2>(V, call);
+    if (p->dtype == SPARBIT_BF16) return by_channels<__nv_bfloat16, 4>(V, call);
+    return by_channels<__half, 4>(V, call);
 }
 
 int sparbit_scan_plan_status(sparbit_scan_plan_t* p) {
