@@ -201,7 +201,6 @@ struct ScanArgs {
     int D;
     const void *gate, *x, *dy;
     int64_t gate_ld, x_ld, dy_ld;
-    int wide;            // rows of all inputs start on multiples of 16 bytes
     const float* first;  // state (gradient) at the start of each chain, or null
     int64_t first_ld;
     float *carry, *summary;
@@ -209,42 +208,79 @@ struct ScanArgs {
     int64_t y_ld, dgate_ld, dx_ld;
 };
 
-// Row t of a staged tensor; a pad of one row after every run keeps the runs of a warp in different
-// banks (R: steps of a run).
-template <int R>
-__device__ __forceinline__ int stage_row(int t) { return (t + t / R) * kTile; }
-constexpr int kStageElems = (kPiece + kPiece / 8) * kTile;  // of one tensor
+// A piece's rows of one tensor in shared memory.  Where all rows start on multiples of 16 bytes (kWide)
+// they lie there as they are; otherwise each is copied from the multiple of 16 bytes before it, so that
+// copies stay 16 bytes wide, and starts where it did within them.  A pad after every run of R rows keeps
+// the runs of a warp in different banks.
+template <typename T, int R, bool kWide>
+struct Stage {
+    static constexpr int kRow = kTile * (int)sizeof(T), kPitch = kRow + (kWide ? 0 : 16), kPad = kWide ? kRow : 64;
+    static constexpr int kBytes = kPiece * kPitch + kPiece / R * kPad;
+    static constexpr int kChunks = kPitch / 16;
+    __device__ __forceinline__ static int row(int t) { return t * kPitch + t / R * kPad; }
+};
+// A thread's run of rows of it.
+template <typename T, int V, int R, bool kWide>
+struct Rows {
+    int at;                // bytes into the dynamic shared memory
+    uint32_t first, step;  // of rows that are not wide: where row j starts within its 16 bytes
+    __device__ __forceinline__ Rows(int stage, int run, int e, const void* src, int64_t ld, int64_t row0, int ch0) {
+        at = stage + Stage<T, R, kWide>::row(run * R) + e * (int)sizeof(T);
+        step = (uint32_t)ld * (uint32_t)sizeof(T);
+        first = (uint32_t)(uintptr_t)src + (uint32_t)(row0 + run * R) * step + (uint32_t)ch0 * (uint32_t)sizeof(T);
+    }
+    __device__ __forceinline__ F<V> operator[](int j) const {
+        extern __shared__ __align__(16) uint8_t raw[];
+        int p = at + j * Stage<T, R, kWide>::kPitch;
+        if (!kWide) p += (int)((first + (uint32_t)j * step) & 15u);
+        return unpack<T, V>(reinterpret_cast<const T*>(raw + p));
+    }
+};
 
-// Starts the copy of a piece's rows of one tensor into shared memory.
-template <typename T, int R, int kThr>
-__device__ __forceinline__ void stage_tensor(T* dst, const T* src, int64_t ld, int64_t row0, int len, int ch0, int D,
-                                             bool wide) {
-    constexpr int kPer = 16 / sizeof(T), kChunks = kTile / kPer, kRows = kThr / kChunks;
-    if (wide) {
-        const int t0 = threadIdx.x / kChunks, e = threadIdx.x % kChunks * kPer, left = D - ch0 - e;
+// Starts the copy of a piece's rows of one tensor.  Reads nothing outside the rows.
+template <typename T, int R, int kThr, bool kWide>
+__device__ __forceinline__ void stage_tensor(char* stage, const T* src, int64_t ld, int64_t row0, int len, int ch0, int D) {
+    using S = Stage<T, R, kWide>;
+    constexpr int kPer = 16 / sizeof(T);
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(stage);
+    if constexpr (kWide) {
+        constexpr int kRows = kThr / S::kChunks;  // rows between the copies of a thread
+        static_assert(kRows % 8 == 0 && (kRows % R == 0 || R % kRows == 0), "");
+        const int t0 = threadIdx.x / S::kChunks, e = threadIdx.x % S::kChunks * kPer, left = D - ch0 - e;
         if (left <= 0) return;
         const int bytes = left < kPer ? left * (int)sizeof(T) : 16;  // the rest becomes zero
         const T* from = src + (row0 + t0) * ld + ch0 + e;
-        const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + stage_row<R>(t0) + e);
-        static_assert(kRows % 8 == 0 && (kRows % R == 0 || R % kRows == 0), "");
-#pragma unroll
+        const uint32_t dst = to + S::row(t0) + e * (int)sizeof(T);
+        // rolled up: copies issued all at once hold up the words that other CTAs wait for (65536 x 2048 bf16
+        // forward 287 us, unrolled 345)
+#pragma unroll 1
         for (int i = 0; i < kPiece / kRows; i++) {
             if (t0 + i * kRows < len)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                 to + (uint32_t)((i * kRows + i * kRows / R) * kTile * sizeof(T))),
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (uint32_t)S::row(i * kRows)),
                              "l"(from), "r"(bytes)
                              : "memory");
             from += kRows * ld;
         }
     } else {
-        // one channel a lane, as many rows a step as there are warps
-        const int e = threadIdx.x % kTile;
-        if (ch0 + e >= D) return;
-        const T* from = src + (row0 + threadIdx.x / kTile) * ld + ch0 + e;
-#pragma unroll 8
-        for (int t = threadIdx.x / kTile; t < len; t += kThr / kTile) {
-            dst[stage_row<R>(t) + e] = *from;
-            from += kThr / kTile * ld;
+        const int need = (D - ch0 < kTile ? D - ch0 : kTile) * (int)sizeof(T);
+        const char* const rows = reinterpret_cast<const char*>(src + row0 * ld + ch0);
+        const int64_t pitch = ld * (int64_t)sizeof(T);
+#pragma unroll 1
+        for (int c = threadIdx.x; c < kPiece * S::kChunks; c += kThr) {
+            const int t = c / S::kChunks, q = c - t * S::kChunks;
+            if (t >= len) break;
+            const char* const start = rows + t * pitch;
+            const int over = (int)((uintptr_t)start & 15);
+            const char* const from = start - over + q * 16;
+            const int bytes = need + over - q * 16 < 16 ? need + over - q * 16 : 16;
+            if (bytes <= 0) continue;
+            const uint32_t dst = to + S::row(t) + q * 16;
+            if (from >= reinterpret_cast<const char*>(src)) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
+            } else {  // the tensor's first bytes: nothing in front of them is touched
+                for (int i = over; i < bytes; i += (int)sizeof(T))
+                    *reinterpret_cast<T*>(stage + S::row(t) + i) = *reinterpret_cast<const T*>(from + i);
+            }
         }
     }
 }
@@ -374,21 +410,22 @@ template <typename T, int kTensors, int V>
 constexpr int kStagesOf = sizeof(T) == 4 || (kTensors == 3 && V == 4) ? 1 : 2;
 
 // Starts the copies of a piece: gate and x, gate and dy, or all three.
-template <typename T, int kTensors, int R, int kThr>
-__device__ __forceinline__ void stage_piece(const ScanArgs& g, T* buf, const Shared& s, int slot, bool against_time) {
+template <typename T, int kTensors, int R, int kThr, bool kWide>
+__device__ __forceinline__ void stage_piece(const ScanArgs& g, char* buf, const Shared& s, int slot, bool against_time) {
+    constexpr int kBytes = Stage<T, R, kWide>::kBytes;
     const int64_t row0 = s.piece[slot].row0;
     const int len = s.piece[slot].len, ch0 = s.tile[slot] * kTile;
-    stage_tensor<T, R, kThr>(buf, (const T*)g.gate, g.gate_ld, row0, len, ch0, g.D, g.wide);
+    stage_tensor<T, R, kThr, kWide>(buf, (const T*)g.gate, g.gate_ld, row0, len, ch0, g.D);
     if (kTensors == 3 || !against_time)
-        stage_tensor<T, R, kThr>(buf + kStageElems, (const T*)g.x, g.x_ld, row0, len, ch0, g.D, g.wide);
+        stage_tensor<T, R, kThr, kWide>(buf + kBytes, (const T*)g.x, g.x_ld, row0, len, ch0, g.D);
     if (against_time)
-        stage_tensor<T, R, kThr>(buf + (kTensors - 1) * kStageElems, (const T*)g.dy, g.dy_ld, row0, len, ch0, g.D, g.wide);
+        stage_tensor<T, R, kThr, kWide>(buf + (kTensors - 1) * kBytes, (const T*)g.dy, g.dy_ld, row0, len, ch0, g.D);
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // What both kernels begin with; returns this launch's tag.
-template <typename T, int kTensors, int V, int R, int kThr>
-__device__ __forceinline__ unsigned begin(const ScanArgs& g, T* stages, Shared& s, bool against_time) {
+template <typename T, int kTensors, int V, int R, int kThr, bool kWide>
+__device__ __forceinline__ unsigned begin(const ScanArgs& g, char* stages, Shared& s, bool against_time) {
     pdl_wait();
     pdl_trigger();
     post_ticket(g, s, 0, draw_ticket(g));
@@ -396,36 +433,39 @@ __device__ __forceinline__ unsigned begin(const ScanArgs& g, T* stages, Shared& 
     if (threadIdx.x == 0) s.epoch = g.ctl->epoch;
     copies_wait();
     __syncthreads();
-    if (kStagesOf<T, kTensors, V> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors, R, kThr>(g, stages, s, 0, against_time);
+    if (kStagesOf<T, kTensors, V> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors, R, kThr, kWide>(g, stages, s, 0, against_time);
     return s.epoch;
 }
 
 // ---- forward (kBack: only what the pieces do to a gradient, for a summary against time) ------------
-template <typename T, int V, bool kBack>
+template <typename T, int V, bool kBack, bool kWide>
 __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs g) {
     constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T, 2, V>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
-    T* stages = reinterpret_cast<T*>(raw);
-    const unsigned tag = begin<T, 2, V, R, kThr>(g, stages, s, kBack);
+    constexpr int kBytes = Stage<T, R, kWide>::kBytes;
+    char* const stages = reinterpret_cast<char*>(raw);
+    const unsigned tag = begin<T, 2, V, R, kThr, kWide>(g, stages, s, kBack);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int n = 0; s.ticket[n & 3] < g.total; n++) {
-        if (S == 1) stage_piece<T, 2, R, kThr>(g, stages, s, n & 3, kBack);
+        if (S == 1) stage_piece<T, 2, R, kThr, kWide>(g, stages, s, n & 3, kBack);
         copies_wait();
         __syncthreads();
         const int drawn = draw_ticket(g);
         if (S == 2 && s.ticket[(n + 1) & 3] < g.total)
-            stage_piece<T, 2, R, kThr>(g, stages + ((n + 1) & 1) * 2 * kStageElems, s, (n + 1) & 3, kBack);
+            stage_piece<T, 2, R, kThr, kWide>(g, stages + ((n + 1) & 1) * 2 * kBytes, s, (n + 1) & 3, kBack);
         const Piece& pc = s.piece[n & 3];
         const int tile = s.tile[n & 3], len = pc.len;
-        const T* in0 = stages + (S == 2 ? n & 1 : 0) * 2 * kStageElems + stage_row<R>(run * R) + e;
-        const T* in1 = in0 + kStageElems;
+        const int staged = (S == 2 ? n & 1 : 0) * 2 * kBytes;
+        const Rows<T, V, R, kWide> in0(staged, run, e, g.gate, g.gate_ld, pc.row0, tile * kTile);
+        const Rows<T, V, R, kWide> in1(staged + kBytes, run, e, kBack ? g.dy : g.x, kBack ? g.dy_ld : g.x_ld, pc.row0,
+                                       tile * kTile);
         F<V> a[R], b[R], A = all<V>(1.0f), H = all<V>(0.0f);
 #pragma unroll
         for (int j = 0; j < R; j++) {
             F<V> keep;
-            gate_pair(unpack<T, V>(in0 + stage_row<R>(j)), a[j], keep);
-            b[j] = unpack<T, V>(in1 + stage_row<R>(j));
+            gate_pair(in0[j], a[j], keep);
+            b[j] = in1[j];
             if (!kBack) b[j] = mul(b[j], keep);
         }
         if (len < kPiece) {  // steps past the end change nothing
@@ -495,36 +535,38 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kern
 
 // ---- backward -------------------------------------------------------------------------------------
 // The states of the piece are computed again from the one that the forward pass left at its start.
-template <typename T, int V>
+template <typename T, int V, bool kWide>
 __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_kernel(const __grid_constant__ ScanArgs g) {
     constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T, 3, V>;
     extern __shared__ __align__(16) uint8_t raw[];
     __shared__ Shared s;
     __shared__ SharedBack sb;
-    T* stages = reinterpret_cast<T*>(raw);
-    const unsigned tag = begin<T, 3, V, R, kThr>(g, stages, s, true);
+    constexpr int kBytes = Stage<T, R, kWide>::kBytes;
+    char* const stages = reinterpret_cast<char*>(raw);
+    const unsigned tag = begin<T, 3, V, R, kThr, kWide>(g, stages, s, true);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int n = 0; s.ticket[n & 3] < g.total; n++) {
         if (S == 1) {
             __syncthreads();  // the last piece's dy has been read
-            stage_piece<T, 3, R, kThr>(g, stages, s, n & 3, true);
+            stage_piece<T, 3, R, kThr, kWide>(g, stages, s, n & 3, true);
         }
         copies_wait();
         __syncthreads();
         const int drawn = draw_ticket(g);
         if (S == 2 && s.ticket[(n + 1) & 3] < g.total)
-            stage_piece<T, 3, R, kThr>(g, stages + ((n + 1) & 1) * 3 * kStageElems, s, (n + 1) & 3, true);
+            stage_piece<T, 3, R, kThr, kWide>(g, stages + ((n + 1) & 1) * 3 * kBytes, s, (n + 1) & 3, true);
         const Piece& pc = s.piece[n & 3];
         const int tile = s.tile[n & 3], len = pc.len;
-        const T* in_g = stages + (S == 2 ? n & 1 : 0) * 3 * kStageElems + stage_row<R>(run * R) + e;
-        const T* in_x = in_g + kStageElems;
-        const T* in_d = in_x + kStageElems;
+        const int staged = (S == 2 ? n & 1 : 0) * 3 * kBytes;
+        const Rows<T, V, R, kWide> in_g(staged, run, e, g.gate, g.gate_ld, pc.row0, tile * kTile);
+        const Rows<T, V, R, kWide> in_x(staged + kBytes, run, e, g.x, g.x_ld, pc.row0, tile * kTile);
+        const Rows<T, V, R, kWide> in_d(staged + 2 * kBytes, run, e, g.dy, g.dy_ld, pc.row0, tile * kTile);
         float carried = 0.0f;
         if (warp == 1 && pc.carry >= 0 && tile * kTile + lane < g.D)
             carried = g.carry[(int64_t)pc.carry * g.D + tile * kTile + lane];
         F<V> a[R], k[R], A = all<V>(1.0f), H = all<V>(0.0f), G = all<V>(0.0f);
 #pragma unroll
-        for (int j = 0; j < R; j++) gate_pair(unpack<T, V>(in_g + stage_row<R>(j)), a[j], k[j]);
+        for (int j = 0; j < R; j++) gate_pair(in_g[j], a[j], k[j]);
         if (len < kPiece) {
 #pragma unroll
             for (int j = 0; j < R; j++)
@@ -534,9 +576,9 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_ker
         for (int j = 0; j < R; j++) {
             if (run * R + j >= len) break;  // what is staged there may be anything
             A = mul(A, a[j]);
-            H = fma(a[j], H, mul(k[j], unpack<T, V>(in_x + stage_row<R>(j))));
+            H = fma(a[j], H, mul(k[j], in_x[j]));
             // the map of a gradient, front to back: this step's dy seen through the steps before
-            G = fma(A, unpack<T, V>(in_d + stage_row<R>(j)), G);
+            G = fma(A, in_d[j], G);
         }
 #pragma unroll
         for (int i = 0; i < V; i++) {
@@ -575,7 +617,7 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_ker
         for (int i = 0; i < V; i++) h.v[i] = sb.hold[run][e + i];
 #pragma unroll
         for (int j = 0; j < R; j++) {
-            const F<V> x = unpack<T, V>(in_x + stage_row<R>(j)), ak = mul(a[j], k[j]);
+            const F<V> x = in_x[j], ak = mul(a[j], k[j]);
             f[j] = mul(fma(x, all<V>(-1.0f), h), ak);
             h = fma(a[j], h, mul(k[j], x));
         }
@@ -590,7 +632,7 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_ker
 #pragma unroll
             for (int j = R - 1; j >= 0; j--, dg -= g.dgate_ld, dx -= g.dx_ld) {
                 if (run * R + j >= len) continue;
-                const F<V> q = add(unpack<T, V>(in_d + stage_row<R>(j)), c);
+                const F<V> q = add(in_d[j], c);
                 c = mul(a[j], q);
                 pack<T, V>(dg, mul(f[j], q));
                 pack<T, V>(dx, mul(k[j], q));
@@ -688,10 +730,10 @@ ScanArgs common_args(const sparbit_scan_plan_s* p, bool against_time) {
 }
 
 // As many CTAs as fit, each taking tickets until there are none.
-template <typename T, int kTensors, int V>
+template <typename T, int kTensors, int V, bool kWide>
 int run(sparbit_scan_plan_s* p, void (*kernel)(ScanArgs), const ScanArgs& g, cudaStream_t st) {
-    constexpr int threads = kThreads<V>;
-    constexpr size_t smem = kStagesOf<T, kTensors, V> * kTensors * kStageElems * sizeof(T);
+    constexpr int threads = kThreads<V>, R = kPiece / (threads / (kTile / V));
+    constexpr size_t smem = kStagesOf<T, kTensors, V> * kTensors * Stage<T, R, kWide>::kBytes;
     auto* fit = p->fits;
     while (fit < p->fits + 3 && fit->kernel && fit->kernel != kernel) fit++;
     if (fit->kernel != kernel) {
@@ -848,17 +890,20 @@ int sparbit_scan_forward(sparbit_scan_plan_t* p, const void* gate, size_t gate_l
     g.gate_ld = (int64_t)gate_ld;
     g.x = x;
     g.x_ld = (int64_t)x_ld;
-    g.wide = common_alignment((uintptr_t)gate | (uintptr_t)x | gate_ld * es | x_ld * es, 16) == 16;
+    const uintptr_t in_bits = (uintptr_t)gate | (uintptr_t)x | gate_ld * es | x_ld * es;
     g.first = h0;
     g.first_ld = (int64_t)h0_ld;
     g.y = y;
     g.y_ld = (int64_t)y_ld;
     g.summary = summary;
     g.carry = carry;
-    const int V = lane_channels(p->dtype, D, y ? (uintptr_t)y | y_ld * es : 0, 0);
+    const int V = lane_channels(p->dtype, D, in_bits | (y ? (uintptr_t)y | y_ld * es : 0), 0);
     // four channels a thread: 8 x 4096 x 2048 bf16 94 us, with two 106; 8 x 8192 x 1024 f32 162 us, with two 171
     return by_type<4>(p->dtype, V, [&]<typename T, int kV>() {
-        return run<T, 2, kV>(p, scan_forward_kernel<T, kV, false>, g, (cudaStream_t)stream);
+        if constexpr (kV * sizeof(T) < 16)
+            if (in_bits % 16 != 0)
+                return run<T, 2, kV, false>(p, scan_forward_kernel<T, kV, false, false>, g, (cudaStream_t)stream);
+        return run<T, 2, kV, true>(p, scan_forward_kernel<T, kV, false, true>, g, (cudaStream_t)stream);
     });
 }
 
@@ -894,13 +939,14 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     g.summary = dsummary;
     uintptr_t in_bits = (uintptr_t)gate | (uintptr_t)dy | gate_ld * es | dy_ld * es;
     if (!dx) {
-        g.wide = common_alignment(in_bits, 16) == 16;
-        return by_type<4>(p->dtype, lane_channels(p->dtype, 4, 0, 0), [&]<typename T, int kV>() {
-            return run<T, 2, kV>(p, scan_forward_kernel<T, kV, true>, g, (cudaStream_t)stream);
+        return by_type<4>(p->dtype, lane_channels(p->dtype, D, in_bits, 0), [&]<typename T, int kV>() {
+            if constexpr (kV * sizeof(T) < 16)
+                if (in_bits % 16 != 0)
+                    return run<T, 2, kV, false>(p, scan_forward_kernel<T, kV, true, false>, g, (cudaStream_t)stream);
+            return run<T, 2, kV, true>(p, scan_forward_kernel<T, kV, true, true>, g, (cudaStream_t)stream);
         });
     }
     in_bits |= (uintptr_t)x | x_ld * es;
-    g.wide = common_alignment(in_bits, 16) == 16;
     g.x = x;
     g.x_ld = (int64_t)x_ld;
     g.carry = (float*)carry;
@@ -911,9 +957,10 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     const uintptr_t out_bits = (uintptr_t)dgate | (uintptr_t)dx | dgate_ld * es | dx_ld * es;
     // four channels a thread of 16-bit types: 8 x 4096 x 2048 bf16 161 us, with two 172; two of 32-bit types:
     // 8 x 8192 x 1024 f32 238 us, with four 248
-    const int V = lane_channels(p->dtype, D, out_bits, 0);
+    const int V = lane_channels(p->dtype, D, in_bits | out_bits, 0);
     const auto call = [&]<typename T, int kV>() {
-        return run<T, 3, kV>(p, scan_backward_kernel<T, kV>, g, (cudaStream_t)stream);
+        return in_bits % 16 == 0 ? run<T, 3, kV, true>(p, scan_backward_kernel<T, kV, true>, g, (cudaStream_t)stream)
+                                 : run<T, 3, kV, false>(p, scan_backward_kernel<T, kV, false>, g, (cudaStream_t)stream);
     };
     if (p->dtype == SPARBIT_F32) return by_channels<float, 2>(V, call);
     if (p->dtype == SPARBIT_BF16) return by_channels<__nv_bfloat16, 4>(V, call);
