@@ -238,7 +238,7 @@ struct Rows {
 };
 
 // Starts the copy of a piece's rows of one tensor.  Reads nothing outside the rows.
-template <typename T, int R, int kThr, bool kWide>
+template <typename T, int R, int kThr, bool kWide, bool kBurst>
 __device__ __forceinline__ void stage_tensor(char* stage, const T* src, int64_t ld, int64_t row0, int len, int ch0, int D) {
     using S = Stage<T, R, kWide>;
     constexpr int kPer = 16 / sizeof(T);
@@ -251,9 +251,11 @@ __device__ __forceinline__ void stage_tensor(char* stage, const T* src, int64_t 
         const int bytes = left < kPer ? left * (int)sizeof(T) : 16;  // the rest becomes zero
         const T* from = src + (row0 + t0) * ld + ch0 + e;
         const uint32_t dst = to + S::row(t0) + e * (int)sizeof(T);
-        // rolled up: copies issued all at once hold up the words that other CTAs wait for (65536 x 2048 bf16
-        // forward 287 us, unrolled 345)
-#pragma unroll 1
+        // Copies of the next piece, issued all at once, hold up the words that other CTAs wait for (65536 x
+        // 2048 bf16 forward 287 us rolled up, 345 unrolled); copies that are waited for at once should be
+        // (8 x 8192 x 1024 f32 forward 162 us unrolled, 175 rolled up).
+        constexpr int kUnroll = kBurst ? kPiece / kRows : 1;
+#pragma unroll kUnroll
         for (int i = 0; i < kPiece / kRows; i++) {
             if (t0 + i * kRows < len)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (uint32_t)S::row(i * kRows)),
@@ -410,16 +412,16 @@ template <typename T, int kTensors, int V>
 constexpr int kStagesOf = sizeof(T) == 4 || (kTensors == 3 && V == 4) ? 1 : 2;
 
 // Starts the copies of a piece: gate and x, gate and dy, or all three.
-template <typename T, int kTensors, int R, int kThr, bool kWide>
+template <typename T, int kTensors, int R, int kThr, bool kWide, bool kBurst>
 __device__ __forceinline__ void stage_piece(const ScanArgs& g, char* buf, const Shared& s, int slot, bool against_time) {
     constexpr int kBytes = Stage<T, R, kWide>::kBytes;
     const int64_t row0 = s.piece[slot].row0;
     const int len = s.piece[slot].len, ch0 = s.tile[slot] * kTile;
-    stage_tensor<T, R, kThr, kWide>(buf, (const T*)g.gate, g.gate_ld, row0, len, ch0, g.D);
+    stage_tensor<T, R, kThr, kWide, kBurst>(buf, (const T*)g.gate, g.gate_ld, row0, len, ch0, g.D);
     if (kTensors == 3 || !against_time)
-        stage_tensor<T, R, kThr, kWide>(buf + kBytes, (const T*)g.x, g.x_ld, row0, len, ch0, g.D);
+        stage_tensor<T, R, kThr, kWide, kBurst>(buf + kBytes, (const T*)g.x, g.x_ld, row0, len, ch0, g.D);
     if (against_time)
-        stage_tensor<T, R, kThr, kWide>(buf + (kTensors - 1) * kBytes, (const T*)g.dy, g.dy_ld, row0, len, ch0, g.D);
+        stage_tensor<T, R, kThr, kWide, kBurst>(buf + (kTensors - 1) * kBytes, (const T*)g.dy, g.dy_ld, row0, len, ch0, g.D);
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
@@ -433,7 +435,7 @@ __device__ __forceinline__ unsigned begin(const ScanArgs& g, char* stages, Share
     if (threadIdx.x == 0) s.epoch = g.ctl->epoch;
     copies_wait();
     __syncthreads();
-    if (kStagesOf<T, kTensors, V> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors, R, kThr, kWide>(g, stages, s, 0, against_time);
+    if (kStagesOf<T, kTensors, V> == 2 && s.ticket[0] < g.total) stage_piece<T, kTensors, R, kThr, kWide, false>(g, stages, s, 0, against_time);
     return s.epoch;
 }
 
@@ -448,12 +450,12 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kern
     const unsigned tag = begin<T, 2, V, R, kThr, kWide>(g, stages, s, kBack);
     const int run = threadIdx.x / kLanes, e = threadIdx.x % kLanes * V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int n = 0; s.ticket[n & 3] < g.total; n++) {
-        if (S == 1) stage_piece<T, 2, R, kThr, kWide>(g, stages, s, n & 3, kBack);
+        if (S == 1) stage_piece<T, 2, R, kThr, kWide, true>(g, stages, s, n & 3, kBack);
         copies_wait();
         __syncthreads();
         const int drawn = draw_ticket(g);
         if (S == 2 && s.ticket[(n + 1) & 3] < g.total)
-            stage_piece<T, 2, R, kThr, kWide>(g, stages + ((n + 1) & 1) * 2 * kBytes, s, (n + 1) & 3, kBack);
+            stage_piece<T, 2, R, kThr, kWide, false>(g, stages + ((n + 1) & 1) * 2 * kBytes, s, (n + 1) & 3, kBack);
         const Piece& pc = s.piece[n & 3];
         const int tile = s.tile[n & 3], len = pc.len;
         const int staged = (S == 2 ? n & 1 : 0) * 2 * kBytes;
@@ -548,13 +550,13 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_ker
     for (int n = 0; s.ticket[n & 3] < g.total; n++) {
         if (S == 1) {
             __syncthreads();  // the last piece's dy has been read
-            stage_piece<T, 3, R, kThr, kWide>(g, stages, s, n & 3, true);
+            stage_piece<T, 3, R, kThr, kWide, true>(g, stages, s, n & 3, true);
         }
         copies_wait();
         __syncthreads();
         const int drawn = draw_ticket(g);
         if (S == 2 && s.ticket[(n + 1) & 3] < g.total)
-            stage_piece<T, 3, R, kThr, kWide>(g, stages + ((n + 1) & 1) * 3 * kBytes, s, (n + 1) & 3, true);
+            stage_piece<T, 3, R, kThr, kWide, false>(g, stages + ((n + 1) & 1) * 3 * kBytes, s, (n + 1) & 3, true);
         const Piece& pc = s.piece[n & 3];
         const int tile = s.tile[n & 3], len = pc.len;
         const int staged = (S == 2 ? n & 1 : 0) * 3 * kBytes;
