@@ -24,8 +24,8 @@ namespace {
 constexpr int kPiece = 128;    // steps of a piece
 constexpr int kTile = 32;      // channels of a tile
 constexpr int kGroup = 8;      // pieces of a group
-// A thread's share of a piece: V channels of a run of steps.  16 runs of 8 steps with two or four
-// channels a thread, 8 runs of 16 with one.
+// A thread's share of a piece: V channels of a run of steps, A of them an access.  16 runs of 8 steps with
+// two or four channels a thread, 8 runs of 16 with one.
 template <int V>
 constexpr int kThreads = V == 4 ? 128 : 256;
 constexpr unsigned long long kWaitNs = 2000000000ull;
@@ -130,20 +130,28 @@ __device__ __forceinline__ void gate_pair(const F<V>& g, F<V>& a, F<V>& keep) {
     keep = mul(t, a);
 }
 
-template <typename T, int V>
+// V neighbouring elements, A of them an access.
+template <typename T, int V, int A>
 __device__ __forceinline__ F<V> unpack(const T* p) {
-    const Pack<T, V> k = *reinterpret_cast<const Pack<T, V>*>(p);
     F<V> f;
 #pragma unroll
-    for (int i = 0; i < V; i++) f.v[i] = to_float(k.v[i]);
+    for (int u = 0; u < V; u += A) {
+        const Pack<T, A> k = *reinterpret_cast<const Pack<T, A>*>(p + u);
+#pragma unroll
+        for (int i = 0; i < A; i++) f.v[u + i] = to_float(k.v[i]);
+    }
     return f;
 }
-template <typename T, int V>
-__device__ __forceinline__ void pack(T* p, const F<V>& f) {
-    Pack<T, V> k;
+// The first `left` of them (a multiple of A) are there to be written.
+template <typename T, int V, int A>
+__device__ __forceinline__ void pack(T* p, const F<V>& f, int left) {
 #pragma unroll
-    for (int i = 0; i < V; i++) k.v[i] = from_float<T>(f.v[i]);
-    *reinterpret_cast<Pack<T, V>*>(p) = k;
+    for (int u = 0; u < V; u += A) {
+        Pack<T, A> k;
+#pragma unroll
+        for (int i = 0; i < A; i++) k.v[i] = from_float<T>(f.v[u + i]);
+        if (A == V || u < left) *reinterpret_cast<Pack<T, A>*>(p + u) = k;
+    }
 }
 
 // ---- published words ----------------------------------------------------------------------------
@@ -220,7 +228,7 @@ struct Stage {
     __device__ __forceinline__ static int row(int t) { return t * kPitch + t / R * kPad; }
 };
 // A thread's run of rows of it.
-template <typename T, int V, int R, bool kWide>
+template <typename T, int V, int A, int R, bool kWide>
 struct Rows {
     int at;                // bytes into the dynamic shared memory
     uint32_t first, step;  // of rows that are not wide: where row j starts within its 16 bytes
@@ -233,7 +241,7 @@ struct Rows {
         extern __shared__ __align__(16) uint8_t raw[];
         int p = at + j * Stage<T, R, kWide>::kPitch;
         if (!kWide) p += (int)((first + (uint32_t)j * step) & 15u);
-        return unpack<T, V>(reinterpret_cast<const T*>(raw + p));
+        return unpack<T, V, A>(reinterpret_cast<const T*>(raw + p));
     }
 };
 
@@ -440,7 +448,7 @@ __device__ __forceinline__ unsigned begin(const ScanArgs& g, char* stages, Share
 }
 
 // ---- forward (kBack: only what the pieces do to a gradient, for a summary against time) ------------
-template <typename T, int V, bool kBack, bool kWide>
+template <typename T, int V, int A, bool kBack, bool kWide>
 __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kernel(const __grid_constant__ ScanArgs g) {
     constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T, 2, V>;
     extern __shared__ __align__(16) uint8_t raw[];
@@ -459,10 +467,10 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kern
         const Piece& pc = s.piece[n & 3];
         const int tile = s.tile[n & 3], len = pc.len;
         const int staged = (S == 2 ? n & 1 : 0) * 2 * kBytes;
-        const Rows<T, V, R, kWide> in0(staged, run, e, g.gate, g.gate_ld, pc.row0, tile * kTile);
-        const Rows<T, V, R, kWide> in1(staged + kBytes, run, e, kBack ? g.dy : g.x, kBack ? g.dy_ld : g.x_ld, pc.row0,
+        const Rows<T, V, A, R, kWide> in0(staged, run, e, g.gate, g.gate_ld, pc.row0, tile * kTile);
+        const Rows<T, V, A, R, kWide> in1(staged + kBytes, run, e, kBack ? g.dy : g.x, kBack ? g.dy_ld : g.x_ld, pc.row0,
                                        tile * kTile);
-        F<V> a[R], b[R], A = all<V>(1.0f), H = all<V>(0.0f);
+        F<V> a[R], b[R], P = all<V>(1.0f), H = all<V>(0.0f);
 #pragma unroll
         for (int j = 0; j < R; j++) {
             F<V> keep;
@@ -477,12 +485,12 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kern
         }
 #pragma unroll
         for (int j = 0; j < R; j++) {
-            A = mul(A, a[j]);
+            P = mul(P, a[j]);
             // against time the map is built front to back: this step's dy seen through the steps before
-            H = kBack ? fma(A, b[j], H) : fma(a[j], H, b[j]);
+            H = kBack ? fma(P, b[j], H) : fma(a[j], H, b[j]);
         }
 #pragma unroll
-        for (int i = 0; i < V; i++) s.run[run][e + i] = make_float2(A.v[i], H.v[i]);
+        for (int i = 0; i < V; i++) s.run[run][e + i] = make_float2(P.v[i], H.v[i]);
         // where only the summary is wanted, a piece inside a group has said all with its pair
         const bool enters = (!kBack && (g.y || g.carry)) || pc.last || pc.at % kGroup == kGroup - 1;
         Looked<kThr> seen = {};
@@ -521,13 +529,13 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kern
 #pragma unroll
                 for (int j = 0; j < R; j++, y += g.y_ld) {
                     h = fma(a[j], h, b[j]);
-                    pack<T, V>(y, h);
+                    pack<T, V, A>(y, h, g.D - ch);
                 }
             } else {
 #pragma unroll
                 for (int j = 0; j < R; j++, y += g.y_ld) {
                     h = fma(a[j], h, b[j]);
-                    if (run * R + j < len) pack<T, V>(y, h);
+                    if (run * R + j < len) pack<T, V, A>(y, h, g.D - ch);
                 }
             }
         }
@@ -537,7 +545,7 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 5 : 4) scan_forward_kern
 
 // ---- backward -------------------------------------------------------------------------------------
 // The states of the piece are computed again from the one that the forward pass left at its start.
-template <typename T, int V, bool kWide>
+template <typename T, int V, int A, bool kWide>
 __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_kernel(const __grid_constant__ ScanArgs g) {
     constexpr int kThr = kThreads<V>, kLanes = kTile / V, kRuns = kThr / kLanes, R = kPiece / kRuns, S = kStagesOf<T, 3, V>;
     extern __shared__ __align__(16) uint8_t raw[];
@@ -560,13 +568,13 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_ker
         const Piece& pc = s.piece[n & 3];
         const int tile = s.tile[n & 3], len = pc.len;
         const int staged = (S == 2 ? n & 1 : 0) * 3 * kBytes;
-        const Rows<T, V, R, kWide> in_g(staged, run, e, g.gate, g.gate_ld, pc.row0, tile * kTile);
-        const Rows<T, V, R, kWide> in_x(staged + kBytes, run, e, g.x, g.x_ld, pc.row0, tile * kTile);
-        const Rows<T, V, R, kWide> in_d(staged + 2 * kBytes, run, e, g.dy, g.dy_ld, pc.row0, tile * kTile);
+        const Rows<T, V, A, R, kWide> in_g(staged, run, e, g.gate, g.gate_ld, pc.row0, tile * kTile);
+        const Rows<T, V, A, R, kWide> in_x(staged + kBytes, run, e, g.x, g.x_ld, pc.row0, tile * kTile);
+        const Rows<T, V, A, R, kWide> in_d(staged + 2 * kBytes, run, e, g.dy, g.dy_ld, pc.row0, tile * kTile);
         float carried = 0.0f;
         if (warp == 1 && pc.carry >= 0 && tile * kTile + lane < g.D)
             carried = g.carry[(int64_t)pc.carry * g.D + tile * kTile + lane];
-        F<V> a[R], k[R], A = all<V>(1.0f), H = all<V>(0.0f), G = all<V>(0.0f);
+        F<V> a[R], k[R], P = all<V>(1.0f), H = all<V>(0.0f), G = all<V>(0.0f);
 #pragma unroll
         for (int j = 0; j < R; j++) gate_pair(in_g[j], a[j], k[j]);
         if (len < kPiece) {
@@ -577,14 +585,14 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_ker
 #pragma unroll
         for (int j = 0; j < R; j++) {
             if (run * R + j >= len) break;  // what is staged there may be anything
-            A = mul(A, a[j]);
+            P = mul(P, a[j]);
             H = fma(a[j], H, mul(k[j], in_x[j]));
             // the map of a gradient, front to back: this step's dy seen through the steps before
-            G = fma(A, in_d[j], G);
+            G = fma(P, in_d[j], G);
         }
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            s.run[run][e + i] = make_float2(A.v[i], G.v[i]);
+            s.run[run][e + i] = make_float2(P.v[i], G.v[i]);
             sb.hold[run][e + i] = H.v[i];
         }
         const Looked<kThr> seen = look_back<kThr>(g, pc, tile);
@@ -636,8 +644,8 @@ __global__ void __launch_bounds__(kThreads<V>, V == 4 ? 4 : 3) scan_backward_ker
                 if (run * R + j >= len) continue;
                 const F<V> q = add(in_d[j], c);
                 c = mul(a[j], q);
-                pack<T, V>(dg, mul(f[j], q));
-                pack<T, V>(dx, mul(k[j], q));
+                pack<T, V, A>(dg, mul(f[j], q), g.D - ch);
+                pack<T, V, A>(dx, mul(k[j], q), g.D - ch);
             }
         }
     }
@@ -656,11 +664,11 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const T* gate, int64_t g
     const int64_t slot = slots ? slots[row] : row;
     F<V> a, keep, y_row = all<V>(0.0f);
     if (slot >= 0 && slot < n_slots) {
-        gate_pair(unpack<T, V>(gate + row * gate_ld + ch), a, keep);
-        y_row = fma(a, unpack<float, V>(state_in + slot * state_ld + ch), mul(keep, unpack<T, V>(x + row * x_ld + ch)));
-        pack<float, V>(state_out + slot * state_ld + ch, y_row);
+        gate_pair(unpack<T, V, V>(gate + row * gate_ld + ch), a, keep);
+        y_row = fma(a, unpack<float, V, V>(state_in + slot * state_ld + ch), mul(keep, unpack<T, V, V>(x + row * x_ld + ch)));
+        pack<float, V, V>(state_out + slot * state_ld + ch, y_row, V);
     }
-    pack<T, V>(y + row * y_ld + ch, y_row);
+    pack<T, V, V>(y + row * y_ld + ch, y_row, V);
 }
 
 __global__ void __launch_bounds__(128) scan_join_kernel(int P, int first_rank, int D, const float* gathered,
@@ -748,27 +756,27 @@ int run(sparbit_scan_plan_s* p, void (*kernel)(ScanArgs), const ScanArgs& g, cud
     return SPARBIT_OK;
 }
 
-// Calls f.template operator()<T, V>() for the plan's type and the number of channels a thread takes.
+// Calls f.template operator()<T, A>() for the plan's type and the channels an access takes.
 template <typename T, int kMost, typename Fn>
-int by_channels(int V, Fn f) {
+int by_access(int A, Fn f) {
     if constexpr (kMost >= 4)
-        if (V == 4) return f.template operator()<T, 4>();
-    if (V >= 2) return f.template operator()<T, 2>();
+        if (A == 4) return f.template operator()<T, 4>();
+    if (A >= 2) return f.template operator()<T, 2>();
     return f.template operator()<T, 1>();
 }
-template <int kMost, typename Fn>
-int by_type(int dtype, int V, Fn f) {
-    if (dtype == SPARBIT_F32) return by_channels<float, kMost>(V, f);
-    if (dtype == SPARBIT_BF16) return by_channels<__nv_bfloat16, kMost>(V, f);
-    return by_channels<__half, kMost>(V, f);
+template <int kMost16, int kMost32, typename Fn>
+int by_type(int dtype, int A, Fn f) {
+    if (dtype == SPARBIT_F32) return by_access<float, kMost32>(A, f);
+    if (dtype == SPARBIT_BF16) return by_access<__nv_bfloat16, kMost16>(A, f);
+    return by_access<__half, kMost16>(A, f);
 }
 
-// Channels a thread takes: the most whose rows start on multiples of them, in the tensors of the
+// Channels an access takes: the most whose rows start on multiples of them, in the tensors of the
 // plan's type (bits of their addresses and pitches) and in 32-bit ones.
-int lane_channels(int dtype, size_t D, uintptr_t bits, uintptr_t bits32) {
+int access_channels(int dtype, size_t D, uintptr_t bits, uintptr_t bits32) {
     const int es = (int)elem_size(dtype);
-    for (int V = 4; V > 1; V /= 2)
-        if (D % V == 0 && bits % (V * es) == 0 && bits32 % (V * 4) == 0) return V;
+    for (int A = 4; A > 1; A /= 2)
+        if (D % A == 0 && bits % (A * es) == 0 && bits32 % (A * 4) == 0) return A;
     return 1;
 }
 
@@ -899,13 +907,14 @@ int sparbit_scan_forward(sparbit_scan_plan_t* p, const void* gate, size_t gate_l
     g.y_ld = (int64_t)y_ld;
     g.summary = summary;
     g.carry = carry;
-    const int V = lane_channels(p->dtype, D, in_bits | (y ? (uintptr_t)y | y_ld * es : 0), 0);
-    // four channels a thread: 8 x 4096 x 2048 bf16 94 us, with two 106; 8 x 8192 x 1024 f32 162 us, with two 171
-    return by_type<4>(p->dtype, V, [&]<typename T, int kV>() {
-        if constexpr (kV * sizeof(T) < 16)
+    const int access = access_channels(p->dtype, D, in_bits | (y ? (uintptr_t)y | y_ld * es : 0), 0);
+    // as many channels a thread as an access takes: 8 x 4096 x 2048 bf16 four 92 us, two 106; rows that allow only
+    // single elements would be written in scattered pairs of bytes by four (8 x 8192 x 2047 409 us against 281)
+    return by_type<4, 4>(p->dtype, access, [&]<typename T, int A>() {
+        if constexpr (A * sizeof(T) < 16)
             if (in_bits % 16 != 0)
-                return run<T, 2, kV, false>(p, scan_forward_kernel<T, kV, false, false>, g, (cudaStream_t)stream);
-        return run<T, 2, kV, true>(p, scan_forward_kernel<T, kV, false, true>, g, (cudaStream_t)stream);
+                return run<T, 2, A, false>(p, scan_forward_kernel<T, A, A, false, false>, g, (cudaStream_t)stream);
+        return run<T, 2, A, true>(p, scan_forward_kernel<T, A, A, false, true>, g, (cudaStream_t)stream);
     });
 }
 
@@ -941,11 +950,11 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     g.summary = dsummary;
     uintptr_t in_bits = (uintptr_t)gate | (uintptr_t)dy | gate_ld * es | dy_ld * es;
     if (!dx) {
-        return by_type<4>(p->dtype, lane_channels(p->dtype, D, in_bits, 0), [&]<typename T, int kV>() {
-            if constexpr (kV * sizeof(T) < 16)
+        return by_type<4, 4>(p->dtype, access_channels(p->dtype, D, in_bits, 0), [&]<typename T, int A>() {
+            if constexpr (A * sizeof(T) < 16)
                 if (in_bits % 16 != 0)
-                    return run<T, 2, kV, false>(p, scan_forward_kernel<T, kV, true, false>, g, (cudaStream_t)stream);
-            return run<T, 2, kV, true>(p, scan_forward_kernel<T, kV, true, true>, g, (cudaStream_t)stream);
+                    return run<T, 2, A, false>(p, scan_forward_kernel<T, A, A, true, false>, g, (cudaStream_t)stream);
+            return run<T, 2, A, true>(p, scan_forward_kernel<T, A, A, true, true>, g, (cudaStream_t)stream);
         });
     }
     in_bits |= (uintptr_t)x | x_ld * es;
@@ -957,16 +966,14 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     g.dx = dx;
     g.dx_ld = (int64_t)dx_ld;
     const uintptr_t out_bits = (uintptr_t)dgate | (uintptr_t)dx | dgate_ld * es | dx_ld * es;
-    // four channels a thread of 16-bit types: 8 x 4096 x 2048 bf16 161 us, with two 172; two of 32-bit types:
-    // 8 x 8192 x 1024 f32 238 us, with four 248
-    const int V = lane_channels(p->dtype, D, in_bits | out_bits, 0);
-    const auto call = [&]<typename T, int kV>() {
-        return in_bits % 16 == 0 ? run<T, 3, kV, true>(p, scan_backward_kernel<T, kV, true>, g, (cudaStream_t)stream)
-                                 : run<T, 3, kV, false>(p, scan_backward_kernel<T, kV, false>, g, (cudaStream_t)stream);
-    };
-    if (p->dtype == SPARBIT_F32) return by_channels<float, 2>(V, call);
-    if (p->dtype == SPARBIT_BF16) return by_channels<__nv_bfloat16, 4>(V, call);
-    return by_channels<__half, 4>(V, call);
+    // four channels a thread of 16-bit types: 8 x 4096 x 2048 bf16 162 us, with two 172 (and 8 x 8192 x 2046, whose
+    // accesses take two, 444 us against 533); two of 32-bit types: 8 x 8192 x 1024 f32 238 us, with four 248; one
+    // where an access takes one
+    return by_type<4, 2>(p->dtype, access_channels(p->dtype, D, in_bits | out_bits, 0), [&]<typename T, int A>() {
+        constexpr int V = A == 1 ? 1 : sizeof(T) == 4 ? 2 : 4;
+        return in_bits % 16 == 0 ? run<T, 3, V, true>(p, scan_backward_kernel<T, V, A, true>, g, (cudaStream_t)stream)
+                                 : run<T, 3, V, false>(p, scan_backward_kernel<T, V, A, false>, g, (cudaStream_t)stream);
+    });
 }
 
 int sparbit_scan_plan_status(sparbit_scan_plan_t* p) {
@@ -1006,8 +1013,8 @@ int sparbit_scan_step(size_t rows, size_t channels, int dtype, const void* gate,
         (state_in != state_out && regions_overlap(ro, ri)))
         return SPARBIT_ERR_ALIAS;
     const uintptr_t bits = (uintptr_t)gate | (uintptr_t)x | (uintptr_t)y | gate_ld * es | x_ld * es | y_ld * es;
-    const int V = lane_channels(dtype, channels, bits, (uintptr_t)state_in | (uintptr_t)state_out | state_ld * 4);
-    return by_type<4>(dtype, V, [&]<typename T, int kV>() {
+    const int V = access_channels(dtype, channels, bits, (uintptr_t)state_in | (uintptr_t)state_out | state_ld * 4);
+    return by_type<4, 4>(dtype, V, [&]<typename T, int kV>() {
         CU(launch(scan_step_kernel<T, kV>, dim3((unsigned)rows, (unsigned)((channels + 128 * kV - 1) / (128 * kV))),
                   dim3(128), 0, (cudaStream_t)stream, (const T*)gate, (int64_t)gate_ld, (const T*)x, (int64_t)x_ld,
                   slots, (int64_t)n_slots, (int)channels, state_in, state_out, (int64_t)state_ld, (T*)y,
