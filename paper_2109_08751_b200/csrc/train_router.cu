@@ -75,7 +75,7 @@ __device__ __forceinline__ float key_value(Key<T> k) {
 
 template <typename K>
 __device__ __forceinline__ void order(K& a, K& b) {
-    const K hi = a > b ? a : b, lo = a > b ? b : a;
+    const K hi = max(a, b), lo = min(a, b);
     a = hi;
     b = lo;
 }
@@ -115,26 +115,43 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
-// A lane's logits of a row: experts (c L + l) V + i; -inf where there is no expert.  wide: rows start on multiples of 16 bytes.
-template <typename T, int L, int C>
+// A lane's logits of a row; -inf where there is no expert.  kWide, where rows start on multiples of 16
+// bytes: experts (c L + l) V + i, 16 bytes a load.  Otherwise every L-th expert from l on, so that the
+// lanes' single elements lie next to one another.
+template <typename T, int L, int C, bool kWide>
 struct Row {
     static constexpr int V = 16 / sizeof(T), N = V * C;
     Pack<T, V> run[C];
-    __device__ __forceinline__ void load(const T* p, int l, int E, bool wide, bool on) {
+    __device__ __forceinline__ static int expert(int l, int n) { return kWide ? (n / V * L + l) * V + n % V : n * L + l; }
+    __device__ __forceinline__ void load(const T* p, int l, int E, bool on) {
         const T none = from_float<T>(-INFINITY);
 #pragma unroll
         for (int c = 0; c < C; c++) {
-            const int e = (c * L + l) * V;
-            if (on && wide && e + V <= E) {
-                run[c] = *reinterpret_cast<const Pack<T, V>*>(p + e);
+            if (kWide && on && expert(l, c * V) + V <= E) {
+                run[c] = *reinterpret_cast<const Pack<T, V>*>(p + expert(l, c * V));
             } else {
 #pragma unroll
                 for (int i = 0; i < V; i++) run[c].v[i] = none;
                 if (on) {
 #pragma unroll
                     for (int i = 0; i < V; i++)
-                        if (e + i < E) run[c].v[i] = p[e + i];
+                        if (expert(l, c * V + i) < E) run[c].v[i] = p[expert(l, c * V + i)];
                 }
+            }
+        }
+    }
+    __device__ __forceinline__ static void store(T* p, int l, int E, const float (&d)[N]) {
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            if (kWide && expert(l, c * V) + V <= E) {
+                Pack<T, V> o;
+#pragma unroll
+                for (int i = 0; i < V; i++) o.v[i] = from_float<T>(d[c * V + i]);
+                *reinterpret_cast<Pack<T, V>*>(p + expert(l, c * V)) = o;
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i++)
+                    if (expert(l, c * V + i) < E) p[expert(l, c * V + i)] = from_float<T>(d[c * V + i]);
             }
         }
     }
@@ -146,7 +163,6 @@ struct Row {
         for (int n = 0; n < N; n++) run[n / V].v[n % V] = none;
     }
     __device__ __forceinline__ float value(int n) const { return to_float(run[n / V].v[n % V]); }
-    __device__ __forceinline__ static int expert(int l, int n) { return (n / V * L + l) * V + n % V; }
     // Keys of all logits; a NaN with a clear sign bit comes out above everything.
     __device__ __forceinline__ void keys(int l, Key<T> (&key)[N]) const {
 #pragma unroll
@@ -157,29 +173,28 @@ struct Row {
                     // two at a time: adding zero makes -0 a 0, then the sign decides which bits turn
                     const uint32_t u = plus_zero(run[c].v[i], run[c].v[i + 1]);
                     const uint32_t o = u ^ (((u >> 15) & 0x00010001u) * 0x7fffu | 0x80008000u);
-                    const uint32_t e = 0xffffu - (uint32_t)((c * L + l) * V + i);
-                    key[c * V + i] = o << 16 | e;
-                    key[c * V + i + 1] = (o & 0xffff0000u) | (e - 1);
+                    key[c * V + i] = o << 16 | (0xffffu - (uint32_t)expert(l, c * V + i));
+                    key[c * V + i + 1] = (o & 0xffff0000u) | (0xffffu - (uint32_t)expert(l, c * V + i + 1));
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < V; i++) {
                     const uint32_t u = __float_as_uint(run[c].v[i] + 0.0f);
                     const uint32_t o = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
-                    key[c * V + i] = (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)((c * L + l) * V + i));
+                    key[c * V + i] = (unsigned long long)o << 32 | (0xffffffffu - (uint32_t)expert(l, c * V + i));
                 }
             }
         }
     }
 };
 
-template <typename T, int L, int C>
+template <typename T, int L, int C, bool kWide>
 __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_kernel(const Slice* slices, const T* logits, int64_t ld,
-                                                                    int wide, const uint8_t* mask, int E, int k,
+                                                                    const uint8_t* mask, int E, int k,
                                                                     int renormalize, int32_t* indices, float* weights,
                                                                     float* lse_out, int32_t* part_counts,
                                                                     float* part_sums) {
-    using R = Row<T, L, C>;
+    using R = Row<T, L, C, kWide>;
     using K = Key<T>;
     constexpr int N = R::N, kGroups = 32 / L;  // tokens of a warp
     constexpr int kSpan = N * L;               // experts there is room for
@@ -197,7 +212,7 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_ke
     for (int i = 0; i < N; i++) acc[i] = 0.0f;
     R now;
     int on_byte = group < sl.rows;  // the mask's byte, looked at when the token's turn comes
-    now.load(logits + ((int64_t)sl.row0 + group) * ld, l, E, wide, on_byte);
+    now.load(logits + ((int64_t)sl.row0 + group) * ld, l, E, on_byte);
     if (mask && on_byte) on_byte = mask[(int64_t)sl.row0 + group];
     for (int t = group; t - lane / L < sl.rows; t += kWarps * kGroups) {
         const int64_t row = (int64_t)sl.row0 + t;
@@ -206,7 +221,7 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_ke
         const int t2 = t + kWarps * kGroups;
         int next_byte = t2 < sl.rows;
         R next;
-        next.load(logits + ((int64_t)sl.row0 + t2) * ld, l, E, wide, next_byte);
+        next.load(logits + ((int64_t)sl.row0 + t2) * ld, l, E, next_byte);
         if (mask && next_byte) next_byte = mask[(int64_t)sl.row0 + t2];
         const bool on = on_byte != 0;
         if (!on) now.leave_out();
@@ -247,7 +262,8 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_ke
             nan = sum != sum;
         }
         const bool part = on && (first >= kLeast<T> || nan);
-        const float inv = __fdividef(1.0f, sum);
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(sum));
         // the chosen ones: lane j gets the j-th
         K mine = 0, won = first;
         for (int j = 0; j < k; j++) {
@@ -366,17 +382,16 @@ __global__ void __launch_bounds__(256) router_balance_kernel(const int32_t* gath
     }
 }
 
-template <typename T, int L, int C>
+template <typename T, int L, int C, bool kWide>
 __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_backward_kernel(const Slice* slices, const T* logits, int64_t ld,
-                                                                     int wide, const uint8_t* mask, int E, int k,
+                                                                     const uint8_t* mask, int E, int k,
                                                                      int renormalize, const int32_t* indices,
                                                                      const float* weights, const float* lse_in,
                                                                      const int32_t* gathered, int G,
                                                                      const float* dweights, float alpha, float beta,
-                                                                     const float* dloss, T* dlogits, int64_t dld,
-                                                                     int wide_out) {
-    using R = Row<T, L, C>;
-    constexpr int N = R::N, V = R::V, kGroups = 32 / L, kSpan = N * L;
+                                                                     const float* dloss, T* dlogits, int64_t dld) {
+    using R = Row<T, L, C, kWide>;
+    constexpr int N = R::N, kGroups = 32 / L, kSpan = N * L;
     __shared__ __align__(16) float s_extra[kWarps * kGroups][kSpan];  // what the chosen weights add to a token's gradient
     __shared__ float s_f[kSpan];
     __shared__ float s_number;
@@ -408,7 +423,7 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_backward_k
     auto fetch = [&](int t, Token& x) {
         const int64_t row = (int64_t)sl.row0 + t;
         const bool inside = t < sl.rows;
-        x.row.load(logits + row * ld, l, E, wide, inside);
+        x.row.load(logits + row * ld, l, E, inside);
         x.on = inside;
         if (mask && inside) x.on = mask[row];
         x.lse = inside ? lse_in[row] : 0.0f;
@@ -440,23 +455,11 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_backward_k
         __syncwarp();
         const float common = cb * now.lse - ca * inner - (renormalize ? 0.0f : dwsum);
         if (t < sl.rows) {
-            T* const out = dlogits + ((int64_t)sl.row0 + t) * dld;
+            float d[N];
 #pragma unroll
-            for (int c = 0; c < C; c++) {
-                const int e = (c * L + l) * V;
-                Pack<T, V> o;
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    o.v[i] = from_float<T>(fmaf(p[c * V + i], fmaf(ca, f[c * V + i], common), s_extra[group][e + i]));
-                }
-                if (wide_out && e + V <= E) {
-                    *reinterpret_cast<Pack<T, V>*>(out + e) = o;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < V; i++)
-                        if (e + i < E) out[e + i] = o.v[i];
-                }
-            }
+            for (int i = 0; i < N; i++)
+                d[i] = fmaf(p[i], fmaf(ca, f[i], common), s_extra[group][R::expert(l, i)]);
+            R::store(dlogits + ((int64_t)sl.row0 + t) * dld, l, E, d);
         }
         __syncwarp();
         if (now.at >= 0) s_extra[group][now.at] = 0.0f;
@@ -492,23 +495,24 @@ int ready(const sparbit_router_plan_s* p) {
 
 // Lanes a token and runs of 16 bytes a lane: the fewest lanes that hold the experts in one run and
 // have one for each choice, then more runs.
-template <typename T, typename F>
+template <typename T, bool kWide, typename F>
 int by_experts(int E, int k, F f) {
     constexpr int V = 16 / sizeof(T);
-    if (E <= 8 * V && k <= 8) return f.template operator()<T, 8, 1>();
-    if (E <= 16 * V && k <= 16) return f.template operator()<T, 16, 1>();
-    if (E <= 32 * V) return f.template operator()<T, 32, 1>();
-    if (E <= 64 * V) return f.template operator()<T, 32, 2>();
-    if (E <= 128 * V) return f.template operator()<T, 32, 4>();
-    if constexpr (V == 4) return f.template operator()<T, 32, 8>();
+    if (E <= 8 * V && k <= 8) return f.template operator()<T, 8, 1, kWide>();
+    if (E <= 16 * V && k <= 16) return f.template operator()<T, 16, 1, kWide>();
+    if (E <= 32 * V) return f.template operator()<T, 32, 1, kWide>();
+    if (E <= 64 * V) return f.template operator()<T, 32, 2, kWide>();
+    if (E <= 128 * V) return f.template operator()<T, 32, 4, kWide>();
+    if constexpr (V == 4) return f.template operator()<T, 32, 8, kWide>();
     return SPARBIT_ERR_LIMIT;
 }
 template <typename F>
-int by_type(int dtype, int E, int k, F f) {
+int by_type(int dtype, int E, int k, bool wide, F f) {
     switch (dtype) {
-        case SPARBIT_F32: return by_experts<float>(E, k, f);
-        case SPARBIT_BF16: return by_experts<__nv_bfloat16>(E, k, f);
-        default: return by_experts<__half>(E, k, f);
+        case SPARBIT_F32: return wide ? by_experts<float, true>(E, k, f) : by_experts<float, false>(E, k, f);
+        case SPARBIT_BF16:
+            return wide ? by_experts<__nv_bfloat16, true>(E, k, f) : by_experts<__nv_bfloat16, false>(E, k, f);
+        default: return wide ? by_experts<__half, true>(E, k, f) : by_experts<__half, false>(E, k, f);
     }
 }
 bool wide_rows(const void* p, size_t ld, size_t es) { return common_alignment((uintptr_t)p | ld * es, 16) == 16; }
@@ -597,10 +601,10 @@ int sparbit_router_forward(sparbit_router_plan_t* p, const void* logits, size_t 
     int32_t* pc = (int32_t*)(p->work + p->off_counts());
     float* ps = (float*)(p->work + p->off_sums());
     if (!p->slices.empty()) {
-        const int rc = by_type(p->dtype, p->E, p->k, [&]<typename T, int L, int C>() {
-            CU(launch(router_forward_kernel<T, L, C>, dim3((unsigned)p->slices.size()), dim3(kWarps * 32), 0, st,
-                      (const Slice*)p->work, (const T*)logits, (int64_t)ld, (int)wide_rows(logits, ld, es), mask, p->E,
-                      p->k, p->renormalize, indices, weights, lse, pc, ps));
+        const int rc = by_type(p->dtype, p->E, p->k, wide_rows(logits, ld, es), [&]<typename T, int L, int C, bool kWide>() {
+            CU(launch(router_forward_kernel<T, L, C, kWide>, dim3((unsigned)p->slices.size()), dim3(kWarps * 32), 0, st,
+                      (const Slice*)p->work, (const T*)logits, (int64_t)ld, mask, p->E, p->k,
+                      p->renormalize, indices, weights, lse, pc, ps));
             return (int)SPARBIT_OK;
         });
         if (rc != SPARBIT_OK) return rc;
@@ -639,11 +643,12 @@ int sparbit_router_backward(sparbit_router_plan_t* p, const void* logits, size_t
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
     if (p->slices.empty()) return SPARBIT_OK;
-    return by_type(p->dtype, p->E, p->k, [&]<typename T, int L, int C>() {
-        CU(launch(router_backward_kernel<T, L, C>, dim3((unsigned)p->slices.size()), dim3(kWarps * 32), 0,
+    const bool wide = wide_rows(logits, ld, es) && wide_rows(dlogits, dlogits_ld, es);
+    return by_type(p->dtype, p->E, p->k, wide, [&]<typename T, int L, int C, bool kWide>() {
+        CU(launch(router_backward_kernel<T, L, C, kWide>, dim3((unsigned)p->slices.size()), dim3(kWarps * 32), 0,
                   (cudaStream_t)stream, (const Slice*)p->work, (const T*)logits, (int64_t)ld,
-                  (int)wide_rows(logits, ld, es), mask, p->E, p->k, p->renormalize, indices, weights, lse, gathered, G,
-                  dweights, alpha, beta, dloss, (T*)dlogits, (int64_t)dlogits_ld, (int)wide_rows(dlogits, dlogits_ld, es)));
+                  mask, p->E, p->k, p->renormalize, indices, weights, lse, gathered, G, dweights, alpha, beta, dloss,
+                  (T*)dlogits, (int64_t)dlogits_ld));
         return (int)SPARBIT_OK;
     });
 }
