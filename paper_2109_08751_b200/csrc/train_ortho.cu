@@ -14,8 +14,9 @@
 // step X is U itself (16-bit inputs are exact in hi; 1 / |U| is folded into the epilogues).  With
 // rounded X in that term the result of a low-rank gradient is 1-2 % off, with the pair 0.1 %, below
 // the rounding of a bf16 result.  Three products (32-bit matrices): hi hi + hi lo + lo hi, and that
-// term from an fp32 copy of X, which hi + lo would cut to 22 bits: about 1e-6.  The shift d = -3/4 (b + c) of the last step takes most of P's diagonal out of its fp16
-// rounding; in earlier steps it would feed the rounding of hi back into small singular values.
+// term from an fp32 copy of X, which hi + lo would cut to 22 bits: about 1e-6.  The shift d = -3/4 (b + c) takes
+// most of P's diagonal out of its rounding.  With one product it is for the last step alone: in earlier
+// ones it would feed the rounding of hi back into small singular values.
 #include <cuda.h>
 #include <math.h>
 #include <string.h>
@@ -28,6 +29,8 @@
 using namespace spb;
 
 namespace {
+
+enum { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 
 // ---- tile geometry ------------------------------------------------------------------------------
 // A pair of CTAs (cta_group::2) makes a tile of 256 x kN: each holds 128 rows of A, half of B and, in
@@ -46,13 +49,16 @@ constexpr int kRing = kThree ? 196608 : 163840;        // 4 stages of 48 KiB; 5 
 template <bool kThree>
 constexpr int kSmem = kRing<kThree> + kOutWarps<kThree> * 32 * 32 * 4 + 1024;  // ring, a block for each warp, alignment
 // The tensor cores cut each partial sum towards zero: over K = 4096 a relative error of 1e-5, which
-// three products would not survive.  They hand over every 128 of K to a sum rounded in registers.
-constexpr int kFlush = 2;
+// three products of 32-bit matrices would not survive.  They hand over every few blocks of K to a sum
+// rounded in registers: every block where the result is then taken from something of its own size (Poly,
+// Apply), every second for Gram; random 256 x 4096 2.0e-6 off, with every second throughout 2.9e-6 (plain
+// 32-bit arithmetic: 1.9e-6), for which 1024 x 4096 x 2 takes 745 us and not 632.  Results of 16 bits do
+// with every eighth.
+constexpr int flush_blocks(int op, bool full) { return !full ? 8 : op == 0 ? 2 : 1; }
 constexpr int kNormParts = 512;                         // CTAs a matrix's norm is summed by
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;   // X and A, P are held times these
 constexpr unsigned long long kWaitNs = 2000000000ull;   // a wait inside the kernel gives up after this
 
-enum { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 
 // ---- PTX ----------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -169,6 +175,7 @@ struct Mat {
 
 struct ProductArgs {
     int M, N, K;            // of the product
+    int flush;              // three products: blocks of K that an accumulator takes
     int n_tiles;            // tiles of one matrix, listed in `tiles` as (row tile << 16 | column tile)
     int total;              // tiles of all matrices
     const uint32_t* tiles;
@@ -393,7 +400,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
     cluster_sync();
     fence_after();
     const uint32_t tmem = tmem_base;
-    const int blocks = (g.K + kTileK - 1) / kTileK, flush = kThree ? kFlush : blocks;
+    const int blocks = (g.K + kTileK - 1) / kTileK, flush = kThree ? g.flush : blocks;
     const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     // the list of tiles and the maps are the plan's own and do not change: read ahead of the wait
     const uint32_t first_rc = g.tiles[pair % g.n_tiles];
@@ -477,14 +484,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                         fence_after();
                         const uint64_t at = a0 + st * (kStageBytes >> 4), bt = b0 + st * (kStageBytes >> 4);
                         if (elect_one()) {
+                            // lo hi and hi lo before hi hi: the sum is small while they come in, and less is cut off
 #pragma unroll
-                            for (int seg = 0; seg < (kThree ? 3 : 1); seg++) {
-                                // hi hi, hi lo, lo hi
+                            for (int seg = kThree ? 2 : 0; seg >= 0; seg--) {
 #pragma unroll
                                 for (int k = 0; k < kTileK / 16; k++)
                                     mma_f16(tmem + slot * kN, at + (seg == 2 ? kPart : 0) + k * (32 >> 4),
                                             bt + (seg == 1 ? kPart : 0) + k * ((kSquare ? 32 : 2048) >> 4), idesc,
-                                            s > s0 || seg > 0 || k > 0);
+                                            s > s0 || seg < (kThree ? 2 : 0) || k > 0);
                             }
                             mma_commit(empty + 8 * st);
                         }
@@ -836,6 +843,7 @@ int product(const sparbit_ortho_plan_s* p, const CUtensorMap& ah, const CUtensor
     g.n_tiles = (int)list.size();
     g.total = g.n_tiles * p->count;
     g.status = (uint32_t*)p->base();
+    g.flush = flush_blocks(kOp, p->dtype == SPARBIT_F32);
     const int n = kSquare ? p->square_n : p->wide_n;
     if (p->parts() == 3) return launch_product<kOp, 128, true>(p, ah, al, bh, bl, g, st);
     return n == 256 ? launch_product<kOp, 256, false>(p, ah, al, bh, bl, g, st)

@@ -41,6 +41,10 @@ def matrices(count, rows, cols, kind="random", seed=0, scale=1e-3):
     r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
     if kind == "random":
         return r(count, rows, cols) * scale
+    if kind == "decay":
+        k = min(rows, cols)
+        left = r(count, rows, k) / torch.arange(1, k + 1, device="cuda")
+        return torch.bmm(left, r(count, k, cols)) * scale
     k = max(1, min(rows, cols) // 8)
     return torch.bmm(r(count, rows, k), r(count, k, cols)) * scale
 
@@ -93,7 +97,7 @@ def test_batches(count, rows, cols, dtype):
 
 
 @pytest.mark.parametrize("dtype,products", [("bf16", 1), ("bf16", 3), ("f16", 3), ("f32", 1), ("f32", 3)])
-@pytest.mark.parametrize("kind", ["random", "lowrank"])
+@pytest.mark.parametrize("kind", ["random", "lowrank", "decay"])
 def test_numbers_of_products(dtype, products, kind):
     check(1, 200, 500, dtype, kind=kind, products=products)
 
