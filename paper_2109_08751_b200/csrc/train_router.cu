@@ -29,6 +29,8 @@ constexpr int kMaxK = SPARBIT_ROUTER_MAX_K;
 constexpr int kSlices = 584;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// Up to so many choices are drawn by unrolled code, in which a lane's list gets shorter with every draw.
+constexpr int kUnrolled = 8;
 // A run of tokens of one rank, worked on by one CTA.
 struct Slice {
     int32_t row0, rows, rank, pad;
@@ -267,13 +269,13 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_ke
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(sum));
         // the chosen ones: lane j gets the j-th
         K mine = 0, won = first;
-        for (int j = 0; j < k; j++) {
+        auto draw = [&](int j, int left) {  // left: draws that may follow
             if (l == j) mine = won;
             if (head == won) {
                 if constexpr (N <= 8) {
 #pragma unroll
-                    for (int i = 0; i + 1 < N; i++) key[i] = key[i + 1];
-                    key[N - 1] = 0;
+                    for (int i = 0; i < N; i++)
+                        if (i < left) key[i] = i + 1 < N ? key[i + 1] : 0;
                     head = key[0];
                 } else {
                     head = 0;
@@ -282,6 +284,15 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_ke
                 }
             }
             if (j + 1 < k) won = group_max<L>(head);
+        };
+        if (N <= 8 && k <= kUnrolled) {
+#pragma unroll
+            for (int j = 0; j < kUnrolled; j++) {
+                if (j >= k) break;
+                draw(j, kUnrolled - 1 - j);
+            }
+        } else {
+            for (int j = 0; j < k; j++) draw(j, N);
         }
         const int index = part && mine >= kLeast<T> ? key_index<T>(mine) : -1;
         float wgt = 0.0f;
