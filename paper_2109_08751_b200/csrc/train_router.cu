@@ -3,8 +3,8 @@
 //
 // L lanes of a warp share a token (8, 16 or 32, whichever holds the experts with 16 bytes of logits a
 // lane, at least k), each with C runs of V = 16 bytes / element neighbouring experts.  The choice: every
-// lane sorts its keys once (a network, up to 8 of them), then k times the largest head of the group
-// wins and its lane moves up.  A key holds the logit's order and, below it, the complement of the
+// lane sorts its keys once (networks, lists of up to 8), then k times the largest head of the group
+// wins and its list moves up.  A key holds the logit's order and, below it, the complement of the
 // expert's index, so that keys differ and equal logits go to the lowest index.  Instructions bound
 // this: 500 a token forward and 240 backward at 256 bf16 experts, k = 8 (56738 tokens: 40 us and 19 us at
 // 60 % and 50 % of the issue slots, where the 29 MB of logits would take 4.5 us to read).
@@ -191,8 +191,10 @@ struct Row {
     }
 };
 
+// Two CTAs per SM with up to 16 experts a lane: 32768 x 257 bf16, k = 8, 44 us, with one 62; 32768 x 257 f32,
+// k = 12, 81 us, with one 110.  One with 32: 8192 x 1000 bf16 32 us, with two 36.
 template <typename T, int L, int C, bool kWide>
-__global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_kernel(const Slice* slices, const T* logits, int64_t ld,
+__global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : C * 16 / sizeof(T) <= 16 ? 2 : 1) router_forward_kernel(const Slice* slices, const T* logits, int64_t ld,
                                                                     const uint8_t* mask, int E, int k,
                                                                     int renormalize, int32_t* indices, float* weights,
                                                                     float* lse_out, int32_t* part_counts,
@@ -200,6 +202,7 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_ke
     using R = Row<T, L, C, kWide>;
     using K = Key<T>;
     constexpr int N = R::N, kGroups = 32 / L;  // tokens of a warp
+    constexpr int kList = N < 8 ? N : 8;       // keys of a sorted list
     constexpr int kSpan = N * L;               // experts there is room for
     __shared__ int32_t s_count[kSpan + 1];
     __shared__ float s_sum[kWarps * kGroups][kSpan + 1];
@@ -230,13 +233,16 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_ke
         if (!on) now.leave_out();
         K key[N], head, first;
         now.keys(l, key);
-        auto find_first = [&]() {
-            if constexpr (N <= 8) sort_keys(key);
-            head = key[0];
-            if constexpr (N > 8) {
+        auto largest_head = [&]() {
+            K most = key[0];
 #pragma unroll
-                for (int i = 1; i < N; i++) head = key[i] > head ? key[i] : head;
-            }
+            for (int q = kList; q < N; q += kList) most = max(most, key[q]);
+            return most;
+        };
+        auto find_first = [&]() {
+#pragma unroll
+            for (int q = 0; q < N; q += kList) sort_keys(reinterpret_cast<K(&)[kList]>(key[q]));
+            head = largest_head();
             first = group_max<L>(head);
         };
         find_first();
@@ -271,28 +277,25 @@ __global__ void __launch_bounds__(kWarps * 32, C == 1 ? 4 : 1) router_forward_ke
         K mine = 0, won = first;
         auto draw = [&](int j, int left) {  // left: draws that may follow
             if (l == j) mine = won;
-            if (head == won) {
-                if constexpr (N <= 8) {
 #pragma unroll
-                    for (int i = 0; i < N; i++)
-                        if (i < left) key[i] = i + 1 < N ? key[i + 1] : 0;
-                    head = key[0];
-                } else {
-                    head = 0;
+            for (int q = 0; q < N; q += kList) {
+                if (key[q] == won) {
 #pragma unroll
-                    for (int i = 0; i < N; i++) head = key[i] < won && key[i] > head ? key[i] : head;
+                    for (int i = 0; i < kList; i++)
+                        if (i < left) key[q + i] = i + 1 < kList ? key[q + i + 1] : 0;
                 }
             }
+            head = largest_head();
             if (j + 1 < k) won = group_max<L>(head);
         };
-        if (N <= 8 && k <= kUnrolled) {
+        if (k <= kUnrolled) {
 #pragma unroll
             for (int j = 0; j < kUnrolled; j++) {
                 if (j >= k) break;
                 draw(j, kUnrolled - 1 - j);
             }
         } else {
-            for (int j = 0; j < k; j++) draw(j, N);
+            for (int j = 0; j < k; j++) draw(j, kList);
         }
         const int index = part && mine >= kLeast<T> ? key_index<T>(mine) : -1;
         float wgt = 0.0f;
