@@ -506,6 +506,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                     __syncwarp();
                 }
             }
+            // The other CTA's warps arrive at `drained` in this one's shared memory: the last arrivals, which no later
+            // product waits for, must have landed before this CTA may end.
+            for (uint32_t i = group > kSlots ? group - kSlots : 0; i < group && ok; i++)
+                ok = bar_wait(drained + 8 * (i % kSlots), (i / kSlots) & 1, &gave_up);
         }
     } else {
         // TMEM lanes go by the warp's number mod 4; the warps of a quarter share the columns
@@ -596,8 +600,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
     }
     __syncthreads();
     if (threadIdx.x == 0 && gave_up) *g.status = 2;
-    // Nobody's barriers or tensor memory are needed any more.  Nothing is handed over here: the stores to global
-    // memory are left to the kernel's end (4 x 256 x 256 bf16 104 us, waiting for them here 110).
+    // Nobody's barriers or tensor memory are needed any more: every remote arrival has been waited for (empty by the
+    // loading warps, done by those that write out, drained by the multiplying warp), so that no order is asked of
+    // this barrier.  The stores to global memory are left to the kernel's end (4 x 256 x 256 bf16 104 us, waiting for
+    // them here 110).
     asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     if (warp == 1) {
         fence_after();
