@@ -225,6 +225,10 @@ int sparbit_ortho_plan_set_workspace(sparbit_ortho_plan_t* plan, void* dev, size
  * gave up since the last call (its results are then incomplete). */
 int sparbit_ortho_plan_status(sparbit_ortho_plan_t* plan);
 
+/* Test hook for those waits: with `withhold` set, later launches never announce a finished product to the
+ * warps that write it out, and give up after timeout_ns (0 = the default 2 s) in each of their 3 kernels a step. */
+int sparbit_ortho_plan_set_wait_test(sparbit_ortho_plan_t* plan, int withhold, uint64_t timeout_ns);
+
 /* update and out: matrix i starts i * stride elements behind the first (stride is ignored for
  * count 1). */
 int sparbit_orthogonalize(sparbit_ortho_plan_t* plan, const void* update, size_t ld, size_t stride, void* out,

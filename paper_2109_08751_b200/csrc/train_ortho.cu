@@ -64,7 +64,6 @@ constexpr int kNormParts = 512;                         // CTAs a matrix's norm 
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;   // X and A, P are held times these
 constexpr unsigned long long kWaitNs = 2000000000ull;   // a wait inside the kernel gives up after this
 
-
 // ---- PTX ----------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t n) {
@@ -89,13 +88,28 @@ __device__ __forceinline__ unsigned long long now_ns() {
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-// Bounded: false once the time is up or another role of the CTA gave up.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+// Bounded: false once the time is up or another role of the CTA gave up.  For one lane.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up,
+                                         unsigned long long limit) {
     if (bar_try(bar, parity)) return true;
-    const unsigned long long until = now_ns() + kWaitNs;
+    const unsigned long long until = now_ns() + limit;
     while (!bar_try(bar, parity)) {
         if (*gave_up) return false;
         if (now_ns() > until) {
+            *gave_up = 1;
+            return false;
+        }
+    }
+    return true;
+}
+// The same for a whole warp: all lanes get one answer.  Each by itself could see the time run out a look before or
+// after another, and what follows a wait (elect, tensor memory) takes all lanes of the warp.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up,
+                                          unsigned long long limit) {
+    if (__all_sync(kAllLanes, bar_try(bar, parity))) return true;
+    const unsigned long long until = now_ns() + limit;
+    while (!__all_sync(kAllLanes, bar_try(bar, parity))) {
+        if (__any_sync(kAllLanes, *gave_up || now_ns() > until)) {
             *gave_up = 1;
             return false;
         }
@@ -198,6 +212,8 @@ struct ProductArgs {
     int transposed, muon;
     float keep, rate;       // W' = keep W - rate X
     uint32_t* status;
+    unsigned long long limit;  // ns that a wait inside the kernel may take
+    int withhold;              // test of that: finished accumulators are not announced
 };
 
 // Four values of a row, the first n of them inside the matrix; `wide`: every row starts on a multiple
@@ -427,7 +443,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                 const int row = (int)(rc >> 16) * kTileM + rank * (kTileM / 2), col = (int)(rc & 0xffff) * kN + rank * (kN / 2);
                 for (int s = 0; s < blocks; s++, n++) {
                     const uint32_t st = n % kStages;
-                    if (n >= kStages && !bar_wait(empty + 8 * st, (n / kStages - 1) & 1, &gave_up)) {
+                    if (n >= kStages && !bar_wait(empty + 8 * st, (n / kStages - 1) & 1, &gave_up, g.limit)) {
                         ok = false;
                         break;
                     }
@@ -452,7 +468,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
             }
             // the products have read every stage, and said so to both CTAs, before either may end
             for (uint32_t i = n > kStages ? n - kStages : 0; i < n && ok; i++)
-                ok = bar_wait(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up);
+                ok = bar_wait(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up, g.limit);
             if (!ok) {  // let the copies under way land before the CTA ends
                 const unsigned long long until = now_ns() + 1000000ull;
                 while (now_ns() < until) {
@@ -474,7 +490,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
             for (int t = pair; t < g.total && ok; t += pairs) {
                 for (int s0 = 0; s0 < blocks && ok; s0 += flush, group++) {
                     const uint32_t slot = group % kSlots;
-                    if (group >= kSlots && !bar_wait(drained + 8 * slot, (group / kSlots - 1) & 1, &gave_up)) {
+                    if (group >= kSlots && !warp_wait(drained + 8 * slot, (group / kSlots - 1) & 1, &gave_up, g.limit)) {
                         ok = false;
                         break;
                     }
@@ -482,7 +498,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                     const int end = s0 + flush < blocks ? s0 + flush : blocks;
                     for (int s = s0; s < end; s++, n++) {
                         const uint32_t st = n % kStages;
-                        if (!bar_wait(full + 8 * st, (n / kStages) & 1, &gave_up)) {
+                        if (!warp_wait(full + 8 * st, (n / kStages) & 1, &gave_up, g.limit)) {
                             ok = false;
                             break;
                         }
@@ -502,14 +518,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                         }
                         __syncwarp();
                     }
-                    if (ok && elect_one()) mma_commit(done + 8 * slot);
+                    if (ok && !g.withhold && elect_one()) mma_commit(done + 8 * slot);
                     __syncwarp();
                 }
             }
             // The other CTA's warps arrive at `drained` in this one's shared memory: the last arrivals, which no later
             // product waits for, must have landed before this CTA may end.
             for (uint32_t i = group > kSlots ? group - kSlots : 0; i < group && ok; i++)
-                ok = bar_wait(drained + 8 * (i % kSlots), (i / kSlots) & 1, &gave_up);
+                ok = warp_wait(drained + 8 * (i % kSlots), (i / kSlots) & 1, &gave_up, g.limit);
         }
     } else {
         // TMEM lanes go by the warp's number mod 4; the warps of a quarter share the columns
@@ -537,7 +553,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                 // predecessor goes out
                 if (wanted(0)) load_addend<kOp, kThree>(g, z, row0, col0, d[0]);
                 const uint32_t slot = group % kSlots;
-                ok = bar_wait(done + 8 * slot, (group / kSlots) & 1, &gave_up);
+                ok = warp_wait(done + 8 * slot, (group / kSlots) & 1, &gave_up, g.limit);
                 if (!ok) break;
                 fence_after();
 #pragma unroll
@@ -568,7 +584,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                 for (int i = 0; i < kCols; i++) acc[i] = 0.0f;
                 for (int s = 0; s < blocks; s += flush, group++) {
                     const uint32_t slot = group % kSlots;
-                    ok = bar_wait(done + 8 * slot, (group / kSlots) & 1, &gave_up);
+                    ok = warp_wait(done + 8 * slot, (group / kSlots) & 1, &gave_up, g.limit);
                     if (!ok) break;
                     fence_after();
 #pragma unroll
@@ -762,6 +778,8 @@ struct sparbit_ortho_plan_s {
     int square_n = 256, wide_n = 256;    // columns of their tiles
     char* work = nullptr;
     int device = -1, sm_count = 0;
+    unsigned long long limit = kWaitNs;
+    int withhold = 0;
     // tensor maps: boxes of A operands, of B operands, of MN-major B operands
     CUtensorMap xa[2][2], xb[2][2], xn[2][2], ga[2], gb[2], pa[2];  // [buffer][hi, lo]
 
@@ -856,6 +874,8 @@ int product(const sparbit_ortho_plan_s* p, const CUtensorMap& ah, const CUtensor
     g.n_tiles = (int)list.size();
     g.total = g.n_tiles * p->count;
     g.status = (uint32_t*)p->base();
+    g.limit = p->limit;
+    g.withhold = p->withhold;
     g.flush = flush_blocks(kOp, p->dtype == SPARBIT_F32);
     const int n = kSquare ? p->square_n : p->wide_n;
     if (p->parts() == 3) return launch_product<kOp, 128, true>(p, ah, al, bh, bl, g, st);
@@ -1082,6 +1102,13 @@ int sparbit_ortho_plan_status(sparbit_ortho_plan_t* p) {
     if (word == 0) return SPARBIT_OK;
     CU(cudaMemset(p->base(), 0, 4));
     return SPARBIT_ERR_TIMEOUT;
+}
+
+int sparbit_ortho_plan_set_wait_test(sparbit_ortho_plan_t* p, int withhold, uint64_t timeout_ns) {
+    if (!p) return SPARBIT_ERR_ARG;
+    p->withhold = withhold != 0;
+    p->limit = timeout_ns ? timeout_ns : kWaitNs;
+    return SPARBIT_OK;
 }
 
 int sparbit_orthogonalize(sparbit_ortho_plan_t* p, const void* update, size_t ld, size_t stride, void* out,

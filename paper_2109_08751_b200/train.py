@@ -48,6 +48,7 @@ SYMBOLS = {
     "sparbit_ortho_plan_workspace_bytes": (_sz, [_vp]),
     "sparbit_ortho_plan_set_workspace": (_i, [_vp, _vp, _sz]),
     "sparbit_ortho_plan_status": (_i, [_vp]),
+    "sparbit_ortho_plan_set_wait_test": (_i, [_vp, _i, ctypes.c_uint64]),
     "sparbit_orthogonalize": (_i, [_vp, _vp, _sz, _sz, _vp, _sz, _sz, _vp]),
     "sparbit_muon_step": (_i, [_vp, ctypes.POINTER(MuonArgs), _vp]),
     "sparbit_router_plan_create": (_i, [_i, _ps, _i, _i, _i, _i, _pp]),
@@ -117,6 +118,11 @@ class _TrainPlan:
             _check(code, name)
         return code
 
+    def set_wait_test(self, withhold: bool, timeout_ns: int = 0) -> None:
+        """Test hook of the bounded waits inside the kernels.  Plans with waits in their kernels."""
+        name = f"sparbit_{self._kind}_plan_set_wait_test"
+        _check(getattr(lib, name)(self._h, int(bool(withhold)), timeout_ns), name)
+
     def destroy(self) -> None:
         if getattr(self, "_h", None):
             h, self._h = self._h, None
@@ -150,10 +156,6 @@ class ScanPlan(_TrainPlan):
     @property
     def carry_bytes(self) -> int:
         return lib.sparbit_scan_plan_carry_bytes(self._h)
-
-    def set_wait_test(self, withhold: bool, timeout_ns: int = 0) -> None:
-        _check(lib.sparbit_scan_plan_set_wait_test(self._h, int(bool(withhold)), timeout_ns),
-               "sparbit_scan_plan_set_wait_test")
 
     def forward(self, gate, x, y, h0=None, summary=None, carry=None, stream=None, gate_ld=None, x_ld=None, y_ld=None,
                 h0_ld=None) -> None:
