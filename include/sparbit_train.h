@@ -141,8 +141,10 @@ int sparbit_scan_join(int P, int first_rank, int n_ranks, size_t channels, const
  * `renormalize` is set.  A token whose mask byte is 0, or whose logits are all -inf, is left out:
  * indices -1, weights and lse 0, gradient 0, and whatever its logits hold (NaN included) reaches
  * nothing.  An expert whose logit is -inf or NaN is not chosen; where fewer than k are left the
- * places hold index -1 and weight 0.  (NaN in a token that takes part makes its weights, lse and
- * gradient NaN, and the sums of its rank.)
+ * places hold index -1 and weight 0.  Finite logits of any size are logits: a token all of whose
+ * experts hold the type's lowest value takes part, with p = 1 / experts (and an lse^2 that 32 bits
+ * may hold as inf only).  NaN or +inf in a token that takes part makes its weights, lse and gradient
+ * NaN, and the sums of its rank; +inf can be chosen.
  *
  * With N the number of tokens that take part over all ranks and f_e = (tokens sent to e) / (N k):
  *   loss of rank r = alpha E sum_e f_e (sum of r's p_e) / N  +  beta (sum of r's lse^2) / N
