@@ -402,7 +402,8 @@ __global__ void __launch_bounds__(256) router_balance_kernel(const int32_t* gath
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < 8; i++) v += s[i];
-        loss[blockIdx.x] = alpha * E / number * v + beta / number * sums[E];
+        // squares that 32 bits do not hold count only where they have a weight
+        loss[blockIdx.x] = alpha * E / number * v + (beta != 0.0f ? beta / number * sums[E] : 0.0f);
     }
 }
 

@@ -142,6 +142,13 @@ def test_fewer_ordinary_logits_than_choices(dtype):
     assert (got["wgt"][:, 2:] == 0).all()
 
 
+def test_no_weight_on_the_squares_is_no_weight(monkeypatch):
+    """beta = 0: squares of lse that 32 bits do not hold stay out of the loss."""
+    l = logits_of(30, 16, "f32", 7)
+    l[4] = -1e30
+    check(l, [30], 2, True, "f32", 20, beta=0.0, monkeypatch=monkeypatch)
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_an_infinite_logit_is_like_a_nan(dtype):
     """inf - inf: the token's weights, lse and gradient are NaN, it is chosen first, other tokens are as ever."""
