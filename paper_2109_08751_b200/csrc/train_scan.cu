@@ -46,7 +46,8 @@ struct alignas(16) Piece {
     int32_t pad[3];
 };
 
-// First words of the workspace.
+// First words of the workspace.  epoch is the number of the launch (its tag, never 0), status that of the last one
+// in which a wait gave up: later launches wait as ever.
 struct Control {
     unsigned ticket, done, epoch, status;
 };
@@ -184,7 +185,7 @@ __device__ __forceinline__ unsigned long long now_ns() {
     return t;
 }
 // Waits for two neighbouring words that were not there at the first look; gives up after the limit, or when
-// anybody did.
+// anybody in this launch did.
 __device__ __noinline__ void wait_words(const ulonglong2* p, unsigned tag, unsigned* status, unsigned long long limit,
                                         ulonglong2& a, ulonglong2& b) {
     const unsigned long long until = now_ns() + limit;
@@ -195,9 +196,9 @@ __device__ __noinline__ void wait_words(const ulonglong2* p, unsigned tag, unsig
             b = look(p + 1);
             if (ready_word(a, tag) && ready_word(b, tag)) return;
         }
-        if (*(volatile unsigned*)status != 0) return;
+        if (*(volatile unsigned*)status == tag) return;
         if (now_ns() > until) {
-            atomicExch(status, 1u);
+            atomicExch(status, tag);
             return;
         }
     }
@@ -414,7 +415,8 @@ __device__ __forceinline__ void finish(const ScanArgs& g) {
     if (atomicAdd(&g.ctl->done, 1u) == gridDim.x - 1) {
         g.ctl->ticket = 0;
         g.ctl->done = 0;
-        g.ctl->epoch++;
+        const unsigned next = g.ctl->epoch + 1;
+        g.ctl->epoch = next != 0 ? next : 1;
     }
 }
 
