@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ Prepa
     }
 }
 
-// X of the first step: U times a power of two that brings its norm to 2048 .. 4096, as hi + lo, and
+// X of the first step: U times a power of two (2^120 at most) that brings its norm to 2048 .. 4096, as hi + lo, and
 // the factor from that to U / (|U| + eps).  Tiles of 64 x 64, transposed through shared memory.
 __global__ void __launch_bounds__(256) convert_kernel(const __grid_constant__ PrepareArgs g) {
     __shared__ double s[8];
@@ -730,7 +730,8 @@ __global__ void __launch_bounds__(256) convert_kernel(const __grid_constant__ Pr
     e = min(12 - e, 120);
     const float scale = fine ? ldexpf(1.0f, e) : 1.0f;
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
-        g.q[z] = norm < INFINITY ? (float)(1.0 / (ldexp(norm, fine ? e : 0) + ldexp((double)g.eps, fine ? e : 0))) : NAN;
+        // zeros stay zeros, whatever eps
+        g.q[z] = fine ? (float)(1.0 / (ldexp(norm, e) + ldexp((double)g.eps, e))) : norm == 0.0 ? 0.0f : NAN;
     const int rows = g.transposed ? g.cols : g.rows, cols = g.transposed ? g.rows : g.cols;
     if (g.transposed) {
 #pragma unroll
