@@ -202,9 +202,11 @@ int sparbit_router_backward(sparbit_router_plan_t* plan, const void* logits, siz
  */
 typedef struct sparbit_ortho_plan_s sparbit_ortho_plan_t;
 
-/* Products of 16-bit operands that make up one product of the iteration.  ONE: error about 1e-3 of
- * the result's norm, below the rounding of a bf16 result.  THREE: about 1e-6, three times the work.
- * AUTO: ONE for SPARBIT_BF16 matrices, THREE for the types with more bits. */
+/* Products of 16-bit operands that make up one product of the iteration.  ONE: error 0.5e-3 (4096 x
+ * 8192) to 1.4e-3 (256 x 256) of the result's norm; rounding to a bf16 result makes 1.7e-3 beside it.
+ * THREE: 1e-6 to 3e-6 where the result has 32 bits, three times the work.  AUTO: ONE for SPARBIT_BF16
+ * matrices, THREE for the types with more bits; the weights of a Muon step do not enter, so that
+ * bf16 gradients of 32-bit weights have to ask for THREE where they want it. */
 enum { SPARBIT_PRODUCTS_AUTO = 0, SPARBIT_PRODUCTS_ONE = 1, SPARBIT_PRODUCTS_THREE = 3 };
 
 /*

@@ -57,8 +57,8 @@ constexpr int kSmem = kRing<kThree> + kOutWarps<kThree> * 32 * 32 * 4 + 1024;  /
 // three products of 32-bit matrices would not survive.  They hand over every few blocks of K to a sum
 // rounded in registers: every block where the result is then taken from something of its own size (Poly,
 // Apply), every second for Gram; random 256 x 4096 2.0e-6 off, with every second throughout 2.9e-6 (plain
-// 32-bit arithmetic: 1.9e-6), for which 1024 x 4096 x 2 takes 745 us and not 632.  Results of 16 bits do
-// with every eighth.
+// 32-bit arithmetic: 1.9e-6), for which 1024 x 4096 x 2 takes 745 us and not 632.  Results of 16 bits of 16-bit
+// matrices do with every eighth (three products of 1024 x 4096 bf16 into 32-bit weights: 4.0e-6 off that way).
 constexpr int flush_blocks(int op, bool full) { return !full ? 8 : op == 0 ? 2 : 1; }
 constexpr int kNormParts = 512;                         // CTAs a matrix's norm is summed by
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;   // X and A, P are held times these
@@ -877,7 +877,7 @@ int product(const sparbit_ortho_plan_s* p, const CUtensorMap& ah, const CUtensor
     g.status = (uint32_t*)p->base();
     g.limit = p->limit;
     g.withhold = p->withhold;
-    g.flush = flush_blocks(kOp, p->dtype == SPARBIT_F32);
+    g.flush = flush_blocks(kOp, p->dtype == SPARBIT_F32 || g.out.type == SPARBIT_F32);
     const int n = kSquare ? p->square_n : p->wide_n;
     if (p->parts() == 3) return launch_product<kOp, 128, true>(p, ah, al, bh, bl, g, st);
     return n == 256 ? launch_product<kOp, 256, false>(p, ah, al, bh, bl, g, st)

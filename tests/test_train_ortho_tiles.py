@@ -89,3 +89,19 @@ def test_muon_step_of_many_tiles(count, rows, cols, dtype, want, weights):
     each = lambda v: v.square().sum((-1, -2)).sqrt()  # noqa: E731
     lim = LIMIT[1 if dtype == "bf16" else 3] * lr * scale * each(x) + (unit / 2 + 2 * 2.0 ** -24) * each(want_w)
     assert (each(w.double() - want_w) <= lim).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(60, 20000), (200, 8000), (1024, 4096), (900, 900)])
+def test_three_products_into_32_bit_weights(rows, cols, dtype):
+    """The update that reaches 32-bit weights has the error of three products, whatever the gradient's type: sums
+    are taken out of the tensor cores every block or two, which leaves 64 to 128 terms' worth of what they cut off, 3e-7
+    of a product: 3e-6 with the operands' 2.4e-6."""
+    t = TYPES[dtype][1]
+    g = matrices(1, rows, cols, "decay", seed=1).to(t)
+    plan = planned(1, rows, cols, dtype, products=3)
+    m, w = torch.zeros(1, rows, cols, device="cuda"), torch.zeros(1, rows, cols, device="cuda")
+    plan.muon_step(g, m, m, w, w, weight_dtype=sp.F32, lr=1.0, momentum=0.0, nesterov=False)
+    assert plan.status() == sp.OK
+    d = far(-w, reference(g))
+    assert d <= 3e-6 + 2.0 ** -24, d
