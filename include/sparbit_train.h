@@ -23,7 +23,8 @@
  * caller.  All calls may be captured into a CUDA graph and replayed (scalars keep the captured
  * values).  Results do not change from run to run: no sum depends on the order in which CTAs run.
  *
- * Matrices are row-major with a row stride ("ld") in ELEMENTS, at least the row's width.  Any
+ * Matrices are row-major with a row stride ("ld") in ELEMENTS, at least the row's width and at most
+ * 2^46 divided by the number of rows (ERR_ARG).  Any
  * alignment that suits the element type gives the right answer; where pointers and strides are
  * multiples of 16 bytes the wide kernels run.  Outputs must overlap neither inputs nor each other
  * (ERR_ALIAS); row-interleaved halves of one buffer do not overlap.
@@ -121,7 +122,8 @@ int sparbit_scan_step(size_t rows, size_t channels, int dtype, const void* gate,
                       size_t state_ld, void* y, size_t y_ld, void* stream);
 
 /*
- * The first states of slices that follow one another in time, from the gathered summaries.  For
+ * The first states of slices that follow one another in time, from the gathered summaries
+ * (ERR_OVERFLOW where those pass 2^46 elements).  For
  * i in 0 .. n_ranks-1, rank r = first_rank + i:
  *   gathered   [n_ranks][P][2][channels]: what the allgather of [2][channels] blocks left in rank
  *              r's receive buffer (n_ranks = P, first_rank = 0: all virtual ranks of one GPU;

@@ -29,6 +29,13 @@ struct Region {
     size_t rows, width, ld;
 };
 
+// A row stride that rows of this width cannot have: below it, or so large (a negative number taken for a size)
+// that the matrix would pass 2^46 elements, more than any memory; offsets below that cannot overflow.
+constexpr size_t kMostElements = (size_t)1 << 46;
+inline bool bad_pitch(size_t ld, size_t width, size_t rows) {
+    return ld < width || ld > kMostElements / (rows ? rows : 1);
+}
+
 // Whether two matrices share a byte.  Rows at the same pitch may interleave (the halves of one
 // buffer); otherwise overlapping address ranges count as overlap.
 inline bool regions_overlap(const Region& a, const Region& b) {

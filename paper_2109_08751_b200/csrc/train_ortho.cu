@@ -989,7 +989,8 @@ Region region(const sparbit_ortho_plan_s* p, const void* q, size_t es, size_t ld
     return {q, 1, ((p->count - 1) * stride + (p->rows - 1) * ld + p->cols) * es, 0};
 }
 bool bad_layout(const sparbit_ortho_plan_s* p, size_t ld, size_t stride) {
-    return ld < p->cols || (p->count > 1 && stride < (p->rows - 1) * ld + p->cols);
+    if (bad_pitch(ld, p->cols, p->rows)) return true;
+    return p->count > 1 && (stride < (p->rows - 1) * ld + p->cols || stride > kMostElements / p->count);
 }
 
 }  // namespace

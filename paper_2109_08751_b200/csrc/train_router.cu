@@ -631,7 +631,7 @@ int sparbit_router_plan_set_workspace(sparbit_router_plan_t* p, void* dev, size_
 
 int sparbit_router_forward(sparbit_router_plan_t* p, const void* logits, size_t ld, const uint8_t* mask,
                            int32_t* indices, float* weights, float* lse, int32_t* counts, float* sums, void* stream) {
-    if (!p || !counts || !sums || ld < (size_t)p->E) return SPARBIT_ERR_ARG;
+    if (!p || !counts || !sums || bad_pitch(ld, p->E, p->rows)) return SPARBIT_ERR_ARG;
     if (p->rows && (!logits || !indices || !weights || !lse)) return SPARBIT_ERR_ARG;
     const size_t es = elem_size(p->dtype), block = (size_t)p->n_ranks * (p->E + 1) * 4;
     const Region ins[] = {{logits, p->rows, p->E * es, ld * es}, {mask, 1, p->rows, 0}, {p->work, 1, p->work_bytes(), 0}};
@@ -677,7 +677,8 @@ int sparbit_router_backward(sparbit_router_plan_t* p, const void* logits, size_t
                             const int32_t* indices, const float* weights, const float* lse, const int32_t* gathered,
                             int G, const float* dweights, float alpha, float beta, const float* dloss, void* dlogits,
                             size_t dlogits_ld, void* stream) {
-    if (!p || !gathered || G < 1 || ld < (size_t)p->E || dlogits_ld < (size_t)p->E) return SPARBIT_ERR_ARG;
+    if (!p || !gathered || G < 1 || bad_pitch(ld, p->E, p->rows) || bad_pitch(dlogits_ld, p->E, p->rows))
+        return SPARBIT_ERR_ARG;
     if (p->rows && (!logits || !indices || !weights || !lse || !dlogits)) return SPARBIT_ERR_ARG;
     const size_t es = elem_size(p->dtype);
     const Region out{dlogits, p->rows, p->E * es, dlogits_ld * es};

@@ -796,7 +796,7 @@ int sparbit_scan_plan_create(int n_seqs, const size_t* lengths, size_t channels,
     *out = nullptr;
     if (!lengths || n_seqs < 1 || channels < 1 || !known_dtype(dtype)) return SPARBIT_ERR_ARG;
     if (channels > (1u << 20) || n_seqs > 65535) return SPARBIT_ERR_LIMIT;
-    const size_t most = ((size_t)1 << 46) / channels, tiles = (channels + kTile - 1) / kTile;
+    const size_t most = kMostElements / channels, tiles = (channels + kTile - 1) / kTile;
     size_t rows = 0, pieces = 0;
     for (int s = 0; s < n_seqs; s++) {
         if (lengths[s] > most - rows) return SPARBIT_ERR_OVERFLOW;
@@ -887,7 +887,9 @@ int sparbit_scan_forward(sparbit_scan_plan_t* p, const void* gate, size_t gate_l
     if (!p) return SPARBIT_ERR_ARG;
     const size_t D = p->D, es = elem_size(p->dtype);
     if (p->rows && (!gate || !x)) return SPARBIT_ERR_ARG;
-    if (gate_ld < D || x_ld < D || (y && y_ld < D) || (h0 && h0_ld < D)) return SPARBIT_ERR_ARG;
+    if (bad_pitch(gate_ld, D, p->rows) || bad_pitch(x_ld, D, p->rows) || (y && bad_pitch(y_ld, D, p->rows)) ||
+        (h0 && bad_pitch(h0_ld, D, p->n_seqs)))
+        return SPARBIT_ERR_ARG;
     const Region rg{gate, p->rows, D * es, gate_ld * es}, rx{x, p->rows, D * es, x_ld * es},
         ry{y, p->rows, D * es, y_ld * es}, rh{h0, (size_t)p->n_seqs, D * 4, h0_ld * 4},
         rs{summary, 1, (size_t)p->n_seqs * 2 * D * 4, 0}, rc{carry, 1, sparbit_scan_plan_carry_bytes(p), 0},
@@ -930,8 +932,10 @@ int sparbit_scan_backward(sparbit_scan_plan_t* p, const void* gate, size_t gate_
     if (!p || !dgate != !dx) return SPARBIT_ERR_ARG;
     const size_t D = p->D, es = elem_size(p->dtype);
     if (p->rows && (!gate || !dy || (dx && (!x || !carry)))) return SPARBIT_ERR_ARG;
-    if (gate_ld < D || dy_ld < D || (dlast && dlast_ld < D)) return SPARBIT_ERR_ARG;
-    if (dx && (x_ld < D || dgate_ld < D || dx_ld < D)) return SPARBIT_ERR_ARG;
+    if (bad_pitch(gate_ld, D, p->rows) || bad_pitch(dy_ld, D, p->rows) || (dlast && bad_pitch(dlast_ld, D, p->n_seqs)))
+        return SPARBIT_ERR_ARG;
+    if (dx && (bad_pitch(x_ld, D, p->rows) || bad_pitch(dgate_ld, D, p->rows) || bad_pitch(dx_ld, D, p->rows)))
+        return SPARBIT_ERR_ARG;
     const Region rg{gate, p->rows, D * es, gate_ld * es}, rd{dy, p->rows, D * es, dy_ld * es},
         rx{dx ? x : nullptr, p->rows, D * es, x_ld * es}, rl{dlast, (size_t)p->n_seqs, D * 4, dlast_ld * 4},
         rc{dx ? carry : nullptr, 1, sparbit_scan_plan_carry_bytes(p), 0}, rw{p->work, 1, p->work_bytes(), 0},
@@ -1007,9 +1011,11 @@ int sparbit_scan_step(size_t rows, size_t channels, int dtype, const void* gate,
     if (channels < 1 || !known_dtype(dtype)) return SPARBIT_ERR_ARG;
     if (rows == 0) return SPARBIT_OK;
     if (!gate || !x || !y || (n_slots && (!state_in || !state_out))) return SPARBIT_ERR_ARG;
-    if (gate_ld < channels || x_ld < channels || y_ld < channels || state_ld < channels) return SPARBIT_ERR_ARG;
     if (!slots && n_slots < rows) return SPARBIT_ERR_ARG;
     if (channels > (1u << 20) || rows > 0x7fffffffu) return SPARBIT_ERR_LIMIT;
+    if (bad_pitch(gate_ld, channels, rows) || bad_pitch(x_ld, channels, rows) || bad_pitch(y_ld, channels, rows) ||
+        bad_pitch(state_ld, channels, n_slots))
+        return SPARBIT_ERR_ARG;
     const size_t es = elem_size(dtype);
     const Region rg{gate, rows, channels * es, gate_ld * es}, rx{x, rows, channels * es, x_ld * es},
         ry{y, rows, channels * es, y_ld * es}, rs{slots, 1, rows * 4, 0},
@@ -1032,8 +1038,10 @@ int sparbit_scan_step(size_t rows, size_t channels, int dtype, const void* gate,
 int sparbit_scan_join(int P, int first_rank, int n_ranks, size_t channels, const float* gathered, const float* h0,
                       float* out, size_t out_ld, int reverse, void* stream) {
     if (P < 1 || first_rank < 0 || n_ranks < 1 || n_ranks > P - first_rank || channels < 1) return SPARBIT_ERR_ARG;
-    if (!gathered || !out || out_ld < channels) return SPARBIT_ERR_ARG;
+    if (!gathered || !out) return SPARBIT_ERR_ARG;
     if (channels > (1u << 20) || n_ranks > 65535) return SPARBIT_ERR_LIMIT;
+    if (bad_pitch(out_ld, channels, n_ranks)) return SPARBIT_ERR_ARG;
+    if ((size_t)P * 2 * channels > kMostElements / n_ranks) return SPARBIT_ERR_OVERFLOW;
     const Region rg{gathered, 1, (size_t)n_ranks * P * 2 * channels * 4, 0}, rh{h0, 1, channels * 4, 0},
         ro{out, (size_t)n_ranks, channels * 4, out_ld * 4};
     if (regions_overlap(ro, rg) || regions_overlap(ro, rh)) return SPARBIT_ERR_ALIAS;
