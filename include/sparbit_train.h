@@ -236,7 +236,8 @@ int sparbit_ortho_plan_status(sparbit_ortho_plan_t* plan);
 int sparbit_ortho_plan_set_wait_test(sparbit_ortho_plan_t* plan, int withhold, uint64_t timeout_ns);
 
 /* update and out: matrix i starts i * stride elements behind the first (stride is ignored for
- * count 1). */
+ * count 1): one behind another, stride >= (rows - 1) * ld + cols, or side by side in the rows of one
+ * buffer, stride >= cols and (count - 1) * stride + cols <= ld; ERR_ARG otherwise. */
 int sparbit_orthogonalize(sparbit_ortho_plan_t* plan, const void* update, size_t ld, size_t stride, void* out,
                           size_t out_ld, size_t out_stride, void* stream);
 

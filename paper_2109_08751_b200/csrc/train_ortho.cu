@@ -982,15 +982,21 @@ int iterate(const sparbit_ortho_plan_s* p, PrepareArgs prep, ProductArgs last, c
     return SPARBIT_OK;
 }
 
-Region region(const sparbit_ortho_plan_s* p, const void* q, size_t es, size_t ld, size_t stride) {
-    // a batch laid out as one matrix of rows where its stride is a multiple of the pitch; the whole range otherwise
-    if (p->count == 1) return {q, p->rows, p->cols * es, ld * es};
-    if (stride % ld == 0) return {q, (stride / ld) * (p->count - 1) + p->rows, p->cols * es, ld * es};
-    return {q, 1, ((p->count - 1) * stride + (p->rows - 1) * ld + p->cols) * es, 0};
+// A batch lies one matrix behind another, or side by side in the rows of one buffer (column blocks).
+bool side_by_side(const sparbit_ortho_plan_s* p, size_t ld, size_t stride) {
+    return p->count > 1 && stride >= p->cols && stride <= ld && (p->count - 1) * stride + p->cols <= ld;
 }
 bool bad_layout(const sparbit_ortho_plan_s* p, size_t ld, size_t stride) {
     if (bad_pitch(ld, p->cols, p->rows)) return true;
-    return p->count > 1 && (stride < (p->rows - 1) * ld + p->cols || stride > kMostElements / p->count);
+    if (p->count == 1 || side_by_side(p, ld, stride)) return false;
+    return stride < (p->rows - 1) * ld + p->cols || stride > kMostElements / p->count;
+}
+Region region(const sparbit_ortho_plan_s* p, const void* q, size_t es, size_t ld, size_t stride) {
+    // one matrix of wide rows; of many rows, where the stride is a multiple of the pitch; the whole range otherwise
+    if (p->count == 1) return {q, p->rows, p->cols * es, ld * es};
+    if (side_by_side(p, ld, stride)) return {q, p->rows, ((p->count - 1) * stride + p->cols) * es, ld * es};
+    if (stride % ld == 0) return {q, (stride / ld) * (p->count - 1) + p->rows, p->cols * es, ld * es};
+    return {q, 1, ((p->count - 1) * stride + (p->rows - 1) * ld + p->cols) * es, 0};
 }
 
 }  // namespace
