@@ -1,8 +1,10 @@
 """ctypes binding of include/sparbit_train.h: argument marshalling only.
 
-Operators of a training step whose state is divided over the ranks of a communicator.  Tensors are
-any objects with `data_ptr()` (or numpy arrays, or addresses); row strides (`*_ld`, in elements)
-default to the row's width.  Everything runs in the library's CUDA kernels; there is no fallback.
+Operators of a training step whose state is divided over the ranks of a communicator.  Tensors are torch
+tensors in device (or pinned host) memory, whose type has to be the operator's (TypeError), or numpy arrays or
+addresses, which are taken as they are; row strides (`*_ld`, in elements) default to the row's width, which a
+tensor with gaps between its rows does not have (ValueError: give its stride).  Everything runs in the
+library's CUDA kernels; there is no fallback.
 """
 from __future__ import annotations
 
@@ -63,19 +65,94 @@ for _name, (_res, _args) in SYMBOLS.items():
     _fn = getattr(lib, _name)  # AttributeError here means the library does not match the header
     _fn.restype = _res
     _fn.argtypes = _args
-_scan_forward, _scan_backward, _scan_step = lib.sparbit_scan_forward, lib.sparbit_scan_backward, lib.sparbit_scan_step
 
 
-# The calls below can be shorter than their own marshalling (a token's step takes the GPU 3 us), so
-# the common cases come first.
-def _ptr(x):
-    """Address of a tensor (or of anything binding._ptr knows)."""
+def _words(name):
+    """The call for arguments that are all integers and addresses, a machine word each: ctypes converts an int to void*
+    faster than to size_t (a token's step 0.5 us), but nothing that only behaves like an int (numpy's), which goes
+    the declared way."""
+    declared = getattr(lib, name)
+    fast = ctypes.CFUNCTYPE(_i, *[_vp] * len(declared.argtypes))((name, lib))
+
+    def call(*args):
+        try:
+            return fast(*args)
+        except ctypes.ArgumentError:
+            return declared(*args)
+
+    return call
+
+
+_scan_step, _router_forward = _words("sparbit_scan_step"), _words("sparbit_router_forward")
+
+
+# What a tensor has to be: device memory of the type that the kernels read, and without gaps where no row stride is
+# given.  The calls below can be shorter than their own marshalling (a token's step takes the GPU 3 us), so the common
+# cases come first; looking costs a token's step 0.4 us and the router's forward pass 1.1.
+_I32, _BYTE = 3, 4
+_NAMES = {F32: "float32", BF16: "bfloat16", F16: "float16", _I32: "int32", _BYTE: "uint8 or bool"}
+_KNOWN = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16, "torch.int32": _I32, "torch.uint8": _BYTE,
+          "torch.int8": _BYTE, "torch.bool": _BYTE}
+_codes = {}  # of the torch types met so far
+_float32 = _int32 = None  # torch's, once met
+
+
+def _address_of(x, code):
+    """Address of a tensor of the type `code` (None: any), or of anything binding._ptr knows."""
     if x is None:
         return None
     try:
-        return x.data_ptr()
+        if (_codes[x.dtype] == code or code is None) and x.is_cuda:
+            return x.data_ptr()
+    except (AttributeError, KeyError):
+        pass
+    return _address_checked(x, code)
+
+
+def _address_checked(x, code):
+    if not hasattr(x, "data_ptr"):
+        return _address(x)  # None, a number, a numpy array: the caller's word
+    global _float32, _int32
+    dtype = str(x.dtype)
+    met = _codes[x.dtype] = _KNOWN.get(dtype, -1)
+    if met == F32:
+        _float32 = x.dtype
+    elif met == _I32:
+        _int32 = x.dtype
+    if code is not None and met != code:
+        raise TypeError(f"a tensor of {_NAMES.get(code, code)} is wanted, not of {dtype}")
+    if not (x.is_cuda or x.is_pinned()):
+        raise TypeError("a tensor on the GPU is wanted")
+    return x.data_ptr()
+
+
+def _stride_of(x, ld, width):
+    """The row stride: the one that is given, or the width for a tensor whose rows follow one another."""
+    if ld is not None:
+        return ld
+    return width if x is None or _dense(x) else None
+
+
+def _dense(x):
+    """True, or ValueError for a tensor with gaps."""
+    try:
+        if x.is_contiguous():
+            return True
     except AttributeError:
-        return _address(x)
+        return True
+    raise ValueError("a tensor with gaps between its rows needs its row stride (*_ld)")
+
+
+def _flat(x, code):
+    """Address of an array that has no row stride."""
+    if x is None:
+        return None
+    try:
+        if (_codes[x.dtype] == code or code is None) and x.is_cuda and x.is_contiguous():
+            return x.data_ptr()
+    except (AttributeError, KeyError):
+        pass
+    return _address_checked(x, code) if _dense(x) else None
 
 
 def _stream_handle(stream):
@@ -107,7 +184,7 @@ class _TrainPlan:
 
     def set_workspace(self, dev, nbytes: int) -> None:
         name = f"sparbit_{self._kind}_plan_set_workspace"
-        _check(getattr(lib, name)(self._h, _ptr(dev), nbytes), name)
+        _check(getattr(lib, name)(self._h, _flat(dev, None), nbytes), name)
         self._workspace = dev  # keep the owner alive
 
     def status(self) -> int:
@@ -151,7 +228,7 @@ class ScanPlan(_TrainPlan):
     def __init__(self, lengths, channels: int, dtype: int = BF16):
         n, arr = _counts(lengths)
         self._create(n, arr, channels, dtype)
-        self.channels = channels
+        self.channels, self.dtype = channels, dtype
 
     @property
     def carry_bytes(self) -> int:
@@ -159,17 +236,20 @@ class ScanPlan(_TrainPlan):
 
     def forward(self, gate, x, y, h0=None, summary=None, carry=None, stream=None, gate_ld=None, x_ld=None, y_ld=None,
                 h0_ld=None) -> None:
-        d = self.channels
-        _check(_scan_forward(self._h, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(h0), h0_ld or d,
-                                        _ptr(y), y_ld or d, _ptr(summary), _ptr(carry), _stream_handle(stream)),
+        d, t = self.channels, self.dtype
+        _check(lib.sparbit_scan_forward(self._h, _address_of(gate, t), _stride_of(gate, gate_ld, d), _address_of(x, t),
+                             _stride_of(x, x_ld, d), _address_of(h0, F32), _stride_of(h0, h0_ld, d), _address_of(y, t),
+                             _stride_of(y, y_ld, d), _flat(summary, F32), _flat(carry, None), _stream_handle(stream)),
                "sparbit_scan_forward")
 
     def backward(self, gate, x, carry, dy, dgate, dx, dlast=None, dsummary=None, stream=None, gate_ld=None, x_ld=None,
                  dy_ld=None, dgate_ld=None, dx_ld=None, dlast_ld=None) -> None:
-        d = self.channels
-        _check(_scan_backward(self._h, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(carry), _ptr(dy),
-                                         dy_ld or d, _ptr(dlast), dlast_ld or d, _ptr(dgate), dgate_ld or d,
-                                         _ptr(dx), dx_ld or d, _ptr(dsummary), _stream_handle(stream)),
+        d, t = self.channels, self.dtype
+        _check(lib.sparbit_scan_backward(self._h, _address_of(gate, t), _stride_of(gate, gate_ld, d), _address_of(x, t),
+                              _stride_of(x, x_ld, d), _flat(carry, None), _address_of(dy, t), _stride_of(dy, dy_ld, d),
+                              _address_of(dlast, F32), _stride_of(dlast, dlast_ld, d), _address_of(dgate, t),
+                              _stride_of(dgate, dgate_ld, d), _address_of(dx, t), _stride_of(dx, dx_ld, d),
+                              _flat(dsummary, F32), _stream_handle(stream)),
                "sparbit_scan_backward")
 
 
@@ -177,16 +257,23 @@ def scan_step(rows: int, channels: int, dtype: int, gate, x, state_in, state_out
               stream=None, gate_ld=None, x_ld=None, y_ld=None, state_ld=None) -> None:
     """One token for each of `rows` running sequences; n_slots defaults to `rows`."""
     d = channels
-    _check(_scan_step(rows, d, dtype, _ptr(gate), gate_ld or d, _ptr(x), x_ld or d, _ptr(slots),
-                                 rows if n_slots is None else n_slots, _ptr(state_in), _ptr(state_out), state_ld or d,
-                                 _ptr(y), y_ld or d, _stream_handle(stream)), "sparbit_scan_step")
+    dense = _flat if state_ld is None else _address_of
+    code = _scan_step(
+        rows, d, dtype, _flat(gate, dtype) if gate_ld is None else _address_of(gate, dtype),
+        d if gate_ld is None else gate_ld, _flat(x, dtype) if x_ld is None else _address_of(x, dtype),
+        d if x_ld is None else x_ld, _flat(slots, _I32), rows if n_slots is None else n_slots, dense(state_in, F32),
+        dense(state_out, F32), d if state_ld is None else state_ld,
+        _flat(y, dtype) if y_ld is None else _address_of(y, dtype), d if y_ld is None else y_ld, _stream_handle(stream))
+    if code != OK:
+        raise SparbitError(code, "sparbit_scan_step")
 
 
 def scan_join(P: int, channels: int, gathered, out, h0=None, reverse: bool = False, first_rank: int = 0,
               n_ranks=None, out_ld=None, stream=None) -> None:
     """First states of the slices first_rank .. first_rank + n_ranks - 1 (default: all P)."""
-    _check(lib.sparbit_scan_join(P, first_rank, P if n_ranks is None else n_ranks, channels, _ptr(gathered), _ptr(h0),
-                                 _ptr(out), out_ld or channels, int(bool(reverse)), _stream_handle(stream)),
+    _check(lib.sparbit_scan_join(P, first_rank, P if n_ranks is None else n_ranks, channels,
+                                 _flat(gathered, F32), _flat(h0, F32), _address_of(out, F32),
+                                 _stride_of(out, out_ld, channels), int(bool(reverse)), _stream_handle(stream)),
            "sparbit_scan_join")
 
 
@@ -198,23 +285,40 @@ class RouterPlan(_TrainPlan):
     def __init__(self, tokens, experts: int, k: int, dtype: int = BF16, renormalize: bool = False):
         n, arr = _counts(tokens)
         self._create(n, arr, experts, k, dtype, int(bool(renormalize)))
-        self.experts, self.k = experts, k
+        self.experts, self.k, self.dtype = experts, k, dtype
 
     def forward(self, logits, indices, weights, lse, counts, sums, mask=None, stream=None, ld=None) -> None:
-        _check(lib.sparbit_router_forward(self._h, _ptr(logits), ld or self.experts, _ptr(mask), _ptr(indices),
-                                          _ptr(weights), _ptr(lse), _ptr(counts), _ptr(sums), _stream_handle(stream)),
-               "sparbit_router_forward")
+        # looked at in one go: by itself each of them takes another 0.1 us
+        t = self.dtype
+        try:
+            usual = (indices.dtype is counts.dtype is _int32 and weights.dtype is lse.dtype is sums.dtype is _float32
+                     and indices.is_cuda and weights.is_cuda and lse.is_cuda and counts.is_cuda and sums.is_cuda
+                     and indices.is_contiguous() and weights.is_contiguous() and lse.is_contiguous()
+                     and counts.is_contiguous() and sums.is_contiguous())
+        except AttributeError:
+            usual = False
+        if usual:
+            outs = indices.data_ptr(), weights.data_ptr(), lse.data_ptr(), counts.data_ptr(), sums.data_ptr()
+        else:
+            outs = _flat(indices, _I32), _flat(weights, F32), _flat(lse, F32), _flat(counts, _I32), _flat(sums, F32)
+        code = _router_forward(self._h, _address_of(logits, t), _stride_of(logits, ld, self.experts),
+                               _flat(mask, _BYTE), *outs, _stream_handle(stream))
+        if code != OK:
+            raise SparbitError(code, "sparbit_router_forward")
 
     def balance(self, gathered, G: int, sums, loss, alpha: float, beta: float = 0.0, stream=None) -> None:
-        _check(lib.sparbit_router_balance(self._h, _ptr(gathered), G, _ptr(sums), alpha, beta, _ptr(loss),
-                                          _stream_handle(stream)), "sparbit_router_balance")
+        _check(lib.sparbit_router_balance(self._h, _flat(gathered, _I32), G, _flat(sums, F32), alpha, beta,
+                                          _flat(loss, F32), _stream_handle(stream)), "sparbit_router_balance")
 
     def backward(self, logits, indices, weights, lse, gathered, G: int, dlogits, dweights=None, alpha: float = 0.0,
                  beta: float = 0.0, dloss=None, mask=None, stream=None, ld=None, dlogits_ld=None) -> None:
-        _check(lib.sparbit_router_backward(self._h, _ptr(logits), ld or self.experts, _ptr(mask), _ptr(indices),
-                                           _ptr(weights), _ptr(lse), _ptr(gathered), G, _ptr(dweights), alpha, beta,
-                                           _ptr(dloss), _ptr(dlogits), dlogits_ld or self.experts,
-                                           _stream_handle(stream)), "sparbit_router_backward")
+        t, e = self.dtype, self.experts
+        _check(lib.sparbit_router_backward(self._h, _address_of(logits, t), _stride_of(logits, ld, e),
+                                           _flat(mask, _BYTE), _flat(indices, _I32), _flat(weights, F32),
+                                           _flat(lse, F32), _flat(gathered, _I32), G, _flat(dweights, F32), alpha, beta,
+                                           _flat(dloss, F32), _address_of(dlogits, t),
+                                           _stride_of(dlogits, dlogits_ld, e), _stream_handle(stream)),
+               "sparbit_router_backward")
 
 
 class OrthoPlan(_TrainPlan):
@@ -233,7 +337,7 @@ class OrthoPlan(_TrainPlan):
                 raise ValueError(f"{steps} steps need {steps} triples of coefficients")
             arr = (_f * len(flat))(*flat)
         self._create(count, rows, cols, dtype, steps, arr, eps)
-        self.rows, self.cols = rows, cols
+        self.rows, self.cols, self.dtype = rows, cols, dtype
         if products != PRODUCTS_AUTO:
             self.set_products(products)
 
@@ -241,19 +345,26 @@ class OrthoPlan(_TrainPlan):
         _check(lib.sparbit_ortho_plan_set_products(self._h, products), "sparbit_ortho_plan_set_products")
 
     def orthogonalize(self, update, out, stream=None, ld=None, stride=None, out_ld=None, out_stride=None) -> None:
-        ld, out_ld = ld or self.cols, out_ld or self.cols
-        _check(lib.sparbit_orthogonalize(self._h, _ptr(update), ld, self.rows * ld if stride is None else stride,
-                                         _ptr(out), out_ld, self.rows * out_ld if out_stride is None else out_stride,
-                                         _stream_handle(stream)), "sparbit_orthogonalize")
+        t, ld, out_ld = self.dtype, _stride_of(update, ld, self.cols), _stride_of(out, out_ld, self.cols)
+        stride = self.rows * ld if stride is None else stride
+        out_stride = self.rows * out_ld if out_stride is None else out_stride
+        _check(lib.sparbit_orthogonalize(self._h, _address_of(update, t), ld, stride, _address_of(out, t), out_ld,
+                                         out_stride, _stream_handle(stream)), "sparbit_orthogonalize")
 
     def muon_step(self, grad, momentum_in, momentum_out, weight_in, weight_out, weight_dtype: int, lr: float,
                   momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale: float = 1.0,
                   stream=None, grad_ld=None, grad_stride=None, momentum_ld=None, momentum_stride=None, weight_ld=None,
                   weight_stride=None) -> None:
-        gl, ml, wl = grad_ld or self.cols, momentum_ld or self.cols, weight_ld or self.cols
-        r = self.rows
-        args = MuonArgs(_ptr(grad), gl, r * gl if grad_stride is None else grad_stride, _ptr(momentum_in),
-                        _ptr(momentum_out), ml, r * ml if momentum_stride is None else momentum_stride,
-                        _ptr(weight_in), _ptr(weight_out), wl, r * wl if weight_stride is None else weight_stride,
+        if momentum_ld is None:
+            _dense(momentum_in)
+        if weight_ld is None:
+            _dense(weight_in)
+        r, c = self.rows, self.cols
+        gl, ml = _stride_of(grad, grad_ld, c), _stride_of(momentum_out, momentum_ld, c)
+        wl = _stride_of(weight_out, weight_ld, c)
+        args = MuonArgs(_address_of(grad, self.dtype), gl, r * gl if grad_stride is None else grad_stride,
+                        _address_of(momentum_in, F32), _address_of(momentum_out, F32), ml,
+                        r * ml if momentum_stride is None else momentum_stride, _address_of(weight_in, weight_dtype),
+                        _address_of(weight_out, weight_dtype), wl, r * wl if weight_stride is None else weight_stride,
                         weight_dtype, int(bool(nesterov)), lr, momentum, weight_decay, scale)
         _check(lib.sparbit_muon_step(self._h, ctypes.byref(args), _stream_handle(stream)), "sparbit_muon_step")
