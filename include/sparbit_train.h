@@ -214,9 +214,10 @@ enum { SPARBIT_PRODUCTS_AUTO = 0, SPARBIT_PRODUCTS_ONE = 1, SPARBIT_PRODUCTS_THR
 /*
  * A plan for `count` matrices of rows x cols, element type dtype.  coefficients: host array
  * [steps][3], copied; NULL = (3.4445, -4.7750, 2.0315) in every step (five steps are usual).
- * Errors: ERR_ARG (count, rows, cols or steps < 1, unknown type, eps negative or not finite,
- * coefficients under which singular values from 0 .. 1 leave 0 .. 7 or the polynomial b s^2 + c s^4
- * leaves -48 .. 48), ERR_LIMIT (rows or cols > 65536, count > 4096, steps > 64, 2^31 tiles of work),
+ * Errors: ERR_ARG (count, rows, cols or steps < 1, unknown type, eps negative or not finite, and
+ * coefficients that what the steps hold has no room for: singular values that start in 0 .. 1 may
+ * have magnitudes up to 6.9 where a step begins and 64 (less 2 %) after the last, and b s^2 + c s^4
+ * up to 48, with and without -3/4 (b + c)), ERR_LIMIT (rows or cols > 65536, count > 4096, steps > 64, 2^31 tiles of work),
  * ERR_NOMEM.  Host-only.
  */
 int sparbit_ortho_plan_create(int count, size_t rows, size_t cols, int dtype, int steps, const float* coefficients,
