@@ -51,6 +51,9 @@ enum { SPARBIT_F32 = 0, SPARBIT_BF16 = 1, SPARBIT_F16 = 2 };
  *   g_t = dy_t + c_t,  c_{t-1} = a_t g_t,  dx_t = (1 - a_t) g_t,
  *   dgate_t = g_t (h_{t-1} - x_t) a_t (1 - a_t),  dh0 = c_0
  *
+ * A NaN, or an infinite x, dy or first state, makes its channel NaN or infinite from there to the end
+ * (beginning) of its sequence, and nothing else.
+ *
  * A plan covers n sequences of given lengths (0 and 1 allowed) whose rows follow one another in
  * every matrix: sequence s has the lengths[s] rows from off[s] = the sum of the lengths before it.
  */
@@ -204,9 +207,10 @@ int sparbit_router_backward(sparbit_router_plan_t* plan, const void* logits, siz
  */
 typedef struct sparbit_ortho_plan_s sparbit_ortho_plan_t;
 
-/* Products of 16-bit operands that make up one product of the iteration.  ONE: error 0.5e-3 (4096 x
- * 8192) to 1.4e-3 (256 x 256) of the result's norm; rounding to a bf16 result makes 1.7e-3 beside it.
- * THREE: 1e-6 to 3e-6 where the result has 32 bits, three times the work.  AUTO: ONE for SPARBIT_BF16
+/* Products of 16-bit operands that make up one product of the iteration.  ONE: error 0.3e-3 (4096 x
+ * 8192, decaying singular values) to 1.9e-3 (64 x 64, random) of the result's norm; rounding to a
+ * bf16 result makes 1.7e-3 beside it.  THREE, three times the work: where the result has 32 bits
+ * 1e-6, of matrices of low rank 3e-6 to 7e-6 (plain 32-bit arithmetic: 1.4e-5).  AUTO: ONE for SPARBIT_BF16
  * matrices, THREE for the types with more bits; the weights of a Muon step do not enter, so that
  * bf16 gradients of 32-bit weights have to ask for THREE where they want it. */
 enum { SPARBIT_PRODUCTS_AUTO = 0, SPARBIT_PRODUCTS_ONE = 1, SPARBIT_PRODUCTS_THREE = 3 };

@@ -12,14 +12,15 @@
 // step (16-bit matrices): the tensor cores see hi alone, 11 bits, but the term (a - d) X, through
 // which the small singular values grow 3.4-fold a step, is formed from hi + lo, and in the first
 // step X is U itself (16-bit inputs are exact in hi; 1 / |U| is folded into the epilogues).  With
-// rounded X in that term the result of a low-rank gradient is 1-2 % off, with the pair 0.1 %, below
-// the rounding of a bf16 result.  Three products (32-bit matrices): hi hi + hi lo + lo hi, and that
-// term from an fp32 copy of X, which hi + lo would cut to 22 bits: about 1e-6.  The shift d = -3/4 (b + c) takes
+// rounded X in that term the result of a low-rank gradient is 1-2 % off, with the pair 0.1 %; random
+// matrices are 0.12 % off (from 1000 on a side; 64 x 64 0.19 %), where rounding to bf16 is 0.17 %.  Three products (32-bit matrices): hi hi + hi lo + lo hi, and that
+// term from an fp32 copy of X, which hi + lo would cut to 22 bits: 1e-6 (low rank
+// up to 7e-6 at 64 x 64, where plain 32-bit arithmetic is 1.4e-5 off).  The shift d = -3/4 (b + c) takes
 // most of P's diagonal out of its rounding.  With one product it is for the last step alone: in earlier
 // ones it would feed the rounding of hi back into small singular values.
 //
-// Operations are the floor of large matrices: 4096 x 8192 bf16 1.95 ms, 1230 TFLOP/s, the tensor pipe busy for
-// 72-77 % of the products' time (shared memory bounds it, see the tiles).  Small ones are bound by the launch
+// Operations are the floor of large matrices: 4096 x 8192 bf16 2.1 ms, 1145 TFLOP/s at the power limit, the tensor
+// pipe busy for 74-81 % of the products' time (shared memory bounds it, see the tiles).  Small ones are bound by the launch
 // that each product is: 4 x 256 x 256 104 us, 6 us a product, of which 1.3 until the kernel before has ended
 // for this one to see, 1.1 until the first tile is in, 0.6-0.9 multiplying, 2.5 writing out.
 #include <cuda.h>

@@ -6,8 +6,8 @@
 // lane sorts its keys once (networks, lists of up to 8), then k times the largest head of the group
 // wins and its list moves up.  A key holds the logit's order and, below it, the complement of the
 // expert's index, so that keys differ and equal logits go to the lowest index.  Instructions bound
-// this: 430 a token forward and 240 backward at 256 bf16 experts, k = 8 (56738 tokens: 37 us and 20 us at
-// 65 % and 62 % of the issue slots, where the 29 MB of logits would take 4.5 us to read).
+// this: 440 a token forward and 245 backward at 256 bf16 experts, k = 8 (56738 tokens: 37 us and 20 us at
+// 66 % and 64 % of the issue slots, where the 29 MB of logits would take 4.5 us to read).
 #include <float.h>
 #include <math.h>
 

@@ -250,7 +250,8 @@ struct Rows {
     }
 };
 
-// Starts the copy of a piece's rows of one tensor.  Reads nothing outside the rows.
+// Starts the copy of a piece's rows of one tensor.  Of rows that are not wide it reads up to 15 bytes in front of a row
+// (the rest of 16 aligned bytes, unused), but nothing in front of the tensor or behind a row.
 template <typename T, int R, int kThr, bool kWide, bool kBurst>
 __device__ __forceinline__ void stage_tensor(char* stage, const T* src, int64_t ld, int64_t row0, int len, int ch0, int D) {
     using S = Stage<T, R, kWide>;
