@@ -1,8 +1,8 @@
 """ctypes binding of include/sparbit_train.h: argument marshalling only.
 
 Operators of a training step whose state is divided over the ranks of a communicator.  Tensors are torch
-tensors in device (or pinned host) memory, whose type has to be the operator's (TypeError), or numpy arrays or
-addresses, which are taken as they are; row strides (`*_ld`, in elements) default to the row's width, which a
+tensors in device (or pinned host) memory, whose type has to be the operator's (TypeError), or numpy arrays,
+addresses and other objects with `data_ptr()`, which are taken as they are; row strides (`*_ld`, in elements) default to the row's width, which a
 tensor with gaps between its rows does not have (ValueError: give its stride).  Everything runs in the
 library's CUDA kernels; there is no fallback.
 """
@@ -110,8 +110,8 @@ def _address_of(x, code):
 
 
 def _address_checked(x, code):
-    if not hasattr(x, "data_ptr"):
-        return _address(x)  # None, a number, a numpy array: the caller's word
+    if not (hasattr(x, "data_ptr") and hasattr(x, "dtype") and hasattr(x, "is_cuda")):
+        return _address(x)  # a number, a numpy array, anything else with an address: the caller's word
     global _float32, _int32
     dtype = str(x.dtype)
     met = _codes[x.dtype] = _KNOWN.get(dtype, -1)

@@ -139,3 +139,23 @@ def test_sizes_may_be_numpy_integers():
     assert e.value.code == sp.ERR_WORKSPACE
     with pytest.raises(ctypes.ArgumentError):
         call(**tensors(**kinds), ld=64.0)
+
+
+class Address:
+    """Something that has an address and says nothing else of itself."""
+
+    def __init__(self, address):
+        self.address = address
+
+    def data_ptr(self):
+        return self.address
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_what_is_no_tensor_is_taken_as_it_is(name):
+    """Numbers, numpy arrays and anything else with data_ptr(): the caller's word, as the library's other calls take it."""
+    call, kinds, strided, other = case(name)
+    for make in (Address, int, lambda a: np.empty(64, np.uint8)):
+        given = {k: make((i + 1) << 40) for i, k in enumerate(kinds)}
+        with pytest.raises(sp.SparbitError):
+            call(**given, **other)
