@@ -210,9 +210,10 @@ typedef struct sparbit_ortho_plan_s sparbit_ortho_plan_t;
 /* Products of 16-bit operands that make up one product of the iteration.  ONE: error 0.3e-3 (4096 x
  * 8192, decaying singular values) to 1.9e-3 (64 x 64, random) of the result's norm; rounding to a
  * bf16 result makes 1.7e-3 beside it.  THREE, three times the work: where the result has 32 bits
- * 1e-6, of matrices of low rank 3e-6 to 7e-6 (plain 32-bit arithmetic: 1.4e-5).  AUTO: ONE for SPARBIT_BF16
- * matrices, THREE for the types with more bits; the weights of a Muon step do not enter, so that
- * bf16 gradients of 32-bit weights have to ask for THREE where they want it. */
+ * 1e-6, of matrices of low rank 3e-6 to 7e-6 (plain 32-bit arithmetic: 1.4e-5).  AUTO: ONE for
+ * SPARBIT_BF16 matrices with no side below 128; THREE for smaller ones, which ONE would leave more
+ * than half as far off again as rounding does, and for the types with more bits.  The weights of a
+ * Muon step do not enter: bf16 gradients of 32-bit weights have to ask for THREE where they want it. */
 enum { SPARBIT_PRODUCTS_AUTO = 0, SPARBIT_PRODUCTS_ONE = 1, SPARBIT_PRODUCTS_THREE = 3 };
 
 /*
