@@ -1,10 +1,10 @@
 """ctypes binding of include/sparbit_train.h: argument marshalling only.
 
 Operators of a training step whose state is divided over the ranks of a communicator.  Tensors are torch
-tensors in device (or pinned host) memory, whose type has to be the operator's (TypeError), or numpy arrays,
-addresses and other objects with `data_ptr()`, which are taken as they are; row strides (`*_ld`, in elements) default to the row's width, which a
-tensor with gaps between its rows does not have (ValueError: give its stride).  Everything runs in the
-library's CUDA kernels; there is no fallback.
+tensors in device (or pinned host) memory, whose type has to be the operator's (TypeError); numpy arrays,
+addresses and other objects with `data_ptr()` are taken as they are.  Row strides (`*_ld`, in elements)
+default to the row's width, which a tensor with gaps between its rows does not have (ValueError: give its
+stride).  Everything runs in the library's CUDA kernels; there is no fallback.
 """
 from __future__ import annotations
 
@@ -68,19 +68,10 @@ for _name, (_res, _args) in SYMBOLS.items():
 
 
 def _words(name):
-    """The call for arguments that are all integers and addresses, a machine word each: ctypes converts an int to void*
-    faster than to size_t (a token's step 0.5 us), but nothing that only behaves like an int (numpy's), which goes
-    the declared way."""
-    declared = getattr(lib, name)
-    fast = ctypes.CFUNCTYPE(_i, *[_vp] * len(declared.argtypes))((name, lib))
-
-    def call(*args):
-        try:
-            return fast(*args)
-        except ctypes.ArgumentError:
-            return declared(*args)
-
-    return call
+    """The function for arguments that are all integers and addresses, a machine word each: ctypes converts an int to
+    void* faster than to size_t (a token's step 0.5 us), but nothing that only behaves like an int (numpy's), which
+    raises ArgumentError and goes the declared way."""
+    return ctypes.CFUNCTYPE(_i, *[_vp] * len(getattr(lib, name).argtypes))((name, lib))
 
 
 _scan_step, _router_forward = _words("sparbit_scan_step"), _words("sparbit_router_forward")
@@ -88,13 +79,13 @@ _scan_step, _router_forward = _words("sparbit_scan_step"), _words("sparbit_route
 
 # What a tensor has to be: device memory of the type that the kernels read, and without gaps where no row stride is
 # given.  The calls below can be shorter than their own marshalling (a token's step takes the GPU 3 us), so the common
-# cases come first; looking costs a token's step 0.4 us and the router's forward pass 1.1.
+# cases come first, and the two shortest calls look at all their tensors in one go.
 _I32, _BYTE = 3, 4
 _NAMES = {F32: "float32", BF16: "bfloat16", F16: "float16", _I32: "int32", _BYTE: "uint8 or bool"}
 _KNOWN = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16, "torch.int32": _I32, "torch.uint8": _BYTE,
           "torch.int8": _BYTE, "torch.bool": _BYTE}
 _codes = {}  # of the torch types met so far
-_float32 = _int32 = None  # torch's, once met
+_types = {}  # and the other way round
 
 
 def _address_of(x, code):
@@ -112,13 +103,9 @@ def _address_of(x, code):
 def _address_checked(x, code):
     if not (hasattr(x, "data_ptr") and hasattr(x, "dtype") and hasattr(x, "is_cuda")):
         return _address(x)  # a number, a numpy array, anything else with an address: the caller's word
-    global _float32, _int32
     dtype = str(x.dtype)
     met = _codes[x.dtype] = _KNOWN.get(dtype, -1)
-    if met == F32:
-        _float32 = x.dtype
-    elif met == _I32:
-        _int32 = x.dtype
+    _types[met] = x.dtype
     if code is not None and met != code:
         raise TypeError(f"a tensor of {_NAMES.get(code, code)} is wanted, not of {dtype}")
     if not (x.is_cuda or x.is_pinned()):
@@ -256,14 +243,32 @@ class ScanPlan(_TrainPlan):
 def scan_step(rows: int, channels: int, dtype: int, gate, x, state_in, state_out, y, slots=None, n_slots=None,
               stream=None, gate_ld=None, x_ld=None, y_ld=None, state_ld=None) -> None:
     """One token for each of `rows` running sequences; n_slots defaults to `rows`."""
+    try:
+        t, f = _types[dtype], _types[F32]
+        usual = (gate.dtype is x.dtype is y.dtype is t and state_in.dtype is state_out.dtype is f
+                 and gate.is_cuda and x.is_cuda and y.is_cuda and state_in.is_cuda and state_out.is_cuda
+                 and (gate_ld is not None or gate.is_contiguous()) and (x_ld is not None or x.is_contiguous())
+                 and (y_ld is not None or y.is_contiguous())
+                 and (state_ld is not None or (state_in.is_contiguous() and state_out.is_contiguous())))
+    except (AttributeError, KeyError):
+        usual = False
+    if usual:
+        gate, x, y, state_in, state_out = (gate.data_ptr(), x.data_ptr(), y.data_ptr(), state_in.data_ptr(),
+                                           state_out.data_ptr())
+    else:
+        gate = _address_of(gate, dtype) if gate_ld is not None else _flat(gate, dtype)
+        x = _address_of(x, dtype) if x_ld is not None else _flat(x, dtype)
+        y = _address_of(y, dtype) if y_ld is not None else _flat(y, dtype)
+        of_state = _address_of if state_ld is not None else _flat
+        state_in, state_out = of_state(state_in, F32), of_state(state_out, F32)
     d = channels
-    dense = _flat if state_ld is None else _address_of
-    code = _scan_step(
-        rows, d, dtype, _flat(gate, dtype) if gate_ld is None else _address_of(gate, dtype),
-        d if gate_ld is None else gate_ld, _flat(x, dtype) if x_ld is None else _address_of(x, dtype),
-        d if x_ld is None else x_ld, _flat(slots, _I32), rows if n_slots is None else n_slots, dense(state_in, F32),
-        dense(state_out, F32), d if state_ld is None else state_ld,
-        _flat(y, dtype) if y_ld is None else _address_of(y, dtype), d if y_ld is None else y_ld, _stream_handle(stream))
+    args = (rows, d, dtype, gate, d if gate_ld is None else gate_ld, x, d if x_ld is None else x_ld, _flat(slots, _I32),
+            rows if n_slots is None else n_slots, state_in, state_out, d if state_ld is None else state_ld, y,
+            d if y_ld is None else y_ld, _stream_handle(stream))
+    try:
+        code = _scan_step(*args)
+    except ctypes.ArgumentError:
+        code = lib.sparbit_scan_step(*args)
     if code != OK:
         raise SparbitError(code, "sparbit_scan_step")
 
@@ -288,21 +293,29 @@ class RouterPlan(_TrainPlan):
         self.experts, self.k, self.dtype = experts, k, dtype
 
     def forward(self, logits, indices, weights, lse, counts, sums, mask=None, stream=None, ld=None) -> None:
-        # looked at in one go: by itself each of them takes another 0.1 us
-        t = self.dtype
         try:
-            usual = (indices.dtype is counts.dtype is _int32 and weights.dtype is lse.dtype is sums.dtype is _float32
-                     and indices.is_cuda and weights.is_cuda and lse.is_cuda and counts.is_cuda and sums.is_cuda
-                     and indices.is_contiguous() and weights.is_contiguous() and lse.is_contiguous()
-                     and counts.is_contiguous() and sums.is_contiguous())
-        except AttributeError:
+            t, f, i = _types[self.dtype], _types[F32], _types[_I32]
+            usual = (logits.dtype is t and indices.dtype is counts.dtype is i
+                     and weights.dtype is lse.dtype is sums.dtype is f and logits.is_cuda and indices.is_cuda
+                     and weights.is_cuda and lse.is_cuda and counts.is_cuda and sums.is_cuda
+                     and (ld is not None or logits.is_contiguous()) and indices.is_contiguous()
+                     and weights.is_contiguous() and lse.is_contiguous() and counts.is_contiguous()
+                     and sums.is_contiguous())
+        except (AttributeError, KeyError):
             usual = False
         if usual:
-            outs = indices.data_ptr(), weights.data_ptr(), lse.data_ptr(), counts.data_ptr(), sums.data_ptr()
+            logits, indices, weights, lse, counts, sums = (logits.data_ptr(), indices.data_ptr(), weights.data_ptr(),
+                                                           lse.data_ptr(), counts.data_ptr(), sums.data_ptr())
         else:
-            outs = _flat(indices, _I32), _flat(weights, F32), _flat(lse, F32), _flat(counts, _I32), _flat(sums, F32)
-        code = _router_forward(self._h, _address_of(logits, t), _stride_of(logits, ld, self.experts),
-                               _flat(mask, _BYTE), *outs, _stream_handle(stream))
+            logits = _address_of(logits, self.dtype) if ld is not None else _flat(logits, self.dtype)
+            indices, weights, lse = _flat(indices, _I32), _flat(weights, F32), _flat(lse, F32)
+            counts, sums = _flat(counts, _I32), _flat(sums, F32)
+        args = (self._h, logits, self.experts if ld is None else ld, _flat(mask, _BYTE), indices, weights, lse, counts,
+                sums, _stream_handle(stream))
+        try:
+            code = _router_forward(*args)
+        except ctypes.ArgumentError:
+            code = lib.sparbit_router_forward(*args)
         if code != OK:
             raise SparbitError(code, "sparbit_router_forward")
 
