@@ -13,6 +13,11 @@
  *   ortho    a matrix update orthogonalised by Newton-Schulz products, alone or with the momentum
  *            in front of it and the weight update behind it.  The ranks gather the rows of the
  *            matrix: a receive buffer of sparbit_allgather IS the matrix, row blocks in rank order.
+ *   linear attention   with a decay for each head: the recurrence with a matrix as its state, forward,
+ *            backward and for single tokens, divided by time as the scan is.
+ *   norm     root-mean-square norm of a row, with the residual's addition in front of it and 8-bit rows
+ *            with scales behind it: the ranks gather those, half the bytes of 16-bit rows.
+ *   clip     the norm of all gradients and their clipping.  The ranks gather one 64-bit sum each.
  *
  * Conventions are those of sparbit.h: error codes, sparbit_strerror, sparbit_last_cuda_error;
  * plans are made on the host without a CUDA call; calls are asynchronous on `stream` (a
@@ -268,6 +273,155 @@ typedef struct {
     float lr, momentum, weight_decay, scale;
 } sparbit_muon;
 int sparbit_muon_step(sparbit_ortho_plan_t* plan, const sparbit_muon* args, void* stream);
+
+/* ---- linear attention with a decay for each head ------------------------------------------------
+ *
+ * For every head, with d = exp(log_decay) and a state S of key_size x value_size in 32 bits,
+ *
+ *   S_t = d S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t
+ *
+ * and, with dS_t the gradient of S_t,
+ *
+ *   dS_t = scale q_t^T do_t + d dS_{t+1},   dq_t = scale S_t do_t,  dk_t = dS_t v_t,  dv_t = k_t dS_t,
+ *   dfirst = d dS_1
+ *
+ * log_decay: [heads] 32-bit on the device, the natural logarithms: 0 keeps everything, -inf nothing; numbers
+ * above 0 are taken as they are.  The decays are constants of the model: they have no gradient here.
+ * 16-bit types: tokens' weights and the state that a chunk of 128 tokens starts with are rounded to 16 bits
+ * for the tensor cores (together they leave o about 1.4 times as far off as its own rounding); states
+ * themselves are sums of products with 32-bit factors.  f32: plain 32-bit arithmetic.
+ * A NaN or an infinity in k or v makes what it reaches NaN or infinite, from its token to the end of its
+ * sequence (in its value's column, for v), and nothing before it; gradients in the same way.
+ *
+ * q, k, o, do and so on: [rows][heads][size] with a row stride in elements; a head's elements follow one
+ * another, and the heads.  Sequences' rows follow one another as in a scan's plan.
+ */
+typedef struct sparbit_linear_attention_plan_s sparbit_linear_attention_plan_t;
+
+#define SPARBIT_LINEAR_ATTENTION_MAX_SIZE 128
+
+/* Errors: ERR_ARG (null, n_seqs, heads or a size < 1, unknown type, scale not finite), ERR_OVERFLOW (rows x
+ * heads x size beyond 2^46), ERR_LIMIT (sizes above the limit, more than 4096 heads or 65535 sequences, a
+ * sequence of more than 2^31-1 tokens, 2^31/3 pieces of work), ERR_NOMEM.  Host-only. */
+int sparbit_linear_attention_plan_create(int n_seqs, const size_t* lengths, int heads, int key_size, int value_size,
+                                         int dtype, float scale, sparbit_linear_attention_plan_t** out);
+int sparbit_linear_attention_plan_destroy(sparbit_linear_attention_plan_t* plan);
+size_t sparbit_linear_attention_plan_workspace_bytes(const sparbit_linear_attention_plan_t* plan);
+int sparbit_linear_attention_plan_set_workspace(sparbit_linear_attention_plan_t* plan, void* dev, size_t bytes);
+/* As sparbit_scan_plan_status; the test hook withholds the states' products of 16-bit types. */
+int sparbit_linear_attention_plan_status(sparbit_linear_attention_plan_t* plan);
+int sparbit_linear_attention_plan_set_wait_test(sparbit_linear_attention_plan_t* plan, int withhold, uint64_t timeout_ns);
+
+/*
+ *   q, k     [rows][heads][key_size], v, o [rows][heads][value_size], of the plan's type; o NULL = only the
+ *            summary is wanted, q is not read then and may be NULL
+ *   first    [n_seqs][heads][key_size][value_size] 32-bit or NULL = zero
+ *   summary  [n_seqs][heads + heads * key_size * value_size] 32-bit or NULL: each head's decay over the
+ *            whole sequence, then the last states (first for a sequence of no rows): the block to gather
+ */
+int sparbit_linear_attention_forward(sparbit_linear_attention_plan_t* plan, const void* q, size_t q_ld, const void* k,
+                                     size_t k_ld, const void* v, size_t v_ld, const float* log_decay, const float* first,
+                                     void* o, size_t o_ld, float* summary, void* stream);
+
+/*
+ *   dlast    gradient of the last states, as first; NULL = zero
+ *   dsummary as summary: the decays, then dfirst
+ * With dq, dk and dv NULL (all or none) only dsummary is computed; k, v and first are then not read.
+ */
+int sparbit_linear_attention_backward(sparbit_linear_attention_plan_t* plan, const void* q, size_t q_ld, const void* k,
+                                      size_t k_ld, const void* v, size_t v_ld, const float* log_decay, const float* first,
+                                      const void* d_o, size_t do_ld, const float* dlast, void* dq, size_t dq_ld, void* dk,
+                                      size_t dk_ld, void* dv, size_t dv_ld, float* dsummary, void* stream);
+
+/* One token for each of `rows` running sequences, as sparbit_scan_step: states [n_slots][heads][key_size]
+ * [value_size] 32-bit, one behind another.  No plan, no workspace. */
+int sparbit_linear_attention_step(size_t rows, int heads, int key_size, int value_size, int dtype, float scale, const void* q,
+                                  size_t q_ld, const void* k, size_t k_ld, const void* v, size_t v_ld, const float* log_decay,
+                                  const int32_t* slots, size_t n_slots, const float* state_in, float* state_out, void* o,
+                                  size_t o_ld, void* stream);
+
+/* The first states of slices that follow one another in time, as sparbit_scan_join.  gathered: [n_ranks][P]
+ * blocks as forward's summary (reverse != 0: backward's dsummary) of one sequence; first: [heads][key_size]
+ * [value_size] or NULL; out: [n_ranks] of that. */
+int sparbit_linear_attention_join(int P, int first_rank, int n_ranks, int heads, int key_size, int value_size,
+                                  const float* gathered, const float* first, float* out, int reverse, void* stream);
+
+/* ---- root-mean-square norm ----------------------------------------------------------------------
+ *
+ *   r = x + residual, rounded to the type;  y = r rstd weight,  rstd = 1 / sqrt(mean(r^2) + eps)
+ *   g = dy weight;  dx = rstd (g - u mean(g u)) + dsum, u = r rstd;  dweight = sum over the rows of dy u
+ *
+ * dx is the gradient of x and of the residual alike; dsum is what reaches r on other ways.  The sum of squares
+ * of finite numbers is right whatever their size.  An infinity or NaN in a row makes the row of y what
+ * the formula makes of it (0 or NaN), and reaches no other row but through dweight.
+ *
+ * 8-bit rows: y in e4m3 (1 byte) over a scale for each row, or each `block` columns of it: scale = max |y| / 448,
+ * from y before it is rounded (at least 1e-30 / 448, so that zeros have one; a block with a NaN or an infinity has
+ * NaN or infinity as its scale, and y8 is NaN where y / scale is).
+ */
+typedef struct sparbit_norm_plan_s sparbit_norm_plan_t;
+
+#define SPARBIT_NORM_MAX_WIDTH 32768
+
+/* dtype: of rows; weight_dtype: F32 or dtype.  block: 0 (a scale for each row), 32, 64, 128 or 256.
+ * Errors: ERR_ARG (width < 1, unknown types or block, eps below 1e-30 or not finite), ERR_LIMIT (width above
+ * the limit), ERR_NOMEM.  Host-only. */
+int sparbit_norm_plan_create(size_t width, int dtype, int weight_dtype, float eps, int block, sparbit_norm_plan_t** out);
+int sparbit_norm_plan_destroy(sparbit_norm_plan_t* plan);
+/* Only backward calls use the workspace (partial sums of dweight). */
+size_t sparbit_norm_plan_workspace_bytes(const sparbit_norm_plan_t* plan);
+int sparbit_norm_plan_set_workspace(sparbit_norm_plan_t* plan, void* dev, size_t bytes);
+
+/*
+ *   x, residual  [rows][width]; residual NULL: r is x
+ *   weight       [width] or NULL = 1
+ *   sum, y       [rows][width] or NULL: r, and y rounded to the type
+ *   y8, scales   [rows][width] bytes and [rows][ceil(width / block)] (block 0: [rows]) 32-bit, both or neither
+ *   rstd         [rows] 32-bit or NULL: for the backward pass
+ * sum may be x or the residual (added in place); other overlaps are ERR_ALIAS.
+ */
+int sparbit_norm_forward(sparbit_norm_plan_t* plan, size_t rows, const void* x, size_t x_ld, const void* residual,
+                         size_t residual_ld, const void* weight, void* sum, size_t sum_ld, void* y, size_t y_ld, void* y8,
+                         size_t y8_ld, float* scales, float* rstd, void* stream);
+
+/*   sum      the forward pass's r (x where there was no residual);  dsum [rows][width] or NULL
+ *   dx       [rows][width]; may be dy or dsum;  dweight [width] 32-bit or NULL */
+int sparbit_norm_backward(sparbit_norm_plan_t* plan, size_t rows, const void* dy, size_t dy_ld, const void* sum,
+                          size_t sum_ld, const void* weight, const float* rstd, const void* dsum, size_t dsum_ld, void* dx,
+                          size_t dx_ld, float* dweight, void* stream);
+
+/* ---- norm of all gradients, and clipping --------------------------------------------------------
+ *
+ *   sums[r] = sum of the squares of all elements of rank r's tensors, in 64 bits
+ *   norm = sqrt(sum over the ranks of sums),  factor = min(1, most / (norm + eps)),  out = factor * in
+ *
+ * A norm that is NaN makes every element NaN, an infinite one makes the factor 0 (and infinite elements NaN).
+ */
+typedef struct sparbit_clip_plan_s sparbit_clip_plan_t;
+
+/* n tensors of the given lengths (0 allowed) and types; ranks: the virtual rank that owns each, 0 .. n_ranks-1, or
+ * NULL = all rank 0's.  Host arrays, copied.  Errors: ERR_ARG, ERR_OVERFLOW (more than 2^46 elements), ERR_LIMIT
+ * (more than 65535 ranks or 2^24 tensors, 2^31-1 pieces of 16384 elements), ERR_NOMEM.  Host-only. */
+int sparbit_clip_plan_create(int n_ranks, size_t n, const size_t* lengths, const int* dtypes, const int* ranks,
+                             sparbit_clip_plan_t** out);
+int sparbit_clip_plan_destroy(sparbit_clip_plan_t* plan);
+size_t sparbit_clip_plan_workspace_bytes(const sparbit_clip_plan_t* plan);
+int sparbit_clip_plan_set_workspace(sparbit_clip_plan_t* plan, void* dev, size_t bytes);
+
+/* Host arrays of n device addresses: what is summed, and what the clipped elements are written to (out[i] may be
+ * in[i]; out NULL: only sums and norms are wanted).  After set_workspace; SYNCHRONISES; holds until the next call.
+ * ERR_ARG: an address is null (of a tensor with elements) or no multiple of its element's size; ERR_ALIAS: an
+ * output overlaps another output, another tensor's input, or part of its own. */
+int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* plan, const void* const* in, void* const* out);
+
+/* sums: [n_ranks] 64-bit.  ERR_WORKSPACE also where no tensors are set. */
+int sparbit_clip_sums(sparbit_clip_plan_t* plan, double* sums, void* stream);
+
+/* gathered: [n_ranks][G] 64-bit, rank r's receive buffer of the allgather of the sums over G ranks.
+ * norms: [n_ranks][2] 32-bit: norm and factor.  Where out was NULL nothing else is written.  A tensor that is its own
+ * output is left alone where the factor is 1.  ERR_ARG: most negative or NaN, eps negative or not finite. */
+int sparbit_clip_scale(sparbit_clip_plan_t* plan, const double* gathered, int G, float most, float eps, float* norms,
+                       void* stream);
 
 #ifdef __cplusplus
 }

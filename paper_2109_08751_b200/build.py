@@ -13,15 +13,17 @@ HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libsparbit_b200.so"
 SOURCES = [CSRC / "api.cu", CSRC / "multi.cu", CSRC / "schedule.cpp", CSRC / "train_scan.cu",
-           CSRC / "train_router.cu", CSRC / "train_ortho.cu"]
+           CSRC / "train_router.cu", CSRC / "train_ortho.cu", CSRC / "train_attention.cu",
+           CSRC / "train_norm.cu", CSRC / "train_clip.cu"]
 HEADERS = [CSRC / "kernels.cuh", CSRC / "phase_desc.h", CSRC / "schedule.h", CSRC / "plan_access.h",
-           CSRC / "train_common.cuh", HERE.parent / "include" / "sparbit.h",
+           CSRC / "train_common.cuh", CSRC / "train_tensor.cuh", HERE.parent / "include" / "sparbit.h",
            HERE.parent / "include" / "sparbit_train.h"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
     "-lineinfo", "-O3", "-std=c++20",
     "-Xcompiler", "-fPIC", "-shared",
+    "--threads", "0",  # the sources side by side
 ]
 
 

@@ -1,0 +1,527 @@
+// Root-mean-square norm of rows, with the residual's addition in front of it and 8-bit rows with scales behind it.
+//
+//   r = x + residual;  y = r rstd weight, rstd = 1 / sqrt(mean(r^2) + eps)
+//   g = dy weight;  dx = rstd (g - u mean(g u)) + dsum, u = r rstd;  dweight = sum dy u
+//
+// Bytes are the floor: a row is read once, stays in registers over the reduction and is written once.  A thread has up
+// to four units of eight neighbouring columns; a row belongs to 4 .. 32 lanes of a warp or to a CTA of its own, as
+// many threads as its units take.
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+
+#include "train_common.cuh"
+
+using namespace spb;
+
+namespace {
+
+constexpr int kUnit = 8;             // columns of a unit
+constexpr int kMostUnits = 4;        // of a thread
+constexpr int kMostThreads = 1024;   // of a row
+constexpr int kShared = 256;         // threads of a CTA whose rows belong to 32 lanes or fewer
+constexpr int kParts = 592;          // CTAs that sum dweight: four an SM
+constexpr int kSms = 148;
+
+struct NormArgs {
+    const void *x, *residual, *weight;
+    void *sum, *y;
+    uint8_t* y8;
+    float *scales, *rstd;
+    int64_t x_ld, residual_ld, sum_ld, y_ld, y8_ld;
+    int64_t rows;
+    int width, lanes;                // lanes: threads of a row
+    int wide, weight_wide, y8_wide;  // rows start on multiples of 16 bytes (y8: 8)
+    int block, scales_ld;            // columns of a scale, 0: all
+    float eps;
+};
+struct NormBackArgs {
+    const void *dy, *sum, *weight, *dsum;
+    const float* rstd;
+    void* dx;
+    float* parts;                    // [CTAs][width], null: dweight is not wanted
+    int64_t dy_ld, sum_ld, dsum_ld, dx_ld;
+    int64_t rows;
+    int width, lanes, wide, weight_wide;
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int n, bool wide, float (&v)[kUnit]) {
+    if (wide && n >= kUnit) {
+        constexpr int A = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kUnit; i += A) {
+            const Pack<T, A> k = *reinterpret_cast<const Pack<T, A>*>(p + i);
+#pragma unroll
+            for (int j = 0; j < A; j++) v[i + j] = to_float(k.v[j]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kUnit; i++) v[i] = i < n ? to_float(p[i]) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&v)[kUnit]) {
+    if (wide && n >= kUnit) {
+        constexpr int A = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kUnit; i += A) {
+            Pack<T, A> k;
+#pragma unroll
+            for (int j = 0; j < A; j++) k.v[j] = from_float<T>(v[i + j]);
+            *reinterpret_cast<Pack<T, A>*>(p + i) = k;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kUnit; i++)
+            if (i < n) p[i] = from_float<T>(v[i]);
+    }
+}
+
+// Reductions over the threads of a row, in one order.  `sm`: a word for each warp, two sets in turn.
+struct RowSum {
+    static __device__ __forceinline__ float of(float a, float b) { return a + b; }
+};
+struct RowMax {  // of non-negative numbers; a NaN is the largest
+    static __device__ __forceinline__ float of(float a, float b) {
+        return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+    }
+};
+template <typename Op>
+__device__ __forceinline__ float over_lanes(float v, int lanes) {
+    for (int o = (lanes < 32 ? lanes : 32) / 2; o; o >>= 1) v = Op::of(v, __shfl_xor_sync(kAllLanes, v, o));
+    return v;
+}
+template <typename Op>
+__device__ __forceinline__ float over_row(float v, int lanes, float* sm, int& turn) {
+    v = over_lanes<Op>(v, lanes);
+    if (lanes <= 32) return v;
+    const int warp = threadIdx.x >> 5, warps = lanes >> 5;
+    sm += (turn ^= 32);
+    if ((threadIdx.x & 31) == 0) sm[warp] = v;
+    __syncthreads();
+    v = sm[0];
+    for (int i = 1; i < warps; i++) v = Op::of(v, sm[i]);
+    return v;
+}
+
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+    unsigned short r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <typename T, typename W, int U, int kMost>
+__global__ void __launch_bounds__(kMost) norm_forward_kernel(const __grid_constant__ NormArgs g) {
+    __shared__ float sm[64];
+    int turn = 0;
+    pdl_wait();
+    pdl_trigger();
+    const int lanes = g.lanes, t = threadIdx.x % lanes;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / lanes) + threadIdx.x / lanes;
+    const bool there = row < g.rows;
+    float r[U][kUnit];
+    float squares = 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
+        if (n > 0) {
+            load8((const T*)g.x + row * g.x_ld + col, n, g.wide, r[u]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) r[u][i] = 0.0f;
+        }
+    }
+    if (g.residual) {
+        float e[U][kUnit];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
+            if (n > 0) load8((const T*)g.residual + row * g.residual_ld + col, n, g.wide, e[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int n = there ? g.width - (u * lanes + t) * kUnit : 0;
+            if (n > 0) {
+                // what is kept is what is normalised
+#pragma unroll
+                for (int i = 0; i < kUnit; i++) r[u][i] = to_float(from_float<T>(r[u][i] + e[u][i]));
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
+        if (g.sum && n > 0) store8((T*)g.sum + row * g.sum_ld + col, n, g.wide, r[u]);
+#pragma unroll
+        for (int i = 0; i < kUnit; i++) squares = fmaf(r[u][i], r[u][i], squares);
+    }
+    squares = over_row<RowSum>(squares, lanes, sm, turn);
+    float rstd = 1.0f / sqrtf(squares / g.width + g.eps);
+    const bool big = !(squares < 1e38f);
+    if (lanes <= 32 ? __any_sync(kAllLanes, big) : big) {
+        // squares that 32 bits do not hold: once more, scaled.  All threads that reduce together take the same way.
+        float most = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) most = RowMax::of(most, fabsf(r[u][i]));
+        most = over_row<RowMax>(most, lanes, sm, turn);
+        const float by = most < INFINITY && most > 0.0f ? exp2f((float)-ilogbf(most)) : 1.0f;
+        float again = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) again = fmaf(r[u][i] * by, r[u][i] * by, again);
+        again = over_row<RowSum>(again, lanes, sm, turn);
+        if (big) rstd = by / sqrtf(again / g.width + g.eps * by * by);
+    }
+    if (g.rstd && there && t == 0) g.rstd[row] = rstd;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
+        if (g.weight && n > 0) {
+            float w[kUnit];
+            load8((const W*)g.weight + col, n, g.weight_wide, w);
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) r[u][i] = i < n ? r[u][i] * rstd * w[i] : 0.0f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) r[u][i] = i < n ? r[u][i] * rstd : 0.0f;
+        }
+        if (g.y && n > 0) store8((T*)g.y + row * g.y_ld + col, n, g.wide, r[u]);
+    }
+    if (!g.y8) return;
+    float row_most = 0.0f;
+    if (!g.block) {
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) row_most = RowMax::of(row_most, fabsf(r[u][i]));
+        row_most = over_row<RowMax>(row_most, lanes, sm, turn);
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
+        float most = row_most;
+        if (g.block) {
+            most = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) most = RowMax::of(most, fabsf(r[u][i]));
+            most = over_lanes<RowMax>(most, min(g.block / kUnit, lanes));
+        }
+        if (n <= 0) continue;
+        if (most < 1e-30f) most = 1e-30f;
+        if (g.block ? col % g.block == 0 : col == 0)
+            g.scales[row * g.scales_ld + (g.block ? col / g.block : 0)] = most / 448.0f;
+        const float by = 448.0f / most;
+        uint2 q;
+        q.x = e4m3x2(r[u][0] * by, r[u][1] * by) | e4m3x2(r[u][2] * by, r[u][3] * by) << 16;
+        q.y = e4m3x2(r[u][4] * by, r[u][5] * by) | e4m3x2(r[u][6] * by, r[u][7] * by) << 16;
+        uint8_t* to = g.y8 + row * g.y8_ld + col;
+        if (g.y8_wide && n >= kUnit) {
+            *reinterpret_cast<uint2*>(to) = q;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kUnit; i++)
+                if (i < n) to[i] = (uint8_t)((i < 4 ? q.x : q.y) >> (i & 3) * 8);
+        }
+    }
+}
+
+template <typename T, typename W, int U, int kMost>
+__global__ void __launch_bounds__(kMost) norm_backward_kernel(const __grid_constant__ NormBackArgs g) {
+    extern __shared__ float partial[];
+    __shared__ float sm[64];
+    int turn = 0;
+    pdl_wait();
+    pdl_trigger();
+    const int lanes = g.lanes, t = threadIdx.x % lanes, together = blockDim.x / lanes;
+    float dw[U][kUnit];
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int i = 0; i < kUnit; i++) dw[u][i] = 0.0f;
+    // all threads of a warp go round equally often
+    for (int64_t row0 = (int64_t)blockIdx.x * together; row0 < g.rows; row0 += (int64_t)gridDim.x * together) {
+        const int64_t row = row0 + threadIdx.x / lanes;
+        const bool there = row < g.rows;
+        const float rstd = there ? g.rstd[row] : 0.0f;
+        float d[U][kUnit], x[U][kUnit];
+        float inner = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
+            if (n > 0) {
+                load8((const T*)g.dy + row * g.dy_ld + col, n, g.wide, d[u]);
+                load8((const T*)g.sum + row * g.sum_ld + col, n, g.wide, x[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kUnit; i++) d[u][i] = x[u][i] = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
+            if (n <= 0) continue;
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) {
+                x[u][i] *= rstd;
+                dw[u][i] = fmaf(d[u][i], x[u][i], dw[u][i]);
+            }
+            if (g.weight) {
+                float w[kUnit];
+                load8((const W*)g.weight + col, n, g.weight_wide, w);
+#pragma unroll
+                for (int i = 0; i < kUnit; i++) d[u][i] *= w[i];
+            }
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) inner = fmaf(d[u][i], x[u][i], inner);
+        }
+        inner = over_row<RowSum>(inner, lanes, sm, turn) / g.width;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
+            if (n <= 0) continue;
+            float more[kUnit];
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) more[i] = 0.0f;
+            if (g.dsum) load8((const T*)g.dsum + row * g.dsum_ld + col, n, g.wide, more);
+#pragma unroll
+            for (int i = 0; i < kUnit; i++) d[u][i] = fmaf(rstd, d[u][i] - x[u][i] * inner, more[i]);
+            store8((T*)g.dx + row * g.dx_ld + col, n, g.wide, d[u]);
+        }
+    }
+    if (!g.parts) return;
+    float* const out = g.parts + (int64_t)blockIdx.x * g.width;
+    if (together == 1) {
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int col = (u * lanes + t) * kUnit;
+            if (col < g.width) store8(out + col, g.width - col, g.width % 4 == 0, dw[u]);
+        }
+        return;
+    }
+    const int columns = U * lanes * kUnit;
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int i = 0; i < kUnit; i++) partial[(threadIdx.x / lanes) * columns + (u * lanes + t) * kUnit + i] = dw[u][i];
+    __syncthreads();
+    for (int col = threadIdx.x; col < g.width; col += blockDim.x) {
+        float s = 0.0f;
+        for (int i = 0; i < together; i++) s += partial[i * columns + col];
+        out[col] = s;
+    }
+}
+
+// dweight from the CTAs' sums, always added in the same order.
+__global__ void __launch_bounds__(256) norm_weight_kernel(const float* __restrict__ parts, int n, int width,
+                                                          float* __restrict__ dweight) {
+    __shared__ float sm[8][33];
+    pdl_wait();
+    pdl_trigger();
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
+    float s = 0.0f;
+    if (col < width)
+#pragma unroll 8
+        for (int i = y; i < n; i += 8) s += parts[(int64_t)i * width + col];
+    sm[y][x] = s;
+    __syncthreads();
+    if (y == 0 && col < width) {
+        for (int i = 1; i < 8; i++) s += sm[i][x];
+        dweight[col] = s;
+    }
+}
+
+}  // namespace
+
+struct sparbit_norm_plan_s {
+    int width = 0, dtype = 0, weight_dtype = 0, block = 0;
+    float eps = 0.0f;
+    char* work = nullptr;
+    int device = -1;
+    size_t work_bytes() const { return (size_t)kParts * width * sizeof(float); }
+};
+
+namespace {
+
+using Plan = sparbit_norm_plan_s;
+
+// Threads of a row and units of a thread.  Many rows: up to four units, which keeps loads in flight; few: one, which
+// is done soonest.
+struct Shape {
+    int lanes, units, threads;
+};
+Shape shape_of(const Plan* p, size_t rows) {
+    const int all = (p->width + kUnit - 1) / kUnit;
+    Shape s;
+    if (all <= 32) {
+        s.lanes = 4, s.units = 1;
+        while (s.lanes < all) s.lanes *= 2;
+    } else {
+        s.units = rows < 4 * kSms ? (all + kMostThreads - 1) / kMostThreads : std::min(kMostUnits, (all + 31) / 32);
+        if (s.units == 3) s.units = 4;
+        s.lanes = ((all + s.units - 1) / s.units + 31) / 32 * 32;
+    }
+    s.threads = s.lanes <= 32 ? kShared : s.lanes;
+    return s;
+}
+
+// f.operator()<T, W, U, kMost>() for the plan's types, the units of a thread and the most threads of a CTA: 256 leave
+// each the registers for four units.
+template <typename T, typename W, typename Fn>
+int by_shape(const Shape& s, Fn f) {
+    if (s.units == 1) return f.template operator()<T, W, 1, 1024>();
+    if (s.units == 2) return f.template operator()<T, W, 2, 1024>();
+    if (s.threads <= 256) return f.template operator()<T, W, 4, 256>();
+    return f.template operator()<T, W, 4, 1024>();
+}
+template <typename Fn>
+int by_types(const Plan* p, const Shape& s, Fn f) {
+    if (p->dtype == SPARBIT_F32) return by_shape<float, float>(s, f);
+    if (p->dtype == SPARBIT_BF16)
+        return p->weight_dtype == SPARBIT_F32 ? by_shape<__nv_bfloat16, float>(s, f)
+                                              : by_shape<__nv_bfloat16, __nv_bfloat16>(s, f);
+    return p->weight_dtype == SPARBIT_F32 ? by_shape<__half, float>(s, f) : by_shape<__half, __half>(s, f);
+}
+
+Region region(const Plan* p, const void* x, size_t rows, size_t ld) {
+    const size_t es = elem_size(p->dtype);
+    return Region{x, rows, p->width * es, ld * es};
+}
+
+}  // namespace
+
+extern "C" {
+
+int sparbit_norm_plan_create(size_t width, int dtype, int weight_dtype, float eps, int block, sparbit_norm_plan_t** out) {
+    if (!out) return SPARBIT_ERR_ARG;
+    *out = nullptr;
+    if (width < 1 || !known_dtype(dtype) || (weight_dtype != SPARBIT_F32 && weight_dtype != dtype) || !(eps >= 1e-30f) ||
+        !isfinite(eps))
+        return SPARBIT_ERR_ARG;
+    if (block != 0 && block != 32 && block != 64 && block != 128 && block != 256) return SPARBIT_ERR_ARG;
+    if (width > SPARBIT_NORM_MAX_WIDTH) return SPARBIT_ERR_LIMIT;
+    Plan* p = new (std::nothrow) Plan();
+    if (!p) return SPARBIT_ERR_NOMEM;
+    p->width = (int)width, p->dtype = dtype, p->weight_dtype = weight_dtype, p->eps = eps, p->block = block;
+    *out = p;
+    return SPARBIT_OK;
+}
+
+int sparbit_norm_plan_destroy(sparbit_norm_plan_t* p) {
+    delete p;
+    return SPARBIT_OK;
+}
+
+size_t sparbit_norm_plan_workspace_bytes(const sparbit_norm_plan_t* p) { return p ? p->work_bytes() : 0; }
+
+int sparbit_norm_plan_set_workspace(sparbit_norm_plan_t* p, void* dev, size_t bytes) {
+    if (!p) return SPARBIT_ERR_ARG;
+    if (!dev || bytes < p->work_bytes() || (uintptr_t)dev % 16) return SPARBIT_ERR_WORKSPACE;
+    p->work = nullptr;
+    CU(cudaGetDevice(&p->device));
+    p->work = (char*)dev;
+    return SPARBIT_OK;
+}
+
+int sparbit_norm_forward(sparbit_norm_plan_t* p, size_t rows, const void* x, size_t x_ld, const void* residual,
+                         size_t residual_ld, const void* weight, void* sum, size_t sum_ld, void* y, size_t y_ld, void* y8,
+                         size_t y8_ld, float* scales, float* rstd, void* stream) {
+    if (!p || !y8 != !scales) return SPARBIT_ERR_ARG;
+    if (rows == 0) return SPARBIT_OK;
+    const size_t w = p->width, es = elem_size(p->dtype), ws = elem_size(p->weight_dtype);
+    if (!x) return SPARBIT_ERR_ARG;
+    if (rows > 0x7fffffffu) return SPARBIT_ERR_LIMIT;
+    if (bad_pitch(x_ld, w, rows) || (residual && bad_pitch(residual_ld, w, rows)) || (sum && bad_pitch(sum_ld, w, rows)) ||
+        (y && bad_pitch(y_ld, w, rows)) || (y8 && bad_pitch(y8_ld, w, rows)))
+        return SPARBIT_ERR_ARG;
+    const size_t per_row = p->block ? (w + p->block - 1) / p->block : 1;
+    const Region rx = region(p, x, rows, x_ld), rr = region(p, residual, rows, residual_ld), rw{weight, 1, w * ws, 0},
+                 rs = region(p, sum, rows, sum_ld), ry = region(p, y, rows, y_ld), r8{y8, rows, w, y8_ld},
+                 rc{scales, 1, rows * per_row * 4, 0}, rt{rstd, 1, rows * 4, 0};
+    const Region outs[] = {rs, ry, r8, rc, rt};
+    for (int i = 0; i < 5; i++) {
+        if (regions_overlap(outs[i], rw)) return SPARBIT_ERR_ALIAS;
+        if (!(i == 0 && sum == x && sum_ld == x_ld) && regions_overlap(outs[i], rx)) return SPARBIT_ERR_ALIAS;
+        if (!(i == 0 && sum == residual && sum_ld == residual_ld) && regions_overlap(outs[i], rr)) return SPARBIT_ERR_ALIAS;
+        for (int j = 0; j < i; j++)
+            if (regions_overlap(outs[i], outs[j])) return SPARBIT_ERR_ALIAS;
+    }
+    if (!sum && !y && !y8 && !rstd) return SPARBIT_OK;
+    NormArgs g = {};
+    g.x = x, g.residual = residual, g.weight = weight, g.sum = sum, g.y = y, g.y8 = (uint8_t*)y8;
+    g.scales = scales, g.rstd = rstd;
+    g.x_ld = (int64_t)x_ld, g.residual_ld = (int64_t)residual_ld, g.sum_ld = (int64_t)sum_ld, g.y_ld = (int64_t)y_ld;
+    g.y8_ld = (int64_t)y8_ld;
+    g.rows = (int64_t)rows, g.width = (int)w;
+    const uintptr_t bits = (uintptr_t)x | x_ld * es | (residual ? (uintptr_t)residual | residual_ld * es : 0) |
+                           (sum ? (uintptr_t)sum | sum_ld * es : 0) | (y ? (uintptr_t)y | y_ld * es : 0);
+    g.wide = bits % 16 == 0;
+    g.weight_wide = (uintptr_t)weight % 16 == 0;
+    g.y8_wide = ((uintptr_t)y8 | y8_ld) % 8 == 0;
+    g.block = p->block, g.scales_ld = (int)per_row, g.eps = p->eps;
+    const Shape s = shape_of(p, rows);
+    g.lanes = s.lanes;
+    const unsigned together = s.threads / s.lanes;
+    return by_types(p, s, [&]<typename T, typename W, int U, int kMost>() {
+        CU(launch(norm_forward_kernel<T, W, U, kMost>, dim3((unsigned)((rows + together - 1) / together)), dim3(s.threads), 0,
+                  (cudaStream_t)stream, g));
+        return (int)SPARBIT_OK;
+    });
+}
+
+int sparbit_norm_backward(sparbit_norm_plan_t* p, size_t rows, const void* dy, size_t dy_ld, const void* sum,
+                          size_t sum_ld, const void* weight, const float* rstd, const void* dsum, size_t dsum_ld, void* dx,
+                          size_t dx_ld, float* dweight, void* stream) {
+    if (!p) return SPARBIT_ERR_ARG;
+    const size_t w = p->width, es = elem_size(p->dtype), ws = elem_size(p->weight_dtype);
+    if (rows && (!dy || !sum || !rstd || !dx)) return SPARBIT_ERR_ARG;
+    if (rows > 0x7fffffffu) return SPARBIT_ERR_LIMIT;
+    if (bad_pitch(dy_ld, w, rows) || bad_pitch(sum_ld, w, rows) || bad_pitch(dx_ld, w, rows) ||
+        (dsum && bad_pitch(dsum_ld, w, rows)))
+        return SPARBIT_ERR_ARG;
+    const Region ry = region(p, dy, rows, dy_ld), rs = region(p, sum, rows, sum_ld), rw{weight, 1, w * ws, 0},
+                 rt{rstd, 1, rows * 4, 0}, rd = region(p, dsum, rows, dsum_ld), rx = region(p, dx, rows, dx_ld),
+                 rg{dweight, 1, w * 4, 0}, rk{p->work, 1, p->work_bytes(), 0};
+    for (const Region& in : {rs, rw, rt, rk})
+        if (regions_overlap(rx, in) || regions_overlap(rg, in)) return SPARBIT_ERR_ALIAS;
+    if ((!(dx == dy && dx_ld == dy_ld) && regions_overlap(rx, ry)) || (!(dx == dsum && dx_ld == dsum_ld) && regions_overlap(rx, rd)) ||
+        regions_overlap(rg, ry) || regions_overlap(rg, rd) || regions_overlap(rg, rx))
+        return SPARBIT_ERR_ALIAS;
+    if (dweight) {
+        if (!p->work) return SPARBIT_ERR_WORKSPACE;
+        int cur = -1;
+        CU(cudaGetDevice(&cur));
+        if (cur != p->device) return SPARBIT_ERR_ARG;
+    }
+    NormBackArgs g = {};
+    g.dy = dy, g.sum = sum, g.weight = weight, g.dsum = dsum, g.rstd = rstd, g.dx = dx;
+    g.parts = dweight ? (float*)p->work : nullptr;
+    g.dy_ld = (int64_t)dy_ld, g.sum_ld = (int64_t)sum_ld, g.dsum_ld = (int64_t)dsum_ld, g.dx_ld = (int64_t)dx_ld;
+    g.rows = (int64_t)rows, g.width = (int)w;
+    const uintptr_t bits = (uintptr_t)dy | dy_ld * es | (uintptr_t)sum | sum_ld * es | (uintptr_t)dx | dx_ld * es |
+                           (dsum ? (uintptr_t)dsum | dsum_ld * es : 0);
+    g.wide = bits % 16 == 0;
+    g.weight_wide = (uintptr_t)weight % 16 == 0;
+    const Shape s = shape_of(p, rows);
+    g.lanes = s.lanes;
+    const size_t together = s.threads / s.lanes;
+    const int grid = (int)std::min<size_t>(kParts, (rows + together - 1) / together);
+    if (grid > 0) {
+        const size_t smem = together > 1 ? sizeof(float) * s.threads * s.units * kUnit : 0;
+        const int e = by_types(p, s, [&]<typename T, typename W, int U, int kMost>() {
+            CU(launch(norm_backward_kernel<T, W, U, kMost>, dim3(grid), dim3(s.threads), smem, (cudaStream_t)stream, g));
+            return (int)SPARBIT_OK;
+        });
+        if (e != SPARBIT_OK) return e;
+    }
+    if (dweight)
+        CU(launch(norm_weight_kernel, dim3((unsigned)((w + 31) / 32)), dim3(256), 0, (cudaStream_t)stream,
+                  (const float*)p->work, grid, (int)w, dweight));
+    return SPARBIT_OK;
+}
+
+}  // extern "C"

@@ -16,6 +16,7 @@ from .binding import _ptr as _address
 F32, BF16, F16 = range(3)
 PRODUCTS_AUTO, PRODUCTS_ONE, PRODUCTS_THREE = 0, 1, 3
 ROUTER_MAX_EXPERTS, ROUTER_MAX_K = 1024, 32
+LINEAR_ATTENTION_MAX_SIZE, NORM_MAX_WIDTH = 128, 32768
 
 _f = ctypes.c_float
 _ps = ctypes.POINTER(_sz)
@@ -60,6 +61,31 @@ SYMBOLS = {
     "sparbit_router_forward": (_i, [_vp, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "sparbit_router_balance": (_i, [_vp, _vp, _i, _vp, _f, _f, _vp, _vp]),
     "sparbit_router_backward": (_i, [_vp, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _i, _vp, _f, _f, _vp, _vp, _sz, _vp]),
+    "sparbit_linear_attention_plan_create": (_i, [_i, _ps, _i, _i, _i, _i, _f, _pp]),
+    "sparbit_linear_attention_plan_destroy": (_i, [_vp]),
+    "sparbit_linear_attention_plan_workspace_bytes": (_sz, [_vp]),
+    "sparbit_linear_attention_plan_set_workspace": (_i, [_vp, _vp, _sz]),
+    "sparbit_linear_attention_plan_status": (_i, [_vp]),
+    "sparbit_linear_attention_plan_set_wait_test": (_i, [_vp, _i, ctypes.c_uint64]),
+    "sparbit_linear_attention_forward": (_i, [_vp, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _vp, _sz, _vp, _vp]),
+    "sparbit_linear_attention_backward": (_i, [_vp, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _vp, _sz, _vp, _vp, _sz, _vp,
+                                               _sz, _vp, _sz, _vp, _vp]),
+    "sparbit_linear_attention_step": (_i, [_sz, _i, _i, _i, _i, _f, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _sz, _vp, _vp,
+                                           _vp, _sz, _vp]),
+    "sparbit_linear_attention_join": (_i, [_i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _i, _vp]),
+    "sparbit_norm_plan_create": (_i, [_sz, _i, _i, _f, _i, _pp]),
+    "sparbit_norm_plan_destroy": (_i, [_vp]),
+    "sparbit_norm_plan_workspace_bytes": (_sz, [_vp]),
+    "sparbit_norm_plan_set_workspace": (_i, [_vp, _vp, _sz]),
+    "sparbit_norm_forward": (_i, [_vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _vp]),
+    "sparbit_norm_backward": (_i, [_vp, _sz, _vp, _sz, _vp, _sz, _vp, _vp, _vp, _sz, _vp, _sz, _vp, _vp]),
+    "sparbit_clip_plan_create": (_i, [_i, _sz, _ps, ctypes.POINTER(_i), ctypes.POINTER(_i), _pp]),
+    "sparbit_clip_plan_destroy": (_i, [_vp]),
+    "sparbit_clip_plan_workspace_bytes": (_sz, [_vp]),
+    "sparbit_clip_plan_set_workspace": (_i, [_vp, _vp, _sz]),
+    "sparbit_clip_plan_set_tensors": (_i, [_vp, _pp, _pp]),
+    "sparbit_clip_sums": (_i, [_vp, _vp, _vp]),
+    "sparbit_clip_scale": (_i, [_vp, _vp, _i, _f, _f, _vp, _vp]),
 }
 for _name, (_res, _args) in SYMBOLS.items():
     _fn = getattr(lib, _name)  # AttributeError here means the library does not match the header
@@ -80,10 +106,11 @@ _scan_step, _router_forward = _words("sparbit_scan_step"), _words("sparbit_route
 # What a tensor has to be: device memory of the type that the kernels read, and without gaps where no row stride is
 # given.  The calls below can be shorter than their own marshalling (a token's step takes the GPU 3 us), so the common
 # cases come first, and the two shortest calls look at all their tensors in one go.
-_I32, _BYTE = 3, 4
-_NAMES = {F32: "float32", BF16: "bfloat16", F16: "float16", _I32: "int32", _BYTE: "uint8 or bool"}
+_I32, _BYTE, _F64, _E4M3 = 3, 4, 5, 6
+_NAMES = {F32: "float32", BF16: "bfloat16", F16: "float16", _I32: "int32", _BYTE: "uint8 or bool", _F64: "float64",
+          _E4M3: "float8_e4m3fn or uint8"}
 _KNOWN = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16, "torch.int32": _I32, "torch.uint8": _BYTE,
-          "torch.int8": _BYTE, "torch.bool": _BYTE}
+          "torch.int8": _BYTE, "torch.bool": _BYTE, "torch.float64": _F64, "torch.float8_e4m3fn": _E4M3}
 _codes = {}  # of the torch types met so far
 _types = {}  # and the other way round
 
@@ -106,7 +133,7 @@ def _address_checked(x, code):
     dtype = str(x.dtype)
     met = _codes[x.dtype] = _KNOWN.get(dtype, -1)
     _types[met] = x.dtype
-    if code is not None and met != code:
+    if code is not None and met != code and not (code == _E4M3 and dtype == "torch.uint8"):
         raise TypeError(f"a tensor of {_NAMES.get(code, code)} is wanted, not of {dtype}")
     if not (x.is_cuda or x.is_pinned()):
         raise TypeError("a tensor on the GPU is wanted")
@@ -381,3 +408,128 @@ class OrthoPlan(_TrainPlan):
                         _address_of(weight_out, weight_dtype), wl, r * wl if weight_stride is None else weight_stride,
                         weight_dtype, int(bool(nesterov)), lr, momentum, weight_decay, scale)
         _check(lib.sparbit_muon_step(self._h, ctypes.byref(args), _stream_handle(stream)), "sparbit_muon_step")
+
+
+class LinearAttentionPlan(_TrainPlan):
+    """Linear attention with a decay for each head over sequences of the given lengths
+    (sparbit_linear_attention_plan_create).  scale: key_size ** -0.5 where it is None.  Row strides default to heads *
+    size; a tensor of [rows][heads][size] that is part of a wider one needs its own."""
+
+    _kind = "linear_attention"
+
+    def __init__(self, lengths, heads: int, key_size: int, value_size: int, dtype: int = BF16, scale=None):
+        n, arr = _counts(lengths)
+        self.scale = key_size ** -0.5 if scale is None and key_size > 0 else 1.0 if scale is None else float(scale)
+        self._create(n, arr, heads, key_size, value_size, dtype, self.scale)
+        self.heads, self.key_size, self.value_size, self.dtype = heads, key_size, value_size, dtype
+
+    def forward(self, q, k, v, log_decay, o, first=None, summary=None, stream=None, q_ld=None, k_ld=None, v_ld=None,
+                o_ld=None) -> None:
+        t, wk, wv = self.dtype, self.heads * self.key_size, self.heads * self.value_size
+        _check(lib.sparbit_linear_attention_forward(
+            self._h, _address_of(q, t), _stride_of(q, q_ld, wk), _address_of(k, t), _stride_of(k, k_ld, wk),
+            _address_of(v, t), _stride_of(v, v_ld, wv), _flat(log_decay, F32), _flat(first, F32), _address_of(o, t),
+            _stride_of(o, o_ld, wv), _flat(summary, F32), _stream_handle(stream)), "sparbit_linear_attention_forward")
+
+    def backward(self, q, k, v, log_decay, do, dq, dk, dv, first=None, dlast=None, dsummary=None, stream=None, q_ld=None,
+                 k_ld=None, v_ld=None, do_ld=None, dq_ld=None, dk_ld=None, dv_ld=None) -> None:
+        t, wk, wv = self.dtype, self.heads * self.key_size, self.heads * self.value_size
+        _check(lib.sparbit_linear_attention_backward(
+            self._h, _address_of(q, t), _stride_of(q, q_ld, wk), _address_of(k, t), _stride_of(k, k_ld, wk),
+            _address_of(v, t), _stride_of(v, v_ld, wv), _flat(log_decay, F32), _flat(first, F32), _address_of(do, t),
+            _stride_of(do, do_ld, wv), _flat(dlast, F32), _address_of(dq, t), _stride_of(dq, dq_ld, wk),
+            _address_of(dk, t), _stride_of(dk, dk_ld, wk), _address_of(dv, t), _stride_of(dv, dv_ld, wv),
+            _flat(dsummary, F32), _stream_handle(stream)), "sparbit_linear_attention_backward")
+
+
+def linear_attention_step(rows: int, heads: int, key_size: int, value_size: int, dtype: int, q, k, v, log_decay, state_in,
+                          state_out, o, scale=None, slots=None, n_slots=None, stream=None, q_ld=None, k_ld=None,
+                          v_ld=None, o_ld=None) -> None:
+    """One token for each of `rows` running sequences; n_slots defaults to `rows`, scale to key_size ** -0.5."""
+    wk, wv = heads * key_size, heads * value_size
+    code = lib.sparbit_linear_attention_step(
+        rows, heads, key_size, value_size, dtype, key_size ** -0.5 if scale is None else scale,
+        _address_of(q, dtype), wk if q_ld is None and _dense(q) else q_ld,
+        _address_of(k, dtype), wk if k_ld is None and _dense(k) else k_ld,
+        _address_of(v, dtype), wv if v_ld is None and _dense(v) else v_ld, _flat(log_decay, F32), _flat(slots, _I32),
+        rows if n_slots is None else n_slots, _flat(state_in, F32), _flat(state_out, F32), _address_of(o, dtype),
+        wv if o_ld is None and _dense(o) else o_ld, _stream_handle(stream))
+    if code != OK:
+        raise SparbitError(code, "sparbit_linear_attention_step")
+
+
+def linear_attention_join(P: int, heads: int, key_size: int, value_size: int, gathered, out, first=None,
+                          reverse: bool = False, first_rank: int = 0, n_ranks=None, stream=None) -> None:
+    """First states of the slices first_rank .. first_rank + n_ranks - 1 (default: all P)."""
+    _check(lib.sparbit_linear_attention_join(P, first_rank, P if n_ranks is None else n_ranks, heads, key_size,
+                                             value_size, _flat(gathered, F32), _flat(first, F32), _flat(out, F32),
+                                             int(bool(reverse)), _stream_handle(stream)),
+           "sparbit_linear_attention_join")
+
+
+class NormPlan(_TrainPlan):
+    """Root-mean-square norm of rows of `width` elements (sparbit_norm_plan_create).  block: columns of a scale of the
+    8-bit rows, 0 = one scale a row; weight_dtype defaults to dtype.  Only `backward` needs the workspace."""
+
+    _kind = "norm"
+
+    def __init__(self, width: int, dtype: int = BF16, weight_dtype=None, eps: float = 1e-6, block: int = 0):
+        weight_dtype = dtype if weight_dtype is None else weight_dtype
+        self._create(width, dtype, weight_dtype, eps, block)
+        self.width, self.dtype, self.weight_dtype = width, dtype, weight_dtype
+
+    def forward(self, rows: int, x, weight=None, residual=None, sum=None, y=None, y8=None, scales=None, rstd=None,
+                stream=None, x_ld=None, residual_ld=None, sum_ld=None, y_ld=None, y8_ld=None) -> None:
+        w, t = self.width, self.dtype
+        code = lib.sparbit_norm_forward(
+            self._h, rows, _address_of(x, t), _stride_of(x, x_ld, w), _address_of(residual, t),
+            _stride_of(residual, residual_ld, w), _flat(weight, self.weight_dtype), _address_of(sum, t),
+            _stride_of(sum, sum_ld, w), _address_of(y, t), _stride_of(y, y_ld, w), _address_of(y8, _E4M3),
+            _stride_of(y8, y8_ld, w), _flat(scales, F32), _flat(rstd, F32), _stream_handle(stream))
+        if code != OK:
+            raise SparbitError(code, "sparbit_norm_forward")
+
+    def backward(self, rows: int, dy, sum, weight, rstd, dx, dweight=None, dsum=None, stream=None, dy_ld=None,
+                 sum_ld=None, dx_ld=None, dsum_ld=None) -> None:
+        w, t = self.width, self.dtype
+        _check(lib.sparbit_norm_backward(
+            self._h, rows, _address_of(dy, t), _stride_of(dy, dy_ld, w), _address_of(sum, t), _stride_of(sum, sum_ld, w),
+            _flat(weight, self.weight_dtype), _flat(rstd, F32), _address_of(dsum, t), _stride_of(dsum, dsum_ld, w),
+            _address_of(dx, t), _stride_of(dx, dx_ld, w), _flat(dweight, F32), _stream_handle(stream)),
+            "sparbit_norm_backward")
+
+
+class ClipPlan(_TrainPlan):
+    """Norm of all gradients and their clipping (sparbit_clip_plan_create): tensors of the given lengths (in elements) and
+    types, each owned by one of n_ranks virtual ranks (all by rank 0 where `ranks` is None)."""
+
+    _kind = "clip"
+
+    def __init__(self, lengths, dtypes, ranks=None, n_ranks: int = 1):
+        n, arr = _counts(lengths)
+        self.dtypes = [int(d) for d in dtypes]
+        if len(self.dtypes) != n or (ranks is not None and len(ranks) != n):
+            raise ValueError("lengths, dtypes and ranks belong together")
+        owners = None if ranks is None else (_i * n)(*[int(r) for r in ranks])
+        self._create(n_ranks, n, arr, (_i * n)(*self.dtypes), owners)
+
+    def set_tensors(self, tensors, out=None) -> None:
+        """The tensors that are summed, and those that get the clipped elements (the same ones: in place; None: only
+        sums and norms are wanted).  Synchronises."""
+        kept, addresses = [], []
+        for given in (tensors, out):
+            given = None if given is None else list(given)
+            if given is not None and len(given) != len(self.dtypes):
+                raise ValueError(f"{len(self.dtypes)} tensors are wanted, not {len(given)}")
+            kept.append(given)
+            addresses.append(None if given is None else (_vp * len(given))(
+                *[_flat(x, t) for x, t in zip(given, self.dtypes)]))
+        _check(lib.sparbit_clip_plan_set_tensors(self._h, addresses[0], addresses[1]), "sparbit_clip_plan_set_tensors")
+        self._tensors = kept  # keep the owners alive
+
+    def sums(self, sums, stream=None) -> None:
+        _check(lib.sparbit_clip_sums(self._h, _flat(sums, _F64), _stream_handle(stream)), "sparbit_clip_sums")
+
+    def scale(self, gathered, G: int, most: float, norms, eps: float = 1e-6, stream=None) -> None:
+        _check(lib.sparbit_clip_scale(self._h, _flat(gathered, _F64), G, most, eps, _flat(norms, F32),
+                                      _stream_handle(stream)), "sparbit_clip_scale")
