@@ -15,8 +15,8 @@
 // Sequences that are too few to fill the GPU are cut into segments: one launch leaves what each segment adds to a
 // state, a fold along the segments makes of it the state that enters each, and the main launch follows.  The
 // same three steps, with an allgather in the middle, are what ranks do that hold slices of a sequence.
+#include <cuda.h>
 #include <math.h>
-#include <string.h>
 
 #include <algorithm>
 #include <new>
@@ -59,6 +59,12 @@ struct Pass {
     int k_step, v_step;
     int in_by_segment, out_by_segment;  // units are segments, not sequences
     int skip_ends;             // what the last segment of a sequence adds is not wanted
+    int tiled;                 // whole chunks are copied by the maps
+};
+
+// Tensors as rows x (heads x size), in boxes of a chunk x 64 elements.
+struct alignas(64) Maps {
+    CUtensorMap a[3], b[3], c[3];  // of the passes
 };
 
 struct Args {
@@ -120,12 +126,42 @@ __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ void tmem_store8(uint32_t addr, const uint32_t (&r)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(r[0]),
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// The same for 16 lanes, laid out as the matrices of ldmatrix and stmatrix: a lane has two neighbouring columns of 32
+// bits (one of them in the store, of two 16-bit numbers) of rows lane / 4 and lane / 4 + 8.
+__device__ __forceinline__ void tmem_load_16x32(uint32_t addr, float* z) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; i++) z[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_store_16x16(uint32_t addr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(r[0]),
                  "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
-__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(r))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long&>(r))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)),
+          "l"(reinterpret_cast<unsigned long long&>(c)));
+    return r;
+}
 // D += A B of one CTA: both operands in shared memory, or A in tensor memory.
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
@@ -140,6 +176,13 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
         "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
         : "memory");
+}
+// A box of 128 rows x 64 elements into a panel.
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
+                     dst),
+                 "l"(map), "r"(bar), "r"(x), "r"(y)
+                 : "memory");
 }
 // Arrives at the barrier once the products issued so far are done.
 __device__ __forceinline__ void mma_done(uint32_t bar) {
@@ -158,9 +201,22 @@ template <>
 struct Bits<__nv_bfloat16> {
     static constexpr bool kScaled = false;  // the exponents of 32 bits: nothing to scale
     static constexpr int kParts = 3;        // parts that hold a number of 32 bits
-    static constexpr uint32_t kFormat = (1u << 7) | (1u << 10), kExponent = 0x7f80u;
+    static constexpr uint32_t kFormat = (1u << 7) | (1u << 10);
+    // The leading 8 bits of two numbers, which are then without them: three of these hold all 24 bits.
+    static __device__ __forceinline__ uint32_t take(float2& x) {
+        const uint32_t a = __float_as_uint(x.x), b = __float_as_uint(x.y);
+        x = fma2(make_float2(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u)), make_float2(-1.0f, -1.0f), x);
+        return __byte_perm(a, b, 0x7632);
+    }
+    static __device__ __forceinline__ bool is_odd(uint32_t v) { return (v & 0x7fffu) >= 0x7f80u || (v >> 16 & 0x7fffu) >= 0x7f80u; }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+    // larger of the magnitudes of two pairs, a NaN being larger than everything
+    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
+        const __nv_bfloat162 v = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a),
+                                             __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
         return *reinterpret_cast<const uint32_t*>(&v);
     }
     static __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
@@ -170,9 +226,20 @@ template <>
 struct Bits<__half> {
     static constexpr bool kScaled = true;
     static constexpr int kParts = 2;
-    static constexpr uint32_t kFormat = 0, kExponent = 0x7c00u;
+    static constexpr uint32_t kFormat = 0;
+    // The leading 11 bits, rounded: two of these hold 22 bits and a sign.
+    static __device__ __forceinline__ uint32_t take(float2& x) {
+        const uint32_t v = pack(x.x, x.y);
+        x = fma2(make_float2(low(v), high(v)), make_float2(-1.0f, -1.0f), x);
+        return v;
+    }
+    static __device__ __forceinline__ bool is_odd(uint32_t v) { return (v & 0x7fffu) >= 0x7c00u || (v >> 16 & 0x7fffu) >= 0x7c00u; }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
+        const __half2 v = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), __habs2(*reinterpret_cast<const __half2*>(&b)));
         return *reinterpret_cast<const uint32_t*>(&v);
     }
     static __device__ __forceinline__ float low(uint32_t v) { return __half2float(__ushort_as_half((unsigned short)v)); }
@@ -189,56 +256,83 @@ __device__ __forceinline__ int exponent_for(float most) {
     const int by = 13 - (e - 127);
     return by > 40 ? 40 : by < -110 ? -110 : by;
 }
+// The largest of the four lanes that share a row of ldmatrix' matrices.
+__device__ __forceinline__ float max_of_row(float v) {
+    v = fmaxf(v, __shfl_xor_sync(kAllLanes, v, 1));
+    return fmaxf(v, __shfl_xor_sync(kAllLanes, v, 2));
+}
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-constexpr int kOutWarps = 4, kStateWarps = 8, kLoadWarps = 4;
-constexpr int kTensorThreads = 32 * (kOutWarps + kStateWarps + kLoadWarps + 1);
+// Warps of a CTA by what they do, in groups of four for tensor memory (whose lanes go by the warp's number mod 4) and
+// for the registers, of which each group gets as many as it needs.
+constexpr int kWeightWarps = 4, kOutWarps = 8, kPartWarps = 4, kStateWarps = 8, kLoadWarps = 2;
+constexpr int kFirstOut = kWeightWarps, kFirstPart = kFirstOut + kOutWarps, kFirstState = kFirstPart + kPartWarps,
+              kFirstLoad = kFirstState + kStateWarps, kMultiply = kFirstLoad + kLoadWarps, kMultiplyState = kMultiply + 1;
+constexpr int kTensorThreads = 32 * (kFirstLoad + 4);
+constexpr int kRegisters = 72, kWeightRegisters = 72, kOutRegisters = 64, kPartRegisters = 56, kStateRegisters = 104,
+              kOtherRegisters = 40;
+static_assert(kWeightRegisters + 2 * kOutRegisters + kPartRegisters + 2 * kStateRegisters + kOtherRegisters <=
+                  kTensorThreads / 128 * kRegisters,
+              "more registers than the CTA has would be waited for without end");
+template <int kCount>
+__device__ __forceinline__ void fewer_registers() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
+}
+template <int kCount>
+__device__ __forceinline__ void more_registers() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
+}
 
-// 128 tokens of one tensor's head into panels of swizzled rows; tokens from n on and columns from `width` on are zero.
-template <int kWide>
-__device__ __forceinline__ void load_tile(uint32_t dst, const char* src, int64_t pitch, int width, int panels, int n, int t) {
-    const int per_row = panels * 8, row0 = t / per_row, piece = t - row0 * per_row;  // 8 or 16 pieces of 16 bytes a row
-    const int step = 128 / per_row;                                                   // a multiple of 8
-    const uint32_t to = dst + (piece >> 3) * kPanel + row0 * 128 + (((piece & 7) ^ (row0 & 7)) << 4);
+// 128 tokens of one tensor's head into panels of swizzled rows, by one warp; tokens from n on and columns from `width`
+// on are zero.
+template <int kWide, int kPanels>
+__device__ __forceinline__ void load_tile(uint32_t dst, const char* src, int64_t pitch, int width, int n) {
+    constexpr int kPieces = kPanels * 8, kRows = 32 / kPieces;  // 16-byte pieces of a row, rows of an instruction
+    const int lane = threadIdx.x & 31, row0 = lane / kPieces, piece = lane % kPieces;
+    const uint32_t to = dst + (piece >> 3) * kPanel + row0 * 128;
     const char* from = src + row0 * pitch + piece * 16;
     const int left = (width - piece * 8) * 2;  // bytes of this piece that the row has
-#pragma unroll 8
-    for (int i = 0; i < kChunk / 8; i++) {
-        if (i * step >= kChunk) break;
-        const int row = row0 + i * step;
-        if constexpr (kWide == 16) {
-            const int bytes = row < n && left > 0 ? 16 : 0;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * step * 128),
-                         "l"(bytes ? from + i * step * pitch : src), "r"(bytes)
-                         : "memory");
-        } else if constexpr (kWide >= 4) {
+    for (int m = 0; m < kChunk; m += 8) {
 #pragma unroll
-            for (int k = 0; k < 16; k += kWide) {
-                const int bytes = row < n && left > k ? kWide : 0;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to + i * step * 128 + k),
-                             "l"(bytes ? from + i * step * pitch + k : src), "n"(kWide), "r"(bytes)
+        for (int y = 0; y < 8; y += kRows, from += kRows * pitch) {
+            const int row = m + row0 + y;
+            const uint32_t at = to + (m + y) * 128 + (((piece & 7) ^ (row0 + y)) << 4);
+            if constexpr (kWide == 16) {
+                const int bytes = row < n && left > 0 ? 16 : 0;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(bytes ? from : src), "r"(bytes)
+                             : "memory");
+            } else if constexpr (kWide >= 4) {
+#pragma unroll
+                for (int k = 0; k < 16; k += kWide) {
+                    const int bytes = row < n && left > k ? kWide : 0;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(at + k),
+                                 "l"(bytes ? from + k : src), "n"(kWide), "r"(bytes)
+                                 : "memory");
+                }
+            } else {
+                uint32_t v[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const unsigned short* p = reinterpret_cast<const unsigned short*>(from + k * 4);
+                    v[k] = row < n && left > k * 4 ? p[0] : 0u;
+                    if (row < n && left > k * 4 + 2) v[k] |= (uint32_t)p[1] << 16;
+                }
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
                              : "memory");
             }
-        } else {
-            uint32_t v[4];
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const unsigned short* p = reinterpret_cast<const unsigned short*>(from + i * step * pitch + k * 4);
-                v[k] = row < n && left > k * 4 ? p[0] : 0u;
-                if (row < n && left > k * 4 + 2) v[k] |= (uint32_t)p[1] << 16;
-            }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + i * step * 128), "r"(v[0]), "r"(v[1]),
-                         "r"(v[2]), "r"(v[3])
-                         : "memory");
         }
     }
 }
-__device__ __forceinline__ void load_any(int wide, uint32_t dst, const char* src, int64_t pitch, int width, int panels, int n,
-                                         int t) {
-    if (wide == 16) load_tile<16>(dst, src, pitch, width, panels, n, t);
-    else if (wide == 8) load_tile<8>(dst, src, pitch, width, panels, n, t);
-    else if (wide == 4) load_tile<4>(dst, src, pitch, width, panels, n, t);
-    else load_tile<2>(dst, src, pitch, width, panels, n, t);
+template <int kPanels>
+__device__ __forceinline__ void load_wide(int wide, uint32_t dst, const char* src, int64_t pitch, int width, int n) {
+    if (wide == 16) load_tile<16, kPanels>(dst, src, pitch, width, n);
+    else if (wide == 8) load_tile<8, kPanels>(dst, src, pitch, width, n);
+    else if (wide == 4) load_tile<4, kPanels>(dst, src, pitch, width, n);
+    else load_tile<2, kPanels>(dst, src, pitch, width, n);
+}
+__device__ __forceinline__ void load_any(int wide, uint32_t dst, const char* src, int64_t pitch, int width, int n) {
+    if (width <= 64) load_wide<1>(wide, dst, src, pitch, width, n);
+    else load_wide<2>(wide, dst, src, pitch, width, n);
 }
 
 // What a CTA is working on.
@@ -259,13 +353,15 @@ __device__ __forceinline__ Work work_of(const Args& g, int w) {
     k.l2 = log2_decay(g.log_decay, k.head);
     return k;
 }
-// First token of a chunk and the way to the next ones, in the order of the pass.
-__device__ __forceinline__ int64_t first_row(const Work& k, int chunk) {
-    return k.p->reverse ? k.s.row0 + k.s.len - 1 - (int64_t)chunk * kChunk : k.s.row0 + (int64_t)chunk * kChunk;
-}
+// A chunk's tokens lie in shared and tensor memory in the order of time; a pass against time goes through the chunks
+// from the last to the first, of which the first is the one that may have fewer.
 __device__ __forceinline__ int tokens_of(const Work& k, int chunk) {
     const int left = k.s.len - chunk * kChunk;
     return left < kChunk ? left : kChunk;
+}
+__device__ __forceinline__ int64_t first_row(const Work& k, int chunk) {
+    const int at = chunk * kChunk;
+    return k.s.row0 + (k.p->reverse ? k.s.len - at - tokens_of(k, chunk) : at);
 }
 // Where a state goes; null where this segment leaves none.
 __device__ __forceinline__ float* state_out(const Work& k) {
@@ -285,105 +381,193 @@ __device__ __forceinline__ void decay_out(const Work& k, const float* log_decay)
             k.s.seq_len ? (float)exp((double)log_decay[k.head] * (double)k.s.seq_len) : 1.0f;
 }
 
-// One CTA per SM, its warps in four roles: four write out (a token each lane), eight hold the state (a value each lane,
-// half of the keys a warp), four load, one issues products.  A chunk is
+// Shared memory: a ring of chunks and Z, then these.
+constexpr int kMostStages = 4;
+constexpr uint32_t kRing = 14 * kPanel;
+struct Tables {
+    uint64_t full[kMostStages], empty[kMostStages], used[kMostStages], scored, scaled, weighted, entered, done, c_ready[2], c_free[2], added,
+        add_free, z_ready, out_free, met;
+    uint32_t tmem, gave_up;
+    uint32_t bad[2];  // number of the last (every other) chunk whose c holds an infinity or a NaN
+    alignas(16) float left[kChunk];           // what a token's part is worth at the end of the chunk
+    // for each warp d^31 .. d^0 (against time d^0 .. d^31), between numbers that are finite
+    alignas(16) float powers[32 * (kWeightWarps + 2)];
+    // fp16: powers of two that rows of Z, of the weights and of c^T are held times
+    alignas(4) signed char z_exp[2][kMostSize], w_exp[2][kChunk], c_exp[2][kMostSize];
+};
+constexpr uint32_t kTensorSmem = kRing + sizeof(Tables);
+static_assert(kTensorSmem <= 232448, "shared memory of a CTA");
+
+// 32 columns of a row of out, rounded into shared memory at `own` (the row's; pieces of 16 bytes in swizzled order).
+template <typename B>
+__device__ __forceinline__ void round_out(const uint32_t (&r)[32], float down, uint32_t own, int b, int lane) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) {
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float2 x = make_float2(__uint_as_float(r[j + 2 * i]), __uint_as_float(r[j + 2 * i + 1]));
+            if constexpr (B::kScaled) x = mul2(x, make_float2(down, down));
+            v[i] = B::pack(x.x, x.y);
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(own + (((b * 4 + j / 8) ^ (lane & 7)) << 4)), "r"(v[0]),
+                     "r"(v[1]), "r"(v[2]), "r"(v[3])
+                     : "memory");
+    }
+}
+// The same where c holds an infinity or a NaN, which a product would carry to the tokens in front of it (times their
+// weight of zero): adds the tokens that count for this lane's row one by one.
+template <typename B>
+__device__ __forceinline__ void round_out_by_hand(uint32_t out, uint32_t weights, uint32_t c_tile, int b, int row, bool reverse,
+                                                  float down, uint32_t own) {
+    const int lane = row & 31;
+    uint32_t r[32];
+    tmem_load32(out, r);
+    for (int j = reverse ? row & ~31 : 0; j <= (reverse ? kChunk - 1 : row | 31); j += 2) {
+        uint32_t pair;
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;"
+                     : "=r"(pair)
+                     : "r"(weights + j / 2)
+                     : "memory");
+        for (int i = 0; i < 2; i++) {
+            const int token = j + i;
+            if (reverse ? token < row : token > row) continue;
+            const float weight = i ? B::high(pair) : B::low(pair);
+#pragma unroll
+            for (int x = 0; x < 32; x += 8) {
+                const int col = b * 32 + x;
+                uint32_t u[4];
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                             : "r"(c_tile + (col >> 6) * kPanel + token * 128 + ((((col >> 3) & 7) ^ (token & 7)) << 4)));
+#pragma unroll
+                for (int y = 0; y < 8; y++) {
+                    const float value = y & 1 ? B::high(u[y / 2]) : B::low(u[y / 2]);
+                    r[x + y] = __float_as_uint(fmaf(weight, value, __uint_as_float(r[x + y])));
+                }
+            }
+        }
+        __syncwarp();
+    }
+    round_out<B>(r, down, own, b, lane);
+}
+
+// One CTA per SM, its warps in roles: weights, output, parts of c, state, loads, products.  A chunk is
 //   score = a b^T;  its weights W = intra d^(i - j) score, causal, rounded to 16 bits into tensor memory
 //   out = a Z (Z rounded to 16 bits in shared memory), scaled by row in tensor memory, + W c
 //   add = (c times gain d^(n - e - j))^T b, the scaled c in two or three 16-bit parts that hold its 32 bits
-// with Z in registers and the three chains side by side.  W and Z are the only roundings to 16 bits on the way:
+// with Z in registers (16 values x 128 keys a warp) and everything side by side.  W and Z are the only roundings to 16 bits on the way:
 // together they leave out about 1.4 times as far off as rounding it to its type does.
+//
+// fp16 has few exponents: rows of W, c^T and Z are held times powers of two that go by their largest elements.
 template <typename T>
-__global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(const __grid_constant__ Args g,
+                                                                            const __grid_constant__ Maps maps) {
     using B = Bits<T>;
-    constexpr int kParts = B::kParts, kMostStages = 4;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * kMostStages + 12];
-    __shared__ uint32_t tmem_base, gave_up;
-    __shared__ uint32_t bad[2];  // number of the last (every other) chunk whose c holds an infinity or a NaN
-    __shared__ __align__(16) float left[kChunk];       // what a token's part is worth at the end of the chunk
-    __shared__ short z_exp[2][kMostSize], part_exp[2][kMostSize];  // fp16: scales of Z, and of each half's share of a row
-    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t z_base = ring + g.stages * g.stage_bytes;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, scored = empty + 8 * kMostStages;
-    const uint32_t weighted = scored + 8, entered = scored + 16, done = scored + 24, c_ready = scored + 32, c_free = scored + 48,
-                   added = scored + 64, z_ready = scored + 72, out_free = scored + 80, met = scored + 88;
+    constexpr int kParts = B::kParts;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    Tables& tab = *reinterpret_cast<Tables*>(smem_raw + kRing);
+    const uint32_t ring = smem_u32(smem_raw), z_base = ring + g.stages * g.stage_bytes;
+    volatile uint32_t* const gave_up = &tab.gave_up;
+    const uint32_t full = smem_u32(tab.full), empty = smem_u32(tab.empty), used = smem_u32(tab.used), scored = smem_u32(&tab.scored),
+                   scaled = smem_u32(&tab.scaled), weighted = smem_u32(&tab.weighted), entered = smem_u32(&tab.entered),
+                   done = smem_u32(&tab.done), c_ready = smem_u32(tab.c_ready), c_free = smem_u32(tab.c_free),
+                   added = smem_u32(&tab.added), add_free = smem_u32(&tab.add_free), z_ready = smem_u32(&tab.z_ready),
+                   out_free = smem_u32(&tab.out_free), met = smem_u32(&tab.met);
     const int warp = __shfl_sync(kAllLanes, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < g.stages; i++) bar_init(full + 8 * i, 32 * kLoadWarps), bar_init(empty + 8 * i, g.full ? kOutWarps : 1);
-        bar_init(scored, 1), bar_init(weighted, kOutWarps), bar_init(entered, 1), bar_init(done, 1);
-        for (int i = 0; i < 2; i++) bar_init(c_ready + 8 * i, kStateWarps), bar_init(c_free + 8 * i, 1);
-        bar_init(added, 1), bar_init(z_ready, kStateWarps), bar_init(out_free, kOutWarps), bar_init(met, kStateWarps);
-        gave_up = bad[0] = bad[1] = 0;
+        for (int i = 0; i < g.stages; i++)
+            bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, g.full ? kOutWarps : 1), bar_init(used + 8 * i, 1);
+        bar_init(scored, 1), bar_init(scaled, kWeightWarps), bar_init(weighted, kWeightWarps + kOutWarps + kPartWarps);
+        bar_init(entered, 1), bar_init(done, 1);
+        for (int i = 0; i < 2; i++) bar_init(c_ready + 8 * i, kPartWarps), bar_init(c_free + 8 * i, 1);
+        bar_init(added, 1), bar_init(add_free, kStateWarps), bar_init(z_ready, kStateWarps), bar_init(out_free, kOutWarps);
+        bar_init(met, kPartWarps);
+        tab.bad[0] = tab.bad[1] = 0;
+        // rows of 128 swizzled bytes go by absolute addresses
+        tab.gave_up = ring % 1024 != 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kOutWarps + kStateWarps + kLoadWarps) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "r"(512)
+    if (warp == kMultiply) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tab.tmem)), "r"(512)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = tmem_base;
+    const uint32_t tmem = tab.tmem;
     pdl_wait();
     pdl_trigger();
-    bool ok = true;
+    bool ok = *gave_up == 0;
     uint32_t c = 0;  // chunks so far, of all that this CTA works on
 
-    if (warp < kOutWarps) {
-        // ---- weights and output
+    if (warp < kFirstOut) {
+        // ---- weights: a token a lane
         const int row = warp * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        float* const powers = tab.powers + 32 + 32 * warp;
+        if (warp == 0) tab.powers[lane] = tab.powers[32 * (kWeightWarps + 1) + lane] = 0.0f;
         for (int w = blockIdx.x; w < g.total && g.full && ok; w += gridDim.x) {
             const Work k = work_of(g, w);
             const Pass& p = *k.p;
-            const int panels_k = (p.kd + 63) / 64, panels_v = (p.vd + 63) / 64;
-            // d^(31 - j) for the lanes of this warp; each warp has its own copy in its lanes
-            const float mine = exp2f(k.l2 * (31 - lane));
-            const float enter = p.inter * exp2f(k.l2 * (row + p.e));
-            for (int chunk = 0; chunk < k.chunks && ok; chunk++, c++) {
-                const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes;
-                const int n = tokens_of(k, chunk);
-                if (!warp_wait(scored, c & 1, &gave_up, g.limit)) { ok = false; break; }
+            __syncwarp();
+            powers[lane] = exp2f(k.l2 * (p.reverse ? lane : 31 - lane));
+            __syncwarp();
+            // blocks of 32 tokens of c whose weights are all wanted: [begin, end); of the warp's own block some are
+            const int begin = p.reverse ? warp + 1 : 0, end = p.reverse ? 4 : warp;
+            const uint32_t causal = p.reverse ? ~0u << lane : 2u << lane, wanted = p.reverse ? causal : causal - 1;
+            for (int chunk = 0; chunk < k.chunks; chunk++, c++) {
+                if (!warp_wait(scored, c & 1, gave_up, g.limit)) { ok = false; break; }
                 fence_after();
-                int shift = 0;  // fp16: the row's weights are held times 2^shift
+                float up = 1.0f;
                 if constexpr (B::kScaled) {
                     float most = 0.0f;
-                    for (int b = 0; b <= warp; b++) {
+#pragma unroll 1
+                    for (int b = min(begin, warp); b < max(end, warp + 1); b++) {
                         uint32_t r[32];
                         tmem_load32(tmem + kColScore + lanes + b * 32, r);
-                        const float far = p.intra * exp2f(k.l2 * (row - b * 32 - 31));
+                        const uint32_t look = b == warp ? wanted : ~0u;
 #pragma unroll
-                        for (int j = 0; j < 32; j++) {
-                            const float d = __shfl_sync(kAllLanes, mine, j);
-                            const float weight = b < warp ? far * d : p.intra * exp2f(k.l2 * (lane >= j ? lane - j : 0));
-                            if (b < warp || lane >= j) most = fmaxf(most, fabsf(__uint_as_float(r[j]) * weight));
-                        }
+                        for (int j = 0; j < 32; j++)
+                            if (look & (1u << j)) most = fmaxf(most, fabsf(__uint_as_float(r[j])));
                     }
-                    shift = exponent_for(most);
+                    const int e = exponent_for(most * fabsf(p.intra));
+                    up = power_of_two(e);
+                    tab.w_exp[c & 1][row] = (signed char)e;
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(scaled);
                 }
-                const float up = power_of_two(shift);
+// loops of few instructions: what the kinds of warps execute at a time has to fit the instruction caches.  In this order
+// the weights of a block lie over scores that have been read.
 #pragma unroll 1
                 for (int b = 0; b < 4; b++) {
                     uint32_t out[16];
-                    if (b < warp) {
+                    if (b == warp) {
                         uint32_t r[32];
                         tmem_load32(tmem + kColScore + lanes + b * 32, r);
-                        const float far = p.intra * exp2f(k.l2 * (row - b * 32 - 31)) * up;
+                        const float f = p.intra * up;
+                        const float* const own = powers + (p.reverse ? -lane : 31 - lane);
 #pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            const float d0 = __shfl_sync(kAllLanes, mine, 2 * j), d1 = __shfl_sync(kAllLanes, mine, 2 * j + 1);
-                            out[j] = B::pack(__uint_as_float(r[2 * j]) * (far * d0), __uint_as_float(r[2 * j + 1]) * (far * d1));
+                        for (int j = 0; j < 32; j += 2) {
+                            // what the score of a token that does not count holds is not looked at
+                            const float x = wanted & (1u << j) ? __uint_as_float(r[j]) * (own[j] * f) : 0.0f;
+                            const float y = wanted & (2u << j) ? __uint_as_float(r[j + 1]) * (own[j + 1] * f) : 0.0f;
+                            out[j / 2] = B::pack(x, y);
                         }
-                    } else if (b == warp) {
+                    } else if (b >= begin && b < end) {
                         uint32_t r[32];
                         tmem_load32(tmem + kColScore + lanes + b * 32, r);
+                        // to the block's nearest token
+                        const float f = exp2f(k.l2 * (p.reverse ? b * 32 - row : row - b * 32 - 31)) * p.intra * up;
 #pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            const int i0 = lane - 2 * j, i1 = i0 - 1;
-                            const float x = __uint_as_float(r[2 * j]) * (p.intra * exp2f(k.l2 * (i0 > 0 ? i0 : 0)) * up);
-                            const float y = __uint_as_float(r[2 * j + 1]) * (p.intra * exp2f(k.l2 * (i1 > 0 ? i1 : 0)) * up);
-                            out[j] = B::pack(i0 >= 0 ? x : 0.0f, i1 >= 0 ? y : 0.0f);
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 d = *reinterpret_cast<const float4*>(powers + j);  // and from there on
+                            const float2 x = mul2(mul2(make_float2(d.x, d.y), make_float2(f, f)),
+                                                  make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])));
+                            const float2 y = mul2(mul2(make_float2(d.z, d.w), make_float2(f, f)),
+                                                  make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])));
+                            out[j / 2] = B::pack(x.x, x.y), out[j / 2 + 1] = B::pack(y.x, y.y);
                         }
                     } else {
 #pragma unroll
@@ -391,18 +575,48 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     }
                     tmem_store16(tmem + kColScore + lanes + b * 16, out);
                 }
-                if (!warp_wait(entered, c & 1, &gave_up, g.limit)) { ok = false; break; }
+                tmem_store_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(weighted);
+            }
+        }
+    } else if (warp < kFirstPart) {
+        // ---- output: a token a lane, half of the values a warp
+        fewer_registers<kOutRegisters>();
+        const int quad = warp & 3, half = (warp - kFirstOut) >> 2, row = quad * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        for (int w = blockIdx.x; w < g.total && g.full && ok; w += gridDim.x) {
+            const Work k = work_of(g, w);
+            const Pass& p = *k.p;
+            const int panels_k = (p.kd + 63) / 64;
+            const int all = (p.vd + 31) / 32, share = (all + 1) / 2, b0 = half * share, b1 = min(all, b0 + share);
+            const uint32_t pitch = (p.vd + 63) / 64 * 128;
+            for (int chunk = 0; chunk < k.chunks; chunk++, c++) {
+                const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes;
+                const int n = tokens_of(k, chunk);
+                // of rows behind the last token whatever comes
+                const float enter = p.inter * exp2f(k.l2 * (p.e + (p.reverse ? n - 1 - row : row)));
+                if (!warp_wait(entered, c & 1, gave_up, g.limit)) { ok = false; break; }
+                float rise = enter, down = 1.0f;
+                if constexpr (B::kScaled) {
+                    if (!warp_wait(scaled, c & 1, gave_up, g.limit)) { ok = false; break; }
+                    const int e = tab.w_exp[c & 1][row];
+                    rise *= power_of_two(e), down = power_of_two(-e);
+                }
                 fence_after();
-                const float rise = enter * up;
 #pragma unroll 1
-                for (int b = 0; b * 32 < p.vd; b++) {
+                for (int b = b0; b < b1; b++) {
                     uint32_t r[32];
                     tmem_load32(tmem + kColOut + lanes + b * 32, r);
 #pragma unroll
-                    for (int j = 0; j < 32; j++) {
-                        float v = __uint_as_float(r[j]) * rise;
-                        if constexpr (B::kScaled) v *= power_of_two(-z_exp[c & 1][b * 32 + j]);
-                        r[j] = __float_as_uint(v);
+                    for (int j = 0; j < 32; j += 2) {
+                        float2 v = mul2(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), make_float2(rise, rise));
+                        if constexpr (B::kScaled) {
+                            const char2 e = *reinterpret_cast<const char2*>(&tab.z_exp[c & 1][b * 32 + j]);
+                            v = mul2(v, make_float2(power_of_two(-e.x), power_of_two(-e.y)));
+                        }
+                        r[j] = __float_as_uint(v.x), r[j + 1] = __float_as_uint(v.y);
                     }
                     tmem_store32(tmem + kColOut + lanes + b * 32, r);
                 }
@@ -410,95 +624,54 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(weighted);
-                if (!warp_wait(done, c & 1, &gave_up, g.limit)) { ok = false; break; }
+                if (!warp_wait(done, c & 1, gave_up, g.limit)) { ok = false; break; }
                 fence_after();
-                const bool by_hand = *(volatile uint32_t*)&bad[c & 1] == c + 1;
-                const float down = power_of_two(-shift);
-                // out in 16 bits, over the tiles of a and b, which nobody needs any more; each warp its own rows
-                const uint32_t pitch = panels_v * 128, own = stage + warp * 32 * pitch;
-                const uint32_t c_tile = stage + 2 * panels_k * kPanel;
+                const bool by_hand = *(volatile uint32_t*)&tab.bad[c & 1] == c + 1;
+                // in 16 bits over the tiles of a and b, once the state's products have read b too
+                if (!warp_wait(used + 8 * st, (c / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
+                const uint32_t own = stage + quad * 32 * pitch;
 #pragma unroll 1
-                for (int b = 0; b * 32 < p.vd; b++) {
+                for (int b = b0; b < b1; b++) {
+                    if (by_hand) {
+                        round_out_by_hand<B>(tmem + kColOut + lanes + b * 32, tmem + kColScore + lanes,
+                                             stage + 2 * panels_k * kPanel, b, row, p.reverse, down, own + lane * pitch);
+                        continue;
+                    }
                     uint32_t r[32];
                     tmem_load32(tmem + kColOut + lanes + b * 32, r);
-                    if (by_hand) {
-                        // c holds an infinity or a NaN, which a product would carry to the tokens in front of it (times
-                        // their weight of zero): the sum over the tokens up to each row, one by one
-                        for (int q = 0; q <= warp; q++) {
-                            uint32_t v[16];
-                            asm volatile(
-                                "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-                                "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-                                "tcgen05.wait::ld.sync.aligned;"
-                                : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
-                                  "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
-                                  "=r"(v[14]), "=r"(v[15])
-                                : "r"(tmem + kColScore + lanes + q * 16)
-                                : "memory");
-#pragma unroll
-                            for (int j = 0; j < 32; j++) {
-                                const int token = q * 32 + j;
-                                if (token > row) continue;
-                                const float weight = j & 1 ? B::high(v[j / 2]) : B::low(v[j / 2]);
-#pragma unroll 4
-                                for (int x = 0; x < 32; x += 8) {
-                                    const int col = b * 32 + x;
-                                    uint32_t u[4];
-                                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                                                 : "r"(c_tile + (col >> 6) * kPanel + token * 128 +
-                                                       ((((col >> 3) & 7) ^ (token & 7)) << 4)));
-#pragma unroll
-                                    for (int y = 0; y < 8; y++) {
-                                        const float value = y & 1 ? B::high(u[y / 2]) : B::low(u[y / 2]);
-                                        r[x + y] = __float_as_uint(fmaf(weight, value, __uint_as_float(r[x + y])));
-                                    }
-                                }
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        uint32_t v[4];
-#pragma unroll
-                        for (int i = 0; i < 4; i++)
-                            v[i] = B::pack(__uint_as_float(r[j + 2 * i]) * down, __uint_as_float(r[j + 2 * i + 1]) * down);
-                        const int piece = b * 4 + j / 8;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(own + lane * pitch +
-                                                                                      ((piece ^ (lane & 7)) << 4)),
-                                     "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
-                                     : "memory");
-                    }
+                    round_out<B>(r, down, own + lane * pitch, b, lane);
                 }
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(out_free);
-                const int64_t row0 = first_row(k, chunk);
-                T* const to = (T*)p.out + (int64_t)k.head * p.vd;
+                T* const to = (T*)p.out + first_row(k, chunk) * p.out_ld + (int64_t)k.head * p.vd;
+                const int64_t way = p.out_ld;
+                const int rows = min(32, n - quad * 32);
                 if (p.out_wide == 16) {
-                    const int per_row = p.vd >> 3;
-                    for (int i = lane; i < 32 * per_row; i += 32) {
-                        const int r = i / per_row, piece = i - r * per_row, token = warp * 32 + r;
-                        if (token >= n) break;
-                        uint32_t v[4];
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                                     : "r"(own + r * pitch + ((piece ^ (r & 7)) << 4))
-                                     : "memory");
-                        const int64_t at = p.reverse ? row0 - token : row0 + token;
-                        *reinterpret_cast<uint4*>(to + at * p.out_ld + piece * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+                    // 4 or 8 lanes to a row
+                    const int per_row = share * 4, piece = b0 * 4 + (lane & (per_row - 1)), r0 = lane / per_row, step = 32 / per_row;
+                    T* q = to + (quad * 32 + r0) * way + piece * 8;
+                    if (piece * 8 < p.vd) {
+#pragma unroll 4
+                        for (int r = r0; r < rows; r += step, q += step * way) {
+                            uint32_t v[4];
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                                         : "r"(own + r * pitch + ((piece ^ (r & 7)) << 4))
+                                         : "memory");
+                            *reinterpret_cast<uint4*>(q) = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
                     }
                 } else {
-                    for (int r = 0; r < 32 && warp * 32 + r < n; r++) {
-                        const int token = warp * 32 + r;
-                        const int64_t at = p.reverse ? row0 - token : row0 + token;
-                        for (int col = lane; col < p.vd; col += 32) {
+                    for (int r = 0; r < rows; r++) {
+                        T* const q = to + (quad * 32 + r) * way;
+                        for (int col = b0 * 32 + lane; col < min(p.vd, b1 * 32); col += 32) {
                             unsigned short v;
                             asm volatile("ld.shared.u16 %0, [%1];"
                                          : "=h"(v)
                                          : "r"(own + r * pitch + (((col >> 3) ^ (r & 7)) << 4) + (col & 7) * 2)
                                          : "memory");
-                            reinterpret_cast<unsigned short*>(to)[at * p.out_ld + col] = v;
+                            reinterpret_cast<unsigned short*>(q)[col] = v;
                         }
                     }
                 }
@@ -508,60 +681,160 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if (lane == 0) bar_arrive(empty + 8 * st);
             }
         }
-    } else if (warp < kOutWarps + kStateWarps) {
-        // ---- the state: lane = value, half of the keys a warp
-        const int quad = warp & 3, half = (warp - kOutWarps) >> 2, value = quad * 32 + lane;
-        const int t = threadIdx.x - 32 * kOutWarps;
-        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        uint32_t pieces = 0;  // of c^T so far
-        uint32_t meetings = 0;
-        // a barrier of the state's warps that gives up like every other wait
+    } else if (warp < kFirstState) {
+        // ---- c^T, scaled and in parts: a warp has 32 values, in two sets of 16; a lane tokens 2 (lane % 4) and the next of
+        // every 8, for rows lane / 4 and lane / 4 + 8 of a set
+        fewer_registers<kPartRegisters>();
+        const int t = threadIdx.x - 32 * kFirstPart, quad = warp & 3, matrix = lane >> 3, line = lane & 7;
+        uint32_t pieces = 0, meetings = 0;
+        // a barrier of these warps that gives up like every other wait
         auto meet = [&] {
             __syncwarp();
             if (lane == 0) bar_arrive(met);
-            ok = ok && warp_wait(met, meetings++ & 1, &gave_up, g.limit);
+            ok = ok && warp_wait(met, meetings++ & 1, gave_up, g.limit);
         };
         for (int w = blockIdx.x; w < g.total && ok; w += gridDim.x) {
             const Work k = work_of(g, w);
             const Pass& p = *k.p;
-            const int panels_k = (p.kd + 63) / 64;
-            const int keys = (p.kd + 15) / 16 * 16, share = (keys / 2 + 15) / 16 * 16;
-            const int key0 = half * share, mine = half ? keys - share : share;  // multiples of 16, at most 64
-            const bool there = quad * 32 < p.vd, inside = value < p.vd;
+            const int panels_k = (p.kd + 63) / 64, sets = min(2, (p.vd - quad * 32 + 15) / 16);
+            for (int chunk = 0; chunk < k.chunks && ok; chunk++, c++) {
+                const uint32_t st = c % g.stages, c_tile = ring + st * g.stage_bytes + 2 * panels_k * kPanel;
+                const int n = tokens_of(k, chunk);
+                if (chunk == 0 || n < kChunk) {  // others are as the one before
+                    meet();
+                    tab.left[t] = t < n ? p.gain * exp2f(k.l2 * (p.reverse ? t + 1 - p.e : n - p.e - t)) : 0.0f;
+                    meet();
+                }
+                if (!ok || !warp_wait(full + 8 * st, (c / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
+                // four 8 x 8 matrices of 16 tokens and the values of a set, transposed
+                auto read = [&](int set, int token, uint32_t (&u)[4]) {
+                    const int v = quad * 4 + set * 2 + (matrix & 1);  // of 8
+                    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                                 : "r"(c_tile + (v >> 3) * kPanel + (token + (matrix >> 1) * 8 + line) * 128 + (((v & 7) ^ line) << 4))
+                                 : "memory");
+                };
+                const float* const left = tab.left + (lane & 3) * 2;
+                if constexpr (B::kScaled) {
+#pragma unroll 1
+                    for (int set = 0; set < sets; set++) {
+                        float most[2] = {0.0f, 0.0f};
+#pragma unroll 1
+                        for (int token = 0; token < kChunk; token += 16) {
+                            uint32_t u[4];
+                            read(set, token, u);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                const float2 f = *reinterpret_cast<const float2*>(left + token + (i >> 1) * 8);
+                                most[i & 1] = fmaxf(most[i & 1], fmaxf(fabsf(B::low(u[i]) * f.x), fabsf(B::high(u[i]) * f.y)));
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            const int e = exponent_for(max_of_row(most[i]));
+                            if ((lane & 3) == 0) tab.c_exp[c & 1][quad * 32 + set * 16 + i * 8 + (lane >> 2)] = (signed char)e;
+                        }
+                    }
+                    __syncwarp();
+                }
+                uint32_t most = 0;
+#pragma unroll 1
+                for (int q = 0; q < 4; q++, pieces++) {
+                    const uint32_t slot = pieces & 1;
+                    if (pieces >= 2 && !warp_wait(c_free + 8 * slot, (pieces / 2 - 1) & 1, gave_up, g.limit)) { ok = false; break; }
+                    fence_after();
+#pragma unroll 1
+                    for (int set = 0; set < sets; set++) {
+                        uint32_t part[kParts][8];
+                        float up[2] = {1.0f, 1.0f};
+                        if constexpr (B::kScaled) {
+#pragma unroll
+                            for (int i = 0; i < 2; i++)
+                                up[i] = power_of_two(tab.c_exp[c & 1][quad * 32 + set * 16 + i * 8 + (lane >> 2)]);
+                        }
+#pragma unroll
+                        for (int half = 0; half < 2; half++) {
+                            uint32_t u[4];
+                            read(set, q * 32 + half * 16, u);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                most = B::most(most, u[i]);
+                                const float2 f = *reinterpret_cast<const float2*>(left + q * 32 + half * 16 + (i >> 1) * 8);
+                                float2 x = mul2(make_float2(B::low(u[i]), B::high(u[i])), f);
+                                if constexpr (B::kScaled) x = mul2(x, make_float2(up[i & 1], up[i & 1]));
+#pragma unroll
+                                for (int y = 0; y < kParts; y++) part[y][half * 4 + i] = B::take(x);
+                            }
+                        }
+#pragma unroll
+                        for (int y = 0; y < kParts; y++)
+                            tmem_store_16x16(tmem + kColC + slot * kSlotCols + y * 16 + ((uint32_t)(quad * 32 + set * 16) << 16),
+                                             part[y]);
+                    }
+                    tmem_store_wait();
+                    if (q == 3 && g.full) {
+                        // not more than a chunk ahead of the output, for which the number of a chunk with odd values is left
+                        if (c > 0 && !warp_wait(done, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
+                        if (B::is_odd(most)) *(volatile uint32_t*)&tab.bad[c & 1] = c + 1;
+                    }
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        bar_arrive(c_ready + 8 * slot);
+                        if (q == 3 && g.full) bar_arrive(weighted);
+                    }
+                }
+            }
+        }
+    } else if (warp < kFirstLoad) {
+        // ---- the state: a warp has 16 values, a lane rows lane / 4 and lane / 4 + 8 of them and every fourth pair of keys:
+        // z[4 m ..]: keys 8 m + 2 (lane % 4) and the next of the first row, the same of the second
+        more_registers<kStateRegisters>();
+        const int v0 = (warp & 3) * 32 + ((warp - kFirstState) >> 2) * 16, value = v0 + (lane >> 2);
+        const uint32_t lanes = (uint32_t)v0 << 16;
+        // where this lane's row of the four 8 x 8 matrices that stmatrix takes lies
+        const int matrix = lane >> 3, line = lane & 7;
+        const uint32_t z_lane = z_base + (v0 + (matrix & 1) * 8 + line) * 128;
+        for (int w = blockIdx.x; w < g.total && ok; w += gridDim.x) {
+            const Work k = work_of(g, w);
+            const Pass& p = *k.p;
+            const int blocks = (p.kd + 15) / 16 * 2;  // of 8 keys
+            const bool there = v0 < p.vd;
             float z[64];
             const float* from = state_in(k);
 #pragma unroll
             for (int i = 0; i < 64; i++) {
-                const int key = key0 + i;
-                z[i] = from && inside && i < mine && key < p.kd ? from[(int64_t)key * p.k_step + (int64_t)value * p.v_step] : 0.0f;
+                const int key = (i >> 2) * 8 + (lane & 3) * 2 + (i & 1), v = value + (i & 2) * 4;
+                z[i] = from && v < p.vd && key < p.kd ? from[(int64_t)key * p.k_step + (int64_t)v * p.v_step] : 0.0f;
             }
             // rounds Z into shared memory for the products with a
             auto put = [&](uint32_t of) {
-                float up = 1.0f;
+                float up[2] = {1.0f, 1.0f};
                 if constexpr (B::kScaled) {
-                    float most = 0.0f;
+                    float most[2] = {0.0f, 0.0f};
 #pragma unroll
-                    for (int i = 0; i < 64; i++)
-                        if (i < mine) most = fmaxf(most, fabsf(z[i]));
-                    part_exp[half][value] = (short)exponent_for(most);
-                    // a half of zeros (or of numbers that are none) asks for nothing
-                    if (!(most > 0.0f && most < INFINITY)) part_exp[half][value] = 127;
-                    meet();
-                    int e = min(part_exp[0][value], part_exp[1][value]);
-                    if (e == 127) e = 0;
-                    if (half == 0) z_exp[of & 1][value] = (short)e;
-                    up = power_of_two(e);
-                    meet();
+                    for (int i = 0; i < 64; i++) most[(i >> 1) & 1] = fmaxf(most[(i >> 1) & 1], fabsf(z[i]));
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const int e = exponent_for(max_of_row(most[i]));
+                        if ((lane & 3) == 0) tab.z_exp[of & 1][value + 8 * i] = (signed char)e;
+                        up[i] = power_of_two(e);
+                    }
                 }
                 if (there) {
 #pragma unroll
-                    for (int i = 0; i < 64; i += 8) {
-                        if (i >= mine) break;
-                        const int col = key0 + i;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                                         z_base + (col >> 6) * kPanel + value * 128 + ((((col >> 3) & 7) ^ (value & 7)) << 4)),
-                                     "r"(B::pack(z[i] * up, z[i + 1] * up)), "r"(B::pack(z[i + 2] * up, z[i + 3] * up)),
-                                     "r"(B::pack(z[i + 4] * up, z[i + 5] * up)), "r"(B::pack(z[i + 6] * up, z[i + 7] * up))
+                    for (int m = 0; m < 16; m += 2) {
+                        if (m >= blocks) break;
+                        uint32_t v[4];
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            float x = z[m * 4 + i * 2], y = z[m * 4 + i * 2 + 1];
+                            if constexpr (B::kScaled) x *= up[i & 1], y *= up[i & 1];
+                            v[i] = B::pack(x, y);
+                        }
+                        asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
+                                         z_lane + (m >> 3) * kPanel + ((((m & 7) | (matrix >> 1)) ^ line) << 4)),
+                                     "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
                                      : "memory");
                     }
                 }
@@ -571,209 +844,179 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
             };
             if (g.full && k.chunks) {
                 // the chunk before has read its Z
-                if (c > 0 && !warp_wait(entered, (c - 1) & 1, &gave_up, g.limit)) { ok = false; break; }
+                if (c > 0 && !warp_wait(entered, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
                 put(c);
             }
-            for (int chunk = 0; chunk < k.chunks && ok; chunk++, c++) {
-                const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes;
-                const int n = tokens_of(k, chunk);
-                if (chunk == 0 || n < kChunk) {  // others are as the one before
-                    meet();
-                    if (t < kChunk) left[t] = t < n ? p.gain * exp2f(k.l2 * (n - p.e - t)) : 0.0f;
-                    meet();
-                }
-                if (!warp_wait(full + 8 * st, (c / g.stages) & 1, &gave_up, g.limit)) { ok = false; break; }
-                const uint32_t c_tile = stage + 2 * panels_k * kPanel;
-                const uint32_t at = c_tile + (value >> 6) * kPanel + (value & 7) * 2;
-                const int piece = (value >> 3) & 7;
-                int shift = 0;
-                if constexpr (B::kScaled) {
-                    float most = 0.0f;
-                    if (there) {
-#pragma unroll 16
-                        for (int j = 0; j < 64; j++) {
-                            const int token = half * 64 + j;
-                            unsigned short u;
-                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(at + token * 128 + ((piece ^ (token & 7)) << 4)));
-                            most = fmaxf(most, fabsf(B::low(u) * left[token]));
-                        }
-                    }
-                    part_exp[half][value] = most > 0.0f && most < INFINITY ? (short)exponent_for(most) : (short)127;
-                    meet();
-                    shift = min(part_exp[0][value], part_exp[1][value]);
-                    if (shift == 127) shift = 0;
-                    meet();
-                }
-                const float up = power_of_two(shift);
-                uint32_t odd = 0;
-                for (int q = 0; q < 4; q++, pieces++) {
-                    const uint32_t slot = pieces & 1;
-                    if (pieces >= 2 && !warp_wait(c_free + 8 * slot, (pieces / 2 - 1) & 1, &gave_up, g.limit)) { ok = false; break; }
-                    fence_after();
-                    if (there) {
-                        uint32_t part[kParts][8];
-#pragma unroll
-                        for (int j = 0; j < 16; j += 2) {
-                            float x[2];
-#pragma unroll
-                            for (int i = 0; i < 2; i++) {
-                                const int token = q * 32 + half * 16 + j + i;
-                                unsigned short u;
-                                asm volatile("ld.shared.u16 %0, [%1];"
-                                             : "=h"(u)
-                                             : "r"(at + token * 128 + ((piece ^ (token & 7)) << 4)));
-                                odd |= (u & B::kExponent) == B::kExponent;
-                                x[i] = B::low(u) * left[token] * up;
-                            }
-#pragma unroll
-                            for (int i = 0; i < kParts; i++) {
-                                part[i][j / 2] = B::pack(x[0], x[1]);
-                                x[0] -= B::low(part[i][j / 2]);
-                                x[1] -= B::high(part[i][j / 2]);
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < kParts; i++)
-                            tmem_store8(tmem + kColC + slot * kSlotCols + i * 16 + half * 8 + lanes, part[i]);
-                        tmem_store_wait();
-                        if (q == 3 && inside && odd) *(volatile uint32_t*)&bad[c & 1] = c + 1;
-                    }
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(c_ready + 8 * slot);
-                }
-                if (!ok || !warp_wait(added, c & 1, &gave_up, g.limit)) { ok = false; break; }
+            for (int chunk = 0; chunk < k.chunks; chunk++, c++) {
+                const float decay = exp2f(k.l2 * tokens_of(k, chunk));
+                if (!warp_wait(added, c & 1, gave_up, g.limit)) { ok = false; break; }
                 fence_after();
-                const float decay = exp2f(k.l2 * n), down = power_of_two(-shift);
                 if (there) {
+                    float down[2] = {1.0f, 1.0f};
+                    if constexpr (B::kScaled) {
+#pragma unroll
+                        for (int i = 0; i < 2; i++) down[i] = power_of_two(-tab.c_exp[c & 1][value + 8 * i]);
+                    }
 #pragma unroll
                     for (int b = 0; b < 4; b++) {
-                        if (b * 16 >= mine) break;
+                        if (b * 4 >= blocks) break;
                         float v[16];
-                        tmem_load16(tmem + kColAdd + lanes + key0 + b * 16, v);
+                        tmem_load_16x32(tmem + kColAdd + lanes + b * 32, v);
 #pragma unroll
-                        for (int i = 0; i < 16; i++) z[b * 16 + i] = fmaf(z[b * 16 + i], decay, B::kScaled ? v[i] * down : v[i]);
+                        for (int i = 0; i < 16; i += 2) {
+                            float2 x = make_float2(v[i], v[i + 1]);
+                            if constexpr (B::kScaled) x = mul2(x, make_float2(down[(i >> 1) & 1], down[(i >> 1) & 1]));
+                            x = fma2(make_float2(z[b * 16 + i], z[b * 16 + i + 1]), make_float2(decay, decay), x);
+                            z[b * 16 + i] = x.x, z[b * 16 + i + 1] = x.y;
+                        }
                     }
-                    fence_before();
                 }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(add_free);
                 if (g.full && chunk + 1 < k.chunks) {
-                    if (!warp_wait(entered, c & 1, &gave_up, g.limit)) { ok = false; break; }
+                    if (!warp_wait(entered, c & 1, gave_up, g.limit)) { ok = false; break; }
                     put(c + 1);
                 }
             }
             if (!ok) break;
             float* const to = state_out(k);
-            if (to && inside) {
+            if (to) {
 #pragma unroll
                 for (int i = 0; i < 64; i++) {
-                    const int key = key0 + i;
-                    if (i < mine && key < p.kd) to[(int64_t)key * p.k_step + (int64_t)value * p.v_step] = z[i];
+                    const int key = (i >> 2) * 8 + (lane & 3) * 2 + (i & 1), v = value + (i & 2) * 4;
+                    if (v < p.vd && key < p.kd) to[(int64_t)key * p.k_step + (int64_t)v * p.v_step] = z[i];
                 }
             }
-            if (t == 0) decay_out(k, g.log_decay);
+            if (warp == kFirstState && lane == 0) decay_out(k, g.log_decay);
         }
-    } else if (warp < kOutWarps + kStateWarps + kLoadWarps) {
-        // ---- loads
-        const int t = threadIdx.x - 32 * (kOutWarps + kStateWarps);
-        for (int w = blockIdx.x; w < g.total && ok; w += gridDim.x) {
-            const Work k = work_of(g, w);
-            const Pass& p = *k.p;
-            const int panels_k = (p.kd + 63) / 64, panels_v = (p.vd + 63) / 64;
-            const int way = p.reverse ? -2 : 2;
-            for (int chunk = 0; chunk < k.chunks; chunk++, c++) {
-                const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes;
-                if (c >= (uint32_t)g.stages && !warp_wait(empty + 8 * st, (c / g.stages - 1) & 1, &gave_up, g.limit)) {
-                    ok = false;
-                    break;
-                }
-                const int n = tokens_of(k, chunk);
-                const int64_t row = first_row(k, chunk);
-                if (g.full)
-                    load_any(p.a_wide, stage, (const char*)p.a + (row * p.a_ld + (int64_t)k.head * p.kd) * 2, way * p.a_ld, p.kd,
-                             panels_k, n, t);
-                load_any(p.b_wide, stage + panels_k * kPanel, (const char*)p.b + (row * p.b_ld + (int64_t)k.head * p.kd) * 2,
-                         way * p.b_ld, p.kd, panels_k, n, t);
-                load_any(p.c_wide, stage + 2 * panels_k * kPanel, (const char*)p.c + (row * p.c_ld + (int64_t)k.head * p.vd) * 2,
-                         way * p.c_ld, p.vd, panels_v, n, t);
-                asm volatile("cp.async.wait_all;" ::: "memory");
-                proxy_fence();
-                bar_arrive(full + 8 * st);
-            }
-        }
-        // all products have reported before the CTA ends
-        for (uint32_t i = c > (uint32_t)g.stages ? c - g.stages : 0; i < c && ok; i++)
-            ok = warp_wait(empty + 8 * (i % g.stages), (i / g.stages) & 1, &gave_up, g.limit);
     } else {
-        // ---- products
-        uint32_t pieces = 0;
-        bool by_hand = false;
-        for (int w = blockIdx.x; w < g.total && ok; w += gridDim.x) {
-            const Work k = work_of(g, w);
-            const Pass& p = *k.p;
-            const int panels_k = (p.kd + 63) / 64;
-            const uint32_t keys = (p.kd + 15) / 16, values = (p.vd + 15) / 16;  // of 16
-            constexpr uint32_t kBase = (1u << 4) | B::kFormat | (128u >> 4) << 24;
-            const uint32_t score_desc = kBase | (128u >> 3) << 17, enter_desc = kBase | (values * 2) << 17,
-                           out_desc = enter_desc | 1u << 16, add_desc = kBase | (keys * 2) << 17 | 1u << 16;
-            for (int chunk = 0; chunk < k.chunks && ok; chunk++, c++) {
-                const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes;
-                const int n = tokens_of(k, chunk);
-                const uint64_t a = smem_desc(stage, 16, 1024), b = smem_desc(stage + panels_k * kPanel, 16, 1024),
-                               z = smem_desc(z_base, 16, 1024);
-                const uint64_t b_turned = smem_desc(stage + panels_k * kPanel, kPanel, 1024),
-                               c_turned = smem_desc(stage + 2 * panels_k * kPanel, kPanel, 1024);
-                if (!warp_wait(full + 8 * st, (c / g.stages) & 1, &gave_up, g.limit)) { ok = false; break; }
-                fence_after();
-                if (g.full) {
+        fewer_registers<kOtherRegisters>();  // all of the group at one place
+        if (warp < kMultiply) {
+            // ---- loads: every other chunk each, so that one chunk's copies fly while the other's are waited for
+            const uint32_t turn = warp - kFirstLoad;
+            for (int w = blockIdx.x; w < g.total && ok; w += gridDim.x) {
+                const Work k = work_of(g, w);
+                const Pass& p = *k.p;
+                const int panels_k = (p.kd + 63) / 64, panels_v = (p.vd + 63) / 64, pass = (int)(k.p - g.pass);
+                for (int chunk = 0; chunk < k.chunks; chunk++, c++) {
+                    if (c % kLoadWarps != turn) continue;
+                    const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes, bar = full + 8 * st;
+                    if (c >= (uint32_t)g.stages && !warp_wait(empty + 8 * st, (c / g.stages - 1) & 1, gave_up, g.limit)) {
+                        ok = false;
+                        break;
+                    }
+                    const int n = tokens_of(k, chunk);
+                    const int64_t row = first_row(k, chunk);
+                    if (p.tiled && n == kChunk) {
+                        if (lane == 0) {
+                            bar_expect(bar, ((g.full ? 2 : 1) * panels_k + panels_v) * kPanel);
+                            for (int i = 0; i < panels_k; i++) {
+                                if (g.full) copy_box(stage + i * kPanel, &maps.a[pass], bar, k.head * p.kd + i * 64, (int)row);
+                                copy_box(stage + (panels_k + i) * kPanel, &maps.b[pass], bar, k.head * p.kd + i * 64, (int)row);
+                            }
+                            for (int i = 0; i < panels_v; i++)
+                                copy_box(stage + (2 * panels_k + i) * kPanel, &maps.c[pass], bar, k.head * p.vd + i * 64, (int)row);
+                        }
+                        __syncwarp();
+                        continue;
+                    }
+                    load_any(p.c_wide, stage + 2 * panels_k * kPanel, (const char*)p.c + (row * p.c_ld + (int64_t)k.head * p.vd) * 2,
+                             p.c_ld * 2, p.vd, n);
+                    load_any(p.b_wide, stage + panels_k * kPanel, (const char*)p.b + (row * p.b_ld + (int64_t)k.head * p.kd) * 2,
+                             p.b_ld * 2, p.kd, n);
+                    if (g.full)
+                        load_any(p.a_wide, stage, (const char*)p.a + (row * p.a_ld + (int64_t)k.head * p.kd) * 2, p.a_ld * 2, p.kd, n);
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(bar);
+                }
+            }
+            // all products have reported before the CTA ends
+            for (uint32_t i = c > (uint32_t)g.stages ? c - g.stages : 0; i < c && ok; i++)
+                ok = warp_wait(empty + 8 * (i % g.stages), (i / g.stages) & 1, gave_up, g.limit);
+            if (!ok) {  // let the copies under way land before the CTA ends
+                const unsigned long long until = now_ns() + 1000000ull;
+                while (now_ns() < until) {
+                }
+            }
+        } else {
+            // ---- products: one warp issues those of out, one those of the state, each in its own order
+            uint32_t pieces = 0;
+            bool by_hand = false;
+            const bool of_state = warp == kMultiplyState;
+            for (int w = blockIdx.x; w < g.total && ok && (of_state || g.full); w += gridDim.x) {
+                const Work k = work_of(g, w);
+                const Pass& p = *k.p;
+                const int panels_k = (p.kd + 63) / 64;
+                const uint32_t keys = (p.kd + 15) / 16, values = (p.vd + 15) / 16;  // of 16
+                constexpr uint32_t kBase = (1u << 4) | B::kFormat | (128u >> 4) << 24;
+                const uint32_t score_desc = kBase | (128u >> 3) << 17, enter_desc = kBase | (values * 2) << 17,
+                               out_desc = enter_desc | 1u << 16, add_desc = kBase | (keys * 2) << 17 | 1u << 16;
+                const uint64_t z = smem_desc(z_base, 16, 1024);
+                for (int chunk = 0; chunk < k.chunks && ok; chunk++, c++) {
+                    const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes, b_tile = stage + panels_k * kPanel;
+                    if (!warp_wait(full + 8 * st, (c / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
+                    if (of_state) {
+                        const uint64_t b_turned = smem_desc(b_tile, kPanel, 1024);
+                        if (c > 0 && !warp_wait(add_free, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
+#pragma unroll 1
+                        for (int q = 0; q < 4 && ok; q++, pieces++) {
+                            const uint32_t slot = pieces & 1;
+                            if (!warp_wait(c_ready + 8 * slot, (pieces / 2) & 1, gave_up, g.limit)) { ok = false; break; }
+                            fence_after();
+                            if (elect_one()) {
+                                // small parts first: less of them is cut off
+#pragma unroll
+                                for (int part = kParts - 1; part >= 0; part--)
+#pragma unroll
+                                    for (int i = 0; i < 2; i++)
+                                        mma_ts(tmem + kColAdd, tmem + kColC + slot * kSlotCols + part * 16 + i * 8,
+                                               b_turned + (q * 2 + i) * (2048 >> 4), add_desc, q > 0 || part < kParts - 1 || i > 0);
+                                mma_done(c_free + 8 * slot);
+                                if (q == 3) {
+                                    if (!g.withhold) mma_done(added);
+                                    mma_done((g.full ? used : empty) + 8 * st);
+                                }
+                            }
+                            __syncwarp();
+                        }
+                        continue;
+                    }
+                    const int n = tokens_of(k, chunk);
+                    const uint64_t a = smem_desc(stage, 16, 1024), b = smem_desc(b_tile, 16, 1024),
+                                   c_turned = smem_desc(stage + 2 * panels_k * kPanel, kPanel, 1024);
                     // the weights of the chunk before, in the place of the scores, are used up
-                    if (c > 0 && !warp_wait(done, (c - 1) & 1, &gave_up, g.limit)) { ok = false; break; }
-                    if (by_hand && !warp_wait(out_free, (c - 1) & 1, &gave_up, g.limit)) { ok = false; break; }
+                    if (c > 0 && !warp_wait(done, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
+                    if (by_hand && !warp_wait(out_free, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
                     fence_after();
                     if (elect_one()) {
+#pragma unroll 1
                         for (uint32_t i = 0; i < keys; i++)
                             mma_ss(tmem + kColScore, a + (i >> 2) * (kPanel >> 4) + (i & 3) * 2, b + (i >> 2) * (kPanel >> 4) + (i & 3) * 2,
                                    score_desc, i > 0);
                         mma_done(scored);
                     }
                     __syncwarp();
-                    if (c > 0 && !warp_wait(out_free, (c - 1) & 1, &gave_up, g.limit)) { ok = false; break; }
-                    if (!warp_wait(z_ready, c & 1, &gave_up, g.limit)) { ok = false; break; }
+                    if (c > 0 && !warp_wait(out_free, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
+                    if (!warp_wait(z_ready, c & 1, gave_up, g.limit)) { ok = false; break; }
                     fence_after();
                     if (elect_one()) {
+#pragma unroll 1
                         for (uint32_t i = 0; i < keys; i++)
                             mma_ss(tmem + kColOut, a + (i >> 2) * (kPanel >> 4) + (i & 3) * 2, z + (i >> 2) * (kPanel >> 4) + (i & 3) * 2,
                                    enter_desc, i > 0);
                         mma_done(entered);
                     }
                     __syncwarp();
-                }
-                for (int q = 0; q < 4 && ok; q++, pieces++) {
-                    const uint32_t slot = pieces & 1;
-                    if (!warp_wait(c_ready + 8 * slot, (pieces / 2) & 1, &gave_up, g.limit)) { ok = false; break; }
+                    if (!warp_wait(weighted, c & 1, gave_up, g.limit)) { ok = false; break; }
                     fence_after();
-                    if (elect_one()) {
-                        // small parts first: less of them is cut off
-#pragma unroll
-                        for (int part = kParts - 1; part >= 0; part--)
-#pragma unroll
-                            for (int i = 0; i < 2; i++)
-                                mma_ts(tmem + kColAdd, tmem + kColC + slot * kSlotCols + part * 16 + i * 8,
-                                       b_turned + (q * 2 + i) * (2048 >> 4), add_desc, q > 0 || part < kParts - 1 || i > 0);
-                        mma_done(c_free + 8 * slot);
-                        if (q == 3 && !g.withhold) mma_done(added);
-                        if (q == 3 && !g.full) mma_done(empty + 8 * st);
-                    }
-                    __syncwarp();
-                }
-                if (!ok) break;
-                if (g.full) {
-                    if (!warp_wait(weighted, c & 1, &gave_up, g.limit)) { ok = false; break; }
-                    fence_after();
-                    by_hand = *(volatile uint32_t*)&bad[c & 1] == c + 1;
+                    by_hand = *(volatile uint32_t*)&tab.bad[c & 1] == c + 1;
                     if (elect_one()) {
                         if (!by_hand) {
-                            const int steps = (n + 15) / 16;
-                            for (int i = 0; i < steps; i++)
+#pragma unroll 1
+                            for (int i = 0; i < (n + 15) / 16; i++)
                                 mma_ts(tmem + kColOut, tmem + kColScore + i * 8, c_turned + i * (2048 >> 4), out_desc, true);
                         }
                         mma_done(done);
@@ -781,18 +1024,18 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     __syncwarp();
                 }
             }
-        }
-        for (uint32_t i = pieces > 2 ? pieces - 2 : 0; i < pieces && ok; i++)
-            ok = warp_wait(c_free + 8 * (i & 1), (i / 2) & 1, &gave_up, g.limit);
-        if (!ok) {  // let the products under way end before the CTA does
-            const unsigned long long until = now_ns() + 1000000ull;
-            while (now_ns() < until) {
+            for (uint32_t i = pieces > 2 ? pieces - 2 : 0; i < pieces && ok; i++)
+                ok = warp_wait(c_free + 8 * (i & 1), (i / 2) & 1, gave_up, g.limit);
+            if (!ok) {  // let the products under way end before the CTA does
+                const unsigned long long until = now_ns() + 1000000ull;
+                while (now_ns() < until) {
+                }
             }
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0 && gave_up) *g.status = 2;
-    if (warp == kOutWarps + kStateWarps + kLoadWarps) {
+    if (threadIdx.x == 0 && *gave_up) *g.status = 2;
+    if (warp == kMultiply) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
@@ -1094,6 +1337,7 @@ struct sparbit_linear_attention_plan_s {
     int device = -1, sm_count = 0;
     unsigned long long limit = kWaitNs;
     int withhold = 0;
+    void* encode = nullptr;            // cuTensorMapEncodeTiled
 
     size_t states() const { return (size_t)heads * kd * vd; }
     size_t block() const { return states() + heads; }
@@ -1155,6 +1399,20 @@ Args common_args(const Plan* p) {
     return g;
 }
 
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// One head's size must be a multiple of the products' 16 elements: a box past it brings the next head's.
+bool encode(const Plan* p, CUtensorMap* map, const void* q, int64_t ld, int size) {
+    const cuuint64_t dims[2] = {(cuuint64_t)p->heads * size, (cuuint64_t)p->rows}, strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {64, kChunk}, one[2] = {1, 1};
+    return ((EncodeFn)p->encode)(map, p->dtype == SPARBIT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                                 2, const_cast<void*>(q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int run(const Plan* p, Args& g, cudaStream_t st) {
     g.total = (int)p->list.size() * p->heads * g.n_passes;
     if (p->dtype == SPARBIT_F32) {
@@ -1171,13 +1429,19 @@ int run(const Plan* p, Args& g, cudaStream_t st) {
         g.stage_bytes = std::max(g.stage_bytes, (2 * pk + pv) * kPanel);
         state = std::max(state, pk * kPanel);
     }
-    constexpr uint32_t kRing = 14 * kPanel;  // with what the kernel declares, all that a CTA can have
-    g.stages = (int)std::min<uint32_t>(4, (kRing - state) / g.stage_bytes);
-    const size_t smem = kRing + 1024;
+    g.stages = (int)std::min<uint32_t>(kMostStages, (kRing - state) / g.stage_bytes);
+    const size_t smem = kTensorSmem;
+    Maps maps;
+    for (int i = 0; i < g.n_passes; i++) {
+        Pass& x = g.pass[i];
+        x.tiled = x.b_wide == 16 && x.c_wide == 16 && (!g.full || x.a_wide == 16) && x.kd % 16 == 0 && x.vd % 16 == 0 &&
+                  p->rows >= kChunk && p->rows <= 0x7fffffffu && encode(p, &maps.b[i], x.b, x.b_ld, x.kd) &&
+                  encode(p, &maps.c[i], x.c, x.c_ld, x.vd) && (!g.full || encode(p, &maps.a[i], x.a, x.a_ld, x.kd));
+    }
     const dim3 grid(std::min(g.total, p->sm_count));
     auto launch_it = [&](auto kernel) {
         CU(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        CU(launch(kernel, grid, dim3(kTensorThreads), smem, st, g));
+        CU(launch(kernel, grid, dim3(kTensorThreads), smem, st, g, maps));
         return (int)SPARBIT_OK;
     };
     return p->dtype == SPARBIT_BF16 ? launch_it(attention_tensor_kernel<__nv_bfloat16>) : launch_it(attention_tensor_kernel<__half>);
@@ -1318,6 +1582,12 @@ int sparbit_linear_attention_plan_set_workspace(sparbit_linear_attention_plan_t*
     p->work = nullptr;
     CU(cudaGetDevice(&p->device));
     CU(cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device));
+    if (p->dtype != SPARBIT_F32) {
+        cudaDriverEntryPointQueryResult found;
+        CU(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p->encode, 12000, cudaEnableDefault, &found));
+        if (!p->encode || found != cudaDriverEntryPointSuccess)
+            return record_cuda_error((int)cudaErrorNotSupported, "cuTensorMapEncodeTiled");
+    }
     char* base = (char*)dev;
     CU(cudaMemset(base, 0, 256));
     CU(cudaMemcpy(base + p->off_time(), p->time.data(), p->time.size() * sizeof(Segment), cudaMemcpyHostToDevice));
