@@ -142,9 +142,9 @@ __device__ __forceinline__ void tmem_load_16x32(uint32_t addr, float* z) {
 #pragma unroll
     for (int i = 0; i < 16; i++) z[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tmem_store_16x16(uint32_t addr, const uint32_t (&r)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), "r"(r[0]),
-                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+__device__ __forceinline__ void tmem_store_16x8(uint32_t addr, const uint32_t (&r)[4]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3])
                  : "memory");
 }
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
@@ -265,13 +265,11 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 
 // Warps of a CTA by what they do, in groups of four for tensor memory (whose lanes go by the warp's number mod 4) and
 // for the registers, of which each group gets as many as it needs.
-constexpr int kWeightWarps = 4, kOutWarps = 8, kPartWarps = 4, kStateWarps = 8, kLoadWarps = 2;
-constexpr int kFirstOut = kWeightWarps, kFirstPart = kFirstOut + kOutWarps, kFirstState = kFirstPart + kPartWarps,
-              kFirstLoad = kFirstState + kStateWarps, kMultiply = kFirstLoad + kLoadWarps, kMultiplyState = kMultiply + 1;
+constexpr int kWeightWarps = 4, kOutWarps = 8, kStateWarps = 8, kLoadWarps = 2;
+constexpr int kFirstOut = kWeightWarps, kFirstState = kFirstOut + kOutWarps, kFirstLoad = kFirstState + kStateWarps, kMultiply = kFirstLoad + kLoadWarps, kMultiplyState = kMultiply + 1;
 constexpr int kTensorThreads = 32 * (kFirstLoad + 4);
-constexpr int kRegisters = 72, kWeightRegisters = 72, kOutRegisters = 64, kPartRegisters = 56, kStateRegisters = 104,
-              kOtherRegisters = 40;
-static_assert(kWeightRegisters + 2 * kOutRegisters + kPartRegisters + 2 * kStateRegisters + kOtherRegisters <=
+constexpr int kRegisters = 80, kWeightRegisters = 64, kOutRegisters = 80, kStateRegisters = 104, kOtherRegisters = 48;
+static_assert(kWeightRegisters + 2 * kOutRegisters + 2 * kStateRegisters + kOtherRegisters <=
                   kTensorThreads / 128 * kRegisters,
               "more registers than the CTA has would be waited for without end");
 template <int kCount>
@@ -392,8 +390,8 @@ struct Tables {
     alignas(16) float left[kChunk];           // what a token's part is worth at the end of the chunk
     // for each warp d^31 .. d^0 (against time d^0 .. d^31), between numbers that are finite
     alignas(16) float powers[32 * (kWeightWarps + 2)];
-    // fp16: powers of two that rows of Z, of the weights and of c^T are held times
-    alignas(4) signed char z_exp[2][kMostSize], w_exp[2][kChunk], c_exp[2][kMostSize];
+    // fp16: powers of two that rows of Z and of the weights are held times
+    alignas(4) signed char z_exp[2][kMostSize], w_exp[2][kChunk];
 };
 constexpr uint32_t kTensorSmem = kRing + sizeof(Tables);
 static_assert(kTensorSmem <= 232448, "shared memory of a CTA");
@@ -478,11 +476,11 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
     if (threadIdx.x == 0) {
         for (int i = 0; i < g.stages; i++)
             bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, g.full ? kOutWarps : 1), bar_init(used + 8 * i, 1);
-        bar_init(scored, 1), bar_init(scaled, kWeightWarps), bar_init(weighted, kWeightWarps + kOutWarps + kPartWarps);
+        bar_init(scored, 1), bar_init(scaled, kWeightWarps), bar_init(weighted, kWeightWarps + kOutWarps + kStateWarps);
         bar_init(entered, 1), bar_init(done, 1);
-        for (int i = 0; i < 2; i++) bar_init(c_ready + 8 * i, kPartWarps), bar_init(c_free + 8 * i, 1);
+        for (int i = 0; i < 2; i++) bar_init(c_ready + 8 * i, kStateWarps), bar_init(c_free + 8 * i, 1);
         bar_init(added, 1), bar_init(add_free, kStateWarps), bar_init(z_ready, kStateWarps), bar_init(out_free, kOutWarps);
-        bar_init(met, kPartWarps);
+        bar_init(met, kStateWarps);
         tab.bad[0] = tab.bad[1] = 0;
         // rows of 128 swizzled bytes go by absolute addresses
         tab.gave_up = ring % 1024 != 0;
@@ -504,6 +502,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
 
     if (warp < kFirstOut) {
         // ---- weights: a token a lane
+        fewer_registers<kWeightRegisters>();
         const int row = warp * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         float* const powers = tab.powers + 32 + 32 * warp;
@@ -581,7 +580,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if (lane == 0) bar_arrive(weighted);
             }
         }
-    } else if (warp < kFirstPart) {
+    } else if (warp < kFirstState) {
         // ---- output: a token a lane, half of the values a warp
         fewer_registers<kOutRegisters>();
         const int quad = warp & 3, half = (warp - kFirstOut) >> 2, row = quad * 32 + lane;
@@ -681,11 +680,19 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if (lane == 0) bar_arrive(empty + 8 * st);
             }
         }
-    } else if (warp < kFirstState) {
-        // ---- c^T, scaled and in parts: a warp has 32 values, in two sets of 16; a lane tokens 2 (lane % 4) and the next of
-        // every 8, for rows lane / 4 and lane / 4 + 8 of a set
-        fewer_registers<kPartRegisters>();
-        const int t = threadIdx.x - 32 * kFirstPart, quad = warp & 3, matrix = lane >> 3, line = lane & 7;
+    } else if (warp < kFirstLoad) {
+        // ---- the state, and c^T for it: a warp has 16 values.  Of Z a lane has rows lane / 4 and lane / 4 + 8 and every
+        // fourth pair of keys - z[4 m ..]: keys 8 m + 2 (lane % 4) and the next of the first row, the same of the second -
+        // and of c^T tokens 2 (lane % 4) and the next of every 8, for the same rows
+        more_registers<kStateRegisters>();
+        const int v0 = (warp & 3) * 32 + ((warp - kFirstState) >> 2) * 16, value = v0 + (lane >> 2);
+        const int t = threadIdx.x - 32 * kFirstState;
+        const uint32_t lanes = (uint32_t)v0 << 16;
+        // where this lane's row of the four 8 x 8 matrices that ldmatrix and stmatrix take lies
+        const int matrix = lane >> 3, line = lane & 7;
+        const uint32_t z_lane = z_base + (v0 + (matrix & 1) * 8 + line) * 128;
+        const uint32_t c_lane = ((matrix >> 1) * 8 + line) * 128 + ((v0 >> 3) + (matrix & 1) >> 3) * kPanel +
+                                (((((v0 >> 3) + (matrix & 1)) & 7) ^ line) << 4);
         uint32_t pieces = 0, meetings = 0;
         // a barrier of these warps that gives up like every other wait
         auto meet = [&] {
@@ -696,109 +703,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
         for (int w = blockIdx.x; w < g.total && ok; w += gridDim.x) {
             const Work k = work_of(g, w);
             const Pass& p = *k.p;
-            const int panels_k = (p.kd + 63) / 64, sets = min(2, (p.vd - quad * 32 + 15) / 16);
-            for (int chunk = 0; chunk < k.chunks && ok; chunk++, c++) {
-                const uint32_t st = c % g.stages, c_tile = ring + st * g.stage_bytes + 2 * panels_k * kPanel;
-                const int n = tokens_of(k, chunk);
-                if (chunk == 0 || n < kChunk) {  // others are as the one before
-                    meet();
-                    tab.left[t] = t < n ? p.gain * exp2f(k.l2 * (p.reverse ? t + 1 - p.e : n - p.e - t)) : 0.0f;
-                    meet();
-                }
-                if (!ok || !warp_wait(full + 8 * st, (c / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
-                // four 8 x 8 matrices of 16 tokens and the values of a set, transposed
-                auto read = [&](int set, int token, uint32_t (&u)[4]) {
-                    const int v = quad * 4 + set * 2 + (matrix & 1);  // of 8
-                    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                                 : "r"(c_tile + (v >> 3) * kPanel + (token + (matrix >> 1) * 8 + line) * 128 + (((v & 7) ^ line) << 4))
-                                 : "memory");
-                };
-                const float* const left = tab.left + (lane & 3) * 2;
-                if constexpr (B::kScaled) {
-#pragma unroll 1
-                    for (int set = 0; set < sets; set++) {
-                        float most[2] = {0.0f, 0.0f};
-#pragma unroll 1
-                        for (int token = 0; token < kChunk; token += 16) {
-                            uint32_t u[4];
-                            read(set, token, u);
-#pragma unroll
-                            for (int i = 0; i < 4; i++) {
-                                const float2 f = *reinterpret_cast<const float2*>(left + token + (i >> 1) * 8);
-                                most[i & 1] = fmaxf(most[i & 1], fmaxf(fabsf(B::low(u[i]) * f.x), fabsf(B::high(u[i]) * f.y)));
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            const int e = exponent_for(max_of_row(most[i]));
-                            if ((lane & 3) == 0) tab.c_exp[c & 1][quad * 32 + set * 16 + i * 8 + (lane >> 2)] = (signed char)e;
-                        }
-                    }
-                    __syncwarp();
-                }
-                uint32_t most = 0;
-#pragma unroll 1
-                for (int q = 0; q < 4; q++, pieces++) {
-                    const uint32_t slot = pieces & 1;
-                    if (pieces >= 2 && !warp_wait(c_free + 8 * slot, (pieces / 2 - 1) & 1, gave_up, g.limit)) { ok = false; break; }
-                    fence_after();
-#pragma unroll 1
-                    for (int set = 0; set < sets; set++) {
-                        uint32_t part[kParts][8];
-                        float up[2] = {1.0f, 1.0f};
-                        if constexpr (B::kScaled) {
-#pragma unroll
-                            for (int i = 0; i < 2; i++)
-                                up[i] = power_of_two(tab.c_exp[c & 1][quad * 32 + set * 16 + i * 8 + (lane >> 2)]);
-                        }
-#pragma unroll
-                        for (int half = 0; half < 2; half++) {
-                            uint32_t u[4];
-                            read(set, q * 32 + half * 16, u);
-#pragma unroll
-                            for (int i = 0; i < 4; i++) {
-                                most = B::most(most, u[i]);
-                                const float2 f = *reinterpret_cast<const float2*>(left + q * 32 + half * 16 + (i >> 1) * 8);
-                                float2 x = mul2(make_float2(B::low(u[i]), B::high(u[i])), f);
-                                if constexpr (B::kScaled) x = mul2(x, make_float2(up[i & 1], up[i & 1]));
-#pragma unroll
-                                for (int y = 0; y < kParts; y++) part[y][half * 4 + i] = B::take(x);
-                            }
-                        }
-#pragma unroll
-                        for (int y = 0; y < kParts; y++)
-                            tmem_store_16x16(tmem + kColC + slot * kSlotCols + y * 16 + ((uint32_t)(quad * 32 + set * 16) << 16),
-                                             part[y]);
-                    }
-                    tmem_store_wait();
-                    if (q == 3 && g.full) {
-                        // not more than a chunk ahead of the output, for which the number of a chunk with odd values is left
-                        if (c > 0 && !warp_wait(done, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
-                        if (B::is_odd(most)) *(volatile uint32_t*)&tab.bad[c & 1] = c + 1;
-                    }
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        bar_arrive(c_ready + 8 * slot);
-                        if (q == 3 && g.full) bar_arrive(weighted);
-                    }
-                }
-            }
-        }
-    } else if (warp < kFirstLoad) {
-        // ---- the state: a warp has 16 values, a lane rows lane / 4 and lane / 4 + 8 of them and every fourth pair of keys:
-        // z[4 m ..]: keys 8 m + 2 (lane % 4) and the next of the first row, the same of the second
-        more_registers<kStateRegisters>();
-        const int v0 = (warp & 3) * 32 + ((warp - kFirstState) >> 2) * 16, value = v0 + (lane >> 2);
-        const uint32_t lanes = (uint32_t)v0 << 16;
-        // where this lane's row of the four 8 x 8 matrices that stmatrix takes lies
-        const int matrix = lane >> 3, line = lane & 7;
-        const uint32_t z_lane = z_base + (v0 + (matrix & 1) * 8 + line) * 128;
-        for (int w = blockIdx.x; w < g.total && ok; w += gridDim.x) {
-            const Work k = work_of(g, w);
-            const Pass& p = *k.p;
-            const int blocks = (p.kd + 15) / 16 * 2;  // of 8 keys
+            const int panels_k = (p.kd + 63) / 64, blocks = (p.kd + 15) / 16 * 2;  // of 8 keys
             const bool there = v0 < p.vd;
             float z[64];
             const float* from = state_in(k);
@@ -847,16 +752,94 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if (c > 0 && !warp_wait(entered, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
                 put(c);
             }
-            for (int chunk = 0; chunk < k.chunks; chunk++, c++) {
-                const float decay = exp2f(k.l2 * tokens_of(k, chunk));
-                if (!warp_wait(added, c & 1, gave_up, g.limit)) { ok = false; break; }
+            const float* const left = tab.left + (lane & 3) * 2;
+            float up[2] = {1.0f, 1.0f};
+            uint32_t most = 0, c_tile = 0;
+            // half a chunk ahead: while a chunk's products are on their way, two quarters of the next one are made
+            c--;
+            for (int chunk = -1; chunk < k.chunks && ok && k.chunks; chunk++, c++) {
+                const float down[2] = {1.0f / up[0], 1.0f / up[1]};
+#pragma unroll 1
+                for (int i = chunk < 0 ? 2 : 0; i < (chunk + 1 < k.chunks ? 4 : 2); i++, pieces++) {
+                    const int q = (i + 2) & 3;
+                    // 16 tokens of the warp's values, transposed
+                    auto read = [&](int token, uint32_t (&u)[4]) {
+                        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                                     : "r"(c_tile + token * 128)
+                                     : "memory");
+                    };
+                    if (i == 2) {
+                        const uint32_t next = c + 1, st = next % g.stages;
+                        const int n = tokens_of(k, chunk + 1);
+                        if (chunk < 0 || n < kChunk) {  // others are as the one before
+                            meet();
+                            if (t < kChunk)
+                                tab.left[t] = t < n ? p.gain * exp2f(k.l2 * (p.reverse ? t + 1 - p.e : n - p.e - t)) : 0.0f;
+                            meet();
+                        }
+                        if (!ok || !warp_wait(full + 8 * st, (next / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
+                        c_tile = ring + st * g.stage_bytes + 2 * panels_k * kPanel + c_lane;
+                        most = 0;
+                        if constexpr (B::kScaled) {
+                            float m[2] = {0.0f, 0.0f};
+                            if (there) {
+#pragma unroll 1
+                                for (int token = 0; token < kChunk; token += 16) {
+                                    uint32_t u[4];
+                                    read(token, u);
+#pragma unroll
+                                    for (int y = 0; y < 4; y++) {
+                                        const float2 f = *reinterpret_cast<const float2*>(left + token + (y >> 1) * 8);
+                                        m[y & 1] = fmaxf(m[y & 1], fmaxf(fabsf(B::low(u[y]) * f.x), fabsf(B::high(u[y]) * f.y)));
+                                    }
+                                }
+                            }
+#pragma unroll
+                            for (int y = 0; y < 2; y++) up[y] = power_of_two(exponent_for(max_of_row(m[y])));
+                        }
+                    }
+                    const uint32_t slot = pieces & 1;
+                    if (pieces >= 2 && !warp_wait(c_free + 8 * slot, (pieces / 2 - 1) & 1, gave_up, g.limit)) { ok = false; break; }
+                    fence_after();
+                    if (there) {
+#pragma unroll 1
+                        for (int token = q * 32; token < q * 32 + 32; token += 16) {
+                            uint32_t part[kParts][4], u[4];
+                            read(token, u);
+#pragma unroll
+                            for (int y = 0; y < 4; y++) {
+                                most = B::most(most, u[y]);
+                                const float2 f = *reinterpret_cast<const float2*>(left + token + (y >> 1) * 8);
+                                float2 x = mul2(make_float2(B::low(u[y]), B::high(u[y])), f);
+                                if constexpr (B::kScaled) x = mul2(x, make_float2(up[y & 1], up[y & 1]));
+#pragma unroll
+                                for (int m = 0; m < kParts; m++) part[m][y] = B::take(x);
+                            }
+#pragma unroll
+                            for (int y = 0; y < kParts; y++)
+                                tmem_store_16x8(tmem + kColC + slot * kSlotCols + y * 16 + (token & 16) / 2 + lanes, part[y]);
+                        }
+                        tmem_store_wait();
+                    }
+                    if (q == 3 && g.full) {
+                        // not more than a chunk ahead of the output, for which the number of a chunk with odd values is left
+                        if (c > 0 && !warp_wait(done, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
+                        if (there && B::is_odd(most)) *(volatile uint32_t*)&tab.bad[c & 1] = c + 1;
+                    }
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        bar_arrive(c_ready + 8 * slot);
+                        if (q == 3 && g.full) bar_arrive(weighted);
+                    }
+                }
+                if (chunk < 0) continue;
+                const int n = tokens_of(k, chunk);
+                const float decay = exp2f(k.l2 * n);
+                if (!ok || !warp_wait(added, c & 1, gave_up, g.limit)) { ok = false; break; }
                 fence_after();
                 if (there) {
-                    float down[2] = {1.0f, 1.0f};
-                    if constexpr (B::kScaled) {
-#pragma unroll
-                        for (int i = 0; i < 2; i++) down[i] = power_of_two(-tab.c_exp[c & 1][value + 8 * i]);
-                    }
 #pragma unroll
                     for (int b = 0; b < 4; b++) {
                         if (b * 4 >= blocks) break;
