@@ -1201,12 +1201,23 @@ __global__ void __launch_bounds__(256) attention_fold_kernel(const __grid_consta
     if (at < g.size) {
         float z = g.first[which] ? g.first[which][s * unit + (int64_t)h * g.size + at] : 0.0f;
         float* const states = g.states[which] + (int64_t)h * g.size + at;
-        for (int i = 0; i < n; i++) {
-            const int id = g.reverse[which] ? lo + n - 1 - i : lo + i;
-            const bool last = i + 1 == n && !g.summary[which];
-            const float here = last ? 0.0f : states[id * unit];
-            states[id * unit] = z;
-            z = fmaf(exp2f(l2 * (float)g.segments[id].len), z, here);
+        // a batch is read before any of it is written: the trips to memory do not wait for one another
+        constexpr int kBatch = 8;
+        for (int i0 = 0; i0 < n; i0 += kBatch) {
+            float here[kBatch], decay[kBatch];
+#pragma unroll
+            for (int y = 0; y < kBatch; y++) {
+                const int i = i0 + y, id = g.reverse[which] ? lo + n - 1 - i : lo + i;
+                here[y] = i + 1 < n || (i < n && g.summary[which]) ? states[id * unit] : 0.0f;
+                decay[y] = i < n ? exp2f(l2 * (float)g.segments[id].len) : 0.0f;
+            }
+#pragma unroll
+            for (int y = 0; y < kBatch; y++) {
+                const int i = i0 + y, id = g.reverse[which] ? lo + n - 1 - i : lo + i;
+                if (i >= n) break;
+                states[id * unit] = z;
+                z = fmaf(decay[y], z, here[y]);
+            }
         }
         if (g.summary[which])
             g.summary[which][s * (unit + g.heads) + g.heads + (int64_t)h * g.size + at] = z;
@@ -1721,7 +1732,7 @@ int sparbit_linear_attention_step(size_t rows, int heads, int key_size, int valu
         return SPARBIT_ERR_ALIAS;
     const bool wide = value_size % 4 == 0 && ((uintptr_t)state_in | (uintptr_t)state_out) % 16 == 0;
     // few rows: a head's values in slices of 32, a CTA each
-    const int slice = rows * heads < 4 * (size_t)kSms && value_size > 32 ? 32 : value_size;
+    const int slice = rows * heads < 2 * (size_t)kSms && value_size > 32 ? 32 : value_size;
     const dim3 grid((unsigned)(rows * heads), (unsigned)((value_size + slice - 1) / slice));
     auto go = [&]<typename T, bool kWide>() {
         CU(launch(attention_step_kernel<T, kWide>, grid, dim3(256), 0, (cudaStream_t)stream, heads, key_size, value_size, slice,

@@ -33,7 +33,7 @@ struct ClipArgs {
     const Tensor* tensors;
     const Chunk* chunks;        // by rank
     const int32_t* cta_begin;   // [CTAs + 1], chunks
-    const int32_t* rank_begin;  // [ranks + 1], chunks
+    const int32_t* rank_parts;  // [ranks][2], parts
     double* parts;              // part of rank r from CTA b at [b + r]: runs meet every rank from left to right
     unsigned* ticket;
     int n_ranks;
@@ -145,19 +145,11 @@ __global__ void __launch_bounds__(kThreads) clip_sums_kernel(const __grid_consta
     __threadfence();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int r = warp; r < g.n_ranks; r += kThreads / 32) {
-        const int begin = g.rank_begin[r], end = g.rank_begin[r + 1];
+        // runs are in order, so that a rank's parts lie side by side
+        const int lo_part = g.rank_parts[2 * r], hi_part = g.rank_parts[2 * r + 1];
         double s = 0.0;
-        if (begin < end) {
-            // CTAs that hold chunks of the rank: runs are in order
-            int first = 0, over = gridDim.x;
-            while (first + 1 < over) {
-                const int mid = (first + over) / 2;
-                if (g.cta_begin[mid] <= begin) first = mid;
-                else over = mid;
-            }
-            for (int b = first + lane; b < (int)gridDim.x && g.cta_begin[b] < end; b += 32)
-                if (g.cta_begin[b + 1] > begin && g.cta_begin[b + 1] > g.cta_begin[b]) s += __ldcg(g.parts + b + r);
-        }
+#pragma unroll 8
+        for (int i = lo_part + lane; i < hi_part; i += 32) s += __ldcg(g.parts + i);
 #pragma unroll
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kAllLanes, s, o);
         if (lane == 0) g.sums[r] = s;
@@ -237,7 +229,7 @@ struct sparbit_clip_plan_s {
     int n_ranks = 0, ctas = 0;
     std::vector<Tensor> tensors;
     std::vector<Chunk> chunks;
-    std::vector<int32_t> cta_begin, rank_begin;
+    std::vector<int32_t> cta_begin, rank_parts;
     char* work = nullptr;
     int device = -1;
     bool set = false, write = false;
@@ -246,7 +238,7 @@ struct sparbit_clip_plan_s {
     size_t off_chunks() const { return off_tensors() + round_up(tensors.size() * sizeof(Tensor), 256); }
     size_t off_ctas() const { return off_chunks() + round_up(chunks.size() * sizeof(Chunk), 256); }
     size_t off_ranks() const { return off_ctas() + round_up(cta_begin.size() * sizeof(int32_t), 256); }
-    size_t off_parts() const { return off_ranks() + round_up(rank_begin.size() * sizeof(int32_t), 256); }
+    size_t off_parts() const { return off_ranks() + round_up(rank_parts.size() * sizeof(int32_t), 256); }
     size_t work_bytes() const { return off_parts() + (size_t)(ctas + n_ranks) * sizeof(double); }
 };
 
@@ -266,7 +258,7 @@ ClipArgs common_args(const Plan* p) {
     g.tensors = (const Tensor*)(p->work + p->off_tensors());
     g.chunks = (const Chunk*)(p->work + p->off_chunks());
     g.cta_begin = (const int32_t*)(p->work + p->off_ctas());
-    g.rank_begin = (const int32_t*)(p->work + p->off_ranks());
+    g.rank_parts = (const int32_t*)(p->work + p->off_ranks());
     g.parts = (double*)(p->work + p->off_parts());
     g.ticket = (unsigned*)p->work;
     g.n_ranks = p->n_ranks;
@@ -302,7 +294,7 @@ int sparbit_clip_plan_create(int n_ranks, size_t n, const size_t* lengths, const
         }
         std::stable_sort(order.begin(), order.end(),
                          [&](int32_t a, int32_t b) { return p->tensors[a].rank < p->tensors[b].rank; });
-        p->rank_begin.assign((size_t)n_ranks + 1, 0);
+        std::vector<int32_t> begin((size_t)n_ranks + 1, 0);  // of each rank's chunks
         // about as many bytes for every CTA; a chunk counts for some more than it has
         std::vector<double> upto{0.0};
         for (int32_t i : order) {
@@ -313,9 +305,9 @@ int sparbit_clip_plan_create(int n_ranks, size_t n, const size_t* lengths, const
                 const double here = (double)std::min<int64_t>(kChunkElements, t.len - (int64_t)j * kChunkElements);
                 upto.push_back(upto.back() + here * (double)elem_size(t.type) + 2048.0);
             }
-            p->rank_begin[t.rank + 1] += each;
+            begin[t.rank + 1] += each;
         }
-        for (int r = 0; r < n_ranks; r++) p->rank_begin[r + 1] += p->rank_begin[r];
+        for (int r = 0; r < n_ranks; r++) begin[r + 1] += begin[r];
         p->ctas = (int)std::max<size_t>(1, std::min<size_t>(kMostCtas, p->chunks.size()));
         for (int b = 0; b <= p->ctas; b++) {
             const double until = upto.back() * b / p->ctas;
@@ -326,6 +318,15 @@ int sparbit_clip_plan_create(int n_ranks, size_t n, const size_t* lengths, const
             p->cta_begin.push_back(b == p->ctas ? (int32_t)p->chunks.size() : (int32_t)std::min(cut, p->chunks.size()));
         }
         p->cta_begin[0] = 0;
+        // the CTA that holds a chunk: the last whose run begins at it or before it
+        auto holder = [&](int32_t chunk) {
+            return (int32_t)(std::upper_bound(p->cta_begin.begin(), p->cta_begin.end() - 1, chunk) - p->cta_begin.begin()) - 1;
+        };
+        for (int r = 0; r < n_ranks; r++) {
+            const bool any = begin[r] < begin[r + 1];
+            p->rank_parts.push_back(any ? holder(begin[r]) + r : 0);
+            p->rank_parts.push_back(any ? holder(begin[r + 1] - 1) + r + 1 : 0);
+        }
     } catch (const std::bad_alloc&) {
         delete p;
         return SPARBIT_ERR_NOMEM;
@@ -352,7 +353,8 @@ int sparbit_clip_plan_set_workspace(sparbit_clip_plan_t* p, void* dev, size_t by
     if (!p->chunks.empty())
         CU(cudaMemcpy(base + p->off_chunks(), p->chunks.data(), p->chunks.size() * sizeof(Chunk), cudaMemcpyHostToDevice));
     CU(cudaMemcpy(base + p->off_ctas(), p->cta_begin.data(), p->cta_begin.size() * sizeof(int32_t), cudaMemcpyHostToDevice));
-    CU(cudaMemcpy(base + p->off_ranks(), p->rank_begin.data(), p->rank_begin.size() * sizeof(int32_t), cudaMemcpyHostToDevice));
+    CU(cudaMemcpy(base + p->off_ranks(), p->rank_parts.data(), p->rank_parts.size() * sizeof(int32_t), cudaMemcpyHostToDevice));
+    CU(cudaMemset(base + p->off_parts(), 0, (size_t)(p->ctas + p->n_ranks) * sizeof(double)));
     CU(cudaDeviceSynchronize());
     p->work = base;
     return SPARBIT_OK;

@@ -4,8 +4,8 @@
 //   g = dy weight;  dx = rstd (g - u mean(g u)) + dsum, u = r rstd;  dweight = sum dy u
 //
 // Bytes are the floor: a row is read once, stays in registers over the reduction and is written once.  A thread has up
-// to four units of eight neighbouring columns; a row belongs to 4 .. 32 lanes of a warp or to a CTA of its own, as
-// many threads as its units take.
+// to four units of eight neighbouring columns; a row belongs to 4 .. 32 lanes of a warp or to a CTA, as many threads as
+// its units take, which goes from row to row with the next one's loads on their way.
 #include <math.h>
 
 #include <algorithm>
@@ -18,7 +18,6 @@ using namespace spb;
 namespace {
 
 constexpr int kUnit = 8;             // columns of a unit
-constexpr int kMostUnits = 4;        // of a thread
 constexpr int kMostThreads = 1024;   // of a row
 constexpr int kShared = 256;         // threads of a CTA whose rows belong to 32 lanes or fewer
 constexpr int kParts = 592;          // CTAs that sum dweight: four an SM
@@ -46,19 +45,41 @@ struct NormBackArgs {
     int width, lanes, wide, weight_wide;
 };
 
+// A unit as it lies in memory: loaded a row ahead, converted when its turn comes.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, bool wide, float (&v)[kUnit]) {
+struct Raw {
+    static constexpr int kPacks = kUnit * sizeof(T) / 16;
+    uint4 v[kPacks];
+};
+template <typename T>
+__device__ __forceinline__ void load_raw(const T* p, int n, bool wide, Raw<T>& r) {
     if (wide && n >= kUnit) {
-        constexpr int A = 16 / sizeof(T);
 #pragma unroll
-        for (int i = 0; i < kUnit; i += A) {
-            const Pack<T, A> k = *reinterpret_cast<const Pack<T, A>*>(p + i);
+        for (int i = 0; i < Raw<T>::kPacks; i++) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+        return;
+    }
+    uint32_t w[Raw<T>::kPacks * 4];
 #pragma unroll
-            for (int j = 0; j < A; j++) v[i + j] = to_float(k.v[j]);
+    for (int i = 0; i < Raw<T>::kPacks * 4; i++) {
+        if constexpr (sizeof(T) == 4) {
+            w[i] = i < n ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
+        } else {
+            const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+            w[i] = 2 * i < n ? q[2 * i] : 0u;
+            if (2 * i + 1 < n) w[i] |= (uint32_t)q[2 * i + 1] << 16;
         }
-    } else {
+    }
 #pragma unroll
-        for (int i = 0; i < kUnit; i++) v[i] = i < n ? to_float(p[i]) : 0.0f;
+    for (int i = 0; i < Raw<T>::kPacks; i++) r.v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+template <typename T>
+__device__ __forceinline__ void convert(const Raw<T>& r, float (&f)[kUnit]) {
+    constexpr int A = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < Raw<T>::kPacks; i++) {
+        const Pack<T, A> k = reinterpret_cast<const Pack<T, A>&>(r.v[i]);
+#pragma unroll
+        for (int j = 0; j < A; j++) f[i * A + j] = to_float(k.v[j]);
     }
 }
 template <typename T>
@@ -112,159 +133,188 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     return r;
 }
 
+// kMost: threads of a CTA; those of 256 come several to an SM.
 template <typename T, typename W, int U, int kMost>
-__global__ void __launch_bounds__(kMost) norm_forward_kernel(const __grid_constant__ NormArgs g) {
+__global__ void __launch_bounds__(kMost, kMost == 256 ? 3 : 1) norm_forward_kernel(const __grid_constant__ NormArgs g) {
     __shared__ float sm[64];
     int turn = 0;
     pdl_wait();
     pdl_trigger();
-    const int lanes = g.lanes, t = threadIdx.x % lanes;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / lanes) + threadIdx.x / lanes;
-    const bool there = row < g.rows;
-    float r[U][kUnit];
-    float squares = 0.0f;
+    const int lanes = g.lanes, t = threadIdx.x % lanes, together = blockDim.x / lanes;
+    Raw<W> weight[U];
+    Raw<T> x[U], e[U];
+    int left[U];  // columns from this unit's first to the end of the row
 #pragma unroll
     for (int u = 0; u < U; u++) {
-        const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
-        if (n > 0) {
-            load8((const T*)g.x + row * g.x_ld + col, n, g.wide, r[u]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kUnit; i++) r[u][i] = 0.0f;
-        }
+        left[u] = g.width - (u * lanes + t) * kUnit;
+        if (g.weight && left[u] > 0) load_raw((const W*)g.weight + (u * lanes + t) * kUnit, left[u], g.weight_wide, weight[u]);
     }
-    if (g.residual) {
-        float e[U][kUnit];
+    auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
-            if (n > 0) load8((const T*)g.residual + row * g.residual_ld + col, n, g.wide, e[u]);
+            if (row >= g.rows || left[u] <= 0) continue;
+            const int col = (u * lanes + t) * kUnit;
+            load_raw((const T*)g.x + row * g.x_ld + col, left[u], g.wide, x[u]);
+            if (g.residual) load_raw((const T*)g.residual + row * g.residual_ld + col, left[u], g.wide, e[u]);
         }
+    };
+    fetch((int64_t)blockIdx.x * together + threadIdx.x / lanes);
+    // all threads of a CTA go round equally often
+    for (int64_t row0 = (int64_t)blockIdx.x * together; row0 < g.rows; row0 += (int64_t)gridDim.x * together) {
+        const int64_t row = row0 + threadIdx.x / lanes;
+        const bool there = row < g.rows;
+        float r[U][kUnit];
+        float squares = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int n = there ? g.width - (u * lanes + t) * kUnit : 0;
-            if (n > 0) {
-                // what is kept is what is normalised
+            if (there && left[u] > 0) {
+                convert(x[u], r[u]);
+                if (g.residual) {
+                    float f[kUnit];
+                    convert(e[u], f);
+                    // what is kept is what is normalised
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) r[u][i] = to_float(from_float<T>(r[u][i] + e[u][i]));
+                    for (int i = 0; i < kUnit; i++) r[u][i] = to_float(from_float<T>(r[u][i] + f[i]));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kUnit; i++) r[u][i] = 0.0f;
             }
         }
-    }
+        fetch(row + (int64_t)gridDim.x * together);
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-        const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
-        if (g.sum && n > 0) store8((T*)g.sum + row * g.sum_ld + col, n, g.wide, r[u]);
+        for (int u = 0; u < U; u++) {
+            if (g.sum && there && left[u] > 0) store8((T*)g.sum + row * g.sum_ld + (u * lanes + t) * kUnit, left[u], g.wide, r[u]);
 #pragma unroll
-        for (int i = 0; i < kUnit; i++) squares = fmaf(r[u][i], r[u][i], squares);
-    }
-    squares = over_row<RowSum>(squares, lanes, sm, turn);
-    float rstd = 1.0f / sqrtf(squares / g.width + g.eps);
-    const bool big = !(squares < 1e38f);
-    if (lanes <= 32 ? __any_sync(kAllLanes, big) : big) {
-        // squares that 32 bits do not hold: once more, scaled.  All threads that reduce together take the same way.
-        float most = 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < kUnit; i++) most = RowMax::of(most, fabsf(r[u][i]));
-        most = over_row<RowMax>(most, lanes, sm, turn);
-        const float by = most < INFINITY && most > 0.0f ? exp2f((float)-ilogbf(most)) : 1.0f;
-        float again = 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < kUnit; i++) again = fmaf(r[u][i] * by, r[u][i] * by, again);
-        again = over_row<RowSum>(again, lanes, sm, turn);
-        if (big) rstd = by / sqrtf(again / g.width + g.eps * by * by);
-    }
-    if (g.rstd && there && t == 0) g.rstd[row] = rstd;
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-        const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
-        if (g.weight && n > 0) {
-            float w[kUnit];
-            load8((const W*)g.weight + col, n, g.weight_wide, w);
-#pragma unroll
-            for (int i = 0; i < kUnit; i++) r[u][i] = i < n ? r[u][i] * rstd * w[i] : 0.0f;
-        } else {
-#pragma unroll
-            for (int i = 0; i < kUnit; i++) r[u][i] = i < n ? r[u][i] * rstd : 0.0f;
+            for (int i = 0; i < kUnit; i++) squares = fmaf(r[u][i], r[u][i], squares);
         }
-        if (g.y && n > 0) store8((T*)g.y + row * g.y_ld + col, n, g.wide, r[u]);
-    }
-    if (!g.y8) return;
-    float row_most = 0.0f;
-    if (!g.block) {
+        squares = over_row<RowSum>(squares, lanes, sm, turn);
+        float rstd = 1.0f / sqrtf(squares / g.width + g.eps);
+        const bool big = !(squares < 1e38f);
+        if (lanes <= 32 ? __any_sync(kAllLanes, big) : big) {
+            // squares that 32 bits do not hold: once more, scaled.  All threads that reduce together take the same way.
+            float most = 0.0f;
 #pragma unroll
-        for (int u = 0; u < U; u++)
+            for (int u = 0; u < U; u++)
 #pragma unroll
-            for (int i = 0; i < kUnit; i++) row_most = RowMax::of(row_most, fabsf(r[u][i]));
-        row_most = over_row<RowMax>(row_most, lanes, sm, turn);
-    }
+                for (int i = 0; i < kUnit; i++) most = RowMax::of(most, fabsf(r[u][i]));
+            most = over_row<RowMax>(most, lanes, sm, turn);
+            const float by = most < INFINITY && most > 0.0f ? exp2f((float)-ilogbf(most)) : 1.0f;
+            float again = 0.0f;
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-        const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
-        float most = row_most;
-        if (g.block) {
-            most = 0.0f;
+            for (int u = 0; u < U; u++)
 #pragma unroll
-            for (int i = 0; i < kUnit; i++) most = RowMax::of(most, fabsf(r[u][i]));
-            most = over_lanes<RowMax>(most, min(g.block / kUnit, lanes));
+                for (int i = 0; i < kUnit; i++) again = fmaf(r[u][i] * by, r[u][i] * by, again);
+            again = over_row<RowSum>(again, lanes, sm, turn);
+            if (big) rstd = by / sqrtf(again / g.width + g.eps * by * by);
         }
-        if (n <= 0) continue;
-        if (most < 1e-30f) most = 1e-30f;
-        if (g.block ? col % g.block == 0 : col == 0)
-            g.scales[row * g.scales_ld + (g.block ? col / g.block : 0)] = most / 448.0f;
-        const float by = 448.0f / most;
-        uint2 q;
-        q.x = e4m3x2(r[u][0] * by, r[u][1] * by) | e4m3x2(r[u][2] * by, r[u][3] * by) << 16;
-        q.y = e4m3x2(r[u][4] * by, r[u][5] * by) | e4m3x2(r[u][6] * by, r[u][7] * by) << 16;
-        uint8_t* to = g.y8 + row * g.y8_ld + col;
-        if (g.y8_wide && n >= kUnit) {
-            *reinterpret_cast<uint2*>(to) = q;
-        } else {
+        if (g.rstd && there && t == 0) g.rstd[row] = rstd;
 #pragma unroll
-            for (int i = 0; i < kUnit; i++)
-                if (i < n) to[i] = (uint8_t)((i < 4 ? q.x : q.y) >> (i & 3) * 8);
+        for (int u = 0; u < U; u++) {
+            if (g.weight && left[u] > 0) {
+                float w[kUnit];
+                convert(weight[u], w);
+#pragma unroll
+                for (int i = 0; i < kUnit; i++) r[u][i] = i < left[u] ? r[u][i] * rstd * w[i] : 0.0f;
+            } else {
+#pragma unroll
+                for (int i = 0; i < kUnit; i++) r[u][i] = i < left[u] ? r[u][i] * rstd : 0.0f;
+            }
+            if (g.y && there && left[u] > 0) store8((T*)g.y + row * g.y_ld + (u * lanes + t) * kUnit, left[u], g.wide, r[u]);
+        }
+        if (!g.y8) continue;
+        float row_most = 0.0f;
+        if (!g.block) {
+#pragma unroll
+            for (int u = 0; u < U; u++)
+#pragma unroll
+                for (int i = 0; i < kUnit; i++) row_most = RowMax::of(row_most, fabsf(r[u][i]));
+            row_most = over_row<RowMax>(row_most, lanes, sm, turn);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int col = (u * lanes + t) * kUnit;
+            float most = row_most;
+            if (g.block) {
+                most = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kUnit; i++) most = RowMax::of(most, fabsf(r[u][i]));
+                most = over_lanes<RowMax>(most, min(g.block / kUnit, lanes));
+            }
+            if (!there || left[u] <= 0) continue;
+            if (most < 1e-30f) most = 1e-30f;
+            if (g.block ? col % g.block == 0 : col == 0)
+                g.scales[row * g.scales_ld + (g.block ? col / g.block : 0)] = most / 448.0f;
+            const float by = 448.0f / most;
+            uint2 q;
+            q.x = e4m3x2(r[u][0] * by, r[u][1] * by) | e4m3x2(r[u][2] * by, r[u][3] * by) << 16;
+            q.y = e4m3x2(r[u][4] * by, r[u][5] * by) | e4m3x2(r[u][6] * by, r[u][7] * by) << 16;
+            uint8_t* to = g.y8 + row * g.y8_ld + col;
+            if (g.y8_wide && left[u] >= kUnit) {
+                *reinterpret_cast<uint2*>(to) = q;
+            } else {
+#pragma unroll
+                for (int i = 0; i < kUnit; i++)
+                    if (i < left[u]) to[i] = (uint8_t)((i < 4 ? q.x : q.y) >> (i & 3) * 8);
+            }
         }
     }
 }
 
 template <typename T, typename W, int U, int kMost>
-__global__ void __launch_bounds__(kMost) norm_backward_kernel(const __grid_constant__ NormBackArgs g) {
+__global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) norm_backward_kernel(const __grid_constant__ NormBackArgs g) {
     extern __shared__ float partial[];
     __shared__ float sm[64];
     int turn = 0;
     pdl_wait();
     pdl_trigger();
     const int lanes = g.lanes, t = threadIdx.x % lanes, together = blockDim.x / lanes;
+    Raw<W> weight[U];
+    Raw<T> raw_d[U], raw_x[U], raw_m[U];
+    float next_rstd = 0.0f;
     float dw[U][kUnit];
+    int left[U];
 #pragma unroll
-    for (int u = 0; u < U; u++)
+    for (int u = 0; u < U; u++) {
+        left[u] = g.width - (u * lanes + t) * kUnit;
+        if (g.weight && left[u] > 0) load_raw((const W*)g.weight + (u * lanes + t) * kUnit, left[u], g.weight_wide, weight[u]);
 #pragma unroll
         for (int i = 0; i < kUnit; i++) dw[u][i] = 0.0f;
-    // all threads of a warp go round equally often
+    }
+    auto fetch = [&](int64_t row) {
+        next_rstd = row < g.rows ? g.rstd[row] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (row >= g.rows || left[u] <= 0) continue;
+            const int col = (u * lanes + t) * kUnit;
+            load_raw((const T*)g.dy + row * g.dy_ld + col, left[u], g.wide, raw_d[u]);
+            load_raw((const T*)g.sum + row * g.sum_ld + col, left[u], g.wide, raw_x[u]);
+            if (g.dsum) load_raw((const T*)g.dsum + row * g.dsum_ld + col, left[u], g.wide, raw_m[u]);
+        }
+    };
+    fetch((int64_t)blockIdx.x * together + threadIdx.x / lanes);
     for (int64_t row0 = (int64_t)blockIdx.x * together; row0 < g.rows; row0 += (int64_t)gridDim.x * together) {
         const int64_t row = row0 + threadIdx.x / lanes;
         const bool there = row < g.rows;
-        const float rstd = there ? g.rstd[row] : 0.0f;
+        const float rstd = next_rstd;
         float d[U][kUnit], x[U][kUnit];
+        Raw<T> more[U];
         float inner = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
-            if (n > 0) {
-                load8((const T*)g.dy + row * g.dy_ld + col, n, g.wide, d[u]);
-                load8((const T*)g.sum + row * g.sum_ld + col, n, g.wide, x[u]);
+            if (there && left[u] > 0) {
+                convert(raw_d[u], d[u]);
+                convert(raw_x[u], x[u]);
+                more[u] = raw_m[u];
             } else {
 #pragma unroll
                 for (int i = 0; i < kUnit; i++) d[u][i] = x[u][i] = 0.0f;
             }
         }
+        fetch(row + (int64_t)gridDim.x * together);
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
-            if (n <= 0) continue;
+            if (!there || left[u] <= 0) continue;
 #pragma unroll
             for (int i = 0; i < kUnit; i++) {
                 x[u][i] *= rstd;
@@ -272,7 +322,7 @@ __global__ void __launch_bounds__(kMost) norm_backward_kernel(const __grid_const
             }
             if (g.weight) {
                 float w[kUnit];
-                load8((const W*)g.weight + col, n, g.weight_wide, w);
+                convert(weight[u], w);
 #pragma unroll
                 for (int i = 0; i < kUnit; i++) d[u][i] *= w[i];
             }
@@ -282,25 +332,25 @@ __global__ void __launch_bounds__(kMost) norm_backward_kernel(const __grid_const
         inner = over_row<RowSum>(inner, lanes, sm, turn) / g.width;
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int col = (u * lanes + t) * kUnit, n = there ? g.width - col : 0;
-            if (n <= 0) continue;
-            float more[kUnit];
+            if (!there || left[u] <= 0) continue;
+            float m[kUnit];
+            if (g.dsum) {
+                convert(more[u], m);
+            } else {
 #pragma unroll
-            for (int i = 0; i < kUnit; i++) more[i] = 0.0f;
-            if (g.dsum) load8((const T*)g.dsum + row * g.dsum_ld + col, n, g.wide, more);
+                for (int i = 0; i < kUnit; i++) m[i] = 0.0f;
+            }
 #pragma unroll
-            for (int i = 0; i < kUnit; i++) d[u][i] = fmaf(rstd, d[u][i] - x[u][i] * inner, more[i]);
-            store8((T*)g.dx + row * g.dx_ld + col, n, g.wide, d[u]);
+            for (int i = 0; i < kUnit; i++) d[u][i] = fmaf(rstd, d[u][i] - x[u][i] * inner, m[i]);
+            store8((T*)g.dx + row * g.dx_ld + (u * lanes + t) * kUnit, left[u], g.wide, d[u]);
         }
     }
     if (!g.parts) return;
     float* const out = g.parts + (int64_t)blockIdx.x * g.width;
     if (together == 1) {
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int col = (u * lanes + t) * kUnit;
-            if (col < g.width) store8(out + col, g.width - col, g.width % 4 == 0, dw[u]);
-        }
+        for (int u = 0; u < U; u++)
+            if (left[u] > 0) store8(out + (u * lanes + t) * kUnit, left[u], g.width % 4 == 0, dw[u]);
         return;
     }
     const int columns = U * lanes * kUnit;
@@ -349,10 +399,10 @@ namespace {
 
 using Plan = sparbit_norm_plan_s;
 
-// Threads of a row and units of a thread.  Many rows: up to four units, which keeps loads in flight; few: one, which
-// is done soonest.
+// Threads of a row, units of a thread, CTAs an SM holds.  Two units a thread with the next row's on their way keep
+// enough loads in flight; one where there are few rows, which is done soonest; four where two do not reach.
 struct Shape {
-    int lanes, units, threads;
+    int lanes, units, threads, per_sm;
 };
 Shape shape_of(const Plan* p, size_t rows) {
     const int all = (p->width + kUnit - 1) / kUnit;
@@ -361,21 +411,23 @@ Shape shape_of(const Plan* p, size_t rows) {
         s.lanes = 4, s.units = 1;
         while (s.lanes < all) s.lanes *= 2;
     } else {
-        s.units = rows < 4 * kSms ? (all + kMostThreads - 1) / kMostThreads : std::min(kMostUnits, (all + 31) / 32);
+        s.units = (all + kMostThreads - 1) / kMostThreads;
+        if (s.units == 1 && rows >= 4 * kSms) s.units = 2;
         if (s.units == 3) s.units = 4;
         s.lanes = ((all + s.units - 1) / s.units + 31) / 32 * 32;
     }
     s.threads = s.lanes <= 32 ? kShared : s.lanes;
+    s.per_sm = s.threads <= 256 ? 768 / s.threads : std::max(1, 1024 / s.threads);
     return s;
 }
 
-// f.operator()<T, W, U, kMost>() for the plan's types, the units of a thread and the most threads of a CTA: 256 leave
-// each the registers for four units.
+// f.operator()<T, W, U, kMost>() for the plan's types, the units of a thread and the most threads of a CTA.
 template <typename T, typename W, typename Fn>
 int by_shape(const Shape& s, Fn f) {
-    if (s.units == 1) return f.template operator()<T, W, 1, 1024>();
-    if (s.units == 2) return f.template operator()<T, W, 2, 1024>();
-    if (s.threads <= 256) return f.template operator()<T, W, 4, 256>();
+    if (s.units == 1)
+        return s.threads <= 256 ? f.template operator()<T, W, 1, 256>() : f.template operator()<T, W, 1, 1024>();
+    if (s.units == 2)
+        return s.threads <= 256 ? f.template operator()<T, W, 2, 256>() : f.template operator()<T, W, 2, 1024>();
     return f.template operator()<T, W, 4, 1024>();
 }
 template <typename Fn>
@@ -465,10 +517,9 @@ int sparbit_norm_forward(sparbit_norm_plan_t* p, size_t rows, const void* x, siz
     g.block = p->block, g.scales_ld = (int)per_row, g.eps = p->eps;
     const Shape s = shape_of(p, rows);
     g.lanes = s.lanes;
-    const unsigned together = s.threads / s.lanes;
+    const size_t together = s.threads / s.lanes, grid = std::min((size_t)(kSms * s.per_sm), (rows + together - 1) / together);
     return by_types(p, s, [&]<typename T, typename W, int U, int kMost>() {
-        CU(launch(norm_forward_kernel<T, W, U, kMost>, dim3((unsigned)((rows + together - 1) / together)), dim3(s.threads), 0,
-                  (cudaStream_t)stream, g));
+        CU(launch(norm_forward_kernel<T, W, U, kMost>, dim3((unsigned)grid), dim3(s.threads), 0, (cudaStream_t)stream, g));
         return (int)SPARBIT_OK;
     });
 }
@@ -509,7 +560,7 @@ int sparbit_norm_backward(sparbit_norm_plan_t* p, size_t rows, const void* dy, s
     const Shape s = shape_of(p, rows);
     g.lanes = s.lanes;
     const size_t together = s.threads / s.lanes;
-    const int grid = (int)std::min<size_t>(kParts, (rows + together - 1) / together);
+    const int grid = (int)std::min<size_t>(std::min(kParts, kSms * s.per_sm), (rows + together - 1) / together);
     if (grid > 0) {
         const size_t smem = together > 1 ? sizeof(float) * s.threads * s.units * kUnit : 0;
         const int e = by_types(p, s, [&]<typename T, typename W, int U, int kMost>() {
