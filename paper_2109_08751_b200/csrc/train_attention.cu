@@ -91,8 +91,8 @@ __device__ __forceinline__ float log2_decay(const float* log_decay, int h) {
 // ---- tensor memory ------------------------------------------------------------------------------
 
 // Columns (32 bits of 128 lanes each): scores, then in their place the weights that multiply c; out; the state's
-// addition; a ring of two pieces of c^T, 32 tokens each in up to three parts.
-constexpr uint32_t kColScore = 0, kColOut = 128, kColAdd = 256, kColC = 384, kSlotCols = 48;
+// addition; a ring of two pieces of c^T, 32 tokens each in up to four parts.
+constexpr uint32_t kColScore = 0, kColOut = 128, kColAdd = 256, kColC = 384, kSlotCols = 64;
 
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
     asm volatile(
@@ -200,23 +200,32 @@ struct Bits;
 template <>
 struct Bits<__nv_bfloat16> {
     static constexpr bool kScaled = false;  // the exponents of 32 bits: nothing to scale
-    static constexpr int kParts = 3;        // parts that hold a number of 32 bits
+    static constexpr int kParts = 4;        // parts that hold a number of 32 bits
     static constexpr uint32_t kFormat = (1u << 7) | (1u << 10);
-    // The leading 8 bits of two numbers, which are then without them: three of these hold all 24 bits.
-    static __device__ __forceinline__ uint32_t take(float2& x) {
-        const uint32_t a = __float_as_uint(x.x), b = __float_as_uint(x.y);
-        x = fma2(make_float2(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u)), make_float2(-1.0f, -1.0f), x);
-        return __byte_perm(a, b, 0x7632);
+    // c times weights w1 + w2 + w3 (the leading, the next and the last 8 bits of 32-bit ones), two tokens: the product with
+    // w1 as the two numbers that hold its 16 bits, that with w2 as its leading and its last bits, to which w3's is added.
+    static __device__ __forceinline__ void parts_of(uint32_t c, const uint4& w, uint32_t (&part)[4]) {
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(part[0]) : "r"(c), "r"(w.x));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(part[1]) : "r"(c), "r"(w.x), "r"(part[0] ^ 0x80008000u));
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(part[2]) : "r"(c), "r"(w.y));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(part[3]) : "r"(c), "r"(w.y), "r"(part[2] ^ 0x80008000u));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(part[3]) : "r"(c), "r"(w.z), "r"(part[3]));
     }
-    static __device__ __forceinline__ bool is_odd(uint32_t v) { return (v & 0x7fffu) >= 0x7f80u || (v >> 16 & 0x7fffu) >= 0x7f80u; }
+    static __device__ __forceinline__ void put_weight(uint32_t* table, int token, float w) {
+#pragma unroll
+        for (int i = 0; i < 3; i++) {
+            const __nv_bfloat16 v = __float2bfloat16_rn(w);
+            reinterpret_cast<__nv_bfloat16*>(table)[(token >> 1) * 8 + i * 2 + (token & 1)] = v;
+            w -= __bfloat162float(v);
+        }
+    }
+    // part 1 of an infinity or a NaN is a NaN, and makes `odd` one
+    static __device__ __forceinline__ void note_odd(uint32_t& odd, uint32_t part) {
+        asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(odd) : "r"(part), "r"(0u));
+    }
+    static __device__ __forceinline__ bool is_odd(uint32_t v) { return (v & 0x7fff7fffu) != 0; }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&v);
-    }
-    // larger of the magnitudes of two pairs, a NaN being larger than everything
-    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
-        const __nv_bfloat162 v = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a),
-                                             __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
         return *reinterpret_cast<const uint32_t*>(&v);
     }
     static __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
@@ -238,9 +247,11 @@ struct Bits<__half> {
         const __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&v);
     }
-    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
-        const __half2 v = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), __habs2(*reinterpret_cast<const __half2*>(&b)));
-        return *reinterpret_cast<const uint32_t*>(&v);
+    static __device__ __forceinline__ void put_weight(uint32_t* table, int token, float w) { table[token] = __float_as_uint(w); }
+    // the larger of the magnitudes, a NaN being larger than everything
+    static __device__ __forceinline__ void note_odd(uint32_t& odd, uint32_t v) {
+        const __half2 m = __hmax2_nan(*reinterpret_cast<const __half2*>(&odd), __habs2(*reinterpret_cast<const __half2*>(&v)));
+        odd = *reinterpret_cast<const uint32_t*>(&m);
     }
     static __device__ __forceinline__ float low(uint32_t v) { return __half2float(__ushort_as_half((unsigned short)v)); }
     static __device__ __forceinline__ float high(uint32_t v) {
@@ -387,7 +398,8 @@ struct Tables {
         add_free, z_ready, out_free, met;
     uint32_t tmem, gave_up;
     uint32_t bad[2];  // number of the last (every other) chunk whose c holds an infinity or a NaN
-    alignas(16) float left[kChunk];           // what a token's part is worth at the end of the chunk
+    // what a token's part is worth at the end of the chunk: fp16 as floats, bf16 as three numbers for each pair of tokens
+    alignas(16) uint32_t left[2 * kChunk];
     // for each warp d^31 .. d^0 (against time d^0 .. d^31), between numbers that are finite
     alignas(16) float powers[32 * (kWeightWarps + 2)];
     // fp16: powers of two that rows of Z and of the weights are held times
@@ -396,37 +408,18 @@ struct Tables {
 constexpr uint32_t kTensorSmem = kRing + sizeof(Tables);
 static_assert(kTensorSmem <= 232448, "shared memory of a CTA");
 
-// 32 columns of a row of out, rounded into shared memory at `own` (the row's; pieces of 16 bytes in swizzled order).
+// c holds an infinity or a NaN, which a product would carry to the tokens in front of it (times their weight of zero):
+// adds the tokens that count for this lane's row one by one, for 32 columns.
 template <typename B>
-__device__ __forceinline__ void round_out(const uint32_t (&r)[32], float down, uint32_t own, int b, int lane) {
-#pragma unroll
-    for (int j = 0; j < 32; j += 8) {
-        uint32_t v[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            float2 x = make_float2(__uint_as_float(r[j + 2 * i]), __uint_as_float(r[j + 2 * i + 1]));
-            if constexpr (B::kScaled) x = mul2(x, make_float2(down, down));
-            v[i] = B::pack(x.x, x.y);
-        }
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(own + (((b * 4 + j / 8) ^ (lane & 7)) << 4)), "r"(v[0]),
-                     "r"(v[1]), "r"(v[2]), "r"(v[3])
-                     : "memory");
-    }
-}
-// The same where c holds an infinity or a NaN, which a product would carry to the tokens in front of it (times their
-// weight of zero): adds the tokens that count for this lane's row one by one.
-template <typename B>
-__device__ __forceinline__ void round_out_by_hand(uint32_t out, uint32_t weights, uint32_t c_tile, int b, int row, bool reverse,
-                                                  float down, uint32_t own) {
-    const int lane = row & 31;
-    uint32_t r[32];
-    tmem_load32(out, r);
+__device__ __forceinline__ void add_by_hand(uint32_t (&r)[32], uint32_t weights, uint32_t c_tile, int b, int row, bool reverse) {
+#pragma unroll 1
     for (int j = reverse ? row & ~31 : 0; j <= (reverse ? kChunk - 1 : row | 31); j += 2) {
         uint32_t pair;
         asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;"
                      : "=r"(pair)
                      : "r"(weights + j / 2)
                      : "memory");
+#pragma unroll 1
         for (int i = 0; i < 2; i++) {
             const int token = j + i;
             if (reverse ? token < row : token > row) continue;
@@ -447,7 +440,6 @@ __device__ __forceinline__ void round_out_by_hand(uint32_t out, uint32_t weights
         }
         __syncwarp();
     }
-    round_out<B>(r, down, own, b, lane);
 }
 
 // One CTA per SM, its warps in roles: weights, output, parts of c, state, loads, products.  A chunk is
@@ -626,23 +618,39 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if (!warp_wait(done, c & 1, gave_up, g.limit)) { ok = false; break; }
                 fence_after();
                 const bool by_hand = *(volatile uint32_t*)&tab.bad[c & 1] == c + 1;
-                // in 16 bits over the tiles of a and b, once the state's products have read b too
-                if (!warp_wait(used + 8 * st, (c / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
+                // in 16 bits over the tiles of a and b
                 const uint32_t own = stage + quad * 32 * pitch;
-#pragma unroll 1
-                for (int b = b0; b < b1; b++) {
-                    if (by_hand) {
-                        round_out_by_hand<B>(tmem + kColOut + lanes + b * 32, tmem + kColScore + lanes,
-                                             stage + 2 * panels_k * kPanel, b, row, p.reverse, down, own + lane * pitch);
-                        continue;
-                    }
+                uint32_t v[2][16];
+#pragma unroll
+                for (int b = 0; b < 2; b++) {
+                    if (b0 + b >= b1) break;
                     uint32_t r[32];
-                    tmem_load32(tmem + kColOut + lanes + b * 32, r);
-                    round_out<B>(r, down, own + lane * pitch, b, lane);
+                    tmem_load32(tmem + kColOut + lanes + (b0 + b) * 32, r);
+                    if (by_hand)
+                        add_by_hand<B>(r, tmem + kColScore + lanes, stage + 2 * panels_k * kPanel, b0 + b, row, p.reverse);
+#pragma unroll
+                    for (int j = 0; j < 16; j++) {
+                        float2 x = make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+                        if constexpr (B::kScaled) x = mul2(x, make_float2(down, down));
+                        v[b][j] = B::pack(x.x, x.y);
+                    }
                 }
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(out_free);
+                // once the state's products have read b too
+                if (!warp_wait(used + 8 * st, (c / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
+#pragma unroll
+                for (int b = 0; b < 2; b++) {
+                    if (b0 + b >= b1) break;
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                                         own + lane * pitch + ((((b0 + b) * 4 + j) ^ (lane & 7)) << 4)),
+                                     "r"(v[b][4 * j]), "r"(v[b][4 * j + 1]), "r"(v[b][4 * j + 2]), "r"(v[b][4 * j + 3])
+                                     : "memory");
+                }
+                __syncwarp();
                 T* const to = (T*)p.out + first_row(k, chunk) * p.out_ld + (int64_t)k.head * p.vd;
                 const int64_t way = p.out_ld;
                 const int rows = min(32, n - quad * 32);
@@ -752,9 +760,10 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if (c > 0 && !warp_wait(entered, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
                 put(c);
             }
-            const float* const left = tab.left + (lane & 3) * 2;
+            const float* const left = reinterpret_cast<const float*>(tab.left) + (lane & 3) * 2;  // fp16
+            const uint4* const pairs = reinterpret_cast<const uint4*>(tab.left) + (lane & 3);     // bf16
             float up[2] = {1.0f, 1.0f};
-            uint32_t most = 0, c_tile = 0;
+            uint32_t odd = 0, c_tile = 0;
             // half a chunk ahead: while a chunk's products are on their way, two quarters of the next one are made
             c--;
             for (int chunk = -1; chunk < k.chunks && ok && k.chunks; chunk++, c++) {
@@ -775,12 +784,12 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                         if (chunk < 0 || n < kChunk) {  // others are as the one before
                             meet();
                             if (t < kChunk)
-                                tab.left[t] = t < n ? p.gain * exp2f(k.l2 * (p.reverse ? t + 1 - p.e : n - p.e - t)) : 0.0f;
+                                B::put_weight(tab.left, t, t < n ? p.gain * exp2f(k.l2 * (p.reverse ? t + 1 - p.e : n - p.e - t)) : 0.0f);
                             meet();
                         }
                         if (!ok || !warp_wait(full + 8 * st, (next / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
                         c_tile = ring + st * g.stage_bytes + 2 * panels_k * kPanel + c_lane;
-                        most = 0;
+                        odd = 0;
                         if constexpr (B::kScaled) {
                             float m[2] = {0.0f, 0.0f};
                             if (there) {
@@ -809,12 +818,19 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                             read(token, u);
 #pragma unroll
                             for (int y = 0; y < 4; y++) {
-                                most = B::most(most, u[y]);
-                                const float2 f = *reinterpret_cast<const float2*>(left + token + (y >> 1) * 8);
-                                float2 x = mul2(make_float2(B::low(u[y]), B::high(u[y])), f);
-                                if constexpr (B::kScaled) x = mul2(x, make_float2(up[y & 1], up[y & 1]));
+                                if constexpr (!B::kScaled) {
+                                    uint32_t four[4];
+                                    B::parts_of(u[y], pairs[token / 2 + (y >> 1) * 4], four);
+                                    B::note_odd(odd, four[1]);
 #pragma unroll
-                                for (int m = 0; m < kParts; m++) part[m][y] = B::take(x);
+                                    for (int m = 0; m < kParts; m++) part[m][y] = four[m];
+                                } else {
+                                    B::note_odd(odd, u[y]);
+                                    const float2 f = *reinterpret_cast<const float2*>(left + token + (y >> 1) * 8);
+                                    float2 x = mul2(mul2(make_float2(B::low(u[y]), B::high(u[y])), f), make_float2(up[y & 1], up[y & 1]));
+#pragma unroll
+                                    for (int m = 0; m < kParts; m++) part[m][y] = B::take(x);
+                                }
                             }
 #pragma unroll
                             for (int y = 0; y < kParts; y++)
@@ -825,7 +841,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     if (q == 3 && g.full) {
                         // not more than a chunk ahead of the output, for which the number of a chunk with odd values is left
                         if (c > 0 && !warp_wait(done, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
-                        if (there && B::is_odd(most)) *(volatile uint32_t*)&tab.bad[c & 1] = c + 1;
+                        if (there && B::is_odd(odd)) *(volatile uint32_t*)&tab.bad[c & 1] = c + 1;
                     }
                     fence_before();
                     __syncwarp();
@@ -1026,30 +1042,34 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
 
 // ---- 32-bit types -------------------------------------------------------------------------------
 
-// The same passes in plain 32-bit arithmetic, in chunks of 32 tokens; a CTA a segment and head, Z in shared memory.
+// The same passes in plain 32-bit arithmetic, in chunks of 32 tokens; a CTA a segment and head.  Z lies in registers, four
+// keys x four values a thread (of every 64 x 64), and in shared memory, where the products with a read it; the next chunk's
+// copies fly while one is worked on.  Shared memory is the bound: a warp's 32 multiply-adds of out take 10 of its cycles.
 constexpr int kPlainChunk = 32, kPlainThreads = 256;
 __host__ __device__ constexpr int plain_pitch(int d) { return (d + 3) / 4 * 4 + 4; }
+constexpr int kWeightPitch = kPlainChunk + 4;
+__host__ __device__ constexpr size_t plain_stage(int kd, int vd) { return (size_t)kPlainChunk * (2 * plain_pitch(kd) + plain_pitch(vd)); }
 __host__ __device__ constexpr size_t plain_smem(int kd, int vd) {
-    return sizeof(float) * ((size_t)kPlainChunk * (2 * plain_pitch(kd) + plain_pitch(vd) + kPlainChunk + 1 + 3) +
-                            (size_t)(kd + 3) / 4 * 4 * plain_pitch(vd));
+    return sizeof(float) * (2 * plain_stage(kd, vd) + kPlainChunk * kWeightPitch + 2 * kPlainChunk + (size_t)(kd + 3) / 4 * 4 * plain_pitch(vd));
 }
 __device__ __forceinline__ void load_plain(float* dst, const float* src, int64_t pitch, int width, bool wide, int n) {
     const int p = plain_pitch(width), quads = (width + 3) / 4;
     for (int i = threadIdx.x; i < kPlainChunk * quads; i += kPlainThreads) {
         const int row = i / quads, col = (i - row * quads) * 4;
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (row < n) {
-            const float* from = src + row * pitch + col;
-            if (wide) {
-                v = *reinterpret_cast<const float4*>(from);
-            } else {
-                v.x = from[0];
-                if (col + 1 < width) v.y = from[1];
-                if (col + 2 < width) v.z = from[2];
-                if (col + 3 < width) v.w = from[3];
+        const float* from = src + row * pitch + col;
+        const uint32_t to = smem_u32(dst + row * p + col);
+        if (wide) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row < n ? from : src), "r"(row < n ? 16 : 0)
+                         : "memory");
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const bool in = row < n && col + k < width;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * k), "l"(in ? from + k : src),
+                             "r"(in ? 4 : 0)
+                             : "memory");
             }
         }
-        *reinterpret_cast<float4*>(dst + row * p + col) = v;
     }
 }
 __device__ __forceinline__ float4 fma4(float a, float4 b, float4 c) {
@@ -1058,123 +1078,180 @@ __device__ __forceinline__ float4 fma4(float a, float4 b, float4 c) {
 __device__ __forceinline__ float dot4(float4 a, float4 b, float c) {
     return fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, c))));
 }
-__global__ void __launch_bounds__(kPlainThreads) attention_plain_kernel(const __grid_constant__ Args g) {
+__device__ __forceinline__ const float4& quad(const float* p) { return *reinterpret_cast<const float4*>(p); }
+// kTiles: tiles of 64 that the larger of keys and values takes.
+template <int kTiles>
+__global__ void __launch_bounds__(kPlainThreads, kTiles == 1 ? 2 : 1) attention_plain_kernel(const __grid_constant__ Args g) {
     extern __shared__ __align__(16) float sm[];
     pdl_wait();
     pdl_trigger();
     const Work k = work_of(g, blockIdx.x);
     const Pass& p = *k.p;
-    const int kd4 = (p.kd + 3) / 4 * 4, vd4 = (p.vd + 3) / 4 * 4, kp = plain_pitch(p.kd), vp = plain_pitch(p.vd);
-    float* const a = sm;
-    float* const b = a + kPlainChunk * kp;
-    float* const c = b + kPlainChunk * kp;
-    float* const weights = c + kPlainChunk * vp;                 // [32][36]
-    float* const z = weights + kPlainChunk * (kPlainChunk + 4);  // [kd4][vp]
-    const int t = threadIdx.x;
-    const float* from = state_in(k);
-    for (int i = t; i < kd4 * vp; i += kPlainThreads) {
-        const int key = i / vp, value = i - key * vp;
-        z[i] = from && key < p.kd && value < p.vd ? from[(int64_t)key * p.k_step + (int64_t)value * p.v_step] : 0.0f;
-    }
-    const int steps = (k.s.len + kPlainChunk - 1) / kPlainChunk;
+    const int kd = p.kd, vd = p.vd, kd4 = (kd + 3) / 4 * 4, vd4 = (vd + 3) / 4 * 4, kp = plain_pitch(kd), vp = plain_pitch(vd);
+    const int stage = (int)plain_stage(kd, vd);
+    float* const weights = sm + 2 * stage;
+    float* const powers = weights + kPlainChunk * kWeightPitch;  // d^0 .. d^31
+    float* const left = powers + kPlainChunk;
+    float* const zs = left + kPlainChunk;                         // [kd4][vp]
+    const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
     const int64_t way = p.reverse ? -1 : 1;
-    for (int chunk = 0; chunk < steps; chunk++) {
+    const int64_t row0 = p.reverse ? k.s.row0 + k.s.len - 1 : k.s.row0;
+    const bool full = g.full;
+    auto fetch = [&](int chunk) {
         const int at = chunk * kPlainChunk, n = min(kPlainChunk, k.s.len - at);
-        const int64_t row = p.reverse ? k.s.row0 + k.s.len - 1 - at : k.s.row0 + at;
-        __syncthreads();
-        if (g.full)
-            load_plain(a, (const float*)p.a + row * p.a_ld + (int64_t)k.head * p.kd, way * p.a_ld, p.kd, p.a_wide == 16, n);
-        load_plain(b, (const float*)p.b + row * p.b_ld + (int64_t)k.head * p.kd, way * p.b_ld, p.kd, p.b_wide == 16, n);
-        load_plain(c, (const float*)p.c + row * p.c_ld + (int64_t)k.head * p.vd, way * p.c_ld, p.vd, p.c_wide == 16, n);
-        __syncthreads();
-        if (g.full) {
-            // weights: a thread has four tokens of c for one of a
-            const int i = t >> 3, j0 = t & 7;
-            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (int x = 0; x < kd4; x += 4) {
-                const float4 u = *reinterpret_cast<const float4*>(a + i * kp + x);
+        const int64_t row = row0 + way * at;
+        float* const to = sm + (chunk & 1) * stage;
+        if (full) load_plain(to, (const float*)p.a + row * p.a_ld + (int64_t)k.head * kd, way * p.a_ld, kd, p.a_wide == 16, n);
+        load_plain(to + kPlainChunk * kp, (const float*)p.b + row * p.b_ld + (int64_t)k.head * kd, way * p.b_ld, kd, p.b_wide == 16, n);
+        load_plain(to + 2 * kPlainChunk * kp, (const float*)p.c + row * p.c_ld + (int64_t)k.head * vd, way * p.c_ld, vd, p.c_wide == 16, n);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    const int chunks = (k.s.len + kPlainChunk - 1) / kPlainChunk;
+    if (chunks) fetch(0);
+    if (t < kPlainChunk) powers[t] = exp2f(k.l2 * t);
+    const float* from = state_in(k);
+    float4 z[kTiles][kTiles][4];
 #pragma unroll
-                for (int y = 0; y < 4; y++) s[y] = dot4(u, *reinterpret_cast<const float4*>(b + (j0 + 8 * y) * kp + x), s[y]);
-            }
+    for (int a = 0; a < kTiles; a++)
+#pragma unroll
+        for (int b = 0; b < kTiles; b++)
 #pragma unroll
             for (int y = 0; y < 4; y++) {
-                const int j = j0 + 8 * y;
-                weights[i * (kPlainChunk + 4) + j] = j <= i ? s[y] * (p.intra * exp2f(k.l2 * (i - j))) : 0.0f;
+                const int key = a * 64 + ty * 4 + y, value = b * 64 + tx * 4;
+                float v[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++)
+                    v[x] = from && key < kd && value + x < vd ? from[(int64_t)key * p.k_step + (int64_t)(value + x) * p.v_step] : 0.0f;
+                z[a][b][y] = make_float4(v[0], v[1], v[2], v[3]);
             }
-            __syncthreads();
-            // out: four tokens (every eighth) and four values a thread
-            for (int v0 = (t & 31) * 4; v0 < vd4; v0 += 128) {
-                const int r0 = t >> 5;
-                float4 o[4];
+    for (int chunk = 0; chunk < chunks; chunk++) {
+        const int at = chunk * kPlainChunk, n = min(kPlainChunk, k.s.len - at);
+        if (chunk + 1 < chunks) {
+            fetch(chunk + 1);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        } else {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        }
+        if (full) {
 #pragma unroll
-                for (int y = 0; y < 4; y++) o[y] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                for (int x = 0; x < kd4; x += 4) {
-                    float4 zz[4];
+            for (int a = 0; a < kTiles; a++)
 #pragma unroll
-                    for (int y = 0; y < 4; y++) zz[y] = *reinterpret_cast<const float4*>(z + (x + y) * vp + v0);
+                for (int b = 0; b < kTiles; b++)
 #pragma unroll
                     for (int y = 0; y < 4; y++) {
-                        const float4 u = *reinterpret_cast<const float4*>(a + (r0 + 8 * y) * kp + x);
-                        o[y] = fma4(u.x, zz[0], fma4(u.y, zz[1], fma4(u.z, zz[2], fma4(u.w, zz[3], o[y]))));
+                        const int key = a * 64 + ty * 4 + y, value = b * 64 + tx * 4;
+                        if (key < kd4 && value < vd4) *reinterpret_cast<float4*>(zs + key * vp + value) = z[a][b][y];
                     }
-                }
+        }
+        if (t < kPlainChunk) left[t] = t < n ? p.gain * exp2f(k.l2 * (n - p.e - t)) : 0.0f;
+        __syncthreads();
+        const float *const as = sm + (chunk & 1) * stage, *const bs = as + kPlainChunk * kp, *const cs = bs + kPlainChunk * kp;
+        if (full) {
+            // weights: two tokens of a and two of c a thread
+            float s[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
+            for (int x = 0; x < kd4; x += 4) {
+                const float4 a0 = quad(as + ty * 2 * kp + x), a1 = quad(as + (ty * 2 + 1) * kp + x);
+                const float4 b0 = quad(bs + tx * kp + x), b1 = quad(bs + (tx + 16) * kp + x);
+                s[0][0] = dot4(a0, b0, s[0][0]), s[0][1] = dot4(a0, b1, s[0][1]);
+                s[1][0] = dot4(a1, b0, s[1][0]), s[1][1] = dot4(a1, b1, s[1][1]);
+            }
 #pragma unroll
-                for (int y = 0; y < 4; y++) {
-                    const float f = p.inter * exp2f(k.l2 * (r0 + 8 * y + p.e));
+            for (int y = 0; y < 2; y++)
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    const int i = ty * 2 + y, j = tx + 16 * x;
+                    weights[i * kWeightPitch + j] = j <= i ? s[y][x] * (p.intra * powers[i - j]) : 0.0f;
+                }
+            // a token after a row's own weighs nothing, whatever it holds: infinities and NaN are kept out of the sums
+            bool odd = false;
+            for (int v0 = tx * 4; v0 < vd4; v0 += 64)
+#pragma unroll
+                for (int y = 0; y < 2; y++) {
+                    const float4 c = quad(cs + (ty * 2 + y) * vp + v0);
+                    odd |= !(fabsf(c.x) < INFINITY && fabsf(c.y) < INFINITY && fabsf(c.z) < INFINITY && fabsf(c.w) < INFINITY);
+                }
+            odd = __syncthreads_or(odd);
+            // out: two tokens and four values a thread
+            for (int v0 = tx * 4; v0 < vd4; v0 += 64) {
+                float4 o[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+                auto step = [&](const float* rows, int pitch, const float* columns, int x) {
+                    const float4 u0 = quad(rows + x), u1 = quad(rows + pitch + x);
+                    const float4 c0 = quad(columns + x * vp), c1 = quad(columns + (x + 1) * vp), c2 = quad(columns + (x + 2) * vp),
+                                 c3 = quad(columns + (x + 3) * vp);
+                    o[0] = fma4(u0.x, c0, fma4(u0.y, c1, fma4(u0.z, c2, fma4(u0.w, c3, o[0]))));
+                    o[1] = fma4(u1.x, c0, fma4(u1.y, c1, fma4(u1.z, c2, fma4(u1.w, c3, o[1]))));
+                };
+#pragma unroll 2
+                for (int x = 0; x < kd4; x += 4) step(as + ty * 2 * kp, kp, zs + v0, x);
+#pragma unroll
+                for (int y = 0; y < 2; y++) {
+                    const float f = p.inter * exp2f(k.l2 * (ty * 2 + y + p.e));
                     o[y] = make_float4(o[y].x * f, o[y].y * f, o[y].z * f, o[y].w * f);
                 }
+                if (!odd) {
+#pragma unroll 2
+                    for (int x = 0; x < ty * 2 + 2; x += 4) step(weights + ty * 2 * kWeightPitch, kWeightPitch, cs + v0, x);
+                } else {
 #pragma unroll
-                for (int y = 0; y < 4; y++) {
-                    const int i = r0 + 8 * y;
-                    // a token after this one weighs nothing, whatever it holds
-                    for (int j = 0; j <= i; j++)
-                        o[y] = fma4(weights[i * (kPlainChunk + 4) + j], *reinterpret_cast<const float4*>(c + j * vp + v0), o[y]);
+                    for (int y = 0; y < 2; y++)
+                        for (int j = 0; j <= ty * 2 + y; j++)
+                            o[y] = fma4(weights[(ty * 2 + y) * kWeightPitch + j], quad(cs + j * vp + v0), o[y]);
+                }
+#pragma unroll
+                for (int y = 0; y < 2; y++) {
+                    const int i = ty * 2 + y;
                     if (i >= n) continue;
-                    float* to = (float*)p.out + (row + way * i) * p.out_ld + (int64_t)k.head * p.vd + v0;
+                    float* to = (float*)p.out + (row0 + way * (at + i)) * p.out_ld + (int64_t)k.head * vd + v0;
                     if (p.out_wide == 16) {
                         *reinterpret_cast<float4*>(to) = o[y];
                     } else {
                         to[0] = o[y].x;
-                        if (v0 + 1 < p.vd) to[1] = o[y].y;
-                        if (v0 + 2 < p.vd) to[2] = o[y].z;
-                        if (v0 + 3 < p.vd) to[3] = o[y].w;
+                        if (v0 + 1 < vd) to[1] = o[y].y;
+                        if (v0 + 2 < vd) to[2] = o[y].z;
+                        if (v0 + 3 < vd) to[3] = o[y].w;
                     }
                 }
             }
-            __syncthreads();
         }
-        // Z: eight keys and eight values a thread
+        // Z
         const float decay = exp2f(k.l2 * n);
-        for (int i = t; i < kPlainChunk; i += kPlainThreads)
-            weights[i] = i < n ? p.gain * exp2f(k.l2 * (n - p.e - i)) : 0.0f;
-        __syncthreads();
-        for (int k0 = (t >> 4) * 4; k0 < kd4; k0 += 64) {
-            for (int v0 = (t & 15) * 4; v0 < vd4; v0 += 64) {
-                float4 s[4];
 #pragma unroll
-                for (int y = 0; y < 4; y++) s[y] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int a = 0; a < kTiles; a++)
+#pragma unroll
+            for (int b = 0; b < kTiles; b++) {
+                const int key = a * 64 + ty * 4, value = b * 64 + tx * 4;
+                if (key >= kd4 || value >= vd4) continue;
+                float4 add[4];
+#pragma unroll
+                for (int y = 0; y < 4; y++) add[y] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
                 for (int j = 0; j < n; j++) {
-                    const float w = weights[j];
-                    float4 u = *reinterpret_cast<const float4*>(b + j * kp + k0);
-                    const float4 v = *reinterpret_cast<const float4*>(c + j * vp + v0);
-                    s[0] = fma4(u.x * w, v, s[0]), s[1] = fma4(u.y * w, v, s[1]);
-                    s[2] = fma4(u.z * w, v, s[2]), s[3] = fma4(u.w * w, v, s[3]);
+                    const float4 u = quad(bs + j * kp + key), v = quad(cs + j * vp + value);
+                    const float w = left[j];
+                    const float4 vw = make_float4(v.x * w, v.y * w, v.z * w, v.w * w);
+                    add[0] = fma4(u.x, vw, add[0]), add[1] = fma4(u.y, vw, add[1]);
+                    add[2] = fma4(u.z, vw, add[2]), add[3] = fma4(u.w, vw, add[3]);
                 }
+#pragma unroll
+                for (int y = 0; y < 4; y++) z[a][b][y] = fma4(decay, z[a][b][y], add[y]);
+            }
+        __syncthreads();
+    }
+    float* const to = state_out(k);
+    if (to) {
+#pragma unroll
+        for (int a = 0; a < kTiles; a++)
+#pragma unroll
+            for (int b = 0; b < kTiles; b++)
 #pragma unroll
                 for (int y = 0; y < 4; y++) {
-                    float4* to = reinterpret_cast<float4*>(z + (k0 + y) * vp + v0);
-                    *to = fma4(decay, *to, s[y]);
+                    const int key = a * 64 + ty * 4 + y, value = b * 64 + tx * 4;
+                    const float v[4] = {z[a][b][y].x, z[a][b][y].y, z[a][b][y].z, z[a][b][y].w};
+#pragma unroll
+                    for (int x = 0; x < 4; x++)
+                        if (key < kd && value + x < vd) to[(int64_t)key * p.k_step + (int64_t)(value + x) * p.v_step] = v[x];
                 }
-            }
-        }
     }
-    __syncthreads();
-    float* const to = state_out(k);
-    if (to)
-        for (int i = t; i < p.kd * p.vd; i += kPlainThreads) {
-            const int key = p.v_step == 1 ? i / p.vd : i % p.kd, value = p.v_step == 1 ? i % p.vd : i / p.kd;
-            to[(int64_t)key * p.k_step + (int64_t)value * p.v_step] = z[key * vp + value];
-        }
     if (t == 0) decay_out(k, g.log_decay);
 }
 
@@ -1412,9 +1489,12 @@ int run(const Plan* p, Args& g, cudaStream_t st) {
     if (p->dtype == SPARBIT_F32) {
         size_t smem = 0;
         for (int i = 0; i < g.n_passes; i++) smem = std::max(smem, plain_smem(g.pass[i].kd, g.pass[i].vd));
-        CU(cudaFuncSetAttribute(attention_plain_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        CU(launch(attention_plain_kernel, dim3(g.total), dim3(kPlainThreads), smem, st, g));
-        return SPARBIT_OK;
+        auto launch_it = [&](auto kernel) {
+            CU(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+            CU(launch(kernel, dim3(g.total), dim3(kPlainThreads), smem, st, g));
+            return (int)SPARBIT_OK;
+        };
+        return std::max(p->kd, p->vd) <= 64 ? launch_it(attention_plain_kernel<1>) : launch_it(attention_plain_kernel<2>);
     }
     uint32_t state = 0;
     g.stage_bytes = 0;
