@@ -59,12 +59,13 @@ struct Pass {
     int k_step, v_step;
     int in_by_segment, out_by_segment;  // units are segments, not sequences
     int skip_ends;             // what the last segment of a sequence adds is not wanted
-    int tiled;                 // whole chunks are copied by the maps
+    int tiled, out_tiled;      // whole chunks are copied by the maps; whole tiles of out too
 };
 
 // Tensors as rows x (heads x size), in boxes of a chunk x 64 elements.
 struct alignas(64) Maps {
     CUtensorMap a[3], b[3], c[3];  // of the passes
+    CUtensorMap out[3];            // boxes of 32 rows x the values of a warp that writes out
 };
 
 struct Args {
@@ -184,6 +185,14 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, u
                  "l"(map), "r"(bar), "r"(x), "r"(y)
                  : "memory");
 }
+// A tile of out from shared memory, in a group of its own.
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t src, int x, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];\n\t"
+        "cp.async.bulk.commit_group;" ::"l"(map),
+        "r"(src), "r"(x), "r"(y)
+        : "memory");
+}
 // Arrives at the barrier once the products issued so far are done.
 __device__ __forceinline__ void mma_done(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -279,17 +288,14 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 constexpr int kWeightWarps = 4, kOutWarps = 8, kStateWarps = 8, kLoadWarps = 2;
 constexpr int kFirstOut = kWeightWarps, kFirstState = kFirstOut + kOutWarps, kFirstLoad = kFirstState + kStateWarps, kMultiply = kFirstLoad + kLoadWarps, kMultiplyState = kMultiply + 1;
 constexpr int kTensorThreads = 32 * (kFirstLoad + 4);
-constexpr int kRegisters = 80, kWeightRegisters = 64, kOutRegisters = 80, kStateRegisters = 104, kOtherRegisters = 48;
+constexpr int kRegisters = 80, kWeightRegisters = 64, kOutRegisters = 88, kStateRegisters = 96, kOtherRegisters = 48;
 static_assert(kWeightRegisters + 2 * kOutRegisters + 2 * kStateRegisters + kOtherRegisters <=
                   kTensorThreads / 128 * kRegisters,
               "more registers than the CTA has would be waited for without end");
 template <int kCount>
-__device__ __forceinline__ void fewer_registers() {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
-}
-template <int kCount>
-__device__ __forceinline__ void more_registers() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
+__device__ __forceinline__ void take_registers() {
+    if constexpr (kCount > kRegisters) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
 }
 
 // 128 tokens of one tensor's head into panels of swizzled rows, by one warp; tokens from n on and columns from `width`
@@ -494,7 +500,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
 
     if (warp < kFirstOut) {
         // ---- weights: a token a lane
-        fewer_registers<kWeightRegisters>();
+        take_registers<kWeightRegisters>();
         const int row = warp * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         float* const powers = tab.powers + 32 + 32 * warp;
@@ -574,7 +580,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
         }
     } else if (warp < kFirstState) {
         // ---- output: a token a lane, half of the values a warp
-        fewer_registers<kOutRegisters>();
+        take_registers<kOutRegisters>();
         const int quad = warp & 3, half = (warp - kFirstOut) >> 2, row = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         for (int w = blockIdx.x; w < g.total && g.full && ok; w += gridDim.x) {
@@ -582,7 +588,9 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
             const Pass& p = *k.p;
             const int panels_k = (p.kd + 63) / 64;
             const int all = (p.vd + 31) / 32, share = (all + 1) / 2, b0 = half * share, b1 = min(all, b0 + share);
-            const uint32_t pitch = (p.vd + 63) / 64 * 128;
+            const uint32_t pitch = share * 64;  // bytes of a row of the warp's values
+            const int turn = share == 2 ? lane & 7 : (lane >> 1) & 3;  // of the 16-byte pieces of this lane's row
+            const int pass = (int)(k.p - g.pass);
             for (int chunk = 0; chunk < k.chunks; chunk++, c++) {
                 const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes;
                 const int n = tokens_of(k, chunk);
@@ -619,7 +627,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 fence_after();
                 const bool by_hand = *(volatile uint32_t*)&tab.bad[c & 1] == c + 1;
                 // in 16 bits over the tiles of a and b
-                const uint32_t own = stage + quad * 32 * pitch;
+                const uint32_t own = stage + (quad * 2 + half) * 4096;
                 uint32_t v[2][16];
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
@@ -646,39 +654,51 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
 #pragma unroll
                     for (int j = 0; j < 4; j++)
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                                         own + lane * pitch + ((((b0 + b) * 4 + j) ^ (lane & 7)) << 4)),
+                                         own + lane * pitch + (((b * 4 + j) ^ turn) << 4)),
                                      "r"(v[b][4 * j]), "r"(v[b][4 * j + 1]), "r"(v[b][4 * j + 2]), "r"(v[b][4 * j + 3])
                                      : "memory");
                 }
-                __syncwarp();
-                T* const to = (T*)p.out + first_row(k, chunk) * p.out_ld + (int64_t)k.head * p.vd;
-                const int64_t way = p.out_ld;
                 const int rows = min(32, n - quad * 32);
+                if (p.out_tiled && rows == 32) {
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0 && b0 < b1) {
+                        store_box(&maps.out[pass], own, k.head * p.vd + b0 * 32, (int)first_row(k, chunk) + quad * 32);
+                        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(empty + 8 * st);
+                    continue;
+                }
+                __syncwarp();
+                T* const to = (T*)p.out + first_row(k, chunk) * p.out_ld + (int64_t)k.head * p.vd + b0 * 32;
+                const int64_t way = p.out_ld;
+                const int width = min(p.vd, b1 * 32) - b0 * 32;  // of the warp's values
                 if (p.out_wide == 16) {
                     // 4 or 8 lanes to a row
-                    const int per_row = share * 4, piece = b0 * 4 + (lane & (per_row - 1)), r0 = lane / per_row, step = 32 / per_row;
+                    const int per_row = share * 4, piece = lane & (per_row - 1), r0 = lane / per_row, step = 32 / per_row;
                     T* q = to + (quad * 32 + r0) * way + piece * 8;
-                    if (piece * 8 < p.vd) {
+                    if (piece * 8 < width) {
 #pragma unroll 4
                         for (int r = r0; r < rows; r += step, q += step * way) {
-                            uint32_t v[4];
+                            uint32_t u[4];
                             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                                         : "r"(own + r * pitch + ((piece ^ (r & 7)) << 4))
+                                         : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                                         : "r"(own + r * pitch + ((piece ^ (share == 2 ? r & 7 : (r >> 1) & 3)) << 4))
                                          : "memory");
-                            *reinterpret_cast<uint4*>(q) = make_uint4(v[0], v[1], v[2], v[3]);
+                            *reinterpret_cast<uint4*>(q) = make_uint4(u[0], u[1], u[2], u[3]);
                         }
                     }
                 } else {
                     for (int r = 0; r < rows; r++) {
                         T* const q = to + (quad * 32 + r) * way;
-                        for (int col = b0 * 32 + lane; col < min(p.vd, b1 * 32); col += 32) {
-                            unsigned short v;
+                        for (int col = lane; col < width; col += 32) {
+                            unsigned short u;
                             asm volatile("ld.shared.u16 %0, [%1];"
-                                         : "=h"(v)
-                                         : "r"(own + r * pitch + (((col >> 3) ^ (r & 7)) << 4) + (col & 7) * 2)
+                                         : "=h"(u)
+                                         : "r"(own + r * pitch + (((col >> 3) ^ (share == 2 ? r & 7 : (r >> 1) & 3)) << 4) + (col & 7) * 2)
                                          : "memory");
-                            reinterpret_cast<unsigned short*>(q)[col] = v;
+                            reinterpret_cast<unsigned short*>(q)[col] = u;
                         }
                     }
                 }
@@ -692,7 +712,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
         // ---- the state, and c^T for it: a warp has 16 values.  Of Z a lane has rows lane / 4 and lane / 4 + 8 and every
         // fourth pair of keys - z[4 m ..]: keys 8 m + 2 (lane % 4) and the next of the first row, the same of the second -
         // and of c^T tokens 2 (lane % 4) and the next of every 8, for the same rows
-        more_registers<kStateRegisters>();
+        take_registers<kStateRegisters>();
         const int v0 = (warp & 3) * 32 + ((warp - kFirstState) >> 2) * 16, value = v0 + (lane >> 2);
         const int t = threadIdx.x - 32 * kFirstState;
         const uint32_t lanes = (uint32_t)v0 << 16;
@@ -890,7 +910,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
             if (warp == kFirstState && lane == 0) decay_out(k, g.log_decay);
         }
     } else {
-        fewer_registers<kOtherRegisters>();  // all of the group at one place
+        take_registers<kOtherRegisters>();  // all of the group at one place
         if (warp < kMultiply) {
             // ---- loads: every other chunk each, so that one chunk's copies fly while the other's are waited for
             const uint32_t turn = warp - kFirstLoad;
@@ -1475,12 +1495,13 @@ typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void
                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 // One head's size must be a multiple of the products' 16 elements: a box past it brings the next head's.
-bool encode(const Plan* p, CUtensorMap* map, const void* q, int64_t ld, int size) {
+bool encode(const Plan* p, CUtensorMap* map, const void* q, int64_t ld, int size, int box_rows = kChunk, int box_width = 64) {
     const cuuint64_t dims[2] = {(cuuint64_t)p->heads * size, (cuuint64_t)p->rows}, strides[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t box[2] = {64, kChunk}, one[2] = {1, 1};
+    const cuuint32_t box[2] = {(cuuint32_t)box_width, (cuuint32_t)box_rows}, one[2] = {1, 1};
     return ((EncodeFn)p->encode)(map, p->dtype == SPARBIT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
                                  2, const_cast<void*>(q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                 box_width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -1511,6 +1532,9 @@ int run(const Plan* p, Args& g, cudaStream_t st) {
         x.tiled = x.b_wide == 16 && x.c_wide == 16 && (!g.full || x.a_wide == 16) && x.kd % 16 == 0 && x.vd % 16 == 0 &&
                   p->rows >= kChunk && p->rows <= 0x7fffffffu && encode(p, &maps.b[i], x.b, x.b_ld, x.kd) &&
                   encode(p, &maps.c[i], x.c, x.c_ld, x.vd) && (!g.full || encode(p, &maps.a[i], x.a, x.a_ld, x.kd));
+        // 64 values a warp of 128, 32 of 64 or 32
+        x.out_tiled = g.full && x.out_wide == 16 && (x.vd == 32 || x.vd == 64 || x.vd == 128) && p->rows >= 32 &&
+                      p->rows <= 0x7fffffffu && encode(p, &maps.out[i], x.out, x.out_ld, x.vd, 32, x.vd == 128 ? 64 : 32);
     }
     const dim3 grid(std::min(g.total, p->sm_count));
     auto launch_it = [&](auto kernel) {
