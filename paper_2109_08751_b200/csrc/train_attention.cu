@@ -92,8 +92,9 @@ __device__ __forceinline__ float log2_decay(const float* log_decay, int h) {
 // ---- tensor memory ------------------------------------------------------------------------------
 
 // Columns (32 bits of 128 lanes each): scores, then in their place the weights that multiply c; out; the state's
-// addition; a ring of two pieces of c^T, 32 tokens each in up to four parts.
-constexpr uint32_t kColScore = 0, kColOut = 128, kColAdd = 256, kColC = 384, kSlotCols = 64;
+// addition; a ring of pieces of c^T, in parts.
+constexpr uint32_t kColScore = 0, kColOut = 128, kColAdd = 256, kColC = 384, kRingCols = 128;
+constexpr int kMostSlots = 4;
 
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
     asm volatile(
@@ -400,7 +401,7 @@ __device__ __forceinline__ void decay_out(const Work& k, const float* log_decay)
 constexpr int kMostStages = 4;
 constexpr uint32_t kRing = 14 * kPanel;
 struct Tables {
-    uint64_t full[kMostStages], empty[kMostStages], used[kMostStages], scored, scaled, weighted, entered, done, c_ready[2], c_free[2], added,
+    uint64_t full[kMostStages], empty[kMostStages], used[kMostStages], scored, scaled, weighted, entered, done, c_ready[kMostSlots], c_free[kMostSlots], added,
         add_free, z_ready, out_free, met;
     uint32_t tmem, gave_up;
     uint32_t bad[2];  // number of the last (every other) chunk whose c holds an infinity or a NaN
@@ -461,6 +462,10 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                                                                             const __grid_constant__ Maps maps) {
     using B = Bits<T>;
     constexpr int kParts = B::kParts;
+    // tokens of a piece of c^T (with 16 what a piece costs beside its tokens takes over: 156 us for 138), the ring's slots
+    constexpr int kPiece = 32, kPieces = kChunk / kPiece, kAhead = kPieces / 2, kSlotCols = kParts * kPiece / 2,
+                  kSlots = kRingCols / kSlotCols;
+    static_assert(kAhead <= kSlots && kSlots <= kMostSlots);
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Tables& tab = *reinterpret_cast<Tables*>(smem_raw + kRing);
     const uint32_t ring = smem_u32(smem_raw), z_base = ring + g.stages * g.stage_bytes;
@@ -476,7 +481,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
             bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, g.full ? kOutWarps : 1), bar_init(used + 8 * i, 1);
         bar_init(scored, 1), bar_init(scaled, kWeightWarps), bar_init(weighted, kWeightWarps + kOutWarps + kStateWarps);
         bar_init(entered, 1), bar_init(done, 1);
-        for (int i = 0; i < 2; i++) bar_init(c_ready + 8 * i, kStateWarps), bar_init(c_free + 8 * i, 1);
+        for (int i = 0; i < kSlots; i++) bar_init(c_ready + 8 * i, kStateWarps), bar_init(c_free + 8 * i, 1);
         bar_init(added, 1), bar_init(add_free, kStateWarps), bar_init(z_ready, kStateWarps), bar_init(out_free, kOutWarps);
         bar_init(met, kStateWarps);
         tab.bad[0] = tab.bad[1] = 0;
@@ -789,8 +794,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
             for (int chunk = -1; chunk < k.chunks && ok && k.chunks; chunk++, c++) {
                 const float down[2] = {1.0f / up[0], 1.0f / up[1]};
 #pragma unroll 1
-                for (int i = chunk < 0 ? 2 : 0; i < (chunk + 1 < k.chunks ? 4 : 2); i++, pieces++) {
-                    const int q = (i + 2) & 3;
+                for (int i = chunk < 0 ? kPieces - kAhead : 0; i < (chunk + 1 < k.chunks ? kPieces : kPieces - kAhead); i++, pieces++) {
+                    const int q = (i + kAhead) % kPieces;
                     // 16 tokens of the warp's values, transposed
                     auto read = [&](int token, uint32_t (&u)[4]) {
                         asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -798,7 +803,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                                      : "r"(c_tile + token * 128)
                                      : "memory");
                     };
-                    if (i == 2) {
+                    if (i == kPieces - kAhead) {
                         const uint32_t next = c + 1, st = next % g.stages;
                         const int n = tokens_of(k, chunk + 1);
                         if (chunk < 0 || n < kChunk) {  // others are as the one before
@@ -828,12 +833,15 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                             for (int y = 0; y < 2; y++) up[y] = power_of_two(exponent_for(max_of_row(m[y])));
                         }
                     }
-                    const uint32_t slot = pieces & 1;
-                    if (pieces >= 2 && !warp_wait(c_free + 8 * slot, (pieces / 2 - 1) & 1, gave_up, g.limit)) { ok = false; break; }
+                    const uint32_t slot = pieces % kSlots;
+                    if (pieces >= kSlots && !warp_wait(c_free + 8 * slot, (pieces / kSlots - 1) & 1, gave_up, g.limit)) {
+                        ok = false;
+                        break;
+                    }
                     fence_after();
                     if (there) {
 #pragma unroll 1
-                        for (int token = q * 32; token < q * 32 + 32; token += 16) {
+                        for (int token = q * kPiece; token < q * kPiece + kPiece; token += 16) {
                             uint32_t part[kParts][4], u[4];
                             read(token, u);
 #pragma unroll
@@ -854,11 +862,11 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                             }
 #pragma unroll
                             for (int y = 0; y < kParts; y++)
-                                tmem_store_16x8(tmem + kColC + slot * kSlotCols + y * 16 + (token & 16) / 2 + lanes, part[y]);
+                                tmem_store_16x8(tmem + kColC + slot * kSlotCols + y * (kPiece / 2) + token % kPiece / 2 + lanes, part[y]);
                         }
                         tmem_store_wait();
                     }
-                    if (q == 3 && g.full) {
+                    if (q == kPieces - 1 && g.full) {
                         // not more than a chunk ahead of the output, for which the number of a chunk with odd values is left
                         if (c > 0 && !warp_wait(done, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
                         if (there && B::is_odd(odd)) *(volatile uint32_t*)&tab.bad[c & 1] = c + 1;
@@ -867,7 +875,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     __syncwarp();
                     if (lane == 0) {
                         bar_arrive(c_ready + 8 * slot);
-                        if (q == 3 && g.full) bar_arrive(weighted);
+                        if (q == kPieces - 1 && g.full) bar_arrive(weighted);
                     }
                 }
                 if (chunk < 0) continue;
@@ -981,20 +989,21 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                         const uint64_t b_turned = smem_desc(b_tile, kPanel, 1024);
                         if (c > 0 && !warp_wait(add_free, (c - 1) & 1, gave_up, g.limit)) { ok = false; break; }
 #pragma unroll 1
-                        for (int q = 0; q < 4 && ok; q++, pieces++) {
-                            const uint32_t slot = pieces & 1;
-                            if (!warp_wait(c_ready + 8 * slot, (pieces / 2) & 1, gave_up, g.limit)) { ok = false; break; }
+                        for (int q = 0; q < kPieces && ok; q++, pieces++) {
+                            const uint32_t slot = pieces % kSlots;
+                            if (!warp_wait(c_ready + 8 * slot, (pieces / kSlots) & 1, gave_up, g.limit)) { ok = false; break; }
                             fence_after();
                             if (elect_one()) {
                                 // small parts first: less of them is cut off
 #pragma unroll
                                 for (int part = kParts - 1; part >= 0; part--)
 #pragma unroll
-                                    for (int i = 0; i < 2; i++)
-                                        mma_ts(tmem + kColAdd, tmem + kColC + slot * kSlotCols + part * 16 + i * 8,
-                                               b_turned + (q * 2 + i) * (2048 >> 4), add_desc, q > 0 || part < kParts - 1 || i > 0);
+                                    for (int i = 0; i < kPiece / 16; i++)
+                                        mma_ts(tmem + kColAdd, tmem + kColC + slot * kSlotCols + part * (kPiece / 2) + i * 8,
+                                               b_turned + (q * (kPiece / 16) + i) * (2048 >> 4), add_desc,
+                                               q > 0 || part < kParts - 1 || i > 0);
                                 mma_done(c_free + 8 * slot);
-                                if (q == 3) {
+                                if (q == kPieces - 1) {
                                     if (!g.withhold) mma_done(added);
                                     mma_done((g.full ? used : empty) + 8 * st);
                                 }
@@ -1043,8 +1052,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     __syncwarp();
                 }
             }
-            for (uint32_t i = pieces > 2 ? pieces - 2 : 0; i < pieces && ok; i++)
-                ok = warp_wait(c_free + 8 * (i & 1), (i / 2) & 1, gave_up, g.limit);
+            for (uint32_t i = pieces > kSlots ? pieces - kSlots : 0; i < pieces && ok; i++)
+                ok = warp_wait(c_free + 8 * (i % kSlots), (i / kSlots) & 1, gave_up, g.limit);
             if (!ok) {  // let the products under way end before the CTA does
                 const unsigned long long until = now_ns() + 1000000ull;
                 while (now_ns() < until) {
@@ -1590,23 +1599,27 @@ int overlaps(const Region* ins, int n, const Region* outs, int m) {
     return SPARBIT_OK;
 }
 
-// Chunks of a segment, at most; chosen for the least estimated time.  Times in chunks: a launch takes the longest SM's
-// chunks and about one more for each segment; the pass over states costs about half of the main one; a fold about
-// four.  8 heads x 4097 tokens in segments of 3 chunks.. see the plan's table of measured sizes.
-int segment_chunks(const std::vector<int64_t>& chunks, int heads) {
-    int64_t longest = 0;
-    for (int64_t c : chunks) longest = std::max(longest, c);
-    int64_t best = longest > 0 ? longest : 1;
+// Tokens that segments are multiples of.
+int unit_of(int dtype) { return dtype == SPARBIT_F32 ? kPlainChunk : kChunk; }
+
+// Units of a segment, at most; chosen for the least estimated time, in units' times: a launch takes what the SM with the
+// most of them has, and about one more for each segment; the launch that leaves the states about two thirds of the main
+// one; the fold between them about two.
+int64_t segment_units(const std::vector<int64_t>& units, int heads, int slots) {
+    int64_t longest = 1;
+    for (int64_t c : units) longest = std::max(longest, c);
+    int64_t best = longest;
     double least = 1e300;
-    for (int64_t len = longest; len >= 1; len = len * 3 / 4) {
+    for (int64_t len = longest;; len = std::min(len - 1, (len * 7 + 7) / 8)) {
+        if (len < 1) break;
         double items = 0, all = 0;
-        for (int64_t c : chunks) items += (double)((c + len - 1) / len), all += (double)c;
+        for (int64_t c : units) items += (double)((c + len - 1) / len), all += (double)c;
         items *= heads, all *= heads;
-        const double rounds = items <= 3 * kSms ? ceil(items / kSms) * (len + 1) : (all + items) / kSms + len * 0.5;
-        const double cost = len < longest ? 1.5 * rounds + 4 : rounds;
+        const double rounds = items <= 3 * slots ? ceil(items / slots) * (len + 1) : (all + items) / slots + len * 0.5;
+        const double cost = len < longest ? 1.67 * rounds + 2 : rounds;
         if (cost < least) least = cost, best = len;
     }
-    return (int)best;
+    return best;
 }
 
 }  // namespace
@@ -1634,12 +1647,14 @@ int sparbit_linear_attention_plan_create(int n_seqs, const size_t* lengths, int 
     try {
         p->n_seqs = n_seqs, p->heads = heads, p->kd = key_size, p->vd = value_size, p->dtype = dtype;
         p->scale = scale, p->rows = rows;
-        std::vector<int64_t> chunks;
-        for (int s = 0; s < n_seqs; s++) chunks.push_back((int64_t)((lengths[s] + kChunk - 1) / kChunk));
-        const int len = segment_chunks(chunks, heads);
+        const int64_t unit = unit_of(dtype);
+        std::vector<int64_t> units;
+        for (int s = 0; s < n_seqs; s++) units.push_back(((int64_t)lengths[s] + unit - 1) / unit);
+        // CTAs of 32-bit heads up to 64 come two to an SM
+        const int64_t len = segment_units(units, heads, dtype == SPARBIT_F32 && std::max(key_size, value_size) <= 64 ? 2 * kSms : kSms);
         int64_t row = 0;
         for (int s = 0; s < n_seqs; s++) {
-            const int64_t n = std::max<int64_t>(1, (chunks[s] + len - 1) / len), each = (chunks[s] + n - 1) / n * kChunk;
+            const int64_t n = std::max<int64_t>(1, (units[s] + len - 1) / len), each = (units[s] + n - 1) / n * unit;
             p->begin.push_back((int32_t)p->time.size());
             for (int64_t at = 0, first = 1; first || at < (int64_t)lengths[s]; at += each, first = 0) {
                 const int64_t left = (int64_t)lengths[s] - at, here = std::min(each, left);

@@ -133,9 +133,9 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     return r;
 }
 
-// kMost: threads of a CTA; those of 256 come several to an SM.
+// kMost: threads of a CTA, at most; those of 256 come several to an SM.
 template <typename T, typename W, int U, int kMost>
-__global__ void __launch_bounds__(kMost, kMost == 256 ? 3 : 1) norm_forward_kernel(const __grid_constant__ NormArgs g) {
+__global__ void __launch_bounds__(kMost, kMost == 256 ? (U == 4 ? 2 : 3) : 1) norm_forward_kernel(const __grid_constant__ NormArgs g) {
     __shared__ float sm[64];
     int turn = 0;
     pdl_wait();
@@ -399,36 +399,38 @@ namespace {
 
 using Plan = sparbit_norm_plan_s;
 
-// Threads of a row, units of a thread, CTAs an SM holds.  Two units a thread with the next row's on their way keep
-// enough loads in flight; one where there are few rows, which is done soonest; four where two do not reach.
+// Threads of a row, units of a thread, the most threads that the kernel is built for, CTAs an SM holds.  With few rows a
+// thread has one unit, which is done soonest.  With many, two or four and the next row's on their way keep enough loads in
+// flight; the registers that they take (80, or 128 from four units and backward) leave room for so many CTAs.
 struct Shape {
-    int lanes, units, threads, per_sm;
+    int lanes, units, threads, most, per_sm;
 };
-Shape shape_of(const Plan* p, size_t rows) {
+Shape shape_of(const Plan* p, size_t rows, bool backward) {
     const int all = (p->width + kUnit - 1) / kUnit;
     Shape s;
     if (all <= 32) {
         s.lanes = 4, s.units = 1;
         while (s.lanes < all) s.lanes *= 2;
     } else {
-        s.units = (all + kMostThreads - 1) / kMostThreads;
-        if (s.units == 1 && rows >= 4 * kSms) s.units = 2;
-        if (s.units == 3) s.units = 4;
+        if (all <= kMostThreads && rows < 4 * kSms) s.units = 1;
+        else s.units = all <= (backward ? 1024 : 512) ? 2 : 4;
         s.lanes = ((all + s.units - 1) / s.units + 31) / 32 * 32;
     }
     s.threads = s.lanes <= 32 ? kShared : s.lanes;
-    s.per_sm = s.threads <= 256 ? 768 / s.threads : std::max(1, 1024 / s.threads);
+    s.most = s.threads <= 256 ? 256 : s.units > 1 && s.threads <= 512 ? 512 : kMostThreads;
+    s.per_sm = std::max(1, (s.most > 256 ? s.most : backward || s.units == 4 ? 512 : 768) / s.threads);
     return s;
 }
 
-// f.operator()<T, W, U, kMost>() for the plan's types, the units of a thread and the most threads of a CTA.
+// f.operator()<T, W, U, kMost>() for the plan's types and a shape.
 template <typename T, typename W, typename Fn>
 int by_shape(const Shape& s, Fn f) {
     if (s.units == 1)
-        return s.threads <= 256 ? f.template operator()<T, W, 1, 256>() : f.template operator()<T, W, 1, 1024>();
+        return s.most == 256 ? f.template operator()<T, W, 1, 256>() : f.template operator()<T, W, 1, 1024>();
     if (s.units == 2)
-        return s.threads <= 256 ? f.template operator()<T, W, 2, 256>() : f.template operator()<T, W, 2, 1024>();
-    return f.template operator()<T, W, 4, 1024>();
+        return s.most == 256 ? f.template operator()<T, W, 2, 256>() : f.template operator()<T, W, 2, 512>();
+    if (s.most == 256) return f.template operator()<T, W, 4, 256>();
+    return s.most == 512 ? f.template operator()<T, W, 4, 512>() : f.template operator()<T, W, 4, 1024>();
 }
 template <typename Fn>
 int by_types(const Plan* p, const Shape& s, Fn f) {
@@ -515,7 +517,7 @@ int sparbit_norm_forward(sparbit_norm_plan_t* p, size_t rows, const void* x, siz
     g.weight_wide = (uintptr_t)weight % 16 == 0;
     g.y8_wide = ((uintptr_t)y8 | y8_ld) % 8 == 0;
     g.block = p->block, g.scales_ld = (int)per_row, g.eps = p->eps;
-    const Shape s = shape_of(p, rows);
+    const Shape s = shape_of(p, rows, false);
     g.lanes = s.lanes;
     const size_t together = s.threads / s.lanes, grid = std::min((size_t)(kSms * s.per_sm), (rows + together - 1) / together);
     return by_types(p, s, [&]<typename T, typename W, int U, int kMost>() {
@@ -557,7 +559,7 @@ int sparbit_norm_backward(sparbit_norm_plan_t* p, size_t rows, const void* dy, s
                            (dsum ? (uintptr_t)dsum | dsum_ld * es : 0);
     g.wide = bits % 16 == 0;
     g.weight_wide = (uintptr_t)weight % 16 == 0;
-    const Shape s = shape_of(p, rows);
+    const Shape s = shape_of(p, rows, true);
     g.lanes = s.lanes;
     const size_t together = s.threads / s.lanes;
     const int grid = (int)std::min<size_t>(std::min(kParts, kSms * s.per_sm), (rows + together - 1) / together);
