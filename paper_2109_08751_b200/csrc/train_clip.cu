@@ -56,52 +56,66 @@ __device__ __forceinline__ double block_sum(double v, double* sm) {
     return v;
 }
 
-// Squares of a few numbers: in 32 bits where those hold them, one by one in 64 otherwise.
+// Squares of a few numbers, one by one in 64 bits: where 32 do not hold their sum.
 template <int N>
-__device__ __forceinline__ double squares_of(const float (&v)[N]) {
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; i++) s = fmaf(v[i], v[i], s);
-    if (s > 1e-30f && s < 1e30f) return (double)s;
+__device__ __noinline__ double squares_in_64(const float (&v)[N]) {
     double d = 0.0;
-    float any = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; i++) any = fmaxf(any, fabsf(v[i]));
-    if (any == 0.0f && s == 0.0f) return 0.0;
-#pragma unroll 1
     for (int i = 0; i < N; i++) d += (double)v[i] * (double)v[i];
     return d;
 }
 
+constexpr int kAhead = 4;  // accesses of a thread that are on their way together
+
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* p, int n) {
-    constexpr int A = 16 / sizeof(T), kAhead = 4;
+    constexpr int A = 16 / sizeof(T);
     double sum = 0.0;
     const int head = min(n, (int)((16 - (uintptr_t)p % 16) % 16 / sizeof(T))), whole = (n - head) / A;
-    float one[1];
-    if ((int)threadIdx.x < head) {
-        one[0] = to_float(p[threadIdx.x]);
-        sum += squares_of(one);
-    }
-    const Pack<T, A>* const v = reinterpret_cast<const Pack<T, A>*>(p + head);
-    for (int i0 = threadIdx.x; i0 < whole; i0 += kThreads * kAhead) {
-        Pack<T, A> k[kAhead];
-#pragma unroll
-        for (int y = 0; y < kAhead; y++)
-            if (i0 + y * kThreads < whole) k[y] = v[i0 + y * kThreads];
+    const int done = head + whole * A;
+    // the elements in front of the first whole access and behind the last
+    if ((int)threadIdx.x < head) sum += (double)to_float(p[threadIdx.x]) * (double)to_float(p[threadIdx.x]);
+    if ((int)threadIdx.x < n - done) sum += (double)to_float(p[done + threadIdx.x]) * (double)to_float(p[done + threadIdx.x]);
+    const uint4* const v = reinterpret_cast<const uint4*>(p + head);
+    uint4 k[2][kAhead];
+    auto fetch = [&](int i0, uint4 (&to)[kAhead]) {
 #pragma unroll
         for (int y = 0; y < kAhead; y++) {
-            if (i0 + y * kThreads >= whole) break;
-            float f[A];
-#pragma unroll
-            for (int i = 0; i < A; i++) f[i] = to_float(k[y].v[i]);
-            sum += squares_of(f);
+            to[y] = make_uint4(0u, 0u, 0u, 0u);
+            if (i0 + y * kThreads < whole) to[y] = v[i0 + y * kThreads];
         }
-    }
-    const int done = head + whole * A;
-    if ((int)threadIdx.x < n - done) {
-        one[0] = to_float(p[done + threadIdx.x]);
-        sum += squares_of(one);
+    };
+    auto add = [&](const uint4 (&from)[kAhead]) {
+        // 32 bits for the squares of one thread's accesses, 64 for their sums
+        float s = 0.0f;
+        uint32_t any = 0;
+#pragma unroll
+        for (int y = 0; y < kAhead; y++) {
+            const Pack<T, A> q = reinterpret_cast<const Pack<T, A>&>(from[y]);
+#pragma unroll
+            for (int i = 0; i < A; i++) s = fmaf(to_float(q.v[i]), to_float(q.v[i]), s);
+            any |= from[y].x | from[y].y | from[y].z | from[y].w;
+        }
+        if (s > 1e-30f && s < 1e30f) {
+            sum += (double)s;
+        } else if (any) {
+#pragma unroll 1
+            for (int y = 0; y < kAhead; y++) {
+                const uint4 u = y == 0 ? from[0] : y == 1 ? from[1] : y == 2 ? from[2] : from[3];
+                const Pack<T, A> q = reinterpret_cast<const Pack<T, A>&>(u);
+                float f[A];
+#pragma unroll
+                for (int i = 0; i < A; i++) f[i] = to_float(q.v[i]);
+                sum += squares_in_64(f);
+            }
+        }
+    };
+    static_assert(kAhead == 4);
+    fetch(threadIdx.x, k[0]);
+    for (int i0 = threadIdx.x; i0 < whole; i0 += 2 * kThreads * kAhead) {
+        fetch(i0 + kThreads * kAhead, k[1]);
+        add(k[0]);
+        fetch(i0 + 2 * kThreads * kAhead, k[0]);
+        add(k[1]);
     }
     return sum;
 }
@@ -114,9 +128,10 @@ __global__ void __launch_bounds__(kThreads) clip_sums_kernel(const __grid_consta
     const int lo = g.cta_begin[blockIdx.x], hi = g.cta_begin[blockIdx.x + 1];
     double sum = 0.0;
     int rank = -1;
+    Chunk k = {};
+    Tensor t = {};
+    if (lo < hi) k = g.chunks[lo], t = g.tensors[k.tensor];
     for (int c = lo; c < hi; c++) {
-        const Chunk k = g.chunks[c];
-        const Tensor t = g.tensors[k.tensor];
         if (t.rank != rank) {
             if (rank >= 0) {
                 sum = block_sum(sum, sm);
@@ -130,6 +145,7 @@ __global__ void __launch_bounds__(kThreads) clip_sums_kernel(const __grid_consta
         if (t.type == SPARBIT_F32) sum += chunk_squares((const float*)t.in + at, n);
         else if (t.type == SPARBIT_BF16) sum += chunk_squares((const __nv_bfloat16*)t.in + at, n);
         else sum += chunk_squares((const __half*)t.in + at, n);
+        if (c + 1 < hi) k = g.chunks[c + 1], t = g.tensors[k.tensor];
     }
     if (rank >= 0) {
         sum = block_sum(sum, sm);
@@ -159,7 +175,7 @@ __global__ void __launch_bounds__(kThreads) clip_sums_kernel(const __grid_consta
 
 template <typename T>
 __device__ __forceinline__ void scale_chunk(const T* in, T* out, int n, float by) {
-    constexpr int A = 16 / sizeof(T), kAhead = 4;
+    constexpr int A = 16 / sizeof(T);
     if (((uintptr_t)in ^ (uintptr_t)out) % 16) {
         for (int i = threadIdx.x; i < n; i += kThreads) out[i] = from_float<T>(to_float(in[i]) * by);
         return;
