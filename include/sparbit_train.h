@@ -418,7 +418,7 @@ int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* plan, const void* const* 
 int sparbit_clip_sums(sparbit_clip_plan_t* plan, double* sums, void* stream);
 
 /* gathered: [n_ranks][G] 64-bit, rank r's receive buffer of the allgather of the sums over G ranks.
- * norms: [n_ranks][2] 32-bit: norm and factor.  Where out was NULL nothing else is written.  A tensor that is its own
+ * norms: [n_ranks][2] 32-bit: norm (infinite where 32 bits do not hold it; the factor goes by 64) and factor.  Where out was NULL nothing else is written.  A tensor that is its own
  * output is left alone where the factor is 1.  ERR_ARG: most negative or NaN, eps negative or not finite. */
 int sparbit_clip_scale(sparbit_clip_plan_t* plan, const double* gathered, int G, float most, float eps, float* norms,
                        void* stream);

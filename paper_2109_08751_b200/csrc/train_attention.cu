@@ -751,7 +751,9 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if constexpr (B::kScaled) {
                     float most[2] = {0.0f, 0.0f};
 #pragma unroll
-                    for (int i = 0; i < 64; i++) most[(i >> 1) & 1] = fmaxf(most[(i >> 1) & 1], fabsf(z[i]));
+                    for (int i = 0; i < 64; i++)
+                        if ((i >> 2) < blocks)  // what lies behind the last key is nobody's
+                            most[(i >> 1) & 1] = fmaxf(most[(i >> 1) & 1], fabsf(z[i]));
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
                         const int e = exponent_for(max_of_row(most[i]));
