@@ -33,7 +33,7 @@ struct NormArgs {
     int width, lanes;                // lanes: threads of a row
     int wide, weight_wide, y8_wide;  // rows start on multiples of 16 bytes (y8: 8)
     int block, scales_ld;            // columns of a scale, 0: all
-    float eps;
+    float eps, inverse;              // inverse: 1 / width
 };
 struct NormBackArgs {
     const void *dy, *sum, *weight, *dsum;
@@ -43,6 +43,7 @@ struct NormBackArgs {
     int64_t dy_ld, sum_ld, dsum_ld, dx_ld;
     int64_t rows;
     int width, lanes, wide, weight_wide;
+    float inverse;  // 1 / width
 };
 
 // A unit as it lies in memory: loaded a row ahead, converted when its turn comes.
@@ -72,31 +73,89 @@ __device__ __forceinline__ void load_raw(const T* p, int n, bool wide, Raw<T>& r
 #pragma unroll
     for (int i = 0; i < Raw<T>::kPacks; i++) r.v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
 }
-template <typename T>
-__device__ __forceinline__ void convert(const Raw<T>& r, float (&f)[kUnit]) {
-    constexpr int A = 16 / sizeof(T);
-#pragma unroll
-    for (int i = 0; i < Raw<T>::kPacks; i++) {
-        const Pack<T, A> k = reinterpret_cast<const Pack<T, A>&>(r.v[i]);
-#pragma unroll
-        for (int j = 0; j < A; j++) f[i * A + j] = to_float(k.v[j]);
-    }
+// Pairs of numbers, for the packed 32-bit instructions: what a row costs beside its bytes is instructions.
+struct Unit {
+    float2 v[kUnit / 2];
+};
+__device__ __forceinline__ unsigned long long& bits_of(float2& v) { return reinterpret_cast<unsigned long long&>(v); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(bits_of(r)) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(bits_of(r)) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(bits_of(r)) : "l"(bits_of(a)), "l"(bits_of(b)), "l"(bits_of(c)));
+    return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+__device__ __forceinline__ float2 pair_of(uint32_t v, __nv_bfloat16) {
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+__device__ __forceinline__ float2 pair_of(uint32_t v, __half) { return __half22float2(reinterpret_cast<const __half2&>(v)); }
+__device__ __forceinline__ uint32_t bits_of_pair(float2 v, __nv_bfloat16) {
+    const __nv_bfloat162 k = __floats2bfloat162_rn(v.x, v.y);
+    return reinterpret_cast<const uint32_t&>(k);
+}
+__device__ __forceinline__ uint32_t bits_of_pair(float2 v, __half) {
+    const __half2 k = __floats2half2_rn(v.x, v.y);
+    return reinterpret_cast<const uint32_t&>(k);
 }
 template <typename T>
-__device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&v)[kUnit]) {
-    if (wide && n >= kUnit) {
-        constexpr int A = 16 / sizeof(T);
+__device__ __forceinline__ Unit convert(const Raw<T>& r) {
+    Unit f;
 #pragma unroll
-        for (int i = 0; i < kUnit; i += A) {
-            Pack<T, A> k;
+    for (int i = 0; i < Raw<T>::kPacks; i++) {
+        const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
 #pragma unroll
-            for (int j = 0; j < A; j++) k.v[j] = from_float<T>(v[i + j]);
-            *reinterpret_cast<Pack<T, A>*>(p + i) = k;
+        for (int j = 0; j < 4; j++) {
+            if constexpr (sizeof(T) == 2) f.v[j] = pair_of(w[j], T());
+            else (j & 1 ? f.v[i * 2 + j / 2].y : f.v[i * 2 + j / 2].x) = __uint_as_float(w[j]);
         }
+    }
+    return f;
+}
+// Rounded to the type.
+template <typename T>
+__device__ __forceinline__ Raw<T> round_to(const Unit& f) {
+    Raw<T> r;
+    if constexpr (sizeof(T) == 2) {
+        r.v[0] = make_uint4(bits_of_pair(f.v[0], T()), bits_of_pair(f.v[1], T()), bits_of_pair(f.v[2], T()), bits_of_pair(f.v[3], T()));
     } else {
 #pragma unroll
-        for (int i = 0; i < kUnit; i++)
-            if (i < n) p[i] = from_float<T>(v[i]);
+        for (int i = 0; i < 2; i++)
+            r.v[i] = make_uint4(__float_as_uint(f.v[2 * i].x), __float_as_uint(f.v[2 * i].y), __float_as_uint(f.v[2 * i + 1].x),
+                                __float_as_uint(f.v[2 * i + 1].y));
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_raw(T* p, int n, bool wide, const Raw<T>& r) {
+    if (wide && n >= kUnit) {
+#pragma unroll
+        for (int i = 0; i < Raw<T>::kPacks; i++) reinterpret_cast<uint4*>(p)[i] = r.v[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < Raw<T>::kPacks; i++) {
+        const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int at = (i * 4 + j) * (int)(4 / sizeof(T));
+            if constexpr (sizeof(T) == 4) {
+                if (at < n) reinterpret_cast<uint32_t*>(p)[at] = w[j];
+            } else {
+                unsigned short* q = reinterpret_cast<unsigned short*>(p);
+                if (at < n) q[at] = (unsigned short)w[j];
+                if (at + 1 < n) q[at + 1] = (unsigned short)(w[j] >> 16);
+            }
+        }
     }
 }
 
@@ -127,9 +186,9 @@ __device__ __forceinline__ float over_row(float v, int lanes, float* sm, int& tu
     return v;
 }
 
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+__device__ __forceinline__ uint32_t e4m3x2(float2 v) {
     unsigned short r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(v.y), "f"(v.x));
     return r;
 }
 
@@ -163,33 +222,34 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? (U == 4 ? 2 : 3) : 1) no
     for (int64_t row0 = (int64_t)blockIdx.x * together; row0 < g.rows; row0 += (int64_t)gridDim.x * together) {
         const int64_t row = row0 + threadIdx.x / lanes;
         const bool there = row < g.rows;
-        float r[U][kUnit];
-        float squares = 0.0f;
+        // columns behind the row's end hold zeros throughout
+        Unit r[U];
+        float2 pairs = both(0.0f);
 #pragma unroll
         for (int u = 0; u < U; u++) {
             if (there && left[u] > 0) {
-                convert(x[u], r[u]);
+                r[u] = convert(x[u]);
                 if (g.residual) {
-                    float f[kUnit];
-                    convert(e[u], f);
-                    // what is kept is what is normalised
+                    const Unit f = convert(e[u]);
 #pragma unroll
-                    for (int i = 0; i < kUnit; i++) r[u][i] = to_float(from_float<T>(r[u][i] + f[i]));
+                    for (int i = 0; i < kUnit / 2; i++) r[u].v[i] = add2(r[u].v[i], f.v[i]);
+                    // what is kept is what is normalised
+                    x[u] = round_to<T>(r[u]);
+                    if constexpr (sizeof(T) == 2) r[u] = convert(x[u]);
                 }
+                if (g.sum) store_raw((T*)g.sum + row * g.sum_ld + (u * lanes + t) * kUnit, left[u], g.wide, x[u]);
             } else {
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) r[u][i] = 0.0f;
+                for (int i = 0; i < kUnit / 2; i++) r[u].v[i] = both(0.0f);
             }
         }
         fetch(row + (int64_t)gridDim.x * together);
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            if (g.sum && there && left[u] > 0) store8((T*)g.sum + row * g.sum_ld + (u * lanes + t) * kUnit, left[u], g.wide, r[u]);
+        for (int u = 0; u < U; u++)
 #pragma unroll
-            for (int i = 0; i < kUnit; i++) squares = fmaf(r[u][i], r[u][i], squares);
-        }
-        squares = over_row<RowSum>(squares, lanes, sm, turn);
-        float rstd = 1.0f / sqrtf(squares / g.width + g.eps);
+            for (int i = 0; i < kUnit / 2; i++) pairs = fma2(r[u].v[i], r[u].v[i], pairs);
+        const float squares = over_row<RowSum>(pairs.x + pairs.y, lanes, sm, turn);
+        float rstd = rsqrtf(fmaf(squares, g.inverse, g.eps));
         const bool big = !(squares < 1e38f);
         if (lanes <= 32 ? __any_sync(kAllLanes, big) : big) {
             // squares that 32 bits do not hold: once more, scaled.  All threads that reduce together take the same way.
@@ -197,58 +257,56 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? (U == 4 ? 2 : 3) : 1) no
 #pragma unroll
             for (int u = 0; u < U; u++)
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) most = RowMax::of(most, fabsf(r[u][i]));
+                for (int i = 0; i < kUnit / 2; i++) most = RowMax::of(RowMax::of(most, fabsf(r[u].v[i].x)), fabsf(r[u].v[i].y));
             most = over_row<RowMax>(most, lanes, sm, turn);
             const float by = most < INFINITY && most > 0.0f ? exp2f((float)-ilogbf(most)) : 1.0f;
             float again = 0.0f;
 #pragma unroll
             for (int u = 0; u < U; u++)
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) again = fmaf(r[u][i] * by, r[u][i] * by, again);
+                for (int i = 0; i < kUnit / 2; i++) {
+                    const float2 v = mul2(r[u].v[i], both(by));
+                    again = fmaf(v.x, v.x, fmaf(v.y, v.y, again));
+                }
             again = over_row<RowSum>(again, lanes, sm, turn);
-            if (big) rstd = by / sqrtf(again / g.width + g.eps * by * by);
+            if (big) rstd = by * rsqrtf(fmaf(again, g.inverse, g.eps * by * by));
         }
         if (g.rstd && there && t == 0) g.rstd[row] = rstd;
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            if (g.weight && left[u] > 0) {
-                float w[kUnit];
-                convert(weight[u], w);
+            if (!there || left[u] <= 0) continue;
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) r[u][i] = i < left[u] ? r[u][i] * rstd * w[i] : 0.0f;
-            } else {
+            for (int i = 0; i < kUnit / 2; i++) r[u].v[i] = mul2(r[u].v[i], both(rstd));
+            if (g.weight) {
+                const Unit w = convert(weight[u]);
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) r[u][i] = i < left[u] ? r[u][i] * rstd : 0.0f;
+                for (int i = 0; i < kUnit / 2; i++) r[u].v[i] = mul2(r[u].v[i], w.v[i]);
             }
-            if (g.y && there && left[u] > 0) store8((T*)g.y + row * g.y_ld + (u * lanes + t) * kUnit, left[u], g.wide, r[u]);
+            if (g.y) store_raw((T*)g.y + row * g.y_ld + (u * lanes + t) * kUnit, left[u], g.wide, round_to<T>(r[u]));
         }
         if (!g.y8) continue;
-        float row_most = 0.0f;
-        if (!g.block) {
+        float unit_most[U], row_most = 0.0f;
 #pragma unroll
-            for (int u = 0; u < U; u++)
+        for (int u = 0; u < U; u++) {
+            unit_most[u] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) row_most = RowMax::of(row_most, fabsf(r[u][i]));
-            row_most = over_row<RowMax>(row_most, lanes, sm, turn);
+            for (int i = 0; i < kUnit / 2; i++)
+                unit_most[u] = RowMax::of(RowMax::of(unit_most[u], fabsf(r[u].v[i].x)), fabsf(r[u].v[i].y));
+            row_most = RowMax::of(row_most, unit_most[u]);
         }
+        if (!g.block) row_most = over_row<RowMax>(row_most, lanes, sm, turn);
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int col = (u * lanes + t) * kUnit;
-            float most = row_most;
-            if (g.block) {
-                most = 0.0f;
-#pragma unroll
-                for (int i = 0; i < kUnit; i++) most = RowMax::of(most, fabsf(r[u][i]));
-                most = over_lanes<RowMax>(most, min(g.block / kUnit, lanes));
-            }
+            float most = g.block ? over_lanes<RowMax>(unit_most[u], min(g.block / kUnit, lanes)) : row_most;
             if (!there || left[u] <= 0) continue;
             if (most < 1e-30f) most = 1e-30f;
             if (g.block ? col % g.block == 0 : col == 0)
                 g.scales[row * g.scales_ld + (g.block ? col / g.block : 0)] = most / 448.0f;
             const float by = 448.0f / most;
             uint2 q;
-            q.x = e4m3x2(r[u][0] * by, r[u][1] * by) | e4m3x2(r[u][2] * by, r[u][3] * by) << 16;
-            q.y = e4m3x2(r[u][4] * by, r[u][5] * by) | e4m3x2(r[u][6] * by, r[u][7] * by) << 16;
+            q.x = e4m3x2(mul2(r[u].v[0], both(by))) | e4m3x2(mul2(r[u].v[1], both(by))) << 16;
+            q.y = e4m3x2(mul2(r[u].v[2], both(by))) | e4m3x2(mul2(r[u].v[3], both(by))) << 16;
             uint8_t* to = g.y8 + row * g.y8_ld + col;
             if (g.y8_wide && left[u] >= kUnit) {
                 *reinterpret_cast<uint2*>(to) = q;
@@ -272,14 +330,14 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) norm_backward_ker
     Raw<W> weight[U];
     Raw<T> raw_d[U], raw_x[U], raw_m[U];
     float next_rstd = 0.0f;
-    float dw[U][kUnit];
+    Unit dw[U];
     int left[U];
 #pragma unroll
     for (int u = 0; u < U; u++) {
         left[u] = g.width - (u * lanes + t) * kUnit;
         if (g.weight && left[u] > 0) load_raw((const W*)g.weight + (u * lanes + t) * kUnit, left[u], g.weight_wide, weight[u]);
 #pragma unroll
-        for (int i = 0; i < kUnit; i++) dw[u][i] = 0.0f;
+        for (int i = 0; i < kUnit / 2; i++) dw[u].v[i] = both(0.0f);
     }
     auto fetch = [&](int64_t row) {
         next_rstd = row < g.rows ? g.rstd[row] : 0.0f;
@@ -297,52 +355,48 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) norm_backward_ker
         const int64_t row = row0 + threadIdx.x / lanes;
         const bool there = row < g.rows;
         const float rstd = next_rstd;
-        float d[U][kUnit], x[U][kUnit];
+        Unit d[U], x[U];
         Raw<T> more[U];
-        float inner = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            if (there && left[u] > 0) {
-                convert(raw_d[u], d[u]);
-                convert(raw_x[u], x[u]);
-                more[u] = raw_m[u];
-            } else {
-#pragma unroll
-                for (int i = 0; i < kUnit; i++) d[u][i] = x[u][i] = 0.0f;
-            }
+            if (!there || left[u] <= 0) continue;
+            d[u] = convert(raw_d[u]);
+            x[u] = convert(raw_x[u]);
+            more[u] = raw_m[u];
         }
         fetch(row + (int64_t)gridDim.x * together);
+        float2 inner = both(0.0f);
 #pragma unroll
         for (int u = 0; u < U; u++) {
             if (!there || left[u] <= 0) continue;
 #pragma unroll
-            for (int i = 0; i < kUnit; i++) {
-                x[u][i] *= rstd;
-                dw[u][i] = fmaf(d[u][i], x[u][i], dw[u][i]);
+            for (int i = 0; i < kUnit / 2; i++) {
+                x[u].v[i] = mul2(x[u].v[i], both(rstd));
+                dw[u].v[i] = fma2(d[u].v[i], x[u].v[i], dw[u].v[i]);
             }
             if (g.weight) {
-                float w[kUnit];
-                convert(weight[u], w);
+                const Unit w = convert(weight[u]);
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) d[u][i] *= w[i];
+                for (int i = 0; i < kUnit / 2; i++) d[u].v[i] = mul2(d[u].v[i], w.v[i]);
             }
 #pragma unroll
-            for (int i = 0; i < kUnit; i++) inner = fmaf(d[u][i], x[u][i], inner);
+            for (int i = 0; i < kUnit / 2; i++) inner = fma2(d[u].v[i], x[u].v[i], inner);
         }
-        inner = over_row<RowSum>(inner, lanes, sm, turn) / g.width;
+        const float mean = over_row<RowSum>(inner.x + inner.y, lanes, sm, turn) * g.inverse;
 #pragma unroll
         for (int u = 0; u < U; u++) {
             if (!there || left[u] <= 0) continue;
-            float m[kUnit];
+            Unit m;
             if (g.dsum) {
-                convert(more[u], m);
+                m = convert(more[u]);
             } else {
 #pragma unroll
-                for (int i = 0; i < kUnit; i++) m[i] = 0.0f;
+                for (int i = 0; i < kUnit / 2; i++) m.v[i] = both(0.0f);
             }
 #pragma unroll
-            for (int i = 0; i < kUnit; i++) d[u][i] = fmaf(rstd, d[u][i] - x[u][i] * inner, m[i]);
-            store8((T*)g.dx + row * g.dx_ld + (u * lanes + t) * kUnit, left[u], g.wide, d[u]);
+            for (int i = 0; i < kUnit / 2; i++)
+                d[u].v[i] = fma2(both(rstd), fma2(x[u].v[i], both(-mean), d[u].v[i]), m.v[i]);
+            store_raw((T*)g.dx + row * g.dx_ld + (u * lanes + t) * kUnit, left[u], g.wide, round_to<T>(d[u]));
         }
     }
     if (!g.parts) return;
@@ -350,14 +404,15 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) norm_backward_ker
     if (together == 1) {
 #pragma unroll
         for (int u = 0; u < U; u++)
-            if (left[u] > 0) store8(out + (u * lanes + t) * kUnit, left[u], g.width % 4 == 0, dw[u]);
+            if (left[u] > 0) store_raw(out + (u * lanes + t) * kUnit, left[u], g.width % 4 == 0, round_to<float>(dw[u]));
         return;
     }
     const int columns = U * lanes * kUnit;
 #pragma unroll
     for (int u = 0; u < U; u++)
 #pragma unroll
-        for (int i = 0; i < kUnit; i++) partial[(threadIdx.x / lanes) * columns + (u * lanes + t) * kUnit + i] = dw[u][i];
+        for (int i = 0; i < kUnit; i++)
+            partial[(threadIdx.x / lanes) * columns + (u * lanes + t) * kUnit + i] = i & 1 ? dw[u].v[i / 2].y : dw[u].v[i / 2].x;
     __syncthreads();
     for (int col = threadIdx.x; col < g.width; col += blockDim.x) {
         float s = 0.0f;
@@ -516,7 +571,7 @@ int sparbit_norm_forward(sparbit_norm_plan_t* p, size_t rows, const void* x, siz
     g.wide = bits % 16 == 0;
     g.weight_wide = (uintptr_t)weight % 16 == 0;
     g.y8_wide = ((uintptr_t)y8 | y8_ld) % 8 == 0;
-    g.block = p->block, g.scales_ld = (int)per_row, g.eps = p->eps;
+    g.block = p->block, g.scales_ld = (int)per_row, g.eps = p->eps, g.inverse = 1.0f / (float)w;
     const Shape s = shape_of(p, rows, false);
     g.lanes = s.lanes;
     const size_t together = s.threads / s.lanes, grid = std::min((size_t)(kSms * s.per_sm), (rows + together - 1) / together);
@@ -554,7 +609,7 @@ int sparbit_norm_backward(sparbit_norm_plan_t* p, size_t rows, const void* dy, s
     g.dy = dy, g.sum = sum, g.weight = weight, g.dsum = dsum, g.rstd = rstd, g.dx = dx;
     g.parts = dweight ? (float*)p->work : nullptr;
     g.dy_ld = (int64_t)dy_ld, g.sum_ld = (int64_t)sum_ld, g.dsum_ld = (int64_t)dsum_ld, g.dx_ld = (int64_t)dx_ld;
-    g.rows = (int64_t)rows, g.width = (int)w;
+    g.rows = (int64_t)rows, g.width = (int)w, g.inverse = 1.0f / (float)w;
     const uintptr_t bits = (uintptr_t)dy | dy_ld * es | (uintptr_t)sum | sum_ld * es | (uintptr_t)dx | dx_ld * es |
                            (dsum ? (uintptr_t)dsum | dsum_ld * es : 0);
     g.wide = bits % 16 == 0;
