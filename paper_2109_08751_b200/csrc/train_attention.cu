@@ -77,6 +77,7 @@ struct Args {
     const float* log_decay;
     uint32_t stage_bytes;
     int stages;
+    int early;           // the tiles of b and c may be copied over before out has left the tile of a
     uint32_t* status;
     unsigned long long limit;
     int withhold;
@@ -401,7 +402,7 @@ __device__ __forceinline__ void decay_out(const Work& k, const float* log_decay)
 constexpr int kMostStages = 4;
 constexpr uint32_t kRing = 14 * kPanel;
 struct Tables {
-    uint64_t full[kMostStages], empty[kMostStages], used[kMostStages], scored, scaled, weighted, entered, done, c_ready[kMostSlots], c_free[kMostSlots], added,
+    uint64_t full[kMostStages], empty[kMostStages], used[kMostStages], spent[kMostStages], scored, scaled, weighted, entered, done, c_ready[kMostSlots], c_free[kMostSlots], added,
         add_free, z_ready, out_free, met;
     uint32_t tmem, gave_up;
     uint32_t bad[2];  // number of the last (every other) chunk whose c holds an infinity or a NaN
@@ -463,14 +464,14 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
     using B = Bits<T>;
     constexpr int kParts = B::kParts;
     // tokens of a piece of c^T (with 16 what a piece costs beside its tokens takes over: 156 us for 138), the ring's slots
-    constexpr int kPiece = 32, kPieces = kChunk / kPiece, kAhead = kPieces / 2, kSlotCols = kParts * kPiece / 2,
-                  kSlots = kRingCols / kSlotCols;
+    constexpr int kPiece = 32, kPieces = kChunk / kPiece, kSlotCols = kParts * kPiece / 2, kSlots = kRingCols / kSlotCols,
+                  kAhead = kSlots / 2;
     static_assert(kAhead <= kSlots && kSlots <= kMostSlots);
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Tables& tab = *reinterpret_cast<Tables*>(smem_raw + kRing);
     const uint32_t ring = smem_u32(smem_raw), z_base = ring + g.stages * g.stage_bytes;
     volatile uint32_t* const gave_up = &tab.gave_up;
-    const uint32_t full = smem_u32(tab.full), empty = smem_u32(tab.empty), used = smem_u32(tab.used), scored = smem_u32(&tab.scored),
+    const uint32_t full = smem_u32(tab.full), empty = smem_u32(tab.empty), used = smem_u32(tab.used), spent = smem_u32(tab.spent), scored = smem_u32(&tab.scored),
                    scaled = smem_u32(&tab.scaled), weighted = smem_u32(&tab.weighted), entered = smem_u32(&tab.entered),
                    done = smem_u32(&tab.done), c_ready = smem_u32(tab.c_ready), c_free = smem_u32(tab.c_free),
                    added = smem_u32(&tab.added), add_free = smem_u32(&tab.add_free), z_ready = smem_u32(&tab.z_ready),
@@ -478,7 +479,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
     const int warp = __shfl_sync(kAllLanes, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < g.stages; i++)
-            bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, g.full ? kOutWarps : 1), bar_init(used + 8 * i, 1);
+            bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, g.full ? kOutWarps : 1), bar_init(used + 8 * i, 1),
+                bar_init(spent + 8 * i, 1);
         bar_init(scored, 1), bar_init(scaled, kWeightWarps), bar_init(weighted, kWeightWarps + kOutWarps + kStateWarps);
         bar_init(entered, 1), bar_init(done, 1);
         for (int i = 0; i < kSlots; i++) bar_init(c_ready + 8 * i, kStateWarps), bar_init(c_free + 8 * i, 1);
@@ -631,8 +633,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if (!warp_wait(done, c & 1, gave_up, g.limit)) { ok = false; break; }
                 fence_after();
                 const bool by_hand = *(volatile uint32_t*)&tab.bad[c & 1] == c + 1;
-                // in 16 bits over the tiles of a and b
-                const uint32_t own = stage + (quad * 2 + half) * 4096;
+                // in 16 bits over the tile of a (and b, where values take more panels than keys)
+                const uint32_t own = stage + (quad * 2 + half) * 32 * pitch;
                 uint32_t v[2][16];
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
@@ -651,7 +653,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(out_free);
-                // once the state's products have read b too
+                // once the state's products have read b
                 if (!warp_wait(used + 8 * st, (c / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
@@ -791,7 +793,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
             const uint4* const pairs = reinterpret_cast<const uint4*>(tab.left) + (lane & 3);     // bf16
             float up[2] = {1.0f, 1.0f};
             uint32_t odd = 0, c_tile = 0;
-            // half a chunk ahead: while a chunk's products are on their way, two quarters of the next one are made
+            // ahead: while a chunk's products are on their way, half of the ring is filled for the next one
             c--;
             for (int chunk = -1; chunk < k.chunks && ok && k.chunks; chunk++, c++) {
                 const float down[2] = {1.0f / up[0], 1.0f / up[1]};
@@ -842,7 +844,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     }
                     fence_after();
                     if (there) {
-#pragma unroll 1
+#pragma unroll
                         for (int token = q * kPiece; token < q * kPiece + kPiece; token += 16) {
                             uint32_t part[kParts][4], u[4];
                             read(token, u);
@@ -931,22 +933,31 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 for (int chunk = 0; chunk < k.chunks; chunk++, c++) {
                     if (c % kLoadWarps != turn) continue;
                     const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes, bar = full + 8 * st;
-                    if (c >= (uint32_t)g.stages && !warp_wait(empty + 8 * st, (c / g.stages - 1) & 1, gave_up, g.limit)) {
+                    const uint32_t before = (c / g.stages - 1) & 1;  // parity of this stage's last use
+                    const int n = tokens_of(k, chunk);
+                    const bool tiled = p.tiled && n == kChunk, early = tiled && g.early && c >= (uint32_t)g.stages;
+                    if (c >= (uint32_t)g.stages && !warp_wait((early ? used : empty) + 8 * st, before, gave_up, g.limit)) {
                         ok = false;
                         break;
                     }
-                    const int n = tokens_of(k, chunk);
                     const int64_t row = first_row(k, chunk);
-                    if (p.tiled && n == kChunk) {
+                    if (tiled) {
+                        // b, c and a in the order in which their tiles become free
                         if (lane == 0) {
                             bar_expect(bar, ((g.full ? 2 : 1) * panels_k + panels_v) * kPanel);
-                            for (int i = 0; i < panels_k; i++) {
-                                if (g.full) copy_box(stage + i * kPanel, &maps.a[pass], bar, k.head * p.kd + i * 64, (int)row);
+                            for (int i = 0; i < panels_k; i++)
                                 copy_box(stage + (panels_k + i) * kPanel, &maps.b[pass], bar, k.head * p.kd + i * 64, (int)row);
-                            }
+                        }
+                        __syncwarp();
+                        if (early && !warp_wait(spent + 8 * st, before, gave_up, g.limit)) { ok = false; break; }
+                        if (lane == 0)
                             for (int i = 0; i < panels_v; i++)
                                 copy_box(stage + (2 * panels_k + i) * kPanel, &maps.c[pass], bar, k.head * p.vd + i * 64, (int)row);
-                        }
+                        __syncwarp();
+                        if (early && !warp_wait(empty + 8 * st, before, gave_up, g.limit)) { ok = false; break; }
+                        if (lane == 0 && g.full)
+                            for (int i = 0; i < panels_k; i++)
+                                copy_box(stage + i * kPanel, &maps.a[pass], bar, k.head * p.kd + i * 64, (int)row);
                         __syncwarp();
                         continue;
                     }
@@ -1050,8 +1061,13 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                                 mma_ts(tmem + kColOut, tmem + kColScore + i * 8, c_turned + i * (2048 >> 4), out_desc, true);
                         }
                         mma_done(done);
+                        if (!by_hand) mma_done(spent + 8 * st);
                     }
                     __syncwarp();
+                    if (by_hand) {  // whoever adds c up has read it
+                        if (!warp_wait(out_free, c & 1, gave_up, g.limit)) { ok = false; break; }
+                        if (lane == 0) bar_arrive(spent + 8 * st);
+                    }
                 }
             }
             for (uint32_t i = pieces > kSlots ? pieces - kSlots : 0; i < pieces && ok; i++)
@@ -1536,6 +1552,12 @@ int run(const Plan* p, Args& g, cudaStream_t st) {
         state = std::max(state, pk * kPanel);
     }
     g.stages = (int)std::min<uint32_t>(kMostStages, (kRing - state) / g.stage_bytes);
+    g.early = g.full;
+    for (int i = 0; i < g.n_passes; i++) {
+        const Pass &x = g.pass[i], &y = g.pass[0];
+        g.early = g.early && (x.kd + 63) / 64 == (y.kd + 63) / 64 && (x.vd + 63) / 64 == (y.vd + 63) / 64 &&
+                  (x.vd + 63) / 64 <= (x.kd + 63) / 64;
+    }
     const size_t smem = kTensorSmem;
     Maps maps;
     for (int i = 0; i < g.n_passes; i++) {
