@@ -77,7 +77,7 @@ struct Args {
     const float* log_decay;
     uint32_t stage_bytes;
     int stages;
-    int early;           // the tiles of b and c may be copied over before out has left the tile of a
+    int early;           // all passes lay their tiles out alike: one may be copied over while others are in use
     uint32_t* status;
     unsigned long long limit;
     int withhold;
@@ -402,7 +402,8 @@ __device__ __forceinline__ void decay_out(const Work& k, const float* log_decay)
 constexpr int kMostStages = 4;
 constexpr uint32_t kRing = 14 * kPanel;
 struct Tables {
-    uint64_t full[kMostStages], empty[kMostStages], used[kMostStages], spent[kMostStages], scored, scaled, weighted, entered, done, c_ready[kMostSlots], c_free[kMostSlots], added,
+    // of a stage: a and b are there, c is; everything, b and a are free again
+    uint64_t full[kMostStages], full_c[kMostStages], empty[kMostStages], used[kMostStages], entered_a[kMostStages], scored, scaled, weighted, entered, done, c_ready[kMostSlots], c_free[kMostSlots], added,
         add_free, z_ready, out_free, met;
     uint32_t tmem, gave_up;
     uint32_t bad[2];  // number of the last (every other) chunk whose c holds an infinity or a NaN
@@ -471,7 +472,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
     Tables& tab = *reinterpret_cast<Tables*>(smem_raw + kRing);
     const uint32_t ring = smem_u32(smem_raw), z_base = ring + g.stages * g.stage_bytes;
     volatile uint32_t* const gave_up = &tab.gave_up;
-    const uint32_t full = smem_u32(tab.full), empty = smem_u32(tab.empty), used = smem_u32(tab.used), spent = smem_u32(tab.spent), scored = smem_u32(&tab.scored),
+    const uint32_t full = smem_u32(tab.full), empty = smem_u32(tab.empty), used = smem_u32(tab.used),
+                   full_c = smem_u32(tab.full_c), entered_a = smem_u32(tab.entered_a), scored = smem_u32(&tab.scored),
                    scaled = smem_u32(&tab.scaled), weighted = smem_u32(&tab.weighted), entered = smem_u32(&tab.entered),
                    done = smem_u32(&tab.done), c_ready = smem_u32(tab.c_ready), c_free = smem_u32(tab.c_free),
                    added = smem_u32(&tab.added), add_free = smem_u32(&tab.add_free), z_ready = smem_u32(&tab.z_ready),
@@ -480,7 +482,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
     if (threadIdx.x == 0) {
         for (int i = 0; i < g.stages; i++)
             bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, g.full ? kOutWarps : 1), bar_init(used + 8 * i, 1),
-                bar_init(spent + 8 * i, 1);
+                bar_init(full_c + 8 * i, 1), bar_init(entered_a + 8 * i, 1);
         bar_init(scored, 1), bar_init(scaled, kWeightWarps), bar_init(weighted, kWeightWarps + kOutWarps + kStateWarps);
         bar_init(entered, 1), bar_init(done, 1);
         for (int i = 0; i < kSlots; i++) bar_init(c_ready + 8 * i, kStateWarps), bar_init(c_free + 8 * i, 1);
@@ -633,8 +635,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 if (!warp_wait(done, c & 1, gave_up, g.limit)) { ok = false; break; }
                 fence_after();
                 const bool by_hand = *(volatile uint32_t*)&tab.bad[c & 1] == c + 1;
-                // in 16 bits over the tile of a (and b, where values take more panels than keys)
-                const uint32_t own = stage + (quad * 2 + half) * 32 * pitch;
+                // in 16 bits over the tile of c
+                const uint32_t own = stage + 2 * panels_k * kPanel + (quad * 2 + half) * 32 * pitch;
                 uint32_t v[2][16];
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
@@ -653,8 +655,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(out_free);
-                // once the state's products have read b
-                if (!warp_wait(used + 8 * st, (c / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
+                // once everybody who adds c up has read it
+                if (by_hand && !warp_wait(out_free, c & 1, gave_up, g.limit)) { ok = false; break; }
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
                     if (b0 + b >= b1) break;
@@ -816,7 +818,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                                 B::put_weight(tab.left, t, t < n ? p.gain * exp2f(k.l2 * (p.reverse ? t + 1 - p.e : n - p.e - t)) : 0.0f);
                             meet();
                         }
-                        if (!ok || !warp_wait(full + 8 * st, (next / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
+                        if (!ok || !warp_wait(full_c + 8 * st, (next / g.stages) & 1, gave_up, g.limit)) { ok = false; break; }
                         c_tile = ring + st * g.stage_bytes + 2 * panels_k * kPanel + c_lane;
                         odd = 0;
                         if constexpr (B::kScaled) {
@@ -936,28 +938,39 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     const uint32_t before = (c / g.stages - 1) & 1;  // parity of this stage's last use
                     const int n = tokens_of(k, chunk);
                     const bool tiled = p.tiled && n == kChunk, early = tiled && g.early && c >= (uint32_t)g.stages;
-                    if (c >= (uint32_t)g.stages && !warp_wait((early ? used : empty) + 8 * st, before, gave_up, g.limit)) {
+                    if (c >= (uint32_t)g.stages && !warp_wait((early ? entered_a : empty) + 8 * st, before, gave_up, g.limit)) {
+                        ok = false;
+                        break;
+                    }
+                    // out leaves a stage without waiting for the state's products
+                    if (c >= (uint32_t)g.stages && g.full && !early && !warp_wait(used + 8 * st, before, gave_up, g.limit)) {
                         ok = false;
                         break;
                     }
                     const int64_t row = first_row(k, chunk);
                     if (tiled) {
-                        // b, c and a in the order in which their tiles become free
+                        // in the order in which the tiles become free: a when its products are done (then b's with it are,
+                        // too), b with the state's products, c when out, which goes through its place, has left
                         if (lane == 0) {
-                            bar_expect(bar, ((g.full ? 2 : 1) * panels_k + panels_v) * kPanel);
-                            for (int i = 0; i < panels_k; i++)
-                                copy_box(stage + (panels_k + i) * kPanel, &maps.b[pass], bar, k.head * p.kd + i * 64, (int)row);
+                            bar_expect(bar, (g.full ? 2 : 1) * panels_k * kPanel);
+                            for (int i = 0; i < panels_k && g.full; i++)
+                                copy_box(stage + i * kPanel, &maps.a[pass], bar, k.head * p.kd + i * 64, (int)row);
                         }
                         __syncwarp();
-                        if (early && !warp_wait(spent + 8 * st, before, gave_up, g.limit)) { ok = false; break; }
+                        if (early && !warp_wait(used + 8 * st, before, gave_up, g.limit)) { ok = false; break; }
                         if (lane == 0)
-                            for (int i = 0; i < panels_v; i++)
-                                copy_box(stage + (2 * panels_k + i) * kPanel, &maps.c[pass], bar, k.head * p.vd + i * 64, (int)row);
+                            for (int i = 0; i < panels_k; i++)
+                                copy_box(stage + (panels_k + i) * kPanel, &maps.b[pass], bar, k.head * p.kd + i * 64, (int)row);
                         __syncwarp();
                         if (early && !warp_wait(empty + 8 * st, before, gave_up, g.limit)) { ok = false; break; }
-                        if (lane == 0 && g.full)
-                            for (int i = 0; i < panels_k; i++)
-                                copy_box(stage + i * kPanel, &maps.a[pass], bar, k.head * p.kd + i * 64, (int)row);
+                        if (lane == 0) {
+                            // armed here and not with the other: the first states of a segment need no c, so that the
+                            // chunk that was here before may have been waiting for its own until now
+                            bar_expect(full_c + 8 * st, panels_v * kPanel);
+                            for (int i = 0; i < panels_v; i++)
+                                copy_box(stage + (2 * panels_k + i) * kPanel, &maps.c[pass], full_c + 8 * st, k.head * p.vd + i * 64,
+                                         (int)row);
+                        }
                         __syncwarp();
                         continue;
                     }
@@ -970,7 +983,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     asm volatile("cp.async.wait_all;" ::: "memory");
                     proxy_fence();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(bar);
+                    if (lane == 0) bar_arrive(bar), bar_arrive(full_c + 8 * st);
                 }
             }
             // all products have reported before the CTA ends
@@ -1049,6 +1062,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                             mma_ss(tmem + kColOut, a + (i >> 2) * (kPanel >> 4) + (i & 3) * 2, z + (i >> 2) * (kPanel >> 4) + (i & 3) * 2,
                                    enter_desc, i > 0);
                         mma_done(entered);
+                        mma_done(entered_a + 8 * st);
                     }
                     __syncwarp();
                     if (!warp_wait(weighted, c & 1, gave_up, g.limit)) { ok = false; break; }
@@ -1061,13 +1075,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                                 mma_ts(tmem + kColOut, tmem + kColScore + i * 8, c_turned + i * (2048 >> 4), out_desc, true);
                         }
                         mma_done(done);
-                        if (!by_hand) mma_done(spent + 8 * st);
                     }
                     __syncwarp();
-                    if (by_hand) {  // whoever adds c up has read it
-                        if (!warp_wait(out_free, c & 1, gave_up, g.limit)) { ok = false; break; }
-                        if (lane == 0) bar_arrive(spent + 8 * st);
-                    }
                 }
             }
             for (uint32_t i = pieces > kSlots ? pieces - kSlots : 0; i < pieces && ok; i++)
@@ -1555,8 +1564,7 @@ int run(const Plan* p, Args& g, cudaStream_t st) {
     g.early = g.full;
     for (int i = 0; i < g.n_passes; i++) {
         const Pass &x = g.pass[i], &y = g.pass[0];
-        g.early = g.early && (x.kd + 63) / 64 == (y.kd + 63) / 64 && (x.vd + 63) / 64 == (y.vd + 63) / 64 &&
-                  (x.vd + 63) / 64 <= (x.kd + 63) / 64;
+        g.early = g.early && (x.kd + 63) / 64 == (y.kd + 63) / 64 && (x.vd + 63) / 64 == (y.vd + 63) / 64;
     }
     const size_t smem = kTensorSmem;
     Maps maps;

@@ -159,6 +159,15 @@ def test_long_sequences_in_segments(name):
     c.check()
 
 
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+@pytest.mark.parametrize("kd,vd,lengths", [(128, 128, [900, 768, 1100]), (64, 64, [1500, 1024, 700]), (64, 128, [900, 640, 641])])
+def test_long_chains_of_chunks(kd, vd, lengths, name):
+    # as many heads as fill the GPU: the plan cuts nothing, and every stage of the kernel's ring is used many times
+    c = Case(lengths, 64, kd, vd, name, seed=4)
+    c.run()
+    c.check()
+
+
 @pytest.mark.parametrize("name", ["bf16", "f32"])
 def test_many_short_sequences(name):
     c = Case([1 + i % 130 for i in range(60)], 4, 32, 64, name)
