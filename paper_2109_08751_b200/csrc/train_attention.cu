@@ -796,8 +796,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
             float up[2] = {1.0f, 1.0f};
             uint32_t odd = 0, c_tile = 0;
             // ahead: while a chunk's products are on their way, half of the ring is filled for the next one
-            c--;
-            for (int chunk = -1; chunk < k.chunks && ok && k.chunks; chunk++, c++) {
+            if (k.chunks) c--;
+            for (int chunk = k.chunks ? -1 : 0; chunk < k.chunks && ok; chunk++, c++) {
                 const float down[2] = {1.0f / up[0], 1.0f / up[1]};
 #pragma unroll 1
                 for (int i = chunk < 0 ? kPieces - kAhead : 0; i < (chunk + 1 < k.chunks ? kPieces : kPieces - kAhead); i++, pieces++) {

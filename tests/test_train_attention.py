@@ -4,6 +4,8 @@ Tolerances.  With u half a step of the type (bf16 2^-8, fp16 2^-11) and M_t the 
 is off by at most u |o_t| for its own rounding and u scale |q_t| M_t for those of the weights (tokens of the chunk) and
 of the state (the tokens before), which share the tokens between them.  Everything else is 32-bit arithmetic: 2^-24 for
 each of some 400 additions and a factor, below 2^-14 of the same magnitude.  States are 32-bit arithmetic only."""
+import random
+
 import pytest
 import torch
 
@@ -164,6 +166,28 @@ def test_long_sequences_in_segments(name):
 def test_long_chains_of_chunks(kd, vd, lengths, name):
     # as many heads as fill the GPU: the plan cuts nothing, and every stage of the kernel's ring is used many times
     c = Case(lengths, 64, kd, vd, name, seed=4)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("lengths,heads", [([2000, 1500, 0, 130, 1, 900], 20), ([0, 0, 5, 0, 300], 70), ([1111], 31),
+                                           ([700, 0, 1000, 129], 40)])
+def test_several_segments_a_processor(lengths, heads, name):
+    # more segments than processors, some of them empty or with nothing to add: whoever goes on to the next one has to
+    # agree with the others on where it is
+    c = Case(lengths, heads, 32, 64, name, seed=6)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_drawn_shapes(seed):
+    r = random.Random(seed)
+    name, sizes = r.choice(["bf16", "f16", "f32"]), [16, 32, 64, 64, 80, 100, 128]
+    n, heads = r.randrange(1, 12), r.choice([1, 2, 3, 5, 9, 16, 32])
+    c = Case([r.choice([0, 1, r.randrange(1, 300), r.randrange(1, 1200)]) for _ in range(n)], heads, r.choice(sizes),
+             r.choice(sizes), name, seed=seed)
     c.run()
     c.check()
 
