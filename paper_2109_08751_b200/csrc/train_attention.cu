@@ -38,7 +38,8 @@ constexpr int kSms = 148;
 // A piece of a sequence that one CTA goes through from end to end.
 struct alignas(16) Segment {
     int64_t row0, seq_len;
-    int32_t len, seq, id;
+    int32_t len, seq;
+    int32_t slot;  // of a sequence that is cut: where its states lie; -1: it is the whole sequence
     int32_t ends;  // 1: it begins its sequence in time, 2: it ends it
 };
 
@@ -51,13 +52,15 @@ struct Pass {
     int a_wide, b_wide, c_wide, out_wide;  // bytes that all their rows of a head start on a multiple of, up to 16
     int reverse, e;
     float inter, intra, gain;
-    // states: element (key, value) of head h of unit u at [u * unit + h * kd * vd + key * k_step + value * v_step]
+    // states: element (key, value) of head h of sequence u at [u * unit + h * kd * vd + key * k_step + value * v_step]
     const float* z_in;         // null: zero
     float* z_out;              // null: not wanted
     float* decay_out;          // [u * unit_out + h]: decay over the whole sequence; null: not wanted
     int64_t unit_in, unit_out;
     int k_step, v_step;
-    int in_by_segment, out_by_segment;  // units are segments, not sequences
+    // of segments of sequences that are cut, in the same way by their slots: what enters them (null: zero), what they add
+    const float* slots_in;
+    float* slots_out;
     int skip_ends;             // what the last segment of a sequence adds is not wanted
     int tiled, out_tiled;      // whole chunks are copied by the maps; whole tiles of out too
 };
@@ -381,19 +384,22 @@ __device__ __forceinline__ int64_t first_row(const Work& k, int chunk) {
     return k.s.row0 + (k.p->reverse ? k.s.len - at - tokens_of(k, chunk) : at);
 }
 // Where a state goes; null where this segment leaves none.
-__device__ __forceinline__ float* state_out(const Work& k) {
+__device__ __forceinline__ bool leaves_state(const Work& k) { return k.s.ends & (k.p->reverse ? 1 : 2); }
+__device__ __forceinline__ float* state_out(const Args& g, const Work& k) {
     const Pass& p = *k.p;
-    if (!p.z_out || !(p.out_by_segment || (k.s.ends & (p.reverse ? 1 : 2)))) return nullptr;
-    return p.z_out + (p.out_by_segment ? k.s.id : k.s.seq) * p.unit_out + (int64_t)k.head * p.kd * p.vd;
+    const int64_t size = (int64_t)p.kd * p.vd;
+    if (k.s.slot >= 0 && p.slots_out) return p.slots_out + (k.s.slot * (int64_t)g.heads + k.head) * size;
+    return p.z_out && leaves_state(k) ? p.z_out + k.s.seq * p.unit_out + k.head * size : nullptr;
 }
-__device__ __forceinline__ const float* state_in(const Work& k) {
+__device__ __forceinline__ const float* state_in(const Args& g, const Work& k) {
     const Pass& p = *k.p;
-    if (!p.z_in) return nullptr;
-    return p.z_in + (p.in_by_segment ? k.s.id : k.s.seq) * p.unit_in + (int64_t)k.head * p.kd * p.vd;
+    const int64_t size = (int64_t)p.kd * p.vd;
+    if (k.s.slot >= 0) return p.slots_in ? p.slots_in + (k.s.slot * (int64_t)g.heads + k.head) * size : nullptr;
+    return p.z_in ? p.z_in + k.s.seq * p.unit_in + k.head * size : nullptr;
 }
 __device__ __forceinline__ void decay_out(const Work& k, const float* log_decay) {
     const Pass& p = *k.p;
-    if (p.decay_out && (k.s.ends & (p.reverse ? 1 : 2)))
+    if (p.decay_out && leaves_state(k) && !(k.s.slot >= 0 && p.slots_out))
         p.decay_out[k.s.seq * p.unit_out + k.head] =
             k.s.seq_len ? (float)exp((double)log_decay[k.head] * (double)k.s.seq_len) : 1.0f;
 }
@@ -743,7 +749,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
             const int panels_k = (p.kd + 63) / 64, blocks = (p.kd + 15) / 16 * 2;  // of 8 keys
             const bool there = v0 < p.vd;
             float z[64];
-            const float* from = state_in(k);
+            const float* from = state_in(g, k);
 #pragma unroll
             for (int i = 0; i < 64; i++) {
                 const int key = (i >> 2) * 8 + (lane & 3) * 2 + (i & 1), v = value + (i & 2) * 4;
@@ -913,7 +919,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 }
             }
             if (!ok) break;
-            float* const to = state_out(k);
+            float* const to = state_out(g, k);
             if (to) {
 #pragma unroll
                 for (int i = 0; i < 64; i++) {
@@ -1165,7 +1171,7 @@ __global__ void __launch_bounds__(kPlainThreads, kTiles == 1 ? 2 : 1) attention_
     const int chunks = (k.s.len + kPlainChunk - 1) / kPlainChunk;
     if (chunks) fetch(0);
     if (t < kPlainChunk) powers[t] = exp2f(k.l2 * t);
-    const float* from = state_in(k);
+    const float* from = state_in(g, k);
     float4 z[kTiles][kTiles][4];
 #pragma unroll
     for (int a = 0; a < kTiles; a++)
@@ -1293,7 +1299,7 @@ __global__ void __launch_bounds__(kPlainThreads, kTiles == 1 ? 2 : 1) attention_
             }
         __syncthreads();
     }
-    float* const to = state_out(k);
+    float* const to = state_out(g, k);
     if (to) {
 #pragma unroll
         for (int a = 0; a < kTiles; a++)
@@ -1314,21 +1320,22 @@ __global__ void __launch_bounds__(kPlainThreads, kTiles == 1 ? 2 : 1) attention_
 // ---- along the segments, along the ranks, single tokens -----------------------------------------
 
 struct FoldArgs {
-    float* states[2];          // [segments][heads][size]: what each adds; on return the state that enters it
+    float* states[2];          // [slots][heads][size]: what each segment adds; on return the state that enters it
     const float* first[2];     // [sequences][heads][size], null: zero
     float* summary[2];         // null: not wanted; else the last segments' additions are there too
     int reverse[2];
-    const Segment* segments;   // in the order of time
-    const int32_t* begin;      // [sequences + 1]
+    const Segment* segments;   // by slot: those of a sequence in the order of time
+    const int32_t* begin;      // [sequences that are cut + 1]
     const float* log_decay;
     int heads, size;
 };
 __global__ void __launch_bounds__(256) attention_fold_kernel(const __grid_constant__ FoldArgs g) {
     pdl_wait();
     pdl_trigger();
-    const int which = blockIdx.z, s = blockIdx.x / g.heads, h = blockIdx.x - s * g.heads;
+    const int which = blockIdx.z, cut = blockIdx.x / g.heads, h = blockIdx.x - cut * g.heads;
     const int at = blockIdx.y * 256 + threadIdx.x;
-    const int lo = g.begin[s], n = g.begin[s + 1] - lo;
+    const int lo = g.begin[cut], n = g.begin[cut + 1] - lo;
+    const int64_t s = g.segments[lo].seq;
     const float l2 = log2_decay(g.log_decay, h);
     const int64_t unit = (int64_t)g.heads * g.size;
     if (at < g.size) {
@@ -1457,23 +1464,23 @@ struct sparbit_linear_attention_plan_s {
     int n_seqs = 0, heads = 0, kd = 0, vd = 0, dtype = 0;
     float scale = 1.0f;
     size_t rows = 0;
-    bool split = false;                // some sequence has several segments
-    std::vector<Segment> time, list;   // segments in the order of time, and the longest first
-    std::vector<int32_t> begin;        // of each sequence's segments
+    std::vector<Segment> slots, list;  // segments of the sequences that are cut, by slot; all, the longest first
+    std::vector<int32_t> begin;        // slots of each sequence that is cut
     char* work = nullptr;
     int device = -1, sm_count = 0;
     unsigned long long limit = kWaitNs;
     int withhold = 0;
     void* encode = nullptr;            // cuTensorMapEncodeTiled
 
+    bool split() const { return !slots.empty(); }
     size_t states() const { return (size_t)heads * kd * vd; }
     size_t block() const { return states() + heads; }
-    size_t off_time() const { return 256; }
-    size_t off_list() const { return off_time() + round_up(time.size() * sizeof(Segment), 256); }
+    size_t off_slots() const { return 256; }
+    size_t off_list() const { return off_slots() + round_up(slots.size() * sizeof(Segment), 256); }
     size_t off_begin() const { return off_list() + round_up(list.size() * sizeof(Segment), 256); }
     size_t off_states(int which) const {
         return off_begin() + round_up(begin.size() * sizeof(int32_t), 256) +
-               (split ? which * round_up(time.size() * states() * sizeof(float), 256) : 0);
+               which * round_up(slots.size() * states() * sizeof(float), 256);
     }
     size_t work_bytes() const { return off_states(2); }
 };
@@ -1587,27 +1594,25 @@ int run(const Plan* p, Args& g, cudaStream_t st) {
 }
 
 int fold(const Plan* p, FoldArgs& f, int n, const float* log_decay, cudaStream_t st) {
-    f.segments = (const Segment*)(p->work + p->off_time());
+    f.segments = (const Segment*)(p->work + p->off_slots());
     f.begin = (const int32_t*)(p->work + p->off_begin());
     f.log_decay = log_decay;
     f.heads = p->heads, f.size = p->kd * p->vd;
     for (int i = 0; i < n; i++) f.states[i] = (float*)(p->work + p->off_states(i));
-    CU(launch(attention_fold_kernel, dim3((unsigned)(p->n_seqs * p->heads), (unsigned)((f.size + 255) / 256), (unsigned)n),
+    CU(launch(attention_fold_kernel, dim3((unsigned)((p->begin.size() - 1) * p->heads), (unsigned)((f.size + 255) / 256), (unsigned)n),
               dim3(256), 0, st, f));
     return SPARBIT_OK;
 }
 
-// What each segment adds to a state of its direction, for fold.
+// What each segment adds to a state of its direction, for fold; `all`: the last ones of a sequence too, and with them the
+// states of the sequences that are whole.
 void local_states(const Plan* p, Pass& x, int which, bool all) {
     x.out = nullptr;
-    x.z_in = nullptr;
-    x.z_out = (float*)(p->work + p->off_states(which));
-    x.out_by_segment = 1;
+    x.slots_out = (float*)(p->work + p->off_states(which));
     x.skip_ends = !all;
 }
 void from_segment(const Plan* p, Pass& x, int which) {
-    x.z_in = (const float*)(p->work + p->off_states(which));
-    x.in_by_segment = 1;
+    if (p->split()) x.slots_in = (const float*)(p->work + p->off_states(which));
 }
 void into_summary(const Plan* p, Pass& x, float* summary) {
     if (!summary) return;
@@ -1687,22 +1692,23 @@ int sparbit_linear_attention_plan_create(int n_seqs, const size_t* lengths, int 
         int64_t row = 0;
         for (int s = 0; s < n_seqs; s++) {
             const int64_t n = std::max<int64_t>(1, (units[s] + len - 1) / len), each = (units[s] + n - 1) / n * unit;
-            p->begin.push_back((int32_t)p->time.size());
-            for (int64_t at = 0, first = 1; first || at < (int64_t)lengths[s]; at += each, first = 0) {
+            if (n > 1) p->begin.push_back((int32_t)p->slots.size());
+            int64_t at = 0;
+            do {
                 const int64_t left = (int64_t)lengths[s] - at, here = std::min(each, left);
-                p->time.push_back(Segment{row + at, (int64_t)lengths[s], (int32_t)here, s, (int32_t)p->time.size(),
+                const int32_t slot = n > 1 ? (int32_t)p->slots.size() : -1;
+                p->list.push_back(Segment{row + at, (int64_t)lengths[s], (int32_t)here, s, slot,
                                           (at == 0 ? 1 : 0) | (here == left ? 2 : 0)});
-                if (each == 0) break;
-            }
-            p->split = p->split || p->time.size() - p->begin.back() > 1;
+                if (slot >= 0) p->slots.push_back(p->list.back());
+                at += here;
+            } while (at < (int64_t)lengths[s]);
             row += (int64_t)lengths[s];
         }
-        p->begin.push_back((int32_t)p->time.size());
-        if (p->time.size() > 0x7fffffffu / 3 / heads) {
+        p->begin.push_back((int32_t)p->slots.size());
+        if (p->list.size() > 0x7fffffffu / 3 / heads) {
             delete p;
             return SPARBIT_ERR_LIMIT;
         }
-        p->list = p->time;
         std::stable_sort(p->list.begin(), p->list.end(), [](const Segment& a, const Segment& b) { return a.len > b.len; });
     } catch (const std::bad_alloc&) {
         delete p;
@@ -1735,7 +1741,8 @@ int sparbit_linear_attention_plan_set_workspace(sparbit_linear_attention_plan_t*
     }
     char* base = (char*)dev;
     CU(cudaMemset(base, 0, 256));
-    CU(cudaMemcpy(base + p->off_time(), p->time.data(), p->time.size() * sizeof(Segment), cudaMemcpyHostToDevice));
+    if (p->split())
+        CU(cudaMemcpy(base + p->off_slots(), p->slots.data(), p->slots.size() * sizeof(Segment), cudaMemcpyHostToDevice));
     CU(cudaMemcpy(base + p->off_list(), p->list.data(), p->list.size() * sizeof(Segment), cudaMemcpyHostToDevice));
     CU(cudaMemcpy(base + p->off_begin(), p->begin.data(), p->begin.size() * sizeof(int32_t), cudaMemcpyHostToDevice));
     CU(cudaDeviceSynchronize());
@@ -1762,20 +1769,24 @@ int sparbit_linear_attention_forward(sparbit_linear_attention_plan_t* p, const v
     Args g = common_args(p);
     g.n_passes = 1;
     g.log_decay = log_decay;
-    if (p->split) {
+    if (p->split()) {
         g.pass[0] = main;
         local_states(p, g.pass[0], 0, !o);
-        e = run(p, g, st);
         FoldArgs f = {};
         f.first[0] = first;
-        f.summary[0] = o ? nullptr : summary;
+        if (!o) {
+            g.pass[0].z_in = first;
+            into_summary(p, g.pass[0], summary);
+            f.summary[0] = summary;
+        }
+        e = run(p, g, st);
         if (e == SPARBIT_OK) e = fold(p, f, 1, log_decay, st);
         if (e != SPARBIT_OK || !o) return e;
     }
     g.full = o != nullptr;
     g.pass[0] = main;
     g.pass[0].z_in = first;
-    if (p->split) from_segment(p, g.pass[0], 0);
+    from_segment(p, g.pass[0], 0);
     into_summary(p, g.pass[0], summary);
     return run(p, g, st);
 }
@@ -1803,24 +1814,26 @@ int sparbit_linear_attention_backward(sparbit_linear_attention_plan_t* p, const 
     Pass by_v = make_pass(p, rk, rq, rd, ov, true);
     Args g = common_args(p);
     g.log_decay = log_decay;
-    if (p->split) {
+    by_v.z_in = dlast;
+    if (p->split()) {
         FoldArgs f = {};
         g.n_passes = dq ? 2 : 1;
         g.pass[0] = by_v;
         local_states(p, g.pass[0], 0, !dq);
         f.first[0] = dlast, f.reverse[0] = 1;
-        f.summary[0] = dq ? nullptr : dsummary;
         if (dq) {
             g.pass[1] = make_pass(p, rq, rk, rv, oq, false);
             local_states(p, g.pass[1], 1, false);
             f.first[1] = first;
+        } else {
+            into_summary(p, g.pass[0], dsummary);
+            f.summary[0] = dsummary;
         }
         e = run(p, g, st);
         if (e == SPARBIT_OK) e = fold(p, f, g.n_passes, log_decay, st);
         if (e != SPARBIT_OK || !dq) return e;
     }
-    by_v.z_in = dlast;
-    if (p->split) from_segment(p, by_v, 0);
+    from_segment(p, by_v, 0);
     g.pass[0] = by_v;
     into_summary(p, g.pass[0], dsummary);
     g.n_passes = 1;
@@ -1828,11 +1841,11 @@ int sparbit_linear_attention_backward(sparbit_linear_attention_plan_t* p, const 
         g.full = 1;
         g.n_passes = 3;
         Pass& by_k = g.pass[1] = make_pass(p, rv, rd, rq, ok, true);
-        by_k.z_in = by_v.z_in, by_k.in_by_segment = by_v.in_by_segment;
+        by_k.z_in = by_v.z_in, by_k.slots_in = by_v.slots_in;
         turned(by_k);
         Pass& by_q = g.pass[2] = make_pass(p, rd, rv, rk, oq, false);
         by_q.z_in = first;
-        if (p->split) from_segment(p, by_q, 1);
+        from_segment(p, by_q, 1);
         turned(by_q);
     }
     return run(p, g, st);

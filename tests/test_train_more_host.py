@@ -191,3 +191,11 @@ def test_norm_and_clip_take_their_own_types():
         clip.sums(OnTheGpu((1,), F))
     with pytest.raises(TypeError):
         clip.scale(OnTheGpu((1,), F), 1, 1.0, OnTheGpu((1, 2), F))
+
+
+def test_linear_attention_keeps_states_of_cut_sequences_only():
+    whole = sp.LinearAttentionPlan([64] * 3000, 4, 128, 128)
+    assert whole.workspace_bytes < 1 << 20
+    cut = sp.LinearAttentionPlan([64] * 3000 + [200000], 4, 128, 128)
+    state = 4 * 128 * 128 * 4
+    assert cut.workspace_bytes < 2 * state * (200000 // 128 + 1) + (1 << 20)
