@@ -285,8 +285,9 @@ int sparbit_muon_step(sparbit_ortho_plan_t* plan, const sparbit_muon* args, void
  *   dS_t = scale q_t^T do_t + d dS_{t+1},   dq_t = scale S_t do_t,  dk_t = dS_t v_t,  dv_t = k_t dS_t,
  *   dfirst = d dS_1
  *
- * log_decay: [heads] 32-bit on the device, the natural logarithms: 0 keeps everything, -inf nothing; numbers
- * above 0 are taken as they are.  The decays are constants of the model: they have no gradient here.
+ * log_decay: [heads] 32-bit on the device, the natural logarithms, at most 0: 0 keeps everything, -inf nothing.  (Above
+ * 0 the formulas are followed while f32 and bf16 hold what grows; fp16's products may not.)  The decays are constants
+ * of the model: they have no gradient here.
  * 16-bit types: tokens' weights and the state that a chunk of 128 tokens starts with are rounded to 16 bits
  * for the tensor cores (together they leave o about 1.4 times as far off as its own rounding); states
  * themselves are sums of products with 32-bit factors.  f32: plain 32-bit arithmetic.

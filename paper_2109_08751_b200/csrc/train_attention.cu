@@ -15,6 +15,11 @@
 // Sequences that are too few to fill the GPU are cut into segments: one launch leaves what each segment adds to a
 // state, a fold along the segments makes of it the state that enters each, and the main launch follows.  The
 // same three steps, with an allgather in the middle, are what ranks do that hold slices of a sequence.
+//
+// A token and head has to move 4 x size elements and takes 4 keys x values operations in the recurrence, in chunks another
+// kChunk x (keys + values): 8 x 4096 tokens, 16 heads of 128 / 128 bf16 are 83 us of bytes and 41 of products forward, at
+// 1669 TFLOP/s; it takes 138 us (backward 485, of 145).  In place of bytes the hand-overs between a chunk's steps bound it,
+// see the kernel.  f32 is bound by plain multiply-adds out of shared memory.
 #include <cuda.h>
 #include <math.h>
 
@@ -153,21 +158,6 @@ __device__ __forceinline__ void tmem_store_16x8(uint32_t addr, const uint32_t (&
                  "r"(r[3])
                  : "memory");
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;"
-        : "=l"(reinterpret_cast<unsigned long long&>(r))
-        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
-    return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<unsigned long long&>(r))
-        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)),
-          "l"(reinterpret_cast<unsigned long long&>(c)));
-    return r;
-}
 // D += A B of one CTA: both operands in shared memory, or A in tensor memory.
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
@@ -274,7 +264,7 @@ struct Bits<__half> {
 };
 
 // The power of two that brings `most` to 2^13 .. 2^14, as an exponent: fp16 has few, so rows of its operands are scaled.
-// Numbers below 2^-27 stay below that: they make nothing that fp16 can hold.
+// Up to 2^40: rows whose largest number is smaller than that allows make nothing that fp16 holds.
 __device__ __forceinline__ int exponent_for(float most) {
     const int e = (int)(__float_as_uint(most) >> 23 & 0xff);
     if (e == 0 || e == 255) return 0;
@@ -457,12 +447,17 @@ __device__ __forceinline__ void add_by_hand(uint32_t (&r)[32], uint32_t weights,
     }
 }
 
-// One CTA per SM, its warps in roles: weights, output, parts of c, state, loads, products.  A chunk is
+// One CTA per SM, its warps in roles: weights, output, state (and the parts of c for it), loads, products.  A chunk is
 //   score = a b^T;  its weights W = intra d^(i - j) score, causal, rounded to 16 bits into tensor memory
 //   out = a Z (Z rounded to 16 bits in shared memory), scaled by row in tensor memory, + W c
-//   add = (c times gain d^(n - e - j))^T b, the scaled c in two or three 16-bit parts that hold its 32 bits
-// with Z in registers (16 values x 128 keys a warp) and everything side by side.  W and Z are the only roundings to 16 bits on the way:
-// together they leave out about 1.4 times as far off as rounding it to its type does.
+//   add = (c times gain d^(n - e - j))^T b, the scaled c in 16-bit parts that hold its 32 bits: bf16 four, fp16 two
+// with Z in registers (16 values x 128 keys a warp).  W and Z are the only roundings to 16 bits on the way: together they
+// leave out about 1.4 times as far off as rounding it to its type does.
+//
+// What bounds it: a chunk of 128 / 128 takes 7,500 cycles, of which the products alone are 4,100 (their operands come from
+// shared memory at 64 bytes a cycle), the copies 3,600; the tensor pipe is busy for half of them, the issue slots for 45 %.
+// With only loads and hand-overs left the same pass takes 81 us of 138.  Tensor memory holds one out, one set of scores
+// and two pieces of c's parts at that size, so that consecutive chunks overlap by half a chunk only.
 //
 // fp16 has few exponents: rows of W, c^T and Z are held times powers of two that go by their largest elements.
 template <typename T>

