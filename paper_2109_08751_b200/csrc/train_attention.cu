@@ -246,7 +246,9 @@ struct Bits<__half> {
         x = fma2(make_float2(low(v), high(v)), make_float2(-1.0f, -1.0f), x);
         return v;
     }
-    static __device__ __forceinline__ bool is_odd(uint32_t v) { return (v & 0x7fffu) >= 0x7c00u || (v >> 16 & 0x7fffu) >= 0x7c00u; }
+    static __device__ __forceinline__ bool is_odd(uint32_t v) {
+        return (v & 0x7fffu) >= 0x7c00u || (v >> 16 & 0x7fffu) >= 0x7c00u;
+    }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&v);
@@ -281,7 +283,8 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 // Warps of a CTA by what they do, in groups of four for tensor memory (whose lanes go by the warp's number mod 4) and
 // for the registers, of which each group gets as many as it needs.
 constexpr int kWeightWarps = 4, kOutWarps = 8, kStateWarps = 8, kLoadWarps = 2;
-constexpr int kFirstOut = kWeightWarps, kFirstState = kFirstOut + kOutWarps, kFirstLoad = kFirstState + kStateWarps, kMultiply = kFirstLoad + kLoadWarps, kMultiplyState = kMultiply + 1;
+constexpr int kFirstOut = kWeightWarps, kFirstState = kFirstOut + kOutWarps, kFirstLoad = kFirstState + kStateWarps,
+              kMultiply = kFirstLoad + kLoadWarps, kMultiplyState = kMultiply + 1;
 constexpr int kTensorThreads = 32 * (kFirstLoad + 4);
 constexpr int kRegisters = 80, kWeightRegisters = 64, kOutRegisters = 88, kStateRegisters = 96, kOtherRegisters = 48;
 static_assert(kWeightRegisters + 2 * kOutRegisters + 2 * kStateRegisters + kOtherRegisters <=
@@ -399,8 +402,8 @@ constexpr int kMostStages = 4;
 constexpr uint32_t kRing = 14 * kPanel;
 struct Tables {
     // of a stage: a and b are there, c is; everything, b and a are free again
-    uint64_t full[kMostStages], full_c[kMostStages], empty[kMostStages], used[kMostStages], entered_a[kMostStages], scored, scaled, weighted, entered, done, c_ready[kMostSlots], c_free[kMostSlots], added,
-        add_free, z_ready, out_free, met;
+    uint64_t full[kMostStages], full_c[kMostStages], empty[kMostStages], used[kMostStages], entered_a[kMostStages];
+    uint64_t scored, scaled, weighted, entered, done, c_ready[kMostSlots], c_free[kMostSlots], added, add_free, z_ready, out_free, met;
     uint32_t tmem, gave_up;
     uint32_t bad[2];  // number of the last (every other) chunk whose c holds an infinity or a NaN
     // what a token's part is worth at the end of the chunk: fp16 as floats, bf16 as three numbers for each pair of tokens
@@ -938,7 +941,9 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                     const uint32_t st = c % g.stages, stage = ring + st * g.stage_bytes, bar = full + 8 * st;
                     const uint32_t before = (c / g.stages - 1) & 1;  // parity of this stage's last use
                     const int n = tokens_of(k, chunk);
-                    const bool tiled = p.tiled && n == kChunk, early = tiled && g.early && c >= (uint32_t)g.stages;
+                    // the chunk that was here before laid its tiles out alike
+                    const bool alike = g.full && (g.early ? c >= (uint32_t)g.stages : chunk >= g.stages);
+                    const bool tiled = p.tiled && n == kChunk, early = tiled && alike;
                     if (c >= (uint32_t)g.stages && !warp_wait((early ? entered_a : empty) + 8 * st, before, gave_up, g.limit)) {
                         ok = false;
                         break;
