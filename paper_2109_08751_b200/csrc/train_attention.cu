@@ -993,8 +993,12 @@ __global__ void __launch_bounds__(kTensorThreads, 1) attention_tensor_kernel(con
                 }
             }
             // all products have reported before the CTA ends
-            for (uint32_t i = c > (uint32_t)g.stages ? c - g.stages : 0; i < c && ok; i++)
-                ok = warp_wait(empty + 8 * (i % g.stages), (i / g.stages) & 1, gave_up, g.limit);
+            for (uint32_t i = c > (uint32_t)g.stages ? c - g.stages : 0; i < c && ok; i++) {
+                const uint32_t at = 8 * (i % g.stages), parity = (i / g.stages) & 1;
+                ok = warp_wait(empty + at, parity, gave_up, g.limit) &&
+                     (!g.full || (warp_wait(used + at, parity, gave_up, g.limit) &&
+                                  warp_wait(entered_a + at, parity, gave_up, g.limit)));
+            }
             if (!ok) {  // let the copies under way land before the CTA ends
                 const unsigned long long until = now_ns() + 1000000ull;
                 while (now_ns() < until) {
