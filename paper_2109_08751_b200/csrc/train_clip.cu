@@ -3,8 +3,9 @@
 //
 // Bytes are the floor: all elements read, read again and written.  The tensors are cut into chunks; every CTA has a
 // run of neighbouring chunks of about the same number of elements as the others'.  The second pass goes through each
-// run backwards, so that what the first read last is found in L2.  475 MB of bf16 and f32 in 200 tensors: 81 us for the sums
-// (5.8 TB/s), 173 for the scaling (5.5).
+// run backwards, so that what the first read last is found in L2.  Four CTAs an SM: eight, a chunk or two each, took 37 us
+// in place of 34 for 43 MB.  475 MB of bf16 and f32 in 200 tensors: 81 us for the sums (5.8 TB/s), 172 for the scaling
+// (5.5); of the whole 264, the rest is the gathered sums' kernel and the starts of the others.
 #include <math.h>
 
 #include <algorithm>
@@ -18,7 +19,7 @@ using namespace spb;
 namespace {
 
 constexpr int kChunkElements = 16384, kThreads = 256;
-constexpr int kMostCtas = 148 * 8;
+constexpr int kMostCtas = 148 * 4;
 
 struct alignas(16) Tensor {
     const void* in;
@@ -183,19 +184,20 @@ __device__ __forceinline__ void scale_chunk(const T* in, T* out, int n, float by
     }
     const int head = min(n, (int)((16 - (uintptr_t)in % 16) % 16 / sizeof(T))), whole = (n - head) / A;
     if ((int)threadIdx.x < head) out[threadIdx.x] = from_float<T>(to_float(in[threadIdx.x]) * by);
-    const Pack<T, A>* const v = reinterpret_cast<const Pack<T, A>*>(in + head);
-    Pack<T, A>* const w = reinterpret_cast<Pack<T, A>*>(out + head);
+    const uint4* const from = reinterpret_cast<const uint4*>(in + head);
+    uint4* const to = reinterpret_cast<uint4*>(out + head);
     for (int i0 = threadIdx.x; i0 < whole; i0 += kThreads * kAhead) {
-        Pack<T, A> k[kAhead];
+        uint4 k[kAhead];
 #pragma unroll
         for (int y = 0; y < kAhead; y++)
-            if (i0 + y * kThreads < whole) k[y] = v[i0 + y * kThreads];
+            if (i0 + y * kThreads < whole) k[y] = from[i0 + y * kThreads];
 #pragma unroll
         for (int y = 0; y < kAhead; y++) {
             if (i0 + y * kThreads >= whole) break;
+            Pack<T, A> q = reinterpret_cast<const Pack<T, A>&>(k[y]);
 #pragma unroll
-            for (int i = 0; i < A; i++) k[y].v[i] = from_float<T>(to_float(k[y].v[i]) * by);
-            w[i0 + y * kThreads] = k[y];
+            for (int i = 0; i < A; i++) q.v[i] = from_float<T>(to_float(q.v[i]) * by);
+            to[i0 + y * kThreads] = reinterpret_cast<const uint4&>(q);
         }
     }
     const int done = head + whole * A;
