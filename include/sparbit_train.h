@@ -358,7 +358,7 @@ int sparbit_linear_attention_join(int P, int first_rank, int n_ranks, int heads,
  *
  * 8-bit rows: y in e4m3 (1 byte) over a scale for each row, or each `block` columns of it: scale = max |y| / 448,
  * from y before it is rounded (at least 1e-30 / 448, so that zeros have one; a block with a NaN or an infinity has
- * NaN or infinity as its scale, and y8 is NaN where y / scale is).
+ * NaN or infinity as its scale, and y8 is NaN where y / scale is).  y8 is the 32-bit quotient y / scale rounded to e4m3.
  */
 typedef struct sparbit_norm_plan_s sparbit_norm_plan_t;
 

@@ -286,12 +286,19 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? (U == 4 ? 2 : 3) : 1) no
             float most = g.block ? over_lanes<RowMax>(unit_most[u], min(g.block / kUnit, lanes)) : row_most;
             if (!there || left[u] <= 0) continue;
             if (most < 1e-30f) most = 1e-30f;
-            if (g.block ? col % g.block == 0 : col == 0)
-                g.scales[row * g.scales_ld + (g.block ? col / g.block : 0)] = most / 448.0f;
-            const float by = 448.0f / most;
-            uint2 q;
-            q.x = e4m3x2(mul2(r[u].v[0], both(by))) | e4m3x2(mul2(r[u].v[1], both(by))) << 16;
-            q.y = e4m3x2(mul2(r[u].v[2], both(by))) | e4m3x2(mul2(r[u].v[3], both(by))) << 16;
+            const float scale = most / 448.0f;
+            if (g.block ? col % g.block == 0 : col == 0) g.scales[row * g.scales_ld + (g.block ? col / g.block : 0)] = scale;
+            // y / scale as a reader of both forms it: y times the inverse, and what that leaves of y once more (a step of
+            // Newton's method; 148 us for 16384 x 5000 f16, 140 without it).  Negated, so that a zero keeps its sign through
+            // the step; no step over an infinite scale.
+            const float by = -__fdividef(1.0f, scale), back = scale < INFINITY ? scale : 0.0f;
+            uint32_t pairs8[kUnit / 2];
+#pragma unroll
+            for (int i = 0; i < kUnit / 2; i++) {
+                const float2 q = mul2(r[u].v[i], both(by));
+                pairs8[i] = e4m3x2(fma2(fma2(q, both(back), r[u].v[i]), both(by), q));
+            }
+            const uint2 q = make_uint2((pairs8[0] | pairs8[1] << 16) ^ 0x80808080u, (pairs8[2] | pairs8[3] << 16) ^ 0x80808080u);
             uint8_t* to = g.y8 + row * g.y8_ld + col;
             if (g.y8_wide && left[u] >= kUnit) {
                 *reinterpret_cast<uint2*>(to) = q;
