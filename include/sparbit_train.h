@@ -410,7 +410,8 @@ size_t sparbit_clip_plan_workspace_bytes(const sparbit_clip_plan_t* plan);
 int sparbit_clip_plan_set_workspace(sparbit_clip_plan_t* plan, void* dev, size_t bytes);
 
 /* Host arrays of n device addresses: what is summed, and what the clipped elements are written to (out[i] may be
- * in[i]; out NULL: only sums and norms are wanted).  After set_workspace; SYNCHRONISES; holds until the next call.
+ * in[i]; out NULL: only sums and norms are wanted).  After set_workspace; SYNCHRONISES; holds until the next call, for
+ * calls that were captured before, too.
  * ERR_ARG: an address is null (of a tensor with elements) or no multiple of its element's size; ERR_ALIAS: an
  * output overlaps another output, another tensor's input, or part of its own. */
 int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* plan, const void* const* in, void* const* out);

@@ -44,7 +44,6 @@ struct ClipArgs {
     int G;
     float most, eps;
     float* norms;
-    int write;
 };
 
 __device__ __forceinline__ double block_sum(double v, double* sm) {
@@ -223,12 +222,12 @@ __global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_const
         factor_of(g, r, sm, norm, factor);
         if (threadIdx.x == 0) g.norms[2 * r] = norm, g.norms[2 * r + 1] = factor;
     }
-    if (!g.write) return;
     const int lo = g.cta_begin[blockIdx.x], hi = g.cta_begin[blockIdx.x + 1];
     int rank = -1;
     for (int c = hi - 1; c >= lo; c--) {
         const Chunk k = g.chunks[c];
         const Tensor t = g.tensors[k.tensor];
+        if (!t.out) break;  // only norms are wanted.  The table says so, which a captured call reads when it is replayed
         if (t.rank != rank) {
             rank = t.rank;
             factor_of(g, rank, sm, norm, factor);
@@ -251,7 +250,7 @@ struct sparbit_clip_plan_s {
     std::vector<int32_t> cta_begin, rank_parts;
     char* work = nullptr;
     int device = -1;
-    bool set = false, write = false;
+    bool set = false;
 
     size_t off_tensors() const { return 256; }
     size_t off_chunks() const { return off_tensors() + round_up(tensors.size() * sizeof(Tensor), 256); }
@@ -419,7 +418,6 @@ int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* p, const void* const* in,
     CU(cudaMemcpy(p->work + p->off_tensors(), p->tensors.data(), n * sizeof(Tensor), cudaMemcpyHostToDevice));
     CU(cudaDeviceSynchronize());
     p->set = true;
-    p->write = out != nullptr;
     return SPARBIT_OK;
 }
 
@@ -442,7 +440,7 @@ int sparbit_clip_scale(sparbit_clip_plan_t* p, const double* gathered, int G, fl
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
     ClipArgs g = common_args(p);
-    g.gathered = gathered, g.G = G, g.most = most, g.eps = eps, g.norms = norms, g.write = p->write;
+    g.gathered = gathered, g.G = G, g.most = most, g.eps = eps, g.norms = norms;
     CU(launch(clip_scale_kernel, dim3(p->ctas), dim3(kThreads), 0, (cudaStream_t)stream, g));
     return SPARBIT_OK;
 }
