@@ -1557,12 +1557,15 @@ int run(const Plan* p, Args& g, cudaStream_t st) {
     if (p->dtype == SPARBIT_F32) {
         size_t smem = 0;
         for (int i = 0; i < g.n_passes; i++) smem = std::max(smem, plain_smem(g.pass[i].kd, g.pass[i].vd));
-        auto launch_it = [&](auto kernel) {
-            CU(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        // what a function is allowed is the function's and not this plan's: the same whatever the plan, since another thread
+        // may be setting it for its own
+        auto launch_it = [&](auto kernel, int most) {
+            CU(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plain_smem(most, most)));
             CU(launch(kernel, dim3(g.total), dim3(kPlainThreads), smem, st, g));
             return (int)SPARBIT_OK;
         };
-        return std::max(p->kd, p->vd) <= 64 ? launch_it(attention_plain_kernel<1>) : launch_it(attention_plain_kernel<2>);
+        return std::max(p->kd, p->vd) <= 64 ? launch_it(attention_plain_kernel<1>, 64)
+                                            : launch_it(attention_plain_kernel<2>, kMostSize);
     }
     uint32_t state = 0;
     g.stage_bytes = 0;
