@@ -416,7 +416,7 @@ int sparbit_clip_plan_set_workspace(sparbit_clip_plan_t* plan, void* dev, size_t
  * output overlaps another output, another tensor's input, or part of its own. */
 int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* plan, const void* const* in, void* const* out);
 
-/* sums: [n_ranks] 64-bit.  ERR_WORKSPACE also where no tensors are set. */
+/* sums: [n_ranks] 64-bit.  ERR_WORKSPACE also where no tensors are set; ERR_ALIAS: sums lie in a tensor that is summed. */
 int sparbit_clip_sums(sparbit_clip_plan_t* plan, double* sums, void* stream);
 
 /* gathered: [n_ranks][G] 64-bit, rank r's receive buffer of the allgather of the sums over G ranks.

@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "train_common.cuh"
@@ -241,6 +242,20 @@ __global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_const
     }
 }
 
+// Address ranges, for the question whether another one meets any of them.
+struct Ranges {
+    std::vector<std::pair<uintptr_t, uintptr_t>> v;  // by their first bytes; second: how far this one and those before it reach
+    void finish() {
+        std::sort(v.begin(), v.end());
+        for (size_t i = 1; i < v.size(); i++) v[i].second = std::max(v[i].second, v[i - 1].second);
+    }
+    bool meet(const void* p, size_t bytes) const {
+        const uintptr_t lo = (uintptr_t)p;
+        const auto behind = std::lower_bound(v.begin(), v.end(), std::pair<uintptr_t, uintptr_t>(lo + bytes, 0));
+        return behind != v.begin() && (behind - 1)->second > lo;
+    }
+};
+
 }  // namespace
 
 struct sparbit_clip_plan_s {
@@ -248,6 +263,7 @@ struct sparbit_clip_plan_s {
     std::vector<Tensor> tensors;
     std::vector<Chunk> chunks;
     std::vector<int32_t> cta_begin, rank_parts;
+    Ranges inputs, outputs;  // of the tensors that are set
     char* work = nullptr;
     int device = -1;
     bool set = false;
@@ -381,6 +397,7 @@ int sparbit_clip_plan_set_workspace(sparbit_clip_plan_t* p, void* dev, size_t by
 int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* p, const void* const* in, void* const* out) {
     if (!p || !in) return SPARBIT_ERR_ARG;
     const size_t n = p->tensors.size();
+    Ranges inputs, outputs;
     try {
         struct Span {
             uintptr_t lo, hi;
@@ -394,6 +411,8 @@ int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* p, const void* const* in,
             if (!in[i] || (uintptr_t)in[i] % es || (out && (!out[i] || (uintptr_t)out[i] % es))) return SPARBIT_ERR_ARG;
             const uintptr_t a = (uintptr_t)in[i], b = out ? (uintptr_t)out[i] : 0, bytes = (uintptr_t)t.len * es;
             if (a + bytes < a || (out && b + bytes < b)) return SPARBIT_ERR_ARG;
+            inputs.v.emplace_back(a, a + bytes);
+            if (out) outputs.v.emplace_back(b, b + bytes);
             if (out) spans.push_back(Span{b, b + bytes, true});
             if (!out || a != b) spans.push_back(Span{a, a + bytes, false});
         }
@@ -405,6 +424,7 @@ int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* p, const void* const* in,
             any = std::max(any, s.hi);
             if (s.written) written = std::max(written, s.hi);
         }
+        inputs.finish(), outputs.finish();
     } catch (const std::bad_alloc&) {
         return SPARBIT_ERR_NOMEM;
     }
@@ -417,6 +437,7 @@ int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* p, const void* const* in,
     CU(cudaDeviceSynchronize());
     CU(cudaMemcpy(p->work + p->off_tensors(), p->tensors.data(), n * sizeof(Tensor), cudaMemcpyHostToDevice));
     CU(cudaDeviceSynchronize());
+    p->inputs = std::move(inputs), p->outputs = std::move(outputs);
     p->set = true;
     return SPARBIT_OK;
 }
@@ -426,6 +447,7 @@ int sparbit_clip_sums(sparbit_clip_plan_t* p, double* sums, void* stream) {
     if (regions_overlap({sums, 1, (size_t)p->n_ranks * 8, 0}, {p->work, 1, p->work_bytes(), 0})) return SPARBIT_ERR_ALIAS;
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
+    if (p->inputs.meet(sums, (size_t)p->n_ranks * 8)) return SPARBIT_ERR_ALIAS;
     ClipArgs g = common_args(p);
     g.sums = sums;
     CU(launch(clip_sums_kernel, dim3(p->ctas), dim3(kThreads), 0, (cudaStream_t)stream, g));
@@ -439,6 +461,8 @@ int sparbit_clip_scale(sparbit_clip_plan_t* p, const double* gathered, int G, fl
     if (regions_overlap(rn, rg) || regions_overlap(rn, {p->work, 1, p->work_bytes(), 0})) return SPARBIT_ERR_ALIAS;
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
+    if (p->inputs.meet(norms, rn.width) || p->outputs.meet(norms, rn.width) || p->outputs.meet(gathered, rg.width))
+        return SPARBIT_ERR_ALIAS;
     ClipArgs g = common_args(p);
     g.gathered = gathered, g.G = G, g.most = most, g.eps = eps, g.norms = norms;
     CU(launch(clip_scale_kernel, dim3(p->ctas), dim3(kThreads), 0, (cudaStream_t)stream, g));
