@@ -393,7 +393,7 @@ int sparbit_norm_backward(sparbit_norm_plan_t* plan, size_t rows, const void* dy
 
 /* ---- norm of all gradients, and clipping --------------------------------------------------------
  *
- *   sums[r] = sum of the squares of all elements of rank r's tensors, in 64 bits
+ *   sums[r] = sum of the squares of all elements of rank r's tensors, in 64 bits throughout
  *   norm = sqrt(sum over the ranks of sums),  factor = min(1, most / (norm + eps)),  out = factor * in
  *
  * A norm that is NaN makes every element NaN, an infinite one makes the factor 0 (and infinite elements NaN).

@@ -58,25 +58,23 @@ __device__ __forceinline__ double block_sum(double v, double* sm) {
     return v;
 }
 
-// Squares of a few numbers, one by one in 64 bits: where 32 do not hold their sum.
-template <int N>
-__device__ __noinline__ double squares_in_64(const float (&v)[N]) {
-    double d = 0.0;
-    for (int i = 0; i < N; i++) d += (double)v[i] * (double)v[i];
-    return d;
-}
-
 constexpr int kAhead = 4;  // accesses of a thread that are on their way together
 
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* p, int n) {
     constexpr int A = 16 / sizeof(T);
-    double sum = 0.0;
+    constexpr int kChains = 4;  // of additions that do not wait for one another
+    double sum[kChains] = {};
+    // squares are exact in 64 bits, of 32-bit numbers too
+    auto square = [&](T x, int chain) {
+        const double v = (double)to_float(x);
+        sum[chain] = fma(v, v, sum[chain]);
+    };
     const int head = min(n, (int)((16 - (uintptr_t)p % 16) % 16 / sizeof(T))), whole = (n - head) / A;
     const int done = head + whole * A;
     // the elements in front of the first whole access and behind the last
-    if ((int)threadIdx.x < head) sum += (double)to_float(p[threadIdx.x]) * (double)to_float(p[threadIdx.x]);
-    if ((int)threadIdx.x < n - done) sum += (double)to_float(p[done + threadIdx.x]) * (double)to_float(p[done + threadIdx.x]);
+    if ((int)threadIdx.x < head) square(p[threadIdx.x], 0);
+    if ((int)threadIdx.x < n - done) square(p[done + threadIdx.x], 1);
     const uint4* const v = reinterpret_cast<const uint4*>(p + head);
     uint4 k[2][kAhead];
     auto fetch = [&](int i0, uint4 (&to)[kAhead]) {
@@ -87,31 +85,13 @@ __device__ __forceinline__ double chunk_squares(const T* p, int n) {
         }
     };
     auto add = [&](const uint4 (&from)[kAhead]) {
-        // 32 bits for the squares of one thread's accesses, 64 for their sums
-        float s = 0.0f;
-        uint32_t any = 0;
 #pragma unroll
         for (int y = 0; y < kAhead; y++) {
             const Pack<T, A> q = reinterpret_cast<const Pack<T, A>&>(from[y]);
 #pragma unroll
-            for (int i = 0; i < A; i++) s = fmaf(to_float(q.v[i]), to_float(q.v[i]), s);
-            any |= from[y].x | from[y].y | from[y].z | from[y].w;
-        }
-        if (s > 1e-30f && s < 1e30f) {
-            sum += (double)s;
-        } else if (any) {
-#pragma unroll 1
-            for (int y = 0; y < kAhead; y++) {
-                const uint4 u = y == 0 ? from[0] : y == 1 ? from[1] : y == 2 ? from[2] : from[3];
-                const Pack<T, A> q = reinterpret_cast<const Pack<T, A>&>(u);
-                float f[A];
-#pragma unroll
-                for (int i = 0; i < A; i++) f[i] = to_float(q.v[i]);
-                sum += squares_in_64(f);
-            }
+            for (int i = 0; i < A; i++) square(q.v[i], i % kChains);
         }
     };
-    static_assert(kAhead == 4);
     fetch(threadIdx.x, k[0]);
     for (int i0 = threadIdx.x; i0 < whole; i0 += 2 * kThreads * kAhead) {
         fetch(i0 + kThreads * kAhead, k[1]);
@@ -119,7 +99,7 @@ __device__ __forceinline__ double chunk_squares(const T* p, int n) {
         fetch(i0 + 2 * kThreads * kAhead, k[0]);
         add(k[1]);
     }
-    return sum;
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 __global__ void __launch_bounds__(kThreads) clip_sums_kernel(const __grid_constant__ ClipArgs g) {
