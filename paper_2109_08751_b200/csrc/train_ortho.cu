@@ -64,6 +64,7 @@ constexpr int kSmem = kRing<kThree> + kOutWarps<kThree> * 32 * 32 * 4 + 1024;  /
 constexpr int flush_blocks(int op, bool full) { return !full ? 8 : op == 0 ? 2 : 1; }
 constexpr int kNormParts = 512;                         // CTAs a matrix's norm is summed by
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;   // X and A, P are held times these
+constexpr uint32_t kSuspendNs = 10000000;               // of one try of a wait
 
 // ---- PTX ----------------------------------------------------------------------------------------
 // Arrival at the barrier at the same place in the pair's first CTA.
@@ -366,7 +367,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                 const int row = (int)(rc >> 16) * kTileM + rank * (kTileM / 2), col = (int)(rc & 0xffff) * kN + rank * (kN / 2);
                 for (int s = 0; s < blocks; s++, n++) {
                     const uint32_t st = n % kStages;
-                    if (n >= kStages && !bar_wait(empty + 8 * st, (n / kStages - 1) & 1, &gave_up, g.limit)) {
+                    if (n >= kStages && !bar_wait<kSuspendNs>(empty + 8 * st, (n / kStages - 1) & 1, &gave_up, g.limit)) {
                         ok = false;
                         break;
                     }
@@ -391,7 +392,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
             }
             // the products have read every stage, and said so to both CTAs, before either may end
             for (uint32_t i = n > kStages ? n - kStages : 0; i < n && ok; i++)
-                ok = bar_wait(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up, g.limit);
+                ok = bar_wait<kSuspendNs>(empty + 8 * (i % kStages), (i / kStages) & 1, &gave_up, g.limit);
             if (!ok) {  // let the copies under way land before the CTA ends
                 const unsigned long long until = now_ns() + 1000000ull;
                 while (now_ns() < until) {
@@ -413,7 +414,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
             for (int t = pair; t < g.total && ok; t += pairs) {
                 for (int s0 = 0; s0 < blocks && ok; s0 += flush, group++) {
                     const uint32_t slot = group % kSlots;
-                    if (group >= kSlots && !warp_wait(drained + 8 * slot, (group / kSlots - 1) & 1, &gave_up, g.limit)) {
+                    if (group >= kSlots && !warp_wait<kSuspendNs>(drained + 8 * slot, (group / kSlots - 1) & 1, &gave_up, g.limit)) {
                         ok = false;
                         break;
                     }
@@ -421,7 +422,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                     const int end = s0 + flush < blocks ? s0 + flush : blocks;
                     for (int s = s0; s < end; s++, n++) {
                         const uint32_t st = n % kStages;
-                        if (!warp_wait(full + 8 * st, (n / kStages) & 1, &gave_up, g.limit)) {
+                        if (!warp_wait<kSuspendNs>(full + 8 * st, (n / kStages) & 1, &gave_up, g.limit)) {
                             ok = false;
                             break;
                         }
@@ -448,7 +449,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
             // The other CTA's warps arrive at `drained` in this one's shared memory: the last arrivals, which no later
             // product waits for, must have landed before this CTA may end.
             for (uint32_t i = group > kSlots ? group - kSlots : 0; i < group && ok; i++)
-                ok = warp_wait(drained + 8 * (i % kSlots), (i / kSlots) & 1, &gave_up, g.limit);
+                ok = warp_wait<kSuspendNs>(drained + 8 * (i % kSlots), (i / kSlots) & 1, &gave_up, g.limit);
         }
     } else {
         // TMEM lanes go by the warp's number mod 4; the warps of a quarter share the columns
@@ -476,7 +477,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                 // predecessor goes out
                 if (wanted(0)) load_addend<kOp, kThree>(g, z, row0, col0, d[0]);
                 const uint32_t slot = group % kSlots;
-                ok = warp_wait(done + 8 * slot, (group / kSlots) & 1, &gave_up, g.limit);
+                ok = warp_wait<kSuspendNs>(done + 8 * slot, (group / kSlots) & 1, &gave_up, g.limit);
                 if (!ok) break;
                 fence_after();
 #pragma unroll
@@ -507,7 +508,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<kThree>, 1)
                 for (int i = 0; i < kCols; i++) acc[i] = 0.0f;
                 for (int s = 0; s < blocks; s += flush, group++) {
                     const uint32_t slot = group % kSlots;
-                    ok = warp_wait(done + 8 * slot, (group / kSlots) & 1, &gave_up, g.limit);
+                    ok = warp_wait<kSuspendNs>(done + 8 * slot, (group / kSlots) & 1, &gave_up, g.limit);
                     if (!ok) break;
                     fence_after();
 #pragma unroll

@@ -14,15 +14,27 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t n) {
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// kSuspendNs: how long the hardware may let the thread sleep in one try; 0: its own limit.
+template <uint32_t kSuspendNs = 0>
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
+    if constexpr (kSuspendNs > 0) {
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity), "n"(kSuspendNs)
+            : "memory");
+    } else {
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    }
     return ok != 0;
 }
 __device__ __forceinline__ unsigned long long now_ns() {
@@ -31,11 +43,12 @@ __device__ __forceinline__ unsigned long long now_ns() {
     return t;
 }
 // Bounded: false once the time is up or another role of the CTA gave up.  For one lane.
+template <uint32_t kSuspendNs = 0>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up,
                                          unsigned long long limit) {
-    if (bar_try(bar, parity)) return true;
+    if (bar_try<kSuspendNs>(bar, parity)) return true;
     const unsigned long long until = now_ns() + limit;
-    while (!bar_try(bar, parity)) {
+    while (!bar_try<kSuspendNs>(bar, parity)) {
         if (*gave_up) return false;
         if (now_ns() > until) {
             *gave_up = 1;
@@ -46,11 +59,12 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
 }
 // The same for a whole warp: all lanes get one answer.  Each by itself could see the time run out a look before or
 // after another, and what follows a wait (elect, tensor memory) takes all lanes of the warp.
+template <uint32_t kSuspendNs = 0>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up,
                                           unsigned long long limit) {
-    if (__all_sync(kAllLanes, bar_try(bar, parity))) return true;
+    if (__all_sync(kAllLanes, bar_try<kSuspendNs>(bar, parity))) return true;
     const unsigned long long until = now_ns() + limit;
-    while (!__all_sync(kAllLanes, bar_try(bar, parity))) {
+    while (!__all_sync(kAllLanes, bar_try<kSuspendNs>(bar, parity))) {
         if (__any_sync(kAllLanes, *gave_up || now_ns() > until)) {
             *gave_up = 1;
             return false;
