@@ -4,7 +4,7 @@ Operators of a training step whose state is divided over the ranks of a communic
 tensors in device (or pinned host) memory, whose type has to be the operator's (TypeError); numpy arrays,
 addresses and other objects with `data_ptr()` are taken as they are.  Row strides (`*_ld`, in elements)
 default to the row's width, which a tensor with gaps between its rows does not have (ValueError: give its
-stride).  Everything runs in the library's CUDA kernels; there is no fallback.
+stride); a view that no row stride describes (heads apart from one another, a padded batch) is a ValueError, too.  Everything runs in the library's CUDA kernels; there is no fallback.
 """
 from __future__ import annotations
 
@@ -140,11 +140,40 @@ def _address_checked(x, code):
     return x.data_ptr()
 
 
-def _stride_of(x, ld, width):
+def _stride_of(x, ld, width, evenly=True):
     """The row stride: the one that is given, or the width for a tensor whose rows follow one another."""
     if ld is not None:
-        return ld
+        return ld if x is None or _in_rows(x, width, evenly) else None
     return width if x is None or _dense(x) else None
+
+
+def _in_rows(x, width, evenly=True):
+    """True, or ValueError for a view that no row stride describes: `width` elements that do not follow one another (heads
+    that lie apart, say), or (`evenly`) rows that do not lie equally far apart (a padded batch)."""
+    try:
+        if x.is_contiguous():
+            return True
+        sizes, strides = x.shape, x.stride()
+    except AttributeError:
+        return True
+    if strides[-1:] == (1,):  # the usual parts of wider rows, plain or in heads
+        if len(strides) == 2 and sizes[1] >= width:
+            return True
+        if len(strides) == 3 and sizes[2] == strides[1] and sizes[1] * sizes[2] == width:
+            return True
+    follow, at = 1, None  # elements of a row so far; behind those how far the next size's elements lie apart
+    for size, stride in zip(reversed(sizes), reversed(strides)):
+        if size == 1:
+            continue
+        if follow < width:
+            if stride != follow:
+                raise ValueError("the elements of a row have to follow one another, those of its heads too")
+            follow *= size
+        else:
+            if evenly and at is not None and stride != at:
+                raise ValueError("the rows have to lie equally far apart")
+            at = stride * size
+    return True
 
 
 def _dense(x):
@@ -167,6 +196,14 @@ def _flat(x, code):
     except (AttributeError, KeyError):
         pass
     return _address_checked(x, code) if _dense(x) else None
+
+
+def _rows_of(x, code, ld, width):
+    """Address of a tensor with the row stride `ld`, or of one without."""
+    if ld is None:
+        return _flat(x, code)
+    address = _address_of(x, code)
+    return address if x is None or _in_rows(x, width) else None
 
 
 def _stream_handle(stream):
@@ -274,20 +311,19 @@ def scan_step(rows: int, channels: int, dtype: int, gate, x, state_in, state_out
         t, f = _types[dtype], _types[F32]
         usual = (gate.dtype is x.dtype is y.dtype is t and state_in.dtype is state_out.dtype is f
                  and gate.is_cuda and x.is_cuda and y.is_cuda and state_in.is_cuda and state_out.is_cuda
-                 and (gate_ld is not None or gate.is_contiguous()) and (x_ld is not None or x.is_contiguous())
-                 and (y_ld is not None or y.is_contiguous())
-                 and (state_ld is not None or (state_in.is_contiguous() and state_out.is_contiguous())))
+                 and (gate.is_contiguous() if gate_ld is None else _in_rows(gate, channels))
+                 and (x.is_contiguous() if x_ld is None else _in_rows(x, channels))
+                 and (y.is_contiguous() if y_ld is None else _in_rows(y, channels))
+                 and (state_in.is_contiguous() and state_out.is_contiguous() if state_ld is None
+                      else _in_rows(state_in, channels) and _in_rows(state_out, channels)))
     except (AttributeError, KeyError):
         usual = False
     if usual:
         gate, x, y, state_in, state_out = (gate.data_ptr(), x.data_ptr(), y.data_ptr(), state_in.data_ptr(),
                                            state_out.data_ptr())
     else:
-        gate = _address_of(gate, dtype) if gate_ld is not None else _flat(gate, dtype)
-        x = _address_of(x, dtype) if x_ld is not None else _flat(x, dtype)
-        y = _address_of(y, dtype) if y_ld is not None else _flat(y, dtype)
-        of_state = _address_of if state_ld is not None else _flat
-        state_in, state_out = of_state(state_in, F32), of_state(state_out, F32)
+        gate, x, y = _rows_of(gate, dtype, gate_ld, channels), _rows_of(x, dtype, x_ld, channels), _rows_of(y, dtype, y_ld, channels)
+        state_in, state_out = _rows_of(state_in, F32, state_ld, channels), _rows_of(state_out, F32, state_ld, channels)
     d = channels
     args = (rows, d, dtype, gate, d if gate_ld is None else gate_ld, x, d if x_ld is None else x_ld, _flat(slots, _I32),
             rows if n_slots is None else n_slots, state_in, state_out, d if state_ld is None else state_ld, y,
@@ -325,7 +361,7 @@ class RouterPlan(_TrainPlan):
             usual = (logits.dtype is t and indices.dtype is counts.dtype is i
                      and weights.dtype is lse.dtype is sums.dtype is f and logits.is_cuda and indices.is_cuda
                      and weights.is_cuda and lse.is_cuda and counts.is_cuda and sums.is_cuda
-                     and (ld is not None or logits.is_contiguous()) and indices.is_contiguous()
+                     and (logits.is_contiguous() if ld is None else _in_rows(logits, self.experts)) and indices.is_contiguous()
                      and weights.is_contiguous() and lse.is_contiguous() and counts.is_contiguous()
                      and sums.is_contiguous())
         except (AttributeError, KeyError):
@@ -334,7 +370,7 @@ class RouterPlan(_TrainPlan):
             logits, indices, weights, lse, counts, sums = (logits.data_ptr(), indices.data_ptr(), weights.data_ptr(),
                                                            lse.data_ptr(), counts.data_ptr(), sums.data_ptr())
         else:
-            logits = _address_of(logits, self.dtype) if ld is not None else _flat(logits, self.dtype)
+            logits = _rows_of(logits, self.dtype, ld, self.experts)
             indices, weights, lse = _flat(indices, _I32), _flat(weights, F32), _flat(lse, F32)
             counts, sums = _flat(counts, _I32), _flat(sums, F32)
         args = (self._h, logits, self.experts if ld is None else ld, _flat(mask, _BYTE), indices, weights, lse, counts,
@@ -385,7 +421,8 @@ class OrthoPlan(_TrainPlan):
         _check(lib.sparbit_ortho_plan_set_products(self._h, products), "sparbit_ortho_plan_set_products")
 
     def orthogonalize(self, update, out, stream=None, ld=None, stride=None, out_ld=None, out_stride=None) -> None:
-        t, ld, out_ld = self.dtype, _stride_of(update, ld, self.cols), _stride_of(out, out_ld, self.cols)
+        # matrices have a stride of their own
+        t, ld, out_ld = self.dtype, _stride_of(update, ld, self.cols, False), _stride_of(out, out_ld, self.cols, False)
         stride = self.rows * ld if stride is None else stride
         out_stride = self.rows * out_ld if out_stride is None else out_stride
         _check(lib.sparbit_orthogonalize(self._h, _address_of(update, t), ld, stride, _address_of(out, t), out_ld,
@@ -395,13 +432,10 @@ class OrthoPlan(_TrainPlan):
                   momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale: float = 1.0,
                   stream=None, grad_ld=None, grad_stride=None, momentum_ld=None, momentum_stride=None, weight_ld=None,
                   weight_stride=None) -> None:
-        if momentum_ld is None:
-            _dense(momentum_in)
-        if weight_ld is None:
-            _dense(weight_in)
         r, c = self.rows, self.cols
-        gl, ml = _stride_of(grad, grad_ld, c), _stride_of(momentum_out, momentum_ld, c)
-        wl = _stride_of(weight_out, weight_ld, c)
+        _stride_of(momentum_in, momentum_ld, c, False), _stride_of(weight_in, weight_ld, c, False)
+        gl, ml = _stride_of(grad, grad_ld, c, False), _stride_of(momentum_out, momentum_ld, c, False)
+        wl = _stride_of(weight_out, weight_ld, c, False)
         args = MuonArgs(_address_of(grad, self.dtype), gl, r * gl if grad_stride is None else grad_stride,
                         _address_of(momentum_in, F32), _address_of(momentum_out, F32), ml,
                         r * ml if momentum_stride is None else momentum_stride, _address_of(weight_in, weight_dtype),
@@ -449,11 +483,11 @@ def linear_attention_step(rows: int, heads: int, key_size: int, value_size: int,
     wk, wv = heads * key_size, heads * value_size
     code = lib.sparbit_linear_attention_step(
         rows, heads, key_size, value_size, dtype, key_size ** -0.5 if scale is None else scale,
-        _address_of(q, dtype), wk if q_ld is None and _dense(q) else q_ld,
-        _address_of(k, dtype), wk if k_ld is None and _dense(k) else k_ld,
-        _address_of(v, dtype), wv if v_ld is None and _dense(v) else v_ld, _flat(log_decay, F32), _flat(slots, _I32),
+        _address_of(q, dtype), _stride_of(q, q_ld, wk),
+        _address_of(k, dtype), _stride_of(k, k_ld, wk),
+        _address_of(v, dtype), _stride_of(v, v_ld, wv), _flat(log_decay, F32), _flat(slots, _I32),
         rows if n_slots is None else n_slots, _flat(state_in, F32), _flat(state_out, F32), _address_of(o, dtype),
-        wv if o_ld is None and _dense(o) else o_ld, _stream_handle(stream))
+        _stride_of(o, o_ld, wv), _stream_handle(stream))
     if code != OK:
         raise SparbitError(code, "sparbit_linear_attention_step")
 
