@@ -31,7 +31,8 @@
  * Matrices are row-major with a row stride ("ld") in ELEMENTS, at least the row's width and at most
  * 2^46 divided by the number of rows (ERR_ARG).  Any
  * alignment that suits the element type gives the right answer; where pointers and strides are
- * multiples of 16 bytes the wide kernels run.  Outputs must overlap neither inputs nor each other
+ * multiples of 16 bytes the wide kernels run.  (Linear attention, norm and clipping refuse an address that is no multiple
+ * of its element's size, ERR_ARG.)  Outputs must overlap neither inputs nor each other
  * (ERR_ALIAS); row-interleaved halves of one buffer do not overlap.
  */
 #ifndef SPARBIT_TRAIN_H

@@ -1769,6 +1769,8 @@ int sparbit_linear_attention_forward(sparbit_linear_attention_plan_t* p, const v
                           {first, 1, states, 0}, {p->work, 1, p->work_bytes(), 0}};
     const Region outs[] = {region(p, ro), {summary, 1, p->n_seqs * p->block() * 4, 0}};
     int e = overlaps(ins, 6, outs, 2);
+    if (e == SPARBIT_OK && (misaligned(elem_size(p->dtype), {rq.p, k, v, o}) || misaligned(4, {log_decay, first, summary})))
+        e = SPARBIT_ERR_ARG;
     if (e == SPARBIT_OK) e = ready(p);
     if (e != SPARBIT_OK || (!o && !summary)) return e;
     const cudaStream_t st = (cudaStream_t)stream;
@@ -1814,6 +1816,9 @@ int sparbit_linear_attention_backward(sparbit_linear_attention_plan_t* p, const 
                           {dq ? first : nullptr, 1, states, 0}, {dlast, 1, states, 0}, {p->work, 1, p->work_bytes(), 0}};
     const Region outs[] = {region(p, oq), region(p, ok), region(p, ov), {dsummary, 1, p->n_seqs * p->block() * 4, 0}};
     int e = overlaps(ins, 8, outs, 4);
+    if (e == SPARBIT_OK && (misaligned(elem_size(p->dtype), {q, rk.p, rv.p, d_o, dq, dk, dv}) ||
+                            misaligned(4, {log_decay, dq ? first : nullptr, dlast, dsummary})))
+        e = SPARBIT_ERR_ARG;
     if (e == SPARBIT_OK) e = ready(p);
     if (e != SPARBIT_OK || (!dq && !dsummary)) return e;
     const cudaStream_t st = (cudaStream_t)stream;
@@ -1901,6 +1906,7 @@ int sparbit_linear_attention_step(size_t rows, int heads, int key_size, int valu
         if (regions_overlap(ro, in) || regions_overlap(so, in)) return SPARBIT_ERR_ALIAS;
     if (regions_overlap(ro, ri) || regions_overlap(ro, so) || (state_in != state_out && regions_overlap(so, ri)))
         return SPARBIT_ERR_ALIAS;
+    if (misaligned(es, {q, k, v, o}) || misaligned(4, {log_decay, slots, state_in, state_out})) return SPARBIT_ERR_ARG;
     const bool wide = value_size % 4 == 0 && ((uintptr_t)state_in | (uintptr_t)state_out) % 16 == 0;
     // few rows: a head's values in slices of 32, a CTA each
     const int slice = rows * heads < 2 * (size_t)kSms && value_size > 32 ? 32 : value_size;
@@ -1930,6 +1936,7 @@ int sparbit_linear_attention_join(int P, int first_rank, int n_ranks, int heads,
     const Region rg{gathered, 1, (size_t)n_ranks * P * block * 4, 0}, rf{first, 1, heads * size * 4, 0},
         ro{out, 1, (size_t)n_ranks * heads * size * 4, 0};
     if (regions_overlap(ro, rg) || regions_overlap(ro, rf)) return SPARBIT_ERR_ALIAS;
+    if (misaligned(4, {gathered, first, out})) return SPARBIT_ERR_ARG;
     CU(launch(attention_join_kernel, dim3((unsigned)((size + 255) / 256), (unsigned)heads, (unsigned)n_ranks), dim3(256), 0,
               (cudaStream_t)stream, P, first_rank, heads, (int)size, gathered, first, out, reverse));
     return SPARBIT_OK;

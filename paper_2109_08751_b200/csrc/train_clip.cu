@@ -425,6 +425,7 @@ int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* p, const void* const* in,
 int sparbit_clip_sums(sparbit_clip_plan_t* p, double* sums, void* stream) {
     if (!p || !sums) return SPARBIT_ERR_ARG;
     if (regions_overlap({sums, 1, (size_t)p->n_ranks * 8, 0}, {p->work, 1, p->work_bytes(), 0})) return SPARBIT_ERR_ALIAS;
+    if (misaligned(8, {sums})) return SPARBIT_ERR_ARG;
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
     if (p->inputs.meet(sums, (size_t)p->n_ranks * 8)) return SPARBIT_ERR_ALIAS;
@@ -439,6 +440,7 @@ int sparbit_clip_scale(sparbit_clip_plan_t* p, const double* gathered, int G, fl
     if (!p || !gathered || !norms || G < 1 || !(most >= 0.0f) || !(eps >= 0.0f) || !isfinite(eps)) return SPARBIT_ERR_ARG;
     const Region rg{gathered, 1, (size_t)p->n_ranks * G * 8, 0}, rn{norms, 1, (size_t)p->n_ranks * 8, 0};
     if (regions_overlap(rn, rg) || regions_overlap(rn, {p->work, 1, p->work_bytes(), 0})) return SPARBIT_ERR_ALIAS;
+    if (misaligned(8, {gathered}) || misaligned(4, {norms})) return SPARBIT_ERR_ARG;
     const int e = ready(p);
     if (e != SPARBIT_OK) return e;
     if (p->inputs.meet(norms, rn.width) || p->outputs.meet(norms, rn.width) || p->outputs.meet(gathered, rg.width))

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "../../include/sparbit_train.h"
 #include "plan_access.h"
 
@@ -45,6 +47,13 @@ inline bool regions_overlap(const Region& a, const Region& b) {
     if (a.ld != b.ld || a.ld == 0) return true;
     const size_t d = x <= y ? (size_t)(y - x) % a.ld : (a.ld - (size_t)(x - y) % a.ld) % a.ld;
     return d < a.width || d + b.width > a.ld;
+}
+
+// Whether one of the addresses (nulls apart) is no multiple of its elements' size: such an access would fault.
+inline bool misaligned(size_t size, std::initializer_list<const void*> list) {
+    for (const void* p : list)
+        if ((uintptr_t)p % size) return true;
+    return false;
 }
 
 // The widest vector (bytes, at most `most`) that every given address and pitch is a multiple of.

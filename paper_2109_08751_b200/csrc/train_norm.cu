@@ -551,6 +551,7 @@ int sparbit_norm_forward(sparbit_norm_plan_t* p, size_t rows, const void* x, siz
         for (int j = 0; j < i; j++)
             if (regions_overlap(outs[i], outs[j])) return SPARBIT_ERR_ALIAS;
     }
+    if (misaligned(es, {x, residual, sum, y}) || misaligned(ws, {weight}) || misaligned(4, {scales, rstd})) return SPARBIT_ERR_ARG;
     if (!sum && !y && !y8 && !rstd) return SPARBIT_OK;
     NormArgs g = {};
     g.x = x, g.residual = residual, g.weight = weight, g.sum = sum, g.y = y, g.y8 = (uint8_t*)y8;
@@ -591,6 +592,7 @@ int sparbit_norm_backward(sparbit_norm_plan_t* p, size_t rows, const void* dy, s
     if ((!(dx == dy && dx_ld == dy_ld) && regions_overlap(rx, ry)) || (!(dx == dsum && dx_ld == dsum_ld) && regions_overlap(rx, rd)) ||
         regions_overlap(rg, ry) || regions_overlap(rg, rd) || regions_overlap(rg, rx))
         return SPARBIT_ERR_ALIAS;
+    if (misaligned(es, {dy, sum, dsum, dx}) || misaligned(ws, {weight}) || misaligned(4, {rstd, dweight})) return SPARBIT_ERR_ARG;
     if (dweight) {
         if (!p->work) return SPARBIT_ERR_WORKSPACE;
         int cur = -1;
