@@ -444,6 +444,11 @@ class OrthoPlan(_TrainPlan):
         _check(lib.sparbit_muon_step(self._h, ctypes.byref(args), _stream_handle(stream)), "sparbit_muon_step")
 
 
+def _attention_scale(key_size, scale):
+    """The usual scale where none is given (any for a size that the library refuses)."""
+    return float(scale) if scale is not None else key_size ** -0.5 if key_size > 0 else 1.0
+
+
 class LinearAttentionPlan(_TrainPlan):
     """Linear attention with a decay for each head over sequences of the given lengths
     (sparbit_linear_attention_plan_create).  scale: key_size ** -0.5 where it is None.  Row strides default to heads *
@@ -453,7 +458,7 @@ class LinearAttentionPlan(_TrainPlan):
 
     def __init__(self, lengths, heads: int, key_size: int, value_size: int, dtype: int = BF16, scale=None):
         n, arr = _counts(lengths)
-        self.scale = key_size ** -0.5 if scale is None and key_size > 0 else 1.0 if scale is None else float(scale)
+        self.scale = _attention_scale(key_size, scale)
         self._create(n, arr, heads, key_size, value_size, dtype, self.scale)
         self.heads, self.key_size, self.value_size, self.dtype = heads, key_size, value_size, dtype
 
@@ -482,7 +487,7 @@ def linear_attention_step(rows: int, heads: int, key_size: int, value_size: int,
     """One token for each of `rows` running sequences; n_slots defaults to `rows`, scale to key_size ** -0.5."""
     wk, wv = heads * key_size, heads * value_size
     code = lib.sparbit_linear_attention_step(
-        rows, heads, key_size, value_size, dtype, key_size ** -0.5 if scale is None else scale,
+        rows, heads, key_size, value_size, dtype, _attention_scale(key_size, scale),
         _address_of(q, dtype), _stride_of(q, q_ld, wk),
         _address_of(k, dtype), _stride_of(k, k_ld, wk),
         _address_of(v, dtype), _stride_of(v, v_ld, wv), _flat(log_decay, F32), _flat(slots, _I32),
