@@ -469,23 +469,27 @@ Shape shape_of(const Plan* p, size_t rows, bool backward) {
     return s;
 }
 
-// f.operator()<T, W, U, kMost>() for the plan's types and a shape.
-template <typename T, typename W, typename Fn>
+// f.operator()<T, W, U, kMost>() for the plan's types and a shape, those that shape_of gives.
+template <bool kBackward, typename T, typename W, typename Fn>
 int by_shape(const Shape& s, Fn f) {
     if (s.units == 1)
         return s.most == 256 ? f.template operator()<T, W, 1, 256>() : f.template operator()<T, W, 1, 1024>();
-    if (s.units == 2)
-        return s.most == 256 ? f.template operator()<T, W, 2, 256>() : f.template operator()<T, W, 2, 512>();
-    if (s.most == 256) return f.template operator()<T, W, 4, 256>();
+    if (s.units == 2) {
+        if constexpr (kBackward)
+            if (s.most == 512) return f.template operator()<T, W, 2, 512>();
+        return f.template operator()<T, W, 2, 256>();
+    }
+    if constexpr (!kBackward)
+        if (s.most == 256) return f.template operator()<T, W, 4, 256>();
     return s.most == 512 ? f.template operator()<T, W, 4, 512>() : f.template operator()<T, W, 4, 1024>();
 }
-template <typename Fn>
+template <bool kBackward, typename Fn>
 int by_types(const Plan* p, const Shape& s, Fn f) {
-    if (p->dtype == SPARBIT_F32) return by_shape<float, float>(s, f);
+    if (p->dtype == SPARBIT_F32) return by_shape<kBackward, float, float>(s, f);
     if (p->dtype == SPARBIT_BF16)
-        return p->weight_dtype == SPARBIT_F32 ? by_shape<__nv_bfloat16, float>(s, f)
-                                              : by_shape<__nv_bfloat16, __nv_bfloat16>(s, f);
-    return p->weight_dtype == SPARBIT_F32 ? by_shape<__half, float>(s, f) : by_shape<__half, __half>(s, f);
+        return p->weight_dtype == SPARBIT_F32 ? by_shape<kBackward, __nv_bfloat16, float>(s, f)
+                                              : by_shape<kBackward, __nv_bfloat16, __nv_bfloat16>(s, f);
+    return p->weight_dtype == SPARBIT_F32 ? by_shape<kBackward, __half, float>(s, f) : by_shape<kBackward, __half, __half>(s, f);
 }
 
 Region region(const Plan* p, const void* x, size_t rows, size_t ld) {
@@ -568,7 +572,7 @@ int sparbit_norm_forward(sparbit_norm_plan_t* p, size_t rows, const void* x, siz
     const Shape s = shape_of(p, rows, false);
     g.lanes = s.lanes;
     const size_t together = s.threads / s.lanes, grid = std::min((size_t)(kSms * s.per_sm), (rows + together - 1) / together);
-    return by_types(p, s, [&]<typename T, typename W, int U, int kMost>() {
+    return by_types<false>(p, s, [&]<typename T, typename W, int U, int kMost>() {
         CU(launch(norm_forward_kernel<T, W, U, kMost>, dim3((unsigned)grid), dim3(s.threads), 0, (cudaStream_t)stream, g));
         return (int)SPARBIT_OK;
     });
@@ -614,7 +618,7 @@ int sparbit_norm_backward(sparbit_norm_plan_t* p, size_t rows, const void* dy, s
     const int grid = (int)std::min<size_t>(std::min(kParts, kSms * s.per_sm), (rows + together - 1) / together);
     if (grid > 0) {
         const size_t smem = together > 1 ? sizeof(float) * s.threads * s.units * kUnit : 0;
-        const int e = by_types(p, s, [&]<typename T, typename W, int U, int kMost>() {
+        const int e = by_types<true>(p, s, [&]<typename T, typename W, int U, int kMost>() {
             CU(launch(norm_backward_kernel<T, W, U, kMost>, dim3(grid), dim3(s.threads), smem, (cudaStream_t)stream, g));
             return (int)SPARBIT_OK;
         });
