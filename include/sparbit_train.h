@@ -397,7 +397,8 @@ int sparbit_norm_backward(sparbit_norm_plan_t* plan, size_t rows, const void* dy
  *   sums[r] = sum of the squares of all elements of rank r's tensors, in 64 bits throughout
  *   norm = sqrt(sum over the ranks of sums),  factor = min(1, most / (norm + eps)),  out = factor * in
  *
- * A norm that is NaN makes every element NaN, an infinite one makes the factor 0 (and infinite elements NaN).
+ * A norm that is NaN makes every element NaN, an infinite one makes the factor 0 (and infinite elements NaN).  The factor is 1
+ * where the norm is 0, whatever `most` and eps, and where `most` is infinite.
  */
 typedef struct sparbit_clip_plan_s sparbit_clip_plan_t;
 
@@ -421,8 +422,9 @@ int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* plan, const void* const* 
 int sparbit_clip_sums(sparbit_clip_plan_t* plan, double* sums, void* stream);
 
 /* gathered: [n_ranks][G] 64-bit, rank r's receive buffer of the allgather of the sums over G ranks.
- * norms: [n_ranks][2] 32-bit: norm (infinite where 32 bits do not hold it; the factor goes by 64) and factor.  Where out was NULL nothing else is written.  A tensor that is its own
- * output is left alone where the factor is 1.  ERR_ARG: most negative or NaN, eps negative or not finite. */
+ * norms: [n_ranks][2] 32-bit: norm (infinite where 32 bits do not hold it; the factor goes by 64) and factor.  Where out
+ * was NULL nothing else is written.  A tensor that is its own output is left alone where the factor is 1.  ERR_ARG: most
+ * negative or NaN, eps negative or not finite; ERR_ALIAS: norms lie in gathered or in a tensor, or gathered in an output. */
 int sparbit_clip_scale(sparbit_clip_plan_t* plan, const double* gathered, int G, float most, float eps, float* norms,
                        void* stream);
 
