@@ -17,9 +17,10 @@
 // same three steps, with an allgather in the middle, are what ranks do that hold slices of a sequence.
 //
 // A token and head has to move 4 x size elements and takes 4 keys x values operations in the recurrence, in chunks another
-// kChunk x (keys + values): 8 x 4096 tokens, 16 heads of 128 / 128 bf16 are 83 us of bytes and 41 of products forward, at
-// 1669 TFLOP/s; it takes 138 us (backward 485, of 145).  In place of bytes the hand-overs between a chunk's steps bound it,
-// see the kernel.  f32 is bound by plain multiply-adds out of shared memory.
+// 2 kChunk x (keys + values): 8 x 4096 tokens, 16 heads of 128 / 128 are 83 us of bytes and 41 of products forward, at
+// 1669 TFLOP/s.  What the kernel issues is more, the state's product once for each part of c: 72 us with bf16's four, 51
+// with fp16's two, so that the tensor cores' work is near the bytes.  It takes 138 us in bf16 (backward 485, of 145 of bytes).
+// In place of either the hand-overs between a chunk's steps bound it, see the kernel.  f32 is bound by plain multiply-adds out of shared memory.
 #include <cuda.h>
 #include <math.h>
 

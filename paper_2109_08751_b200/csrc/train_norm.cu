@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? (U == 4 ? 2 : 3) : 1) no
             const float scale = most / 448.0f;
             if (g.block ? col % g.block == 0 : col == 0) g.scales[row * g.scales_ld + (g.block ? col / g.block : 0)] = scale;
             // y / scale as a reader of both forms it: y times the inverse, and what that leaves of y once more (a step of
-            // Newton's method; 148 us for 16384 x 5000 f16, 140 without it).  Negated, so that a zero keeps its sign through
+            // Newton's method; 143 us for 16384 x 5000 f16, 134 without it).  Negated, so that a zero keeps its sign through
             // the step; no step over an infinite scale.
             const float by = -__fdividef(1.0f, scale), back = scale < INFINITY ? scale : 0.0f;
             uint32_t pairs8[kUnit / 2];
@@ -448,7 +448,10 @@ using Plan = sparbit_norm_plan_s;
 
 // Threads of a row, units of a thread, the most threads that the kernel is built for, CTAs an SM holds.  With few rows a
 // thread has one unit, which is done soonest.  With many, two or four and the next row's on their way keep enough loads in
-// flight; the registers that they take (80, or 128 from four units and backward) leave room for so many CTAs.
+// flight; the registers that they take (80, or 128 from four units and backward) leave room for so many CTAs.  Four units do
+// not fit everywhere: backward above 8192 columns (16384) spills 0.8 to 1.9 KB a thread (2.0 to 2.9), forward above 16384 0.9 to
+// 1.5 KB, which costs two to seven times the bytes' time: 8192 x 12288 bf16 335 us backward and 145 forward, of 125;
+// 4096 x 20000 726 and 311, of 101; 2048 x 32768 689 and 250, of 83 (8192 x 8192: 105 and 90, of 83).
 struct Shape {
     int lanes, units, threads, most, per_sm;
 };
