@@ -39,7 +39,7 @@ struct ClipArgs {
     const int32_t* cta_begin;   // [CTAs + 1], chunks
     const int32_t* rank_parts;  // [ranks][2], parts
     double* parts;              // part of rank r from CTA b at [b + r]: runs meet every rank from left to right
-    unsigned* ticket;
+    unsigned* control;          // ticket of the sums; whether the tensors that are set have outputs
     int n_ranks;
     double* sums;
     const double* gathered;
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kThreads) clip_sums_kernel(const __grid_consta
     // the CTA that comes last adds the parts, always in the same order
     if (threadIdx.x == 0) {
         __threadfence();
-        last = atomicAdd(g.ticket, 1u) == gridDim.x - 1;
+        last = atomicAdd(g.control, 1u) == gridDim.x - 1;
     }
     __syncthreads();
     if (!last) return;
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) clip_sums_kernel(const __grid_consta
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kAllLanes, s, o);
         if (lane == 0) g.sums[r] = s;
     }
-    if (threadIdx.x == 0) *g.ticket = 0;
+    if (threadIdx.x == 0) g.control[0] = 0;
 }
 
 template <typename T>
@@ -199,17 +199,19 @@ __global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_const
     __shared__ double sm[kThreads / 32];
     pdl_wait();
     pdl_trigger();
+    // not an argument: a captured call follows what is set when it is replayed
+    const bool write = g.control[1] != 0;
     float norm, factor = 1.0f;
     for (int r = blockIdx.x; r < g.n_ranks; r += gridDim.x) {
         factor_of(g, r, sm, norm, factor);
         if (threadIdx.x == 0) g.norms[2 * r] = norm, g.norms[2 * r + 1] = factor;
     }
+    if (!write) return;
     const int lo = g.cta_begin[blockIdx.x], hi = g.cta_begin[blockIdx.x + 1];
     int rank = -1;
     for (int c = hi - 1; c >= lo; c--) {
         const Chunk k = g.chunks[c];
         const Tensor t = g.tensors[k.tensor];
-        if (!t.out) break;  // only norms are wanted.  The table says so, which a captured call reads when it is replayed
         if (t.rank != rank) {
             rank = t.rank;
             factor_of(g, rank, sm, norm, factor);
@@ -248,6 +250,7 @@ struct sparbit_clip_plan_s {
     char* work = nullptr;
     int device = -1;
     bool set = false;
+    unsigned write = 0;  // as it stands in the workspace
 
     size_t off_tensors() const { return 256; }
     size_t off_chunks() const { return off_tensors() + round_up(tensors.size() * sizeof(Tensor), 256); }
@@ -275,7 +278,7 @@ ClipArgs common_args(const Plan* p) {
     g.cta_begin = (const int32_t*)(p->work + p->off_ctas());
     g.rank_parts = (const int32_t*)(p->work + p->off_ranks());
     g.parts = (double*)(p->work + p->off_parts());
-    g.ticket = (unsigned*)p->work;
+    g.control = (unsigned*)p->work;
     g.n_ranks = p->n_ranks;
     return g;
 }
@@ -362,6 +365,7 @@ int sparbit_clip_plan_set_workspace(sparbit_clip_plan_t* p, void* dev, size_t by
     if (!dev || bytes < p->work_bytes() || (uintptr_t)dev % 16) return SPARBIT_ERR_WORKSPACE;
     p->work = nullptr;
     p->set = false;
+    p->write = 0;
     CU(cudaGetDevice(&p->device));
     char* base = (char*)dev;
     CU(cudaMemset(base, 0, 256));
@@ -417,6 +421,9 @@ int sparbit_clip_plan_set_tensors(sparbit_clip_plan_t* p, const void* const* in,
     for (size_t i = 0; i < n; i++) p->tensors[i].in = in[i], p->tensors[i].out = out ? out[i] : nullptr;
     CU(cudaDeviceSynchronize());
     CU(cudaMemcpy(p->work + p->off_tensors(), p->tensors.data(), n * sizeof(Tensor), cudaMemcpyHostToDevice));
+    const unsigned write = out != nullptr;
+    if (write != p->write) CU(cudaMemcpy(p->work + sizeof write, &write, sizeof write, cudaMemcpyHostToDevice));
+    p->write = write;
     CU(cudaDeviceSynchronize());
     p->inputs = std::move(inputs), p->outputs = std::move(outputs);
     p->set = true;
